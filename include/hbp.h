@@ -317,6 +317,89 @@ int hbp_hash_keys(const uint32_t *n, int64_t count, int32_t a, int32_t rows_per_
  * may be running), and with it the memory of freed handles (see hbp_free), on every device. */
 int hbp_release_workspace(void);
 
+/* ---------------------------------------------------------------------------------------------------------------------
+ * Operators beside the sparse products: what a model does before, between and after its matrix-vector products.  All of
+ * them are asynchronous on `stream` and allocate nothing, so they may be captured into a HIP graph; arrays that have to be somewhere in the
+ * meantime lie in a `workspace` that the caller hands in (DEVICE, 256-byte aligned, of at least as many bytes as the ..._workspace
+ * call says; not shared by calls that overlap in time; NULL where that call says 0).  Arrays are of the device that is current.
+ * A call with an error that an earlier HIP call of the thread has left returns HBP_ERR_HIP and launches nothing.
+ * Sums, softmax statistics and norms are held in fp32 whatever the arrays' type; every result is rounded once, to nearest even,
+ * when it is written.  Every sum has one order: the same call gives the same bits.
+ * Row strides (ld...) count values, are at least the row's length and need no alignment beyond the value's. */
+typedef enum { HBP_F32 = 0, HBP_F16 = 1, HBP_BF16 = 2 } hbp_type;
+
+/* A dense matrix of 4-bit codes: W[r][k] = scale[r][k / group] * (code[r][k] - zero[r][k / group]).
+ *   codes  DEVICE, 16-byte aligned, n_rows rows of 16 * ceil(n_cols / 32) bytes: byte j of a row holds column 2j in its low four
+ *          bits and column 2j+1 in its high ones.  What lies behind column n_cols is not looked at (hbp_q4_pack writes zeros).
+ *   scales, zeros  DEVICE [n_rows][ceil(n_cols / group)] of scale_type; zeros NULL: 8 for all.  Both finite.
+ *   group  columns that share a scale: 32, 64, 128, 256 or 512; the last group of a row may be shorter. */
+typedef struct {
+    void *codes, *scales, *zeros;
+    int64_t n_rows, n_cols;   /* 1 .. 2^31 - 512 */
+    int32_t group, scale_type;
+} hbp_q4_matrix_t;
+
+/* Rounds a dense matrix w (DEVICE, `type`, row stride ldw) into a's codes, scales and, where a->zeros is not NULL, zero points.  Without
+ * zero points: scale = max |w| / 7 over the group, code = rint(w / scale) + 8.  With them: low = min(w, 0), high = max(w, 0), scale =
+ * (high - low) / 15, zero = rint(-low / scale) (so that 0 is a code), code = rint(w / scale + zero).  The scale is rounded to its type
+ * first (at most that type's largest value) and the codes, clamped to 0..15, go by the rounded one; a scale of 0 gives the codes of 0.  A group with a NaN or an infinity gets a NaN
+ * scale (and zero point 0, codes 8).  *a HOST. */
+int hbp_q4_pack(const hbp_q4_matrix_t *a, int type, const void *w, int64_t ldw, void *stream);
+/* w = the values that the codes stand for, rounded to `type`. */
+int hbp_q4_unpack(const hbp_q4_matrix_t *a, int type, void *w, int64_t ldw, void *stream);
+
+/* Products with `vectors` vectors at once (rows of x and y: x [vectors][n_cols], y [vectors][n_rows], both of `type`; x and y must not
+ * overlap): y[m][r] = sum over k of W[r][k] x[m][k].  The weights are read once for 64 vectors.  vectors = 0 does nothing. */
+int hbp_q4_mv(const hbp_q4_matrix_t *a, int type, const void *x, int64_t ldx, void *y, int64_t ldy, int64_t vectors, void *stream);
+/* The transposed product, which is the gradient of hbp_q4_mv for its x: y[m][k] = sum over r of W[r][k] x[m][r], x [vectors][n_rows],
+ * y [vectors][n_cols]. */
+int hbp_q4_mv_t(const hbp_q4_matrix_t *a, int type, const void *x, int64_t ldx, void *y, int64_t ldy, int64_t vectors, void *workspace,
+                size_t workspace_bytes, void *stream);
+int hbp_q4_mv_t_workspace(const hbp_q4_matrix_t *a, int64_t vectors, size_t *bytes /* HOST */);
+
+/* Residual sum, gate and norms (root mean square) between two blocks, row by row of [tokens][width]:
+ *   n = y * r1 * w_post, r1 = (mean y^2 + eps)^-1/2      the norm behind the block whose result is y
+ *   h_out = h + scale * gate * n                         the residual stream
+ *   x_out = h_out * r2 * w_pre, r2 = (mean h_out^2 + eps)^-1/2    the norm before the next block (h_out before it is rounded)
+ * h, y, h_out, x_out and gate of `type`; h_out may be h, x_out may be y.  w_post, w_pre [width] of `type`, or NULL for ones.
+ * gate by gate_kind: NONE (1; gate NULL), CHANNEL [width], TOKEN [tokens], FULL [tokens][width] with row stride ldg.
+ * rstd DEVICE float [tokens][2] = r1, r2, or NULL (the backward call needs it).  width at most 16384, eps > 0.  tokens = 0 does nothing. */
+typedef enum { HBP_GATE_NONE = 0, HBP_GATE_CHANNEL = 1, HBP_GATE_TOKEN = 2, HBP_GATE_FULL = 3 } hbp_gate_kind;
+typedef struct {
+    int64_t tokens, width;
+    int32_t type, gate_kind;
+    const void *w_post, *w_pre, *gate;
+    int64_t ldg;
+    float scale, eps;
+} hbp_norms_t;
+int hbp_residual_norms(const hbp_norms_t *n /* HOST */, const void *h, int64_t ldh, const void *y, int64_t ldy, void *h_out, int64_t ldho,
+                       void *x_out, int64_t ldxo, float *rstd, void *stream);
+/* Its gradients, from d_h_out and d_x_out (either may be NULL: zero), the forward call's inputs (h and y as they were) and rstd: d_h, d_y and a FULL gate's
+ * d_gate of `type` (d_gate row stride ldg, too); d_w_post, d_w_pre [width], a CHANNEL's [width] and a TOKEN's [tokens] d_gate in fp32, each may
+ * be NULL.  d_h may be d_h_out, d_y may be d_x_out.  tokens = 0 sets the gradients of the weights (and of a CHANNEL gate) to zero. */
+int hbp_residual_norms_backward(const hbp_norms_t *n, const void *d_h_out, int64_t lddho, const void *d_x_out, int64_t lddxo, const void *h,
+                                int64_t ldh, const void *y, int64_t ldy, const float *rstd, void *d_h, int64_t lddh, void *d_y, int64_t lddy,
+                                float *d_w_post, float *d_w_pre, void *d_gate, void *workspace, size_t workspace_bytes, void *stream);
+int hbp_residual_norms_backward_workspace(const hbp_norms_t *n, size_t *bytes);
+
+/* Log probabilities of given tokens, entropies and most likely tokens of `tokens` rows of logits [tokens][vocabulary] (`type`, row stride ldz).
+ *   ids    DEVICE int32 or int64 (id_bytes 4 or 8) [tokens], or NULL: logp is not written.  A negative id is no token: logp 0 and no
+ *          gradient.  An id of `vocabulary` or more: logp NaN, and a gradient of NaN.
+ *   logp, entropy, lse  DEVICE float [tokens], each may be NULL: z[id] - lse, lse - sum p z, lse = log(sum exp z)
+ *   top_ids int32, top_logp float, DEVICE [tokens][top], top = 0..64 and at most vocabulary; top_ids and top_logp may not be NULL where
+ *          top > 0: the largest logits in descending order, among equal ones the lowest index first (NaN counts as larger than
+ *          any number, -0 equals 0)
+ * A logit of -inf is a masked token: p = 0, logp -inf, no part in the entropy, no gradient.  A row with nothing else: lse = -inf, every logp
+ * -inf, entropy 0, gradient 0.  A row with a NaN or +inf: lse, logp and entropy NaN.  vocabulary at most 2^31 - 512.  tokens = 0 does nothing. */
+int hbp_token_logprobs(int type, const void *logits, int64_t ldz, int64_t tokens, int64_t vocabulary, const void *ids, int id_bytes, float *logp,
+                       float *entropy, float *lse, int top, int32_t *top_ids, float *top_logp, void *workspace, size_t workspace_bytes, void *stream);
+int hbp_token_logprobs_workspace(int type, int64_t tokens, int64_t vocabulary, int top, size_t *bytes);
+/* The logits' gradient from g_logp and g_entropy (DEVICE float [tokens], either may be NULL: zero) and the forward call's lse and entropy:
+ * d[v] = g_logp ((v is the token) - p_v) - g_entropy p_v (z_v - lse + entropy), of `type`, row stride ldd; d_logits may be the logits. */
+int hbp_token_logprobs_backward(int type, const void *logits, int64_t ldz, int64_t tokens, int64_t vocabulary, const void *ids, int id_bytes,
+                                const float *lse, const float *entropy, const float *g_logp, const float *g_entropy, void *d_logits, int64_t ldd,
+                                void *stream);
+
 const char *hbp_status_string(int status);
 /* hipError_t of the most recent HBP_ERR_HIP on this thread, as int. */
 int hbp_last_hip_error(void);

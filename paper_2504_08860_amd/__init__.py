@@ -43,6 +43,9 @@ EXPORTED_SYMBOLS = (
     "hbp_csr_spmv", "hbp_status_string", "hbp_last_hip_error",
     "hbp_build_f64", "hbp_spmv_f64", "hbp_spmv_timed_f64", "hbp_csr_spmv_f64", "hbp_release_workspace", "hbp_hash_keys",
     "hbp_spmv_static_scratch", "hbp_spmv_sized",
+    # operators beside the sparse products (operators.py)
+    "hbp_q4_pack", "hbp_q4_unpack", "hbp_q4_mv", "hbp_q4_mv_t", "hbp_q4_mv_t_workspace", "hbp_residual_norms", "hbp_residual_norms_backward",
+    "hbp_residual_norms_backward_workspace", "hbp_token_logprobs", "hbp_token_logprobs_workspace", "hbp_token_logprobs_backward",
 )
 
 
@@ -114,6 +117,7 @@ def lib() -> ctypes.CDLL:
         L.hbp_last_hip_error.argtypes = []
         L.hbp_release_workspace.argtypes = []
         L.hbp_hash_keys.argtypes = [vp, i64, i32, i32, vp, vp]
+        operators.declare(L)
         for name in EXPORTED_SYMBOLS:
             if name not in ("hbp_status_string",):
                 getattr(L, name).restype = ctypes.c_int
@@ -132,6 +136,10 @@ def _stream_ptr(stream) -> int:
             return _raw_stream(_device())
         return _torch.cuda.current_stream().cuda_stream
     return int(getattr(stream, "cuda_stream", stream))
+
+
+def _current_device() -> int:
+    return _device() if _device is not None else _torch.cuda.current_device()
 
 
 def _dev_i32(t, what):
@@ -298,3 +306,8 @@ def hbp_hash_keys(n, a: int, rows_per_block: int, stream=None):
 def hbp_release_workspace() -> None:
     """Gives back the scratch memory hbp_build keeps between builds and the memory kept of freed handles (at most 4 GiB per device)."""
     _check(lib().hbp_release_workspace(), "hbp_release_workspace")
+
+
+from . import operators  # noqa: E402  (which reaches back into this module)
+from .operators import (hbp_norms_t, hbp_q4_matrix_t, hbp_q4_mv, hbp_q4_mv_t, hbp_q4_pack, hbp_q4_shapes, hbp_q4_unpack,  # noqa: E402,F401
+                        hbp_residual_norms, hbp_residual_norms_backward, hbp_token_logprobs, hbp_token_logprobs_backward)

@@ -8,7 +8,7 @@ from concurrent.futures import ThreadPoolExecutor
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(_HERE)
-SOURCES = ["hbp_api.hip", "hbp_build.hip", "hbp_spmv.hip", "hbp_spmv_f64.hip"]
+SOURCES = ["hbp_api.hip", "hbp_build.hip", "hbp_spmv.hip", "hbp_spmv_f64.hip", "hbp_q4.hip", "hbp_norms.hip", "hbp_logprobs.hip"]
 LIB = os.path.join(_HERE, "libhbp.so")
 
 # Packed-fp32 code generation is turned off for all device code.

@@ -1,0 +1,349 @@
+// Residual sum, gate and norms between two blocks, and their gradients (hbp_residual_norms, hbp_residual_norms_backward).
+#include "hbp_ops.h"
+
+namespace hbp {
+namespace {
+
+constexpr int64_t kMaxWidth = 16384;
+
+struct NormArgs {
+    int64_t tokens, ldh, ldy, ldho, ldxo, ldg;
+    int32_t width;
+    float scale, eps;
+    const void *h, *y, *w_post, *w_pre, *gate;
+    void *h_out, *x_out;
+    float *rstd;
+};
+
+// Forward.  A row is a workgroup's: THREADS threads with CHUNKS times eight columns each, which stay in registers from the only
+// read to the writes; two sums over the row lie between.
+template <typename T, int THREADS, int CHUNKS, int GATE>
+__global__ __launch_bounds__(THREADS) void k_residual_norms(NormArgs n)
+{
+    __shared__ float slots[2][THREADS / kWave];
+    const int64_t t = blockIdx.x;
+    const T *h = static_cast<const T *>(n.h) + t * n.ldh, *y = static_cast<const T *>(n.y) + t * n.ldy;
+    const T *g = GATE == HBP_GATE_FULL ? static_cast<const T *>(n.gate) + t * n.ldg : static_cast<const T *>(n.gate);
+    const T *w_post = static_cast<const T *>(n.w_post), *w_pre = static_cast<const T *>(n.w_pre);
+    Eight<T> yy[CHUNKS], hh[CHUNKS], gg[CHUNKS];
+    float row_gate = n.scale;
+    if constexpr (GATE == HBP_GATE_TOKEN) row_gate *= to_f32(g[t]);
+#pragma unroll
+    for (int c = 0; c < CHUNKS; c++) {
+        const int col = (c * THREADS + threadIdx.x) * 8;
+        yy[c].load_first(y + col, n.width - col);
+        hh[c].load_first(h + col, n.width - col);
+        if constexpr (GATE == HBP_GATE_FULL || GATE == HBP_GATE_CHANNEL) gg[c].load_first(g + col, n.width - col);
+    }
+    float sum[1] = {0};
+#pragma unroll
+    for (int c = 0; c < CHUNKS; c++)
+#pragma unroll
+        for (int i = 0; i < 8; i++) sum[0] += yy[c].get(i) * yy[c].get(i);
+    block_sums<1, THREADS>(sum, slots[0]);
+    const float r1 = rsqrtf(sum[0] / n.width + n.eps);
+    float next[CHUNKS][8];
+    sum[0] = 0;
+#pragma unroll
+    for (int c = 0; c < CHUNKS; c++) {
+        const int col = (c * THREADS + threadIdx.x) * 8;
+        Eight<T> w;
+        if (w_post) w.load_first(w_post + col, n.width - col);
+#pragma unroll
+        for (int i = 0; i < 8; i++) {
+            float v = yy[c].get(i) * r1;
+            if (w_post) v *= w.get(i);
+            if constexpr (GATE == HBP_GATE_FULL || GATE == HBP_GATE_CHANNEL) v *= gg[c].get(i);
+            next[c][i] = hh[c].get(i) + row_gate * v;
+            sum[0] += next[c][i] * next[c][i];
+        }
+    }
+    block_sums<1, THREADS>(sum, slots[1]);
+    const float r2 = rsqrtf(sum[0] / n.width + n.eps);
+    T *h_out = static_cast<T *>(n.h_out) + t * n.ldho, *x_out = static_cast<T *>(n.x_out) + t * n.ldxo;
+#pragma unroll
+    for (int c = 0; c < CHUNKS; c++) {
+        const int col = (c * THREADS + threadIdx.x) * 8;
+        Eight<T> w, a, b;
+        if (w_pre) w.load_first(w_pre + col, n.width - col);
+#pragma unroll
+        for (int i = 0; i < 8; i++) {
+            a.set(i, next[c][i]);
+            const float v = next[c][i] * r2;
+            b.set(i, w_pre ? v * w.get(i) : v);
+        }
+        a.store_first(h_out + col, n.width - col);
+        b.store_first(x_out + col, n.width - col);
+    }
+    if (n.rstd && threadIdx.x == 0) {
+        n.rstd[2 * t] = r1;
+        n.rstd[2 * t + 1] = r2;
+    }
+}
+
+struct NormBackArgs {
+    int64_t tokens, ldh, ldy, ldg, lddho, lddxo, lddh, lddy;
+    int32_t width;
+    float scale;
+    const void *d_h_out, *d_x_out, *h, *y, *w_post, *w_pre, *gate;
+    const float *rstd;
+    void *d_h, *d_y, *d_gate;
+    float *partial;  // [workgroups][3][width]: d_w_post, d_w_pre, a CHANNEL's d_gate
+};
+
+// Backward.  With a = d_x_out w_pre, e = d_h_out + r2 (a - h' r2^2 mean(a h')) is d_h, and b = scale g w_post e goes through the
+// first norm: d_y = r1 (b - y r1^2 mean(b y)).  e in the second mean is spelled out, so that all three sums of a row, of
+// a h', of w y (d_h_out + r2 a) and of w y h' with w = scale g w_post, are taken together: one wait for the others per row.
+// h' is computed again from h, y and the gate, which are read anyway: not the rounded one, and no read more.
+template <typename T, int THREADS, int CHUNKS, int GATE>
+__global__ __launch_bounds__(THREADS) void k_residual_norms_backward(NormBackArgs n)
+{
+    __shared__ float slots[2][THREADS / kWave * 3];
+    const T *w_post = static_cast<const T *>(n.w_post), *w_pre = static_cast<const T *>(n.w_pre);
+    float sum_post[CHUNKS][8] = {}, sum_pre[CHUNKS][8] = {}, sum_gate[CHUNKS][8] = {};
+    const float inverse_width = 1.0f / n.width;
+    int odd = 0;
+    for (int64_t t = blockIdx.x; t < n.tokens; t += gridDim.x, odd ^= 1) {
+        const T *h = static_cast<const T *>(n.h) + t * n.ldh, *y = static_cast<const T *>(n.y) + t * n.ldy;
+        const T *g = GATE == HBP_GATE_FULL ? static_cast<const T *>(n.gate) + t * n.ldg : static_cast<const T *>(n.gate);
+        const float r1 = n.rstd[2 * t], r2 = n.rstd[2 * t + 1];
+        const float row_gate = GATE == HBP_GATE_TOKEN ? to_f32(g[t]) : 1.0f;
+        Eight<T> yy[CHUNKS], gg[CHUNKS], dx[CHUNKS], dh[CHUNKS];
+        float next[CHUNKS][8];
+        float sum[3] = {0, 0, 0};
+#pragma unroll
+        for (int c = 0; c < CHUNKS; c++) {
+            const int col = (c * THREADS + threadIdx.x) * 8;
+            const int left = n.width - col;
+            Eight<T> hh, wp, wq;
+            yy[c].load_first(y + col, left);
+            hh.load_first(h + col, left);
+            dx[c].clear();
+            dh[c].clear();
+            if (n.d_x_out) dx[c].load_first(static_cast<const T *>(n.d_x_out) + t * n.lddxo + col, left);
+            if (n.d_h_out) dh[c].load_first(static_cast<const T *>(n.d_h_out) + t * n.lddho + col, left);
+            if constexpr (GATE == HBP_GATE_FULL || GATE == HBP_GATE_CHANNEL) gg[c].load_first(g + col, left);
+            if (w_post) wp.load_first(w_post + col, left);
+            if (w_pre) wq.load_first(w_pre + col, left);
+#pragma unroll
+            for (int i = 0; i < 8; i++) {
+                float w = n.scale;
+                if constexpr (GATE == HBP_GATE_FULL || GATE == HBP_GATE_CHANNEL) w *= gg[c].get(i);
+                if (w_post) w *= wp.get(i);
+                const float wy = w * yy[c].get(i);
+                next[c][i] = hh.get(i) + row_gate * (r1 * wy);
+                const float a = w_pre ? dx[c].get(i) * wq.get(i) : dx[c].get(i);
+                sum[0] += a * next[c][i];
+                sum[1] += wy * (dh[c].get(i) + r2 * a);
+                sum[2] += wy * next[c][i];
+            }
+        }
+        block_sums<3, THREADS>(sum, slots[odd]);
+        const float along2 = r2 * r2 * r2 * (sum[0] * inverse_width);
+        const float through = sum[1] - along2 * sum[2];  // sum of b y, a row's gate left out
+        const float along1 = r1 * r1 * r1 * (row_gate * through * inverse_width);
+        if (GATE == HBP_GATE_TOKEN && n.d_gate && threadIdx.x == 0) static_cast<float *>(n.d_gate)[t] = r1 * through;
+#pragma unroll
+        for (int c = 0; c < CHUNKS; c++) {
+            const int col = (c * THREADS + threadIdx.x) * 8;
+            const int left = n.width - col;
+            Eight<T> wp, wq, de, dy, dg;
+            if (w_post) wp.load_first(w_post + col, left);
+            if (w_pre) wq.load_first(w_pre + col, left);
+#pragma unroll
+            for (int i = 0; i < 8; i++) {
+                const float yv = yy[c].get(i), xv = dx[c].get(i);
+                const float a = w_pre ? xv * wq.get(i) : xv;
+                const float e = dh[c].get(i) + r2 * a - along2 * next[c][i];
+                float gate = n.scale * row_gate;
+                if constexpr (GATE == HBP_GATE_FULL || GATE == HBP_GATE_CHANNEL) gate *= gg[c].get(i);
+                const float ge = gate * e, unit = yv * r1;
+                const float b = w_post ? ge * wp.get(i) : ge;
+                de.set(i, e);
+                dy.set(i, r1 * b - along1 * yv);
+                sum_post[c][i] += ge * unit;
+                sum_pre[c][i] += xv * (next[c][i] * r2);
+                if constexpr (GATE == HBP_GATE_FULL || GATE == HBP_GATE_CHANNEL) {
+                    const float d = n.scale * e * (w_post ? unit * wp.get(i) : unit);
+                    if constexpr (GATE == HBP_GATE_FULL) dg.set(i, d);
+                    else sum_gate[c][i] += d;
+                }
+            }
+            de.store_first(static_cast<T *>(n.d_h) + t * n.lddh + col, left);
+            dy.store_first(static_cast<T *>(n.d_y) + t * n.lddy + col, left);
+            if constexpr (GATE == HBP_GATE_FULL)
+                if (n.d_gate) dg.store_first(static_cast<T *>(n.d_gate) + t * n.ldg + col, left);
+        }
+    }
+    float *mine = n.partial + (int64_t)blockIdx.x * 3 * n.width;
+#pragma unroll
+    for (int c = 0; c < CHUNKS; c++) {
+        const int col = (c * THREADS + threadIdx.x) * 8;
+#pragma unroll
+        for (int i = 0; i < 8; i++)
+            if (col + i < n.width) {
+                mine[col + i] = sum_post[c][i];
+                mine[n.width + col + i] = sum_pre[c][i];
+                if constexpr (GATE == HBP_GATE_CHANNEL) mine[2 * n.width + col + i] = sum_gate[c][i];
+            }
+    }
+}
+
+// out[which][col] = sum over the workgroups of partial[workgroup][which][col], in ascending order within each quarter
+__global__ __launch_bounds__(256) void k_norm_weight_sums(const float *partial, int32_t workgroups, int32_t width, float *d_w_post, float *d_w_pre,
+                                                          float *d_gate)
+{
+    __shared__ float quarter[4][64];
+    const int lane = threadIdx.x % 64, part = threadIdx.x / 64, col = blockIdx.x * 64 + lane;
+    float *out = blockIdx.y == 0 ? d_w_post : blockIdx.y == 1 ? d_w_pre : d_gate;
+    if (!out) return;
+    float sum = 0;
+    if (col < width)
+        for (int b = part; b < workgroups; b += 4) sum += partial[((int64_t)b * 3 + blockIdx.y) * width + col];
+    quarter[part][lane] = sum;
+    __syncthreads();
+    if (part == 0 && col < width) out[col] = quarter[0][lane] + quarter[1][lane] + quarter[2][lane] + quarter[3][lane];
+}
+
+// Threads and chunks for a width: f(threads, chunks) as compile-time constants
+template <int V> struct Int { static constexpr int value = V; };
+template <typename F> int by_width_forward(int64_t width, F f)
+{
+    if (width <= 512) return f(Int<64>(), Int<1>());
+    if (width <= 2048) return f(Int<256>(), Int<1>());
+    if (width <= 4096) return f(Int<512>(), Int<1>());
+    if (width <= 8192) return f(Int<1024>(), Int<1>());
+    return f(Int<1024>(), Int<2>());
+}
+template <typename F> int by_gate(int kind, F f)
+{
+    switch (kind) {
+    case HBP_GATE_NONE: return f(Int<HBP_GATE_NONE>());
+    case HBP_GATE_CHANNEL: return f(Int<HBP_GATE_CHANNEL>());
+    case HBP_GATE_TOKEN: return f(Int<HBP_GATE_TOKEN>());
+    default: return f(Int<HBP_GATE_FULL>());
+    }
+}
+
+int64_t backward_workgroups(int64_t tokens, int64_t width)
+{
+    const int64_t threads = width <= 512 ? 64 : width <= 2048 ? 256 : width <= 4096 ? 512 : 1024;
+    const int64_t most = 256 * 1024 / threads;  // 16 wavefronts for each of 256 compute units
+    return tokens < most ? tokens : most;
+}
+
+int check_norms(const hbp_norms_t *n)
+{
+    if (!n || n->tokens < 0 || n->width < 1 || !is_type(n->type) || n->gate_kind < HBP_GATE_NONE || n->gate_kind > HBP_GATE_FULL) return HBP_ERR_INVALID_ARGUMENT;
+    if ((n->gate != nullptr) != (n->gate_kind != HBP_GATE_NONE) && n->tokens > 0) return HBP_ERR_INVALID_ARGUMENT;
+    if (n->gate_kind == HBP_GATE_FULL && n->ldg < n->width) return HBP_ERR_INVALID_ARGUMENT;
+    if (!(n->eps > 0)) return HBP_ERR_INVALID_ARGUMENT;
+    const int64_t bytes = type_bytes(n->type);
+    if (!aligned(n->w_post, bytes) || !aligned(n->w_pre, bytes) || !aligned(n->gate, bytes)) return HBP_ERR_INVALID_ARGUMENT;
+    if (n->width > kMaxWidth || n->tokens >= (int64_t(1) << 31)) return HBP_ERR_TOO_LARGE;
+    return HBP_OK;
+}
+
+}  // namespace
+}  // namespace hbp
+
+extern "C" {
+
+int hbp_residual_norms(const hbp_norms_t *n, const void *h, int64_t ldh, const void *y, int64_t ldy, void *h_out, int64_t ldho, void *x_out,
+                       int64_t ldxo, float *rstd, void *stream)
+{
+    using namespace hbp;
+    int rc = check_norms(n);
+    if (rc != HBP_OK) return rc;
+    if (n->tokens == 0) return HBP_OK;
+    const int64_t bytes = type_bytes(n->type);
+    for (const void *p : {h, y, (const void *)h_out, (const void *)x_out})
+        if (!p || !aligned(p, bytes)) return HBP_ERR_INVALID_ARGUMENT;
+    for (int64_t ld : {ldh, ldy, ldho, ldxo})
+        if (ld < n->width) return HBP_ERR_INVALID_ARGUMENT;
+    if (!aligned(rstd, 4)) return HBP_ERR_INVALID_ARGUMENT;
+    rc = earlier_error();
+    if (rc != HBP_OK) return rc;
+    NormArgs a{};
+    a.tokens = n->tokens; a.width = (int32_t)n->width;
+    a.ldh = ldh; a.ldy = ldy; a.ldho = ldho; a.ldxo = ldxo; a.ldg = n->ldg;
+    a.scale = n->scale; a.eps = n->eps;
+    a.h = h; a.y = y; a.w_post = n->w_post; a.w_pre = n->w_pre; a.gate = n->gate;
+    a.h_out = h_out; a.x_out = x_out; a.rstd = rstd;
+    return by_type(n->type, [&](auto type) -> int {
+        using T = decltype(type);
+        return by_gate(n->gate_kind, [&](auto gate) -> int {
+            return by_width_forward(n->width, [&](auto threads, auto chunks) -> int {
+                constexpr int kThreads = decltype(threads)::value;
+                k_residual_norms<T, kThreads, decltype(chunks)::value, decltype(gate)::value>
+                    <<<dim3((unsigned)a.tokens), kThreads, 0, (hipStream_t)stream>>>(a);
+                HBP_HIP(hipGetLastError());
+                return HBP_OK;
+            });
+        });
+    });
+}
+
+int hbp_residual_norms_backward_workspace(const hbp_norms_t *n, size_t *bytes)
+{
+    const int rc = hbp::check_norms(n);
+    if (rc != HBP_OK || !bytes) return rc != HBP_OK ? rc : HBP_ERR_INVALID_ARGUMENT;
+    *bytes = (size_t)(hbp::backward_workgroups(n->tokens, n->width) * 3 * n->width) * sizeof(float);
+    return HBP_OK;
+}
+
+int hbp_residual_norms_backward(const hbp_norms_t *n, const void *d_h_out, int64_t lddho, const void *d_x_out, int64_t lddxo, const void *h,
+                                int64_t ldh, const void *y, int64_t ldy, const float *rstd, void *d_h, int64_t lddh, void *d_y, int64_t lddy,
+                                float *d_w_post, float *d_w_pre, void *d_gate, void *workspace, size_t workspace_bytes, void *stream)
+{
+    using namespace hbp;
+    size_t need = 0;
+    int rc = hbp_residual_norms_backward_workspace(n, &need);
+    if (rc != HBP_OK) return rc;
+    const int64_t bytes = type_bytes(n->type);
+    if (n->tokens > 0) {
+        for (const void *p : {h, y, (const void *)rstd, (const void *)d_h, (const void *)d_y})
+            if (!p || !aligned(p, bytes)) return HBP_ERR_INVALID_ARGUMENT;
+        for (int64_t ld : {ldh, ldy, lddh, lddy, d_h_out ? lddho : n->width, d_x_out ? lddxo : n->width})
+            if (ld < n->width) return HBP_ERR_INVALID_ARGUMENT;
+        if (!aligned(d_h_out, bytes) || !aligned(d_x_out, bytes)) return HBP_ERR_INVALID_ARGUMENT;
+    }
+    if (!aligned(rstd, 4) || !aligned(d_w_post, 4) || !aligned(d_w_pre, 4) || !aligned(d_gate, n->gate_kind == HBP_GATE_FULL ? bytes : 4)) return HBP_ERR_INVALID_ARGUMENT;
+    if (n->gate_kind == HBP_GATE_NONE && d_gate) return HBP_ERR_INVALID_ARGUMENT;
+    if (need && (!workspace || workspace_bytes < need || !aligned(workspace, 256))) return HBP_ERR_INVALID_ARGUMENT;
+    rc = earlier_error();
+    if (rc != HBP_OK) return rc;
+    const int32_t workgroups = (int32_t)backward_workgroups(n->tokens, n->width);
+    hipStream_t st = (hipStream_t)stream;
+    if (workgroups > 0) {
+        NormBackArgs a{};
+        a.tokens = n->tokens; a.width = (int32_t)n->width;
+        a.ldh = ldh; a.ldy = ldy; a.ldg = n->ldg; a.lddho = lddho; a.lddxo = lddxo; a.lddh = lddh; a.lddy = lddy;
+        a.scale = n->scale;
+        a.d_h_out = d_h_out; a.d_x_out = d_x_out; a.h = h; a.y = y; a.w_post = n->w_post; a.w_pre = n->w_pre; a.gate = n->gate;
+        a.rstd = rstd; a.d_h = d_h; a.d_y = d_y; a.d_gate = d_gate;
+        a.partial = static_cast<float *>(workspace);
+        rc = by_type(n->type, [&](auto type) -> int {
+            using T = decltype(type);
+            return by_gate(n->gate_kind, [&](auto gate) -> int {
+                return by_width_forward(n->width, [&](auto threads, auto chunks) -> int {
+                    constexpr int kThreads = decltype(threads)::value;
+                    k_residual_norms_backward<T, kThreads, decltype(chunks)::value, decltype(gate)::value>
+                        <<<dim3((unsigned)workgroups), kThreads, 0, st>>>(a);
+                    HBP_HIP(hipGetLastError());
+                    return HBP_OK;
+                });
+            });
+        });
+        if (rc != HBP_OK) return rc;
+    }
+    float *channel = n->gate_kind == HBP_GATE_CHANNEL ? static_cast<float *>(d_gate) : nullptr;
+    if (d_w_post || d_w_pre || channel) {
+        k_norm_weight_sums<<<dim3((unsigned)((n->width + 63) / 64), channel ? 3 : 2), 256, 0, st>>>(
+            static_cast<const float *>(workspace), workgroups, (int32_t)n->width, d_w_post, d_w_pre, channel);
+        HBP_HIP(hipGetLastError());
+    }
+    return HBP_OK;
+}
+
+}  // extern "C"
