@@ -335,7 +335,7 @@ typedef enum { HBP_F32 = 0, HBP_F16 = 1, HBP_BF16 = 2 } hbp_type;
  *   group  columns that share a scale: 32, 64, 128, 256 or 512; the last group of a row may be shorter. */
 typedef struct {
     void *codes, *scales, *zeros;
-    int64_t n_rows, n_cols;   /* 1 .. 2^31 - 512 */
+    int64_t n_rows, n_cols;   /* at most 2^31 - 512 and 2^28 */
     int32_t group, scale_type;
 } hbp_q4_matrix_t;
 

@@ -8,7 +8,8 @@ from concurrent.futures import ThreadPoolExecutor
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(_HERE)
-SOURCES = ["hbp_api.hip", "hbp_build.hip", "hbp_spmv.hip", "hbp_spmv_f64.hip", "hbp_q4.hip", "hbp_norms.hip", "hbp_logprobs.hip"]
+SOURCES = ["hbp_api.hip", "hbp_build.hip", "hbp_spmv.hip", "hbp_spmv_f64.hip", "hbp_q4.hip", *(f"hbp_q4_mv_{t}.hip" for t in ("f32", "f16", "bf16", "f32_zeros", "f16_zeros", "bf16_zeros")),
+           "hbp_norms.hip", "hbp_logprobs.hip"]
 LIB = os.path.join(_HERE, "libhbp.so")
 
 # Packed-fp32 code generation is turned off for all device code.

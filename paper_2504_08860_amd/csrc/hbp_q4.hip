@@ -1,15 +1,8 @@
 // Matrices held in 4 bits with group scales: packing, and products with a few vectors (hbp_q4_pack, hbp_q4_unpack, hbp_q4_mv, hbp_q4_mv_t).
-#include "hbp_ops.h"
+#include "hbp_q4.h"
 
 namespace hbp {
 namespace {
-
-struct Q4 {
-    const uint8_t *codes;
-    const void *scales, *zeros;
-    int64_t pitch;   // bytes of a row of codes
-    int32_t n_rows, n_cols, groups, shift;  // column k is of group k >> shift
-};
 
 template <typename S> __device__ __forceinline__ float scale_of(const Q4 &a, int64_t row, int group)
 {
@@ -84,47 +77,6 @@ template <typename T, typename S> __global__ __launch_bounds__(256) void k_q4_un
     out.store_first(static_cast<T *>(w) + row * ldw + col, left);
 }
 
-// y[m][r]: a wavefront per row, a lane takes 32 columns at a time for up to four vectors
-template <typename T, typename S> __global__ __launch_bounds__(256) void k_q4_mv(Q4 a, const void *x_, int64_t ldx, void *y_, int64_t ldy, int64_t vectors)
-{
-    const int64_t row = (int64_t)blockIdx.x * 4 + threadIdx.x / kWave;
-    const int lane = threadIdx.x % kWave;
-    if (row >= a.n_rows) return;
-    const T *x = static_cast<const T *>(x_);
-    T *y = static_cast<T *>(y_);
-    for (int64_t m0 = blockIdx.y * 4; m0 < vectors; m0 += (int64_t)gridDim.y * 4) {
-        float acc[4] = {};
-        const int count = vectors - m0 < 4 ? (int)(vectors - m0) : 4;
-        for (int64_t col = lane * 32; col < a.n_cols; col += kWave * 32) {
-            const uint4 c = *reinterpret_cast<const uint4 *>(a.codes + row * a.pitch + col / 2);
-            const int group = (int)(col >> a.shift);
-            const float s = scale_of<S>(a, row, group), zero = zero_of<S>(a, row, group);
-            const uint32_t words[4] = {c.x, c.y, c.z, c.w};
-#pragma unroll
-            for (int j = 0; j < 4; j++)
-                for (int m = 0; m < count; m++) {
-                    const int64_t at = col + 8 * j;
-                    Eight<T> v;
-                    if (at < a.n_cols) v.load_first(x + (m0 + m) * ldx + at, a.n_cols - at);
-                    else v.clear();
-                    float sum = 0;
-#pragma unroll
-                    for (int i = 0; i < 8; i++) {
-                        const float w = at + i < a.n_cols ? s * ((float)(words[j] >> 4 * i & 15u) - zero) : 0.0f;
-                        sum += w * v.get(i);
-                    }
-#pragma unroll
-                    for (int k = 0; k < 4; k++) acc[k] += k == m ? sum : 0.0f;
-                }
-        }
-#pragma unroll
-        for (int k = 0; k < 4; k++) {
-            const float v = wave_sum(acc[k]);
-            if (lane == 0 && k < count) y[(m0 + k) * ldy + row] = from_f32<T>(v);
-        }
-    }
-}
-
 // transposed: a thread per eight columns and vector, over a part of the rows; the parts are summed by a second kernel
 template <typename T, typename S> __global__ __launch_bounds__(256) void k_q4_mv_t(Q4 a, const void *x_, int64_t ldx, float *partial, int64_t vectors, int64_t part)
 {
@@ -167,7 +119,7 @@ int parts_of(const Q4 &a)
 int view(const hbp_q4_matrix_t *m, Q4 *a)
 {
     if (!m || !m->codes || !m->scales || m->n_rows < 1 || m->n_cols < 1 || !is_type(m->scale_type)) return HBP_ERR_INVALID_ARGUMENT;
-    if (m->n_rows > (int64_t(1) << 31) - 512 || m->n_cols > (int64_t(1) << 31) - 512) return HBP_ERR_TOO_LARGE;
+    if (m->n_rows > (int64_t(1) << 31) - 512 || m->n_cols > int64_t(1) << 28) return HBP_ERR_TOO_LARGE;
     int shift = 5;
     while (shift < 9 && (1 << shift) != m->group) shift++;
     const int64_t bytes = type_bytes(m->scale_type);
@@ -241,15 +193,10 @@ int hbp_q4_mv(const hbp_q4_matrix_t *m, int type, const void *x, int64_t ldx, vo
     if (rc != HBP_OK || vectors == 0) return rc;
     rc = earlier_error();
     if (rc != HBP_OK) return rc;
-    const int64_t fours = (vectors + 3) / 4;
-    const dim3 grid((unsigned)((m->n_rows + 3) / 4), (unsigned)(fours < 1024 ? fours : 1024));
-    return by_type(type, [&](auto t) -> int {
-        return by_type(m->scale_type, [&](auto s) -> int {
-            k_q4_mv<decltype(t), decltype(s)><<<grid, 256, 0, (hipStream_t)stream>>>(a, x, ldx, y, ldy, vectors);
-            HBP_HIP(hipGetLastError());
-            return HBP_OK;
-        });
-    });
+    const Q4Product p{a, x, y, ldx, ldy, vectors, m->scale_type};
+    hipStream_t st = (hipStream_t)stream;
+    if (a.zeros) return type == HBP_F32 ? launch_q4_mv_f32_zeros(p, st) : type == HBP_F16 ? launch_q4_mv_f16_zeros(p, st) : launch_q4_mv_bf16_zeros(p, st);
+    return type == HBP_F32 ? launch_q4_mv_f32(p, st) : type == HBP_F16 ? launch_q4_mv_f16(p, st) : launch_q4_mv_bf16(p, st);
 }
 
 int hbp_q4_mv_t_workspace(const hbp_q4_matrix_t *m, int64_t vectors, size_t *bytes)

@@ -7,6 +7,7 @@ that stream, unless one is given.  Outputs are written in place; which inputs th
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import functools
 
@@ -26,14 +27,16 @@ class hbp_norms_t(ctypes.Structure):
                 ("scale", ctypes.c_float), ("eps", ctypes.c_float)]
 
 
-_types = None  # torch's value types by the library's numbers; set with the library's argument types
+_torch = _uint8 = _i32 = _i64 = _f32 = None
+_types = {}  # the library's numbers of torch's value types; set, as those above, with the library's argument types
 
 
 def declare(L) -> None:
     """Sets the argument types of the operators' entry points."""
-    global _types
+    global _torch, _uint8, _i32, _i64, _f32
     import torch
-    _types = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
+    _torch, _uint8, _i32, _i64, _f32 = torch, torch.uint8, torch.int32, torch.int64, torch.float32
+    _types.update({torch.float32: 0, torch.float16: 1, torch.bfloat16: 2})
     vp, i32, i64, size = ctypes.c_void_p, ctypes.c_int, ctypes.c_int64, ctypes.c_size_t
     matrix, norms, size_out = ctypes.POINTER(hbp_q4_matrix_t), ctypes.POINTER(hbp_norms_t), ctypes.POINTER(size)
     L.hbp_q4_pack.argtypes = L.hbp_q4_unpack.argtypes = [matrix, i32, vp, i64, vp]
@@ -48,42 +51,51 @@ def declare(L) -> None:
     L.hbp_token_logprobs_backward.argtypes = [i32, vp, i64, i64, i64, vp, i32] + [vp] * 5 + [i64, vp]
 
 
-def _rows(t, what, shape, dtype):
-    """(address, row stride) of a tensor of this shape and type on the current device, rows contiguous in themselves."""
-    assert t.is_cuda and t.dtype == dtype and tuple(t.shape) == shape, f"{what}: {dtype} CUDA tensor of shape {shape} required"
-    assert t.get_device() == _core._current_device(), f"{what}: a tensor of the current device required"
-    if len(shape) == 1:
-        stride = shape[0]
-        assert shape[0] < 2 or t.stride(0) == 1, f"{what}: contiguous values required"
-    else:
-        stride = t.stride(0) if shape[0] > 1 else shape[1]
-        assert (shape[1] < 2 or t.stride(1) == 1) and stride >= shape[1], f"{what}: rows of contiguous values required"
-    return t.data_ptr(), stride
+# (A small operator is 3 to 5 us of GPU time, and these checks are much of what a loop of them waits for.  A tensor's shape, strides, type,
+# device and address cost 0.1 us each: each is asked for once, and the current device once a call.)
+def _rows(t, what, shape, dtype, device):
+    """(address, row stride) of a tensor of this shape and type on the device, rows contiguous in themselves."""
+    if t.dtype is dtype and t.shape == shape and t.get_device() == device:
+        if len(shape) == 1:
+            if t.is_contiguous():
+                return t.data_ptr(), shape[0]
+        else:
+            apart, step = t.stride()
+            if shape[0] < 2:
+                apart = shape[1]
+            if apart >= shape[1] and (step == 1 or shape[1] < 2):
+                return t.data_ptr(), apart
+    raise AssertionError(f"{what}: {dtype} tensor of shape {tuple(shape)} on the current CUDA device required, rows contiguous in themselves")
 
 
-def _whole(t, what, shape, dtype):
-    """Address of a contiguous tensor of this shape and type on the current device; None for None."""
+def _whole(t, what, shape, dtype, device):
+    """Address of a contiguous tensor of this shape and type on the device; None for None."""
     if t is None:
         return None
-    assert t.is_cuda and t.dtype == dtype and tuple(t.shape) == shape and t.is_contiguous(), f"{what}: contiguous {dtype} CUDA tensor of shape {shape} required"
-    assert t.get_device() == _core._current_device(), f"{what}: a tensor of the current device required"
-    return t.data_ptr()
+    if t.dtype is dtype and t.shape == shape and t.get_device() == device and t.is_contiguous():
+        return t.data_ptr()
+    raise AssertionError(f"{what}: contiguous {dtype} tensor of shape {tuple(shape)} on the current CUDA device required")
 
 
-def _space(workspace, need, stream):
+def _on(stream):
+    """Allocations of the block go to the stream that uses them: their memory may be handed out again, on that stream, as soon as the call is over."""
+    if stream is None:
+        return contextlib.nullcontext()
+    return _torch.cuda.stream(stream if hasattr(stream, "cuda_stream") else _torch.cuda.ExternalStream(int(stream)))
+
+
+def _space(workspace, need, stream, device):
     """(address, bytes, what keeps it) of a workspace of at least ``need`` bytes."""
-    import torch
     if workspace is not None:
-        assert workspace.is_cuda and workspace.is_contiguous() and workspace.get_device() == _core._current_device(), \
-            "workspace: contiguous CUDA tensor of the current device required"
+        assert workspace.get_device() == device and workspace.is_contiguous(), "workspace: contiguous tensor on the current CUDA device required"
         return workspace.data_ptr(), workspace.numel() * workspace.element_size(), workspace
     if not need:
         return None, 0, None
     if stream is None:
-        t = torch.empty(need, dtype=torch.uint8, device="cuda")
-    else:  # memory of the stream that uses it: it may be handed out again, on that stream, as soon as the call has returned
-        with torch.cuda.stream(stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(int(stream))):
-            t = torch.empty(need, dtype=torch.uint8, device="cuda")
+        t = _torch.empty(need, dtype=_uint8, device="cuda")
+    else:
+        with _on(stream):
+            t = _torch.empty(need, dtype=_uint8, device="cuda")
     return t.data_ptr(), need, t
 
 
@@ -94,57 +106,58 @@ def hbp_q4_shapes(n_rows: int, n_cols: int, group: int = 128):
     return (n_rows, (n_cols + 31) // 32 * 16), (n_rows, (n_cols + group - 1) // group)
 
 
-def _matrix(codes, scales, zeros, n_cols, group):
-    import torch
-    codes_shape, scales_shape = hbp_q4_shapes(codes.shape[0], n_cols, group)
-    assert scales.dtype in _types, "scales: float32, float16 or bfloat16 required"
-    return hbp_q4_matrix_t(_whole(codes, "codes", codes_shape, torch.uint8), _whole(scales, "scales", scales_shape, scales.dtype),
-                           _whole(zeros, "zeros", scales_shape, scales.dtype), codes_shape[0], n_cols, group, _types[scales.dtype])
+def _matrix(codes, scales, zeros, n_cols, group, device):
+    n_rows = codes.shape[0]
+    kind = scales.dtype
+    assert kind in _types, "scales: float32, float16 or bfloat16 required"
+    groups = (n_rows, (n_cols + group - 1) // group)
+    return hbp_q4_matrix_t(_whole(codes, "codes", (n_rows, (n_cols + 31) // 32 * 16), _uint8, device), _whole(scales, "scales", groups, kind, device),
+                           _whole(zeros, "zeros", groups, kind, device), n_rows, n_cols, group, _types[kind])
 
 
 def _start():
-    return _core._lib or _core.lib()
+    """(the library, the current device)"""
+    return _core._lib or _core.lib(), _core._current_device()
 
 
 def hbp_q4_pack(w, codes, scales, group: int = 128, zeros=None, stream=None) -> None:
     """Rounds the matrix ``w`` [rows, cols] into ``codes``, ``scales`` and, if given, ``zeros`` (shapes: hbp_q4_shapes)."""
-    L = _start()
+    L, device = _start()
     assert w.dtype in _types and w.dim() == 2, "w: matrix of float32, float16 or bfloat16 required"
-    m = _matrix(codes, scales, zeros, w.shape[1], group)
-    at, ld = _rows(w, "w", (m.n_rows, m.n_cols), w.dtype)
+    m = _matrix(codes, scales, zeros, w.shape[1], group, device)
+    at, ld = _rows(w, "w", (m.n_rows, m.n_cols), w.dtype, device)
     _core._check(L.hbp_q4_pack(m, _types[w.dtype], at, ld, _core._stream_ptr(stream)), "hbp_q4_pack")
 
 
 def hbp_q4_unpack(codes, scales, n_cols: int, group: int = 128, zeros=None, out=None, stream=None):
     """The values that the codes stand for [rows, n_cols]: in ``out``, or in a new float32 tensor."""
-    import torch
-    L = _start()
-    m = _matrix(codes, scales, zeros, n_cols, group)
+    L, device = _start()
+    m = _matrix(codes, scales, zeros, n_cols, group, device)
     if out is None:
-        out = torch.empty(codes.shape[0], n_cols, dtype=torch.float32, device=codes.device)
+        with _on(stream):
+            out = _torch.empty(codes.shape[0], n_cols, dtype=_torch.float32, device="cuda")
     assert out.dtype in _types, "out: float32, float16 or bfloat16 required"
-    at, ld = _rows(out, "out", (m.n_rows, m.n_cols), out.dtype)
+    at, ld = _rows(out, "out", (m.n_rows, m.n_cols), out.dtype, device)
     _core._check(L.hbp_q4_unpack(m, _types[out.dtype], at, ld, _core._stream_ptr(stream)), "hbp_q4_unpack")
     return out
 
 
-def _vectors(x, y):
-    assert x.dtype in _types and y.dtype == x.dtype and x.dim() in (1, 2) and x.dim() == y.dim(), \
-        "x and y: one vector each, or as many rows, of one type (float32, float16 or bfloat16) required"
-    if x.dim() == 1:
-        return x.unsqueeze(0), y.unsqueeze(0)
-    return x, y
+def _vectors(x, y, n_x, n_y, device):
+    """(type, address and row stride of x and of y, how many vectors)"""
+    dtype = x.dtype
+    assert dtype in _types, "x: float32, float16 or bfloat16 required"
+    one = x.dim() == 1
+    count = 1 if one else x.shape[0]
+    x_at, ldx = _rows(x, "x", (n_x,) if one else (count, n_x), dtype, device)
+    y_at, ldy = _rows(y, "y", (n_y,) if one else (count, n_y), dtype, device)
+    return _types[dtype], x_at, ldx, y_at, ldy, count
 
 
 def hbp_q4_mv(codes, scales, x, y, group: int = 128, zeros=None, stream=None) -> None:
     """y = x W^T with the 4-bit matrix W [rows, cols]: ``x`` [cols] and ``y`` [rows], or [vectors, cols] and [vectors, rows]."""
-    L = _start()
-    x, y = _vectors(x, y)
-    m = _matrix(codes, scales, zeros, x.shape[1], group)
-    count = x.shape[0]
-    x_at, ldx = _rows(x, "x", (count, m.n_cols), x.dtype)
-    y_at, ldy = _rows(y, "y", (count, m.n_rows), x.dtype)
-    status = L.hbp_q4_mv(m, _types[x.dtype], x_at, ldx, y_at, ldy, count, _core._stream_ptr(stream))
+    L, device = _start()
+    m = _matrix(codes, scales, zeros, x.shape[-1], group, device)
+    status = L.hbp_q4_mv(m, *_vectors(x, y, m.n_cols, m.n_rows, device), _core._stream_ptr(stream))
     if status:
         raise _core.HbpError(status, "hbp_q4_mv")
 
@@ -153,54 +166,47 @@ def hbp_q4_mv(codes, scales, x, y, group: int = 128, zeros=None, stream=None) ->
 def _mv_t_bytes(n_rows, n_cols, group, scale_type, vectors):
     need = ctypes.c_size_t()
     m = hbp_q4_matrix_t(4096, 4096, None, n_rows, n_cols, group, scale_type)  # (sizes alone are looked at)
-    _core._check(_start().hbp_q4_mv_t_workspace(m, vectors, need), "hbp_q4_mv_t_workspace")
+    _core._check(_core.lib().hbp_q4_mv_t_workspace(m, vectors, need), "hbp_q4_mv_t_workspace")
     return need.value
 
 
 def hbp_q4_mv_t(codes, scales, x, y, group: int = 128, zeros=None, workspace=None, stream=None) -> None:
     """y = x W with the 4-bit matrix W [rows, cols], the gradient of hbp_q4_mv for its x: ``x`` [rows] and ``y`` [cols], or [vectors,
     rows] and [vectors, cols]."""
-    L = _start()
-    x, y = _vectors(x, y)
-    m = _matrix(codes, scales, zeros, y.shape[1], group)
-    count = x.shape[0]
-    x_at, ldx = _rows(x, "x", (count, m.n_rows), x.dtype)
-    y_at, ldy = _rows(y, "y", (count, m.n_cols), x.dtype)
-    at, size, kept = _space(workspace, _mv_t_bytes(m.n_rows, m.n_cols, group, m.scale_type, count), stream)
-    status = L.hbp_q4_mv_t(m, _types[x.dtype], x_at, ldx, y_at, ldy, count, at, size, _core._stream_ptr(stream))
+    L, device = _start()
+    m = _matrix(codes, scales, zeros, y.shape[-1], group, device)
+    v = _vectors(x, y, m.n_rows, m.n_cols, device)
+    at, size, kept = _space(workspace, _mv_t_bytes(m.n_rows, m.n_cols, group, m.scale_type, v[5]), stream, device)
+    status = L.hbp_q4_mv_t(m, *v, at, size, _core._stream_ptr(stream))
     if status:
         raise _core.HbpError(status, "hbp_q4_mv_t")
 
 
 # ------------------------------------------------------------------------------------ residual norms
 
-def _norms(shape, dtype, w_post, w_pre, gate, scale, eps):
+def _norms(shape, dtype, w_post, w_pre, gate, scale, eps, device):
     assert dtype in _types and len(shape) == 2, "h: matrix of float32, float16 or bfloat16 required"
-    kind, at, ldg = GATE_NONE, None, 0
+    kind, at, ldg, wide = GATE_NONE, None, 0, (shape[1],)
     if gate is not None:
         if gate.dim() == 1:
-            kind, at = GATE_CHANNEL, _whole(gate, "gate", shape[1:], dtype)
+            kind, at = GATE_CHANNEL, _whole(gate, "gate", wide, dtype, device)
         elif gate.shape[1] == 1 and shape[1] != 1:
-            kind, at = GATE_TOKEN, _whole(gate, "gate", (shape[0], 1), dtype)
+            kind, at = GATE_TOKEN, _whole(gate, "gate", (shape[0], 1), dtype, device)
         else:
             kind = GATE_FULL
-            at, ldg = _rows(gate, "gate", shape, dtype)
-    return hbp_norms_t(shape[0], shape[1], _types[dtype], kind, _whole(w_post, "w_post", shape[1:], dtype), _whole(w_pre, "w_pre", shape[1:], dtype),
+            at, ldg = _rows(gate, "gate", shape, dtype, device)
+    return hbp_norms_t(shape[0], shape[1], _types[dtype], kind, _whole(w_post, "w_post", wide, dtype, device), _whole(w_pre, "w_pre", wide, dtype, device),
                        at, ldg, scale, eps)
 
 
 def hbp_residual_norms(h, y, h_out, x_out, rstd=None, w_post=None, w_pre=None, gate=None, scale: float = 1.0, eps: float = 1e-6, stream=None) -> None:
     """h_out = h + scale gate norm(y) w_post, x_out = norm(h_out) w_pre, row by row of [tokens, width].  ``gate``: None, [width], [tokens, 1]
     or [tokens, width]; ``rstd`` float32 [tokens, 2]: both norms' factors, for the backward call."""
-    import torch
-    L = _start()
-    shape, dtype = tuple(h.shape), h.dtype
-    n = _norms(shape, dtype, w_post, w_pre, gate, scale, eps)
-    h_at, ldh = _rows(h, "h", shape, dtype)
-    y_at, ldy = _rows(y, "y", shape, dtype)
-    ho_at, ldho = _rows(h_out, "h_out", shape, dtype)
-    xo_at, ldxo = _rows(x_out, "x_out", shape, dtype)
-    status = L.hbp_residual_norms(n, h_at, ldh, y_at, ldy, ho_at, ldho, xo_at, ldxo, _whole(rstd, "rstd", (shape[0], 2), torch.float32),
+    L, device = _start()
+    shape, dtype = h.shape, h.dtype
+    n = _norms(shape, dtype, w_post, w_pre, gate, scale, eps, device)
+    status = L.hbp_residual_norms(n, *_rows(h, "h", shape, dtype, device), *_rows(y, "y", shape, dtype, device), *_rows(h_out, "h_out", shape, dtype, device),
+                                  *_rows(x_out, "x_out", shape, dtype, device), _whole(rstd, "rstd", (shape[0], 2), _f32, device),
                                   _core._stream_ptr(stream))
     if status:
         raise _core.HbpError(status, "hbp_residual_norms")
@@ -210,7 +216,7 @@ def hbp_residual_norms(h, y, h_out, x_out, rstd=None, w_post=None, w_pre=None, g
 def _norms_bytes(tokens, width, dtype_number):
     need = ctypes.c_size_t()
     n = hbp_norms_t(tokens, width, dtype_number, GATE_NONE, None, None, None, 0, 1.0, 1.0)  # (sizes alone are looked at)
-    _core._check(_start().hbp_residual_norms_backward_workspace(n, need), "hbp_residual_norms_backward_workspace")
+    _core._check(_core.lib().hbp_residual_norms_backward_workspace(n, need), "hbp_residual_norms_backward_workspace")
     return need.value
 
 
@@ -218,67 +224,61 @@ def hbp_residual_norms_backward(d_h_out, d_x_out, h, y, rstd, d_h, d_y, d_w_post
                                 gate=None, scale: float = 1.0, workspace=None, stream=None) -> None:
     """Gradients of hbp_residual_norms from those of its outputs (either may be None: zero), its inputs and ``rstd``.  ``d_w_post``, ``d_w_pre``
     and the ``d_gate`` of a [width] or [tokens, 1] gate are float32, that of a full gate has its type (and row stride)."""
-    import torch
-    L = _start()
-    shape, dtype = tuple(h.shape), h.dtype
-    n = _norms(shape, dtype, w_post, w_pre, gate, scale, 1.0)
-    dho_at, lddho = (None, 0) if d_h_out is None else _rows(d_h_out, "d_h_out", shape, dtype)
-    dxo_at, lddxo = (None, 0) if d_x_out is None else _rows(d_x_out, "d_x_out", shape, dtype)
-    h_at, ldh = _rows(h, "h", shape, dtype)
-    y_at, ldy = _rows(y, "y", shape, dtype)
-    dh_at, lddh = _rows(d_h, "d_h", shape, dtype)
-    dy_at, lddy = _rows(d_y, "d_y", shape, dtype)
-    dg_at = None
+    L, device = _start()
+    shape, dtype = h.shape, h.dtype
+    n = _norms(shape, dtype, w_post, w_pre, gate, scale, 1.0, device)
+    wide, dg_at = (shape[1],), None
     if d_gate is not None:
         assert gate is not None, "d_gate: no gate was given"
         if n.gate_kind == GATE_FULL:
-            dg_at, lddg = _rows(d_gate, "d_gate", shape, dtype)
+            dg_at, lddg = _rows(d_gate, "d_gate", shape, dtype, device)
             assert lddg == n.ldg, "d_gate: the gate's row stride required"
         else:
-            dg_at = _whole(d_gate, "d_gate", tuple(gate.shape), torch.float32)
-    at, size, kept = _space(workspace, _norms_bytes(n.tokens, n.width, n.type), stream)
-    f32 = torch.float32
-    status = L.hbp_residual_norms_backward(n, dho_at, lddho, dxo_at, lddxo, h_at, ldh, y_at, ldy, _whole(rstd, "rstd", (shape[0], 2), f32), dh_at, lddh,
-                                           dy_at, lddy, _whole(d_w_post, "d_w_post", shape[1:], f32), _whole(d_w_pre, "d_w_pre", shape[1:], f32), dg_at,
-                                           at, size, _core._stream_ptr(stream))
+            dg_at = _whole(d_gate, "d_gate", gate.shape, _f32, device)
+    none = (None, 0)
+    at, size, kept = _space(workspace, _norms_bytes(n.tokens, n.width, n.type), stream, device)
+    status = L.hbp_residual_norms_backward(
+        n, *(none if d_h_out is None else _rows(d_h_out, "d_h_out", shape, dtype, device)),
+        *(none if d_x_out is None else _rows(d_x_out, "d_x_out", shape, dtype, device)), *_rows(h, "h", shape, dtype, device),
+        *_rows(y, "y", shape, dtype, device), _whole(rstd, "rstd", (shape[0], 2), _f32, device), *_rows(d_h, "d_h", shape, dtype, device),
+        *_rows(d_y, "d_y", shape, dtype, device), _whole(d_w_post, "d_w_post", wide, _f32, device), _whole(d_w_pre, "d_w_pre", wide, _f32, device), dg_at,
+        at, size, _core._stream_ptr(stream))
     if status:
         raise _core.HbpError(status, "hbp_residual_norms_backward")
 
 
 # ------------------------------------------------------------------------------------ token log probabilities
 
-def _ids(tokens, count):
-    import torch
+def _ids(tokens, count, device):
     if tokens is None:
         return None, 0
-    assert tokens.dtype in (torch.int32, torch.int64), "tokens: int32 or int64 required"
-    return _whole(tokens, "tokens", (count,), tokens.dtype), tokens.element_size()
+    kind = tokens.dtype
+    assert kind is _i64 or kind is _i32, "tokens: int32 or int64 required"
+    return _whole(tokens, "tokens", (count,), kind, device), 8 if kind is _i64 else 4
 
 
 @functools.lru_cache(maxsize=1024)
 def _logprobs_bytes(dtype_number, tokens, vocabulary, top):
     need = ctypes.c_size_t()
-    _core._check(_start().hbp_token_logprobs_workspace(dtype_number, tokens, vocabulary, top, need), "hbp_token_logprobs_workspace")
+    _core._check(_core.lib().hbp_token_logprobs_workspace(dtype_number, tokens, vocabulary, top, need), "hbp_token_logprobs_workspace")
     return need.value
 
 
 def hbp_token_logprobs(logits, tokens, logp=None, entropy=None, lse=None, top_ids=None, top_logp=None, workspace=None, stream=None) -> None:
     """Of every row of ``logits`` [n, vocabulary]: the log probability of its token (``tokens`` [n], int32 or int64, negative: none), the entropy, the
     logarithm of the sum of exponentials (float32 [n] each) and the ``top_ids`` (int32) with their ``top_logp`` (float32), both [n, top]."""
-    import torch
-    L = _start()
-    assert logits.dtype in _types and logits.dim() == 2, "logits: matrix of float32, float16 or bfloat16 required"
-    count, vocabulary = logits.shape
-    z_at, ldz = _rows(logits, "logits", (count, vocabulary), logits.dtype)
-    ids_at, id_bytes = _ids(tokens, count)
+    L, device = _start()
+    shape, dtype = logits.shape, logits.dtype
+    assert dtype in _types and len(shape) == 2, "logits: matrix of float32, float16 or bfloat16 required"
+    count, vocabulary = shape
     assert (top_ids is None) == (top_logp is None), "top_ids and top_logp go together"
     top = 0 if top_ids is None else top_ids.shape[1]
-    f32 = torch.float32
-    number = _types[logits.dtype]
-    at, size, kept = _space(workspace, _logprobs_bytes(number, count, vocabulary, top), stream)
-    status = L.hbp_token_logprobs(number, z_at, ldz, count, vocabulary, ids_at, id_bytes, _whole(logp, "logp", (count,), f32),
-                                  _whole(entropy, "entropy", (count,), f32), _whole(lse, "lse", (count,), f32), top,
-                                  _whole(top_ids, "top_ids", (count, top), torch.int32), _whole(top_logp, "top_logp", (count, top), f32), at, size,
+    number, each, best = _types[dtype], (count,), (count, top)
+    at, size, kept = _space(workspace, _logprobs_bytes(number, count, vocabulary, top), stream, device)
+    z_at, ldz = _rows(logits, "logits", shape, dtype, device)
+    status = L.hbp_token_logprobs(number, z_at, ldz, count, vocabulary, *_ids(tokens, count, device), _whole(logp, "logp", each, _f32, device),
+                                  _whole(entropy, "entropy", each, _f32, device), _whole(lse, "lse", each, _f32, device), top,
+                                  _whole(top_ids, "top_ids", best, _i32, device), _whole(top_logp, "top_logp", best, _f32, device), at, size,
                                   _core._stream_ptr(stream))
     if status:
         raise _core.HbpError(status, "hbp_token_logprobs")
@@ -287,16 +287,15 @@ def hbp_token_logprobs(logits, tokens, logp=None, entropy=None, lse=None, top_id
 def hbp_token_logprobs_backward(logits, tokens, lse, entropy, g_logp, g_entropy, d_logits, stream=None) -> None:
     """The gradient for ``logits``, of their type, from those of logp and entropy (float32 [n], either may be None: zero) and the forward call's
     ``lse`` and ``entropy``.  ``d_logits`` may be ``logits``."""
-    import torch
-    L = _start()
-    assert logits.dtype in _types and logits.dim() == 2, "logits: matrix of float32, float16 or bfloat16 required"
-    count, vocabulary = logits.shape
-    z_at, ldz = _rows(logits, "logits", (count, vocabulary), logits.dtype)
-    d_at, ldd = _rows(d_logits, "d_logits", (count, vocabulary), logits.dtype)
-    ids_at, id_bytes = _ids(tokens, count)
-    f32 = torch.float32
-    status = L.hbp_token_logprobs_backward(_types[logits.dtype], z_at, ldz, count, vocabulary, ids_at, id_bytes, _whole(lse, "lse", (count,), f32),
-                                           _whole(entropy, "entropy", (count,), f32), _whole(g_logp, "g_logp", (count,), f32),
-                                           _whole(g_entropy, "g_entropy", (count,), f32), d_at, ldd, _core._stream_ptr(stream))
+    L, device = _start()
+    shape, dtype = logits.shape, logits.dtype
+    assert dtype in _types and len(shape) == 2, "logits: matrix of float32, float16 or bfloat16 required"
+    count, vocabulary = shape
+    each = (count,)
+    z_at, ldz = _rows(logits, "logits", shape, dtype, device)
+    status = L.hbp_token_logprobs_backward(_types[dtype], z_at, ldz, count, vocabulary, *_ids(tokens, count, device), _whole(lse, "lse", each, _f32, device),
+                                           _whole(entropy, "entropy", each, _f32, device), _whole(g_logp, "g_logp", each, _f32, device),
+                                           _whole(g_entropy, "g_entropy", each, _f32, device), *_rows(d_logits, "d_logits", shape, dtype, device),
+                                           _core._stream_ptr(stream))
     if status:
         raise _core.HbpError(status, "hbp_token_logprobs_backward")
