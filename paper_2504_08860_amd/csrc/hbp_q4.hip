@@ -77,43 +77,185 @@ template <typename T, typename S> __global__ __launch_bounds__(256) void k_q4_un
     out.store_first(static_cast<T *>(w) + row * ldw + col, left);
 }
 
-// transposed: a thread per eight columns and vector, over a part of the rows; the parts are summed by a second kernel
-template <typename T, typename S> __global__ __launch_bounds__(256) void k_q4_mv_t(Q4 a, const void *x_, int64_t ldx, float *partial, int64_t vectors, int64_t part)
-{
-    const int64_t col = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 8;
-    if (col >= a.n_cols) return;
-    const int64_t begin = blockIdx.y * part, end = min(begin + part, (int64_t)a.n_rows);
-    const int group = (int)(col >> a.shift);
-    for (int64_t m = 0; m < vectors; m++) {
-        const T *x = static_cast<const T *>(x_) + m * ldx;
-        float acc[8] = {};
-        for (int64_t r = begin; r < end; r++) {
-            const uint32_t word = *reinterpret_cast<const uint32_t *>(a.codes + r * a.pitch + col / 2);
-            const float zero = zero_of<S>(a, r, group), u = scale_of<S>(a, r, group) * to_f32(x[r]);
+// y = x W, the transposed product.  A lane takes C neighbouring columns (of one group) and adds code * (scale x) row by row, in fp32, for up to M vectors;
+// what the zero points take away, zero (scale x), is one sum for all C.  A wavefront has 64 C columns and every eighth batch of kRows rows of its
+// workgroup's part; the wavefronts are added up by LDS, the parts by a second kernel.
+//
+// Bound: vector instructions, 1.4 + M a weight (a conversion for each code and an fma for each vector; 39 T lanes/s).  Not by the matrix cores: there the scale, which
+// differs from row to row, would have to go into x, in parts, for every group anew.
+// As in the products, code * (scale x) may be infinite where the sum is not: such results are computed again from the definition.
+constexpr int kTransposedWaves = 8, kTransposedRows = 1024;  // rows whose x lies in LDS at a time
+// What a lane loads of ROWS rows.
+template <typename S, bool ZERO, int C, int ROWS> struct Rows {
+    uint32_t w[ROWS][C / 8];
+    S scale[ROWS], zero[ZERO ? ROWS : 1];
+    // at: bytes of the lane's columns in a row of codes; scale_at: of its group in a row of scales
+    __device__ __forceinline__ void load(const Q4 &a, int64_t row0, int r, int rows, uint32_t at, uint32_t scale_at)
+    {
+        const int64_t apart = (int64_t)a.groups * (int64_t)sizeof(S);
+        const uint8_t *codes = a.codes + (row0 + r) * a.pitch;
+        const char *scales = static_cast<const char *>(a.scales) + (row0 + r) * apart, *zeros = static_cast<const char *>(a.zeros) + (row0 + r) * apart;
 #pragma unroll
-            for (int i = 0; i < 8; i++) acc[i] += ((float)(word >> 4 * i & 15u) - zero) * u;
+        for (int i = 0; i < ROWS; i++) {
+            if constexpr (C == 16) {
+                const uint2 two = *reinterpret_cast<const uint2 *>(codes + at);
+                w[i][0] = two.x;
+                w[i][1] = two.y;
+            } else {
+                w[i][0] = *reinterpret_cast<const uint32_t *>(codes + at);
+            }
+            scale[i] = *reinterpret_cast<const S *>(scales + scale_at);
+            if constexpr (ZERO) zero[i] = *reinterpret_cast<const S *>(zeros + scale_at);
+            const bool more = r + i + 1 < rows;  // (behind the last row it is read again: x is 0 there)
+            codes += more ? a.pitch : 0;
+            scales += more ? apart : 0;
+            if constexpr (ZERO) zeros += more ? apart : 0;
         }
+    }
+    template <int M> __device__ __forceinline__ void add(const float *x, int apart, float (&acc)[M][C], float (&taken)[M]) const
+    {
 #pragma unroll
-        for (int i = 0; i < 8; i++)
-            if (col + i < a.n_cols) partial[(blockIdx.y * vectors + m) * a.n_cols + col + i] = acc[i];
+        for (int i0 = 0; i0 < ROWS; i0 += 4) {
+            float4 x4[M];
+#pragma unroll
+            for (int m = 0; m < M; m++) x4[m] = *reinterpret_cast<const float4 *>(x + m * apart + i0);
+#pragma unroll
+            for (int k = 0; k < 4; k++) {
+                const int i = i0 + k;
+                const float s = to_f32(scale[i]);
+                float f[C];
+#pragma unroll
+                for (int j = 0; j < C / 8; j++) {
+                    const uint32_t even = w[i][j] & 0x0f0f0f0fu, odd = w[i][j] >> 4 & 0x0f0f0f0fu;
+#pragma unroll
+                    for (int b = 0; b < 4; b++) {
+                        f[8 * j + 2 * b] = (float)(even >> 8 * b & 255u);
+                        f[8 * j + 2 * b + 1] = (float)(odd >> 8 * b & 255u);
+                    }
+                }
+#pragma unroll
+                for (int m = 0; m < M; m++) {
+                    const float u = s * (k == 0 ? x4[m].x : k == 1 ? x4[m].y : k == 2 ? x4[m].z : x4[m].w);
+                    taken[m] += ZERO ? u * to_f32(zero[ZERO ? i : 0]) : u;
+#pragma unroll
+                    for (int c = 0; c < C; c++) acc[m][c] += f[c] * u;
+                }
+            }
+        }
+    }
+};
+
+template <typename T, typename S, bool ZERO, int M, int C, int ROWS>
+__global__ __launch_bounds__(kTransposedWaves * kWave) void k_q4_mv_t(Q4 a, const void *x_, int64_t ldx, float *partial, int64_t vectors, int64_t part)
+{
+    extern __shared__ float4 lds4[];
+    float *lds = reinterpret_cast<float *>(lds4);  // x of up to kTransposedRows rows of the part, [M][apart]; then the sums of one vector, [wavefront][64 C]
+    const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    const int64_t vector0 = (int64_t)blockIdx.z * M;
+    const int64_t part0 = (int64_t)blockIdx.y * part, end = min(part0 + part, (int64_t)a.n_rows);
+    const int apart = (int)min(part, (int64_t)kTransposedRows);
+    const T *x = static_cast<const T *>(x_);
+    const int col = blockIdx.x * (kWave * C) + lane * C;
+    const uint32_t at = min(col, (int)(a.pitch * 2) - C) / 2;  // (lanes behind the last column read its codes again)
+    const uint32_t scale_at = min(col >> a.shift, a.groups - 1) * sizeof(S);
+    float acc[M][C] = {}, taken[M] = {};
+    constexpr int kStep = kTransposedWaves * ROWS;
+    for (int64_t row0 = part0; row0 < end; row0 += apart) {
+        const int rows = (int)min((int64_t)apart, end - row0);
+        Rows<S, ZERO, C, ROWS> one, two;
+        int r = wave * ROWS;
+        if (r < rows) one.load(a, row0, r, rows, at, scale_at);
+        if (row0 > part0) __syncthreads();
+#pragma unroll
+        for (int m = 0; m < M; m++)
+            for (int i = threadIdx.x; i < apart; i += blockDim.x) lds[m * apart + i] = vector0 + m < vectors && i < rows ? to_f32(x[(vector0 + m) * ldx + row0 + i]) : 0.0f;
+        __syncthreads();
+        for (; r < rows; r += 2 * kStep) {  // (the next rows' loads are issued before this one's are waited for)
+            if (r + kStep < rows) two.load(a, row0, r + kStep, rows, at, scale_at);
+            one.template add<M>(lds + r, apart, acc, taken);
+            if (r + kStep < rows) {
+                if (r + 2 * kStep < rows) one.load(a, row0, r + 2 * kStep, rows, at, scale_at);
+                two.template add<M>(lds + r + kStep, apart, acc, taken);
+            }
+        }
+    }
+#pragma unroll
+    for (int m = 0; m < M; m++) {
+        __syncthreads();
+#pragma unroll
+        for (int c = 0; c < C; c += 4) {
+            const float off = ZERO ? taken[m] : 8.0f * taken[m];
+            reinterpret_cast<float4 *>(lds)[(wave * (kWave * C) + lane * C + c) / 4] = float4{acc[m][c] - off, acc[m][c + 1] - off, acc[m][c + 2] - off, acc[m][c + 3] - off};
+        }
+        __syncthreads();
+        if (vector0 + m < vectors)
+            for (int c = threadIdx.x; c < kWave * C; c += blockDim.x) {
+                float sum = 0;
+#pragma unroll
+                for (int w = 0; w < kTransposedWaves; w++) sum += lds[w * (kWave * C) + c];
+                const int64_t k = (int64_t)blockIdx.x * (kWave * C) + c;
+                if (k < a.n_cols) partial[((int64_t)blockIdx.y * vectors + vector0 + m) * a.n_cols + k] = sum;
+            }
     }
 }
 
-template <typename T> __global__ __launch_bounds__(256) void k_q4_sum_parts(const float *partial, int parts, int64_t vectors, int64_t n_cols, void *y, int64_t ldy)
+// The parts' sum, in their order; a wavefront has 64 columns of one vector.
+template <typename T, typename S> __global__ __launch_bounds__(256) void k_q4_sum_parts(Q4 a, const void *x_, int64_t ldx, const float *partial, int parts, int64_t vectors, void *y, int64_t ldy)
 {
-    const int64_t col = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (col >= n_cols) return;
-    for (int64_t m = blockIdx.y; m < vectors; m += gridDim.y) {
-        float sum = 0;
-        for (int p = 0; p < parts; p++) sum += partial[(p * vectors + m) * n_cols + col];
-        static_cast<T *>(y)[m * ldy + col] = from_f32<T>(sum);
+    const int lane = threadIdx.x % kWave;
+    const int64_t m = (int64_t)blockIdx.y * 4 + threadIdx.x / kWave;
+    if (m >= vectors) return;
+    const int64_t col = (int64_t)blockIdx.x * kWave + lane;
+    const bool mine = col < a.n_cols;
+    float sum = 0;
+    if (mine) {
+        const float *at = partial + m * a.n_cols + col;
+        const int64_t apart = vectors * a.n_cols;
+        int i = 0;
+        for (; i + 8 <= parts; i += 8) {
+            float v[8];
+#pragma unroll
+            for (int k = 0; k < 8; k++) v[k] = at[(i + k) * apart];
+#pragma unroll
+            for (int k = 0; k < 8; k++) sum += v[k];
+        }
+        for (; i < parts; i++) sum += at[i * apart];
     }
+    uint64_t again = __ballot(mine && !(fabsf(sum) < INFINITY));
+    while (again) {  // from the definition, by the whole wavefront
+        const int from = __builtin_ctzll(again);
+        again &= again - 1;
+        const int64_t k = (int64_t)blockIdx.x * kWave + from;
+        float exact = 0;
+        for (int64_t r = lane; r < a.n_rows; r += kWave) {
+            const float q = (float)(a.codes[r * a.pitch + k / 2] >> (k & 1) * 4 & 15);
+            exact += scale_of<S>(a, r, (int)(k >> a.shift)) * (q - zero_of<S>(a, r, (int)(k >> a.shift))) * to_f32(static_cast<const T *>(x_)[m * ldx + r]);
+        }
+        exact = wave_sum(exact);
+        if (lane == from) sum = exact;
+    }
+    if (mine) static_cast<T *>(y)[m * ldy + col] = from_f32<T>(sum);
 }
 
-int parts_of(const Q4 &a)
+// How a transposed product is cut: vectors, columns and rows at a time a lane takes, rows of a part.  Enough parts that every compute unit has two
+// workgroups, none of fewer rows than its wavefronts take at a time.
+struct TransposedShape {
+    int m, c, rows;
+    int64_t part, wide, parts;
+};
+TransposedShape transposed_shape(const Q4 &a, int64_t vectors)
 {
-    const int64_t wide = (a.n_cols + 2047) / 2048, wanted = (1024 + wide - 1) / wide, most = (a.n_rows + 31) / 32;
-    return (int)(wanted < most ? wanted : most);
+    TransposedShape s;
+    s.m = vectors <= 1 ? 1 : vectors <= 2 ? 2 : vectors <= 4 ? 4 : 8;
+    s.c = s.m <= 2 ? 16 : 8;
+    s.rows = 8;
+    s.wide = (a.n_cols + kWave * s.c - 1) / (kWave * s.c);
+    const int64_t passes = (vectors + s.m - 1) / s.m, least = s.rows * kTransposedWaves;
+    const int64_t most = (a.n_rows + least - 1) / least, wanted = (512 + s.wide * passes - 1) / (s.wide * (passes > 0 ? passes : 1));
+    s.parts = wanted < most ? wanted : most;
+    s.part = ((a.n_rows + s.parts - 1) / s.parts + least - 1) / least * least;
+    s.parts = (a.n_rows + s.part - 1) / s.part;
+    return s;
 }
 
 int view(const hbp_q4_matrix_t *m, Q4 *a)
@@ -206,7 +348,7 @@ int hbp_q4_mv_t_workspace(const hbp_q4_matrix_t *m, int64_t vectors, size_t *byt
     const int rc = view(m, &a);
     if (rc != HBP_OK) return rc;
     if (!bytes || vectors < 0) return HBP_ERR_INVALID_ARGUMENT;
-    *bytes = (size_t)parts_of(a) * (size_t)vectors * (size_t)a.n_cols * sizeof(float);
+    *bytes = (size_t)transposed_shape(a, vectors).parts * (size_t)vectors * (size_t)a.n_cols * sizeof(float);
     return HBP_OK;
 }
 
@@ -223,17 +365,37 @@ int hbp_q4_mv_t(const hbp_q4_matrix_t *m, int type, const void *x, int64_t ldx, 
     if (need && (!workspace || workspace_bytes < need || !aligned(workspace, 256))) return HBP_ERR_INVALID_ARGUMENT;
     rc = earlier_error();
     if (rc != HBP_OK) return rc;
-    const int parts = parts_of(a);
-    const int64_t part = (a.n_rows + parts - 1) / parts;
-    const unsigned wide = (unsigned)((a.n_cols + 2047) / 2048);
+    const TransposedShape s = transposed_shape(a, vectors);
     float *partial = static_cast<float *>(workspace);
+    hipStream_t st = (hipStream_t)stream;
     return by_type(type, [&](auto t) -> int {
-        return by_type(m->scale_type, [&](auto s) -> int {
-            k_q4_mv_t<decltype(t), decltype(s)><<<dim3(wide, parts), 256, 0, (hipStream_t)stream>>>(a, x, ldx, partial, vectors, part);
-            HBP_HIP(hipGetLastError());
-            k_q4_sum_parts<decltype(t)><<<dim3((unsigned)((a.n_cols + 255) / 256), (unsigned)(vectors < 64 ? vectors : 64)), 256, 0, (hipStream_t)stream>>>(
-                partial, parts, vectors, a.n_cols, y, ldy);
-            HBP_HIP(hipGetLastError());
+        return by_type(m->scale_type, [&](auto scale) -> int {
+            using T = decltype(t);
+            using S = decltype(scale);
+            constexpr int64_t kPasses = 32768;
+            for (int64_t first = 0; first < vectors; first += kPasses * s.m) {  // (the grid's third dimension ends at 65535)
+                const int64_t count = vectors - first < kPasses * s.m ? vectors - first : kPasses * s.m;
+                const dim3 grid((unsigned)s.wide, (unsigned)s.parts, (unsigned)((count + s.m - 1) / s.m));
+                const size_t x_bytes = (size_t)s.m * (s.part < kTransposedRows ? s.part : kTransposedRows) * 4, sum_bytes = (size_t)kTransposedWaves * kWave * s.c * 4;
+                const size_t bytes = x_bytes > sum_bytes ? x_bytes : sum_bytes;
+                const T *x_at = static_cast<const T *>(x) + first * ldx;
+                auto go = [&](auto kernel) { kernel<<<grid, kTransposedWaves * kWave, bytes, st>>>(a, x_at, ldx, partial, count, s.part); };
+                if (a.zeros) {
+                    if (s.m == 1) go(k_q4_mv_t<T, S, true, 1, 16, 8>);
+                    else if (s.m == 2) go(k_q4_mv_t<T, S, true, 2, 16, 8>);
+                    else if (s.m == 4) go(k_q4_mv_t<T, S, true, 4, 8, 8>);
+                    else go(k_q4_mv_t<T, S, true, 8, 8, 8>);
+                } else {
+                    if (s.m == 1) go(k_q4_mv_t<T, S, false, 1, 16, 8>);
+                    else if (s.m == 2) go(k_q4_mv_t<T, S, false, 2, 16, 8>);
+                    else if (s.m == 4) go(k_q4_mv_t<T, S, false, 4, 8, 8>);
+                    else go(k_q4_mv_t<T, S, false, 8, 8, 8>);
+                }
+                HBP_HIP(hipGetLastError());
+                k_q4_sum_parts<T, S><<<dim3((unsigned)((a.n_cols + kWave - 1) / kWave), (unsigned)((count + 3) / 4)), 256, 0, st>>>(
+                    a, x_at, ldx, partial, (int)s.parts, count, static_cast<T *>(y) + first * ldy, ldy);
+                HBP_HIP(hipGetLastError());
+            }
             return HBP_OK;
         });
     });
