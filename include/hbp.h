@@ -390,7 +390,7 @@ int hbp_residual_norms_backward_workspace(const hbp_norms_t *n, size_t *bytes);
  *          top > 0: the largest logits in descending order, among equal ones the lowest index first (NaN counts as larger than
  *          any number, -0 equals 0)
  * A logit of -inf is a masked token: p = 0, logp -inf, no part in the entropy, no gradient.  A row with nothing else: lse = -inf, every logp
- * -inf, entropy 0, gradient 0.  A row with a NaN or +inf: lse, logp and entropy NaN.  vocabulary at most 2^31 - 512.  tokens = 0 does nothing. */
+ * -inf, entropy 0, gradient 0.  A row with a NaN or +inf: lse, logp and entropy NaN.  vocabulary at most 2^30.  tokens = 0 does nothing. */
 int hbp_token_logprobs(int type, const void *logits, int64_t ldz, int64_t tokens, int64_t vocabulary, const void *ids, int id_bytes, float *logp,
                        float *entropy, float *lse, int top, int32_t *top_ids, float *top_logp, void *workspace, size_t workspace_bytes, void *stream);
 int hbp_token_logprobs_workspace(int type, int64_t tokens, int64_t vocabulary, int top, size_t *bytes);

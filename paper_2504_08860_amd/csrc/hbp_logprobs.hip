@@ -5,59 +5,53 @@
 namespace hbp {
 namespace {
 
-// The statistics of a part of a row, with m the largest logit in it, s = sum exp(z - m) and u = sum exp(z - m) (z - m), so that
-// lse = m + log s and the entropy is log s - u / s.  A part without an unmasked token has m = -inf, s = u = 0.
+// The statistics of a part of a row, with m the largest logit in it (the lowest number there is: none) and d = (z - m) / log 2: s = sum 2^d and u = sum d 2^d,
+// so that lse = m + log s and the entropy is log s - u log 2 / s.  A part without an unmasked token has s = u = 0.
 struct Stats {
     float m, s, u;
 };
+constexpr float kLowest = -3.4028234663852886e38f, kPerLog2 = 1.4426950408889634f, kLog2 = 0.6931471805599453f;
+constexpr float kFar = -1000.0f;  // 2 to it is 0; stands for what lies further down, where 0 times it has to be 0
 
-__device__ __forceinline__ void add_logit(Stats &a, float z)
+__device__ __forceinline__ void move_to(Stats &a, float m)  // m >= a.m; sums from below: each d grows by the same
 {
-    const float e = __expf(z - a.m);
-    a.s += e;
-    a.u += e > 0.0f ? e * (z - a.m) : 0.0f;  // (0 times -inf: a masked token, or one too far down to count)
-}
-
-__device__ __forceinline__ void move_to(Stats &a, float m)  // m >= a.m
-{
-    if (m == a.m || !(m > -INFINITY)) return;
-    const float d = a.m - m, f = __expf(d);
-    a.u = a.s > 0.0f ? f * (a.u + a.s * d) : a.u * f;  // sums from below: (z - m) = (z - a.m) + d
-    if (f == 0.0f && a.s == a.s) a.u = 0.0f;
+    const float d = fmaxf((a.m - m) * kPerLog2, kFar), f = __builtin_amdgcn_exp2f(d);
+    a.u = f * (a.u + a.s * d);
     a.s *= f;
     a.m = m;
 }
 
-__device__ __forceinline__ Stats join(Stats a, Stats b)
+// (A NaN makes s NaN: the largest logit passes it over, but its own exponential does not.)
+__device__ __forceinline__ void add_eight(Stats &a, const float (&z)[8])
 {
-    const float m = fmaxf(a.m, b.m);
-    const bool nan = !(a.s == a.s) || !(b.s == b.s);
-    move_to(a, m);
-    move_to(b, m);
-    Stats r{m, a.s + b.s, a.u + b.u};
-    if (nan) r.s = NAN;
-    return r;
+    float m = a.m;
+#pragma unroll
+    for (int i = 0; i < 8; i += 2) asm("v_max3_f32 %0, %1, %2, %0" : "+v"(m) : "v"(z[i]), "v"(z[i + 1]));  // (fmaxf would make each value canonical first)
+    if (m > a.m) move_to(a, m);
+#pragma unroll
+    for (int i = 0; i < 8; i++) {
+        // (z / log 2 - m / log 2 would be one instruction, and off by as much as a large m's last bits)
+        const float d = (z[i] - m) * kPerLog2, e = __builtin_amdgcn_exp2f(d);
+        a.s += e;
+        a.u += e * fmaxf(d, kFar);
+    }
 }
 
+// of all lanes, the same in each: the largest logit first, so that each lane's sums are moved once
 __device__ __forceinline__ Stats wave_join(Stats a)
 {
-#pragma unroll
-    for (int d = 1; d < kWave; d *= 2) {
-        Stats b{__shfl_xor(a.m, d), __shfl_xor(a.s, d), __shfl_xor(a.u, d)};
-        a = join(a, b);
-    }
-    return a;
+    move_to(a, wave_max(a.m));
+    return Stats{a.m, wave_sum(a.s), wave_sum(a.u)};
 }
 
-// A logit and its place as one number that is the larger the earlier it comes among the alternatives: descending value, then
-// ascending index.  -0 equals 0, and NaN is the largest.  Below every one of them: 0.
+// A logit as a number that is the larger the earlier it comes among the alternatives: -0 equals 0, NaN is the largest, and none is 0.  With the complement of
+// its index below it, it is an alternative: descending value, then ascending index.
 __device__ __forceinline__ uint32_t order_of(float z)
 {
     z += 0.0f;
     const uint32_t bits = z == z ? __float_as_uint(z) : 0x7fc00000u;
     return bits ^ ((uint32_t)((int32_t)bits >> 31) | 0x80000000u);
 }
-__device__ __forceinline__ uint64_t alternative(float z, uint32_t index) { return (uint64_t)order_of(z) << 32 | (uint32_t)~index; }
 __device__ __forceinline__ float value_of(uint64_t a)
 {
     const uint32_t o = (uint32_t)(a >> 32);
@@ -65,32 +59,7 @@ __device__ __forceinline__ float value_of(uint64_t a)
 }
 __device__ __forceinline__ int32_t index_of(uint64_t a) { return (int32_t)~(uint32_t)a; }
 
-__device__ __forceinline__ uint64_t lane_value(uint64_t v, int lane)
-{
-    return (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(v >> 32), lane) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)v, lane);
-}
-
-// The `top` (up to 64) first alternatives seen by a wavefront, in order, one to a lane.
-struct Best {
-    uint64_t mine = 0, last = 0;  // this lane's; the one that a new one has to beat, the same in every lane
-    __device__ __forceinline__ void offer(uint64_t a, int top)  // one (or 0) from every lane
-    {
-        uint64_t waiting = __ballot(a > last);
-        while (waiting) {
-            const int from = __builtin_ctzll(waiting);
-            waiting &= waiting - 1;
-            const uint64_t v = lane_value(a, from);
-            if (v <= last) continue;
-            const int lane = threadIdx.x % kWave;
-            const int at = __popcll(__ballot(mine > v));
-            const uint64_t above = __shfl_up(mine, 1);
-            mine = lane < at ? mine : lane == at ? v : above;
-            last = lane_value(mine, top - 1);
-        }
-    }
-};
-
-constexpr int kStatThreads = 512, kStatWaves = kStatThreads / kWave;
+constexpr int kMostThreads = 512, kMostWaves = kMostThreads / kWave, kMostTop = kWave;
 
 struct LogprobArgs {
     const void *logits;
@@ -101,7 +70,7 @@ struct LogprobArgs {
     int32_t *top_ids;
     float *top_logp;
     Stats *stats;        // [tokens][parts]
-    uint64_t *best;      // [tokens][parts][top]
+    uint64_t *best;      // [tokens][parts][top], 0 where there are fewer
 };
 
 __device__ __forceinline__ int64_t id_at(const void *ids, int id_bytes, int64_t t)
@@ -109,17 +78,55 @@ __device__ __forceinline__ int64_t id_at(const void *ids, int id_bytes, int64_t 
     return id_bytes == 8 ? static_cast<const int64_t *>(ids)[t] : static_cast<const int32_t *>(ids)[t];
 }
 
-// what a row's results are, from the statistics and alternatives of all of it; one wavefront
-template <typename T> __device__ __forceinline__ void finish_row(const LogprobArgs &p, int64_t t, Stats a, const Best &best)
+// The alternatives in question, in LDS: `count` of them in any order, all different.  What is kept of them is the `top` first, found by counting for each
+// how many come before it.
+template <int MOST> struct Candidates {
+    uint64_t all[MOST], sorted[kMostTop];
+    int count;
+    __device__ __forceinline__ void append(uint64_t a) { all[atomicAdd(&count, 1)] = a; }
+    // all threads, behind a barrier; behind the next one `sorted` holds the first ones (as many as there are, up to top)
+    __device__ __forceinline__ void select(int top)
+    {
+        const int n = count;
+        for (int i = threadIdx.x; i < n; i += blockDim.x) {
+            const uint64_t a = all[i];
+            int before = 0, j = 0;
+            for (; j + 8 <= n; j += 8) {
+                uint64_t b[8];
+#pragma unroll
+                for (int k = 0; k < 8; k++) b[k] = all[j + k];
+#pragma unroll
+                for (int k = 0; k < 8; k++) before += b[k] > a ? 1 : 0;
+            }
+            for (; j < n; j++) before += all[j] > a ? 1 : 0;
+            if (before < top) sorted[before] = a;
+        }
+    }
+};
+
+// The one of the lanes that has `rank` others before it, larger ones and equal ones of lower lanes; 0 where that is none or 0.
+__device__ __forceinline__ uint32_t of_rank(uint32_t a, int rank)
 {
-    const int lane = threadIdx.x % kWave;
-    const bool none = !(a.m > -INFINITY) && a.s == a.s;  // nothing is left
+    int before = 0;
+#pragma unroll 8
+    for (int j = 0; j < kWave; j++) {
+        const uint32_t b = (uint32_t)__builtin_amdgcn_readlane((int)a, j);
+        const uint64_t higher = ~0ull << j << 1;  // lanes above j
+        before += (__ballot(b > a) | (__ballot(b == a) & higher)) >> (threadIdx.x % kWave) & 1;
+    }
+    const uint64_t lanes = __ballot(before == rank);
+    return lanes ? (uint32_t)__builtin_amdgcn_readlane((int)a, __builtin_ctzll(lanes)) : 0;
+}
+
+// what a row's results are, from the statistics and alternatives of all of it
+template <typename T> __device__ __forceinline__ void finish_row(const LogprobArgs &p, int64_t t, Stats a, const uint64_t *sorted)
+{
+    const bool none = a.s == 0.0f;  // nothing is left
     const float log_s = logf(a.s);
     // (a.m + log_s would round away what log_s adds to a large m: differences to m are taken first)
-    const float lse = none ? -INFINITY : a.m + log_s;
-    if (lane == 0) {
-        if (p.lse) p.lse[t] = lse;
-        if (p.entropy) p.entropy[t] = none ? 0.0f : log_s - a.u / a.s;
+    if (threadIdx.x == 0) {
+        if (p.lse) p.lse[t] = none ? -INFINITY : a.m + log_s;
+        if (p.entropy) p.entropy[t] = none ? 0.0f : log_s - kLog2 * (a.u / a.s);
         if (p.logp && p.ids) {
             const int64_t id = id_at(p.ids, p.id_bytes, t);
             float v = 0.0f;
@@ -128,72 +135,169 @@ template <typename T> __device__ __forceinline__ void finish_row(const LogprobAr
             p.logp[t] = v;
         }
     }
-    if (lane < p.top) {
-        p.top_ids[t * p.top + lane] = index_of(best.mine);
-        p.top_logp[t * p.top + lane] = none ? -INFINITY : value_of(best.mine) - a.m - log_s;
+    if ((int)threadIdx.x < p.top) {
+        const uint64_t best = sorted[threadIdx.x];
+        p.top_ids[t * p.top + threadIdx.x] = index_of(best);
+        p.top_logp[t * p.top + threadIdx.x] = none ? -INFINITY : value_of(best) - a.m - log_s;
     }
 }
 
-template <typename T, bool TOP> __global__ __launch_bounds__(kStatThreads) void k_logprobs(LogprobArgs p)
+// One pass over a part of a row: statistics in every lane, eight logits at a time.
+//
+// Alternatives: the threads' eights of one turn are a block.  Whatever is below `least` (as order_of has it) cannot be among the top first ones, so only lanes whose largest
+// of eight is not matter, and after the first block hardly any is.  In a block with such lanes `least` is raised before anything is handed over: to the top'th of
+// the first top / waves lanes' largest of all wavefronts, which for logits in no order leaves about as many candidates as are wanted; and, in a wavefront with more than
+// top such lanes all the same, to its own top'th one, so that it hands over no more than 8 top, whatever the order.  Of logits that equal `least` the
+// first top lanes' do.
+template <typename T, bool TOP, int UNROLL> __global__ __launch_bounds__(kMostThreads) void k_logprobs(LogprobArgs p)
 {
-    __shared__ Stats wave_stats[kStatWaves];
-    __shared__ uint64_t wave_best[kStatWaves][TOP ? kWave : 1];
+    __shared__ Stats wave_stats[kMostWaves];
+    __shared__ uint32_t wave_first[TOP ? kWave : 1], block_least;
+    __shared__ Candidates<TOP ? 8 * kMostThreads + kMostTop : 1> candidates;  // (a block and what is kept)
     const int64_t t = blockIdx.y;
-    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, waves = blockDim.x / kWave;
     const T *z = static_cast<const T *>(p.logits) + t * p.ldz;
     const int64_t begin = (int64_t)blockIdx.x * p.part, end = min(begin + p.part, p.vocabulary);
-    Stats a{-INFINITY, 0.0f, 0.0f};
-    Best best;
-    for (int64_t at = begin; at < end; at += kStatThreads * 8) {  // (the same number of turns in every lane: alternatives go by wavefronts)
-        const int64_t col = at + threadIdx.x * 8;
-        const int64_t left = end - col;
-        Eight<T> v;
-        if (left > 0) v.load_first(z + col, left);
-        if (left > 0) {
-            float m = a.m;
+    const int block = blockDim.x * 8;
+    Stats a{kLowest, 0.0f, 0.0f};
+    uint32_t least = 1;
+    if constexpr (TOP)
+        if (threadIdx.x == 0) candidates.count = 0;
+    // (columns count from the part's first one on, in 32 bits)
+    const int count = (int)(end - begin), turn = UNROLL * block, last = count - 8;
+    const T *part = z + begin;
+    const bool few = p.vocabulary < 8;
+    auto load = [&](Eight<T> (&v)[UNROLL], int at) {
+        if (at + turn <= count) {
 #pragma unroll
-            for (int i = 0; i < 8; i++)
-                if (i < left) m = fmaxf(m, v.get(i));
-            move_to(a, m);
+            for (int k = 0; k < UNROLL; k++) v[k].load(part + at + k * block + threadIdx.x * 8);
+        } else if (!few) {  // (the eight that reach beyond the end are read from 8 logits before it: no load depends on a condition)
 #pragma unroll
-            for (int i = 0; i < 8; i++)
-                if (i < left && (m > -INFINITY || v.get(i) != v.get(i))) add_logit(a, v.get(i));
+            for (int k = 0; k < UNROLL; k++) v[k].load(part + min(at + k * block + (int)threadIdx.x * 8, last));
+        } else {
+            v[0].load_first(part, threadIdx.x == 0 ? count : 0);
         }
-        if constexpr (TOP)
+    };
+    auto take = [&](const Eight<T> (&v)[UNROLL], int at) {
 #pragma unroll
-            for (int i = 0; i < 8; i++) best.offer(i < left ? alternative(v.get(i), (uint32_t)(col + i)) : 0, p.top);
+        for (int k = 0; k < UNROLL; k++) {
+            float f[8];
+#pragma unroll
+            for (int i = 0; i < 8; i++) f[i] = v[k].get(i);
+            const int mine_at = at + k * block + threadIdx.x * 8;
+            int col = mine_at, from = 0, to = 8;  // the eight's first column, and which of them are this thread's
+            if (at + turn > count) {
+                col = few ? 0 : min(mine_at, last);
+                from = min(mine_at - col, 8);
+                to = min(count - col, 8);
+                if (from > 0 || to < 8)
+#pragma unroll
+                    for (int i = 0; i < 8; i++) f[i] = i >= from && i < to ? f[i] : -INFINITY;
+            }
+            add_eight(a, f);
+            if constexpr (TOP) {
+                if (at + k * block >= count) break;  // (the same in every thread)
+                float largest = -INFINITY;
+                bool nan = false;
+#pragma unroll
+                for (int i = 0; i < 8; i++) {
+                    largest = fmaxf(largest, f[i]);
+                    nan |= f[i] != f[i];
+                }
+                const uint32_t first = from < to ? order_of(nan ? NAN : largest) : 0;
+                if (!__syncthreads_or(first >= least)) continue;
+                const int firsts = min((p.top + waves - 1) / waves, kWave / waves);
+                uint32_t left = first >= least ? first : 0;
+                for (int i = 0; i < firsts; i++) {
+                    const uint32_t largest_left = wave_max(left);
+                    if (lane == 0) wave_first[wave * firsts + i] = largest_left;
+                    if (lane == __builtin_ctzll(__ballot(left == largest_left))) left = 0;
+                }
+                __syncthreads();
+                if (wave == 0) {
+                    const uint32_t raised = of_rank(lane < waves * firsts ? wave_first[lane] : 0, p.top - 1);
+                    if (lane == 0) block_least = max(least, raised);
+                }
+                __syncthreads();
+                least = block_least;
+                uint32_t mine = least;
+                if (__popcll(__ballot(first >= least)) > p.top) mine = max(least, of_rank(first, p.top - 1));
+                if (__ballot(first >= mine)) {
+                    uint32_t order[8];
+                    bool equal = false;
+#pragma unroll
+                    for (int i = 0; i < 8; i++) {
+                        order[i] = i >= from && i < to ? order_of(f[i]) : 0;
+                        equal |= order[i] == mine;
+                    }
+                    if (__popcll(__ballot(equal) & ((1ull << lane) - 1)) >= p.top) mine++;
+#pragma unroll
+                    for (int i = 0; i < 8; i++)
+                        if (order[i] >= mine) candidates.append((uint64_t)order[i] << 32 | (uint32_t) ~(uint32_t)(begin + col + i));
+                }
+                __syncthreads();
+                candidates.select(p.top);
+                const int n = candidates.count;
+                __syncthreads();
+                if ((int)threadIdx.x < min(n, p.top)) candidates.all[threadIdx.x] = candidates.sorted[threadIdx.x];
+                if (threadIdx.x == 0) candidates.count = min(n, p.top);
+                if (n >= p.top) least = (uint32_t)(candidates.sorted[p.top - 1] >> 32) + 1;  // (an equal one comes later)
+                __syncthreads();
+            }
+        }
+    };
+    Eight<T> one[UNROLL], two[UNROLL];
+    load(one, 0);
+    for (int at = 0; at < count; at += 2 * turn) {  // (the next logits are on their way while these are taken)
+        const int next = at + turn;
+        if (next < count) load(two, next);
+        take(one, at);
+        if (next < count) {
+            if (next + turn < count) load(one, next + turn);
+            take(two, next);
+        }
     }
     a = wave_join(a);
     if (lane == 0) wave_stats[wave] = a;
-    if constexpr (TOP) wave_best[wave][lane] = best.mine;
     __syncthreads();
-    if (wave != 0) return;
-    a = lane < kStatWaves ? wave_stats[lane] : Stats{-INFINITY, 0.0f, 0.0f};
-    a = wave_join(a);
-    if constexpr (TOP)
-        for (int w = 1; w < kStatWaves; w++) best.offer(lane < p.top ? wave_best[w][lane] : 0, p.top);
+    a = wave_join(lane < waves ? wave_stats[lane] : Stats{kLowest, 0.0f, 0.0f});
     if (p.parts == 1) {
-        finish_row<T>(p, t, a, best);
+        finish_row<T>(p, t, a, candidates.sorted);
     } else {
         const int64_t at = t * p.parts + blockIdx.x;
-        if (lane == 0) p.stats[at] = a;
-        if (lane < p.top) p.best[at * p.top + lane] = best.mine;
+        if (threadIdx.x == 0) p.stats[at] = a;
+        if constexpr (TOP)
+            if ((int)threadIdx.x < p.top) p.best[at * p.top + threadIdx.x] = (int)threadIdx.x < candidates.count ? candidates.sorted[threadIdx.x] : 0;
     }
 }
 
-// joins the parts of a row
-template <typename T> __global__ __launch_bounds__(kWave) void k_logprobs_join(LogprobArgs p)
+// Joins the parts of a row.  Of the parts' alternatives only those matter that are not behind the last one of any part that has `top` of them, nor behind the
+// top'th of the parts' first ones.
+constexpr int kJoinThreads = 256, kMostParts = 64;
+template <typename T> __global__ __launch_bounds__(kJoinThreads) void k_logprobs_join(LogprobArgs p)
 {
+    __shared__ Candidates<kMostParts * kMostTop> candidates;
     const int64_t t = blockIdx.x;
-    const int lane = threadIdx.x;
-    Stats a{-INFINITY, 0.0f, 0.0f};
-    for (int i = lane; i < p.parts; i += kWave) a = join(a, p.stats[t * p.parts + i]);
-    a = wave_join(a);
-    Best best;
+    const int lane = threadIdx.x % kWave;
     const uint64_t *all = p.best + t * p.parts * p.top;
-    const int count = p.parts * p.top;
-    for (int i = 0; i < count; i += kWave) best.offer(i + lane < count ? all[i + lane] : 0, p.top);
-    finish_row<T>(p, t, a, best);
+    Stats a = lane < p.parts ? p.stats[t * p.parts + lane] : Stats{kLowest, 0.0f, 0.0f};
+    if (p.top) {
+        const int firsts = min((p.top + p.parts - 1) / p.parts, kWave / p.parts);
+        const uint32_t one = lane < p.parts * firsts ? (uint32_t)(all[lane % p.parts * p.top + lane / p.parts] >> 32) : 0;
+        uint32_t least = wave_max(lane < p.parts ? (uint32_t)(all[lane * p.top + p.top - 1] >> 32) : 0);
+        least = max(least, of_rank(one, p.top - 1));
+        if (threadIdx.x == 0) candidates.count = 0;
+        __syncthreads();
+        for (int i = threadIdx.x; i < p.parts * p.top; i += kJoinThreads) {
+            const uint64_t a = all[i];
+            if (a >> 32 >= least && a) candidates.append(a);
+        }
+        __syncthreads();
+        candidates.select(p.top);
+    }
+    a = wave_join(a);
+    __syncthreads();
+    finish_row<T>(p, t, a, candidates.sorted);
 }
 
 struct LogprobBackArgs {
@@ -223,7 +327,7 @@ template <typename T> __global__ __launch_bounds__(256) void k_logprobs_backward
 #pragma unroll
     for (int i = 0; i < 8; i++) {
         const float lp = v.get(i) - lse;
-        const float prob = __expf(lp);
+        const float prob = __builtin_amdgcn_exp2f(lp * kPerLog2);
         float g = prob * (u + (prob > 0.0f ? w * (lp + entropy) : 0.0f));
         g = col + i == id ? u - g : -g;
         if (none) g = u == u ? 0.0f : u;
@@ -235,15 +339,15 @@ template <typename T> __global__ __launch_bounds__(256) void k_logprobs_backward
 // parts of a row: enough workgroups for the chip, none of fewer than 4096 logits
 int64_t parts_of(int64_t tokens, int64_t vocabulary)
 {
-    const int64_t most = (vocabulary + 4095) / 4096, wanted = (512 + tokens - 1) / (tokens > 0 ? tokens : 1);
+    const int64_t most = (vocabulary + 4095) / 4096, wanted = (2048 + tokens - 1) / (tokens > 0 ? tokens : 1);
     const int64_t parts = wanted < most ? wanted : most;
-    return parts < 64 ? parts : 64;
+    return parts < kMostParts ? parts : kMostParts;
 }
 
 int check_logits(int type, int64_t ldz, int64_t tokens, int64_t vocabulary)
 {
     if (!is_type(type) || tokens < 0 || vocabulary < 1 || (tokens > 1 && ldz < vocabulary)) return HBP_ERR_INVALID_ARGUMENT;
-    if (vocabulary > (int64_t(1) << 31) - 512 || tokens > (int64_t(1) << 31) - 512) return HBP_ERR_TOO_LARGE;
+    if (vocabulary > (int64_t(1) << 30) || tokens > (int64_t(1) << 31) - 512) return HBP_ERR_TOO_LARGE;
     return HBP_OK;
 }
 
@@ -302,11 +406,19 @@ int hbp_token_logprobs(int type, const void *logits, int64_t ldz, int64_t tokens
             if (top) { q.top_ids += at * top; q.top_logp += at * top; }
             if (p.parts > 1) { q.best += at * p.parts * top; q.stats += at * p.parts; }
             const dim3 grid((unsigned)p.parts, (unsigned)rows);
-            if (top) k_logprobs<T, true><<<grid, kStatThreads, 0, st>>>(q);
-            else k_logprobs<T, false><<<grid, kStatThreads, 0, st>>>(q);
+            const int64_t eights = (p.part + 7) / 8;
+            const int threads = (int)(eights < kMostThreads ? (eights + kWave - 1) / kWave * kWave : kMostThreads);
+            const bool longer = p.part > kMostThreads * 8;
+            if (top) {
+                if (longer) k_logprobs<T, true, 2><<<grid, threads, 0, st>>>(q);
+                else k_logprobs<T, true, 1><<<grid, threads, 0, st>>>(q);
+            } else {
+                if (longer) k_logprobs<T, false, 2><<<grid, threads, 0, st>>>(q);
+                else k_logprobs<T, false, 1><<<grid, threads, 0, st>>>(q);
+            }
             HBP_HIP(hipGetLastError());
             if (p.parts > 1) {
-                k_logprobs_join<T><<<dim3((unsigned)rows), kWave, 0, st>>>(q);
+                k_logprobs_join<T><<<dim3((unsigned)rows), kJoinThreads, 0, st>>>(q);
                 HBP_HIP(hipGetLastError());
             }
         }

@@ -98,11 +98,36 @@ template <typename T> struct Eight {
     }
 };
 
+// op over the 64 lanes, the same result in all of them, by lane exchanges of the vector unit alone (quads, halves of rows, rows, quarters, halves).
+template <typename V, typename F> __device__ __forceinline__ V wave_reduce(V v, F op)
+{
+    static_assert(sizeof(V) == 4, "");
+    auto dpp = [&](auto control) {
+        return __builtin_bit_cast(V, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), decltype(control)::value, 0xf, 0xf, true));
+    };
+    v = op(v, dpp(std::integral_constant<int, 0xb1>()));   // quad_perm 1 0 3 2
+    v = op(v, dpp(std::integral_constant<int, 0x4e>()));   // quad_perm 2 3 0 1
+    v = op(v, dpp(std::integral_constant<int, 0x141>()));  // row_half_mirror
+    v = op(v, dpp(std::integral_constant<int, 0x140>()));  // row_mirror
+    const uint32_t w = __builtin_bit_cast(uint32_t, v);
+    auto a = __builtin_amdgcn_permlane16_swap(w, w, false, false);
+    v = op(__builtin_bit_cast(V, (uint32_t)a[0]), __builtin_bit_cast(V, (uint32_t)a[1]));
+    const uint32_t x = __builtin_bit_cast(uint32_t, v);
+    auto b = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+    return op(__builtin_bit_cast(V, (uint32_t)b[0]), __builtin_bit_cast(V, (uint32_t)b[1]));
+}
 __device__ __forceinline__ float wave_sum(float v)
 {
-#pragma unroll
-    for (int d = 1; d < kWave; d *= 2) v += __shfl_xor(v, d);
-    return v;
+    return wave_reduce(v, [](float a, float b) { return a + b; });
+}
+__device__ __forceinline__ float wave_max(float v)  // (passes over NaN)
+{
+    return wave_reduce(v, [](float a, float b) { return fmaxf(a, b); });
+}
+
+__device__ __forceinline__ uint32_t wave_max(uint32_t v)
+{
+    return wave_reduce(v, [](uint32_t a, uint32_t b) { return a > b ? a : b; });
 }
 
 // Sums of N values over the THREADS of a workgroup, the same in every thread. `slots`: LDS, THREADS / 64 * N floats, that no other
