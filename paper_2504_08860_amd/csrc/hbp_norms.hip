@@ -95,49 +95,58 @@ struct NormBackArgs {
 // first norm: d_y = r1 (b - y r1^2 mean(b y)).  e in the second mean is spelled out, so that all three sums of a row, of
 // a h', of w y (d_h_out + r2 a) and of w y h' with w = scale g w_post, are taken together: one wait for the others per row.
 // h' is computed again from h, y and the gate, which are read anyway: not the rounded one, and no read more.
+//
+// A workgroup walks through every so many rows and keeps its columns' sums for the weights in registers; workgroups' sums are added by a second kernel, in their
+// order.  Of a row, what was read stays in registers as it came (h' is cheaper to compute twice than to keep), and so do the weights.
 template <typename T, int THREADS, int CHUNKS, int GATE>
 __global__ __launch_bounds__(THREADS) void k_residual_norms_backward(NormBackArgs n)
 {
     __shared__ float slots[2][THREADS / kWave * 3];
-    const T *w_post = static_cast<const T *>(n.w_post), *w_pre = static_cast<const T *>(n.w_pre);
-    float sum_post[CHUNKS][8] = {}, sum_pre[CHUNKS][8] = {}, sum_gate[CHUNKS][8] = {};
+    constexpr bool kFull = GATE == HBP_GATE_FULL, kChannel = GATE == HBP_GATE_CHANNEL;
+    Eight<T> wp[CHUNKS], wq[CHUNKS], gg[CHUNKS];
+#pragma unroll
+    for (int c = 0; c < CHUNKS; c++) {
+        const int col = (c * THREADS + threadIdx.x) * 8, left = n.width - col;
+#pragma unroll
+        for (int i = 0; i < 8; i++) {
+            wp[c].set(i, 1.0f);
+            wq[c].set(i, 1.0f);
+        }
+        if (n.w_post) wp[c].load_first(static_cast<const T *>(n.w_post) + col, left);
+        if (n.w_pre) wq[c].load_first(static_cast<const T *>(n.w_pre) + col, left);
+        if constexpr (kChannel) gg[c].load_first(static_cast<const T *>(n.gate) + col, left);
+    }
+    float sum_post[CHUNKS][8] = {}, sum_pre[CHUNKS][8] = {}, sum_gate[kChannel ? CHUNKS : 1][8] = {};
     const float inverse_width = 1.0f / n.width;
     int odd = 0;
     for (int64_t t = blockIdx.x; t < n.tokens; t += gridDim.x, odd ^= 1) {
         const T *h = static_cast<const T *>(n.h) + t * n.ldh, *y = static_cast<const T *>(n.y) + t * n.ldy;
-        const T *g = GATE == HBP_GATE_FULL ? static_cast<const T *>(n.gate) + t * n.ldg : static_cast<const T *>(n.gate);
         const float r1 = n.rstd[2 * t], r2 = n.rstd[2 * t + 1];
-        const float row_gate = GATE == HBP_GATE_TOKEN ? to_f32(g[t]) : 1.0f;
-        Eight<T> yy[CHUNKS], gg[CHUNKS], dx[CHUNKS], dh[CHUNKS];
-        float next[CHUNKS][8];
-        float sum[3] = {0, 0, 0};
+        const float row_gate = GATE == HBP_GATE_TOKEN ? to_f32(static_cast<const T *>(n.gate)[t]) : 1.0f;
+        Eight<T> yy[CHUNKS], hh[CHUNKS], dx[CHUNKS], dh[CHUNKS];
 #pragma unroll
         for (int c = 0; c < CHUNKS; c++) {
-            const int col = (c * THREADS + threadIdx.x) * 8;
-            const int left = n.width - col;
-            Eight<T> hh, wp, wq;
+            const int col = (c * THREADS + threadIdx.x) * 8, left = n.width - col;
             yy[c].load_first(y + col, left);
-            hh.load_first(h + col, left);
+            hh[c].load_first(h + col, left);
             dx[c].clear();
             dh[c].clear();
             if (n.d_x_out) dx[c].load_first(static_cast<const T *>(n.d_x_out) + t * n.lddxo + col, left);
             if (n.d_h_out) dh[c].load_first(static_cast<const T *>(n.d_h_out) + t * n.lddho + col, left);
-            if constexpr (GATE == HBP_GATE_FULL || GATE == HBP_GATE_CHANNEL) gg[c].load_first(g + col, left);
-            if (w_post) wp.load_first(w_post + col, left);
-            if (w_pre) wq.load_first(w_pre + col, left);
+            if constexpr (kFull) gg[c].load_first(static_cast<const T *>(n.gate) + t * n.ldg + col, left);
+        }
+        float sum[3] = {0, 0, 0};
+#pragma unroll
+        for (int c = 0; c < CHUNKS; c++)
 #pragma unroll
             for (int i = 0; i < 8; i++) {
-                float w = n.scale;
-                if constexpr (GATE == HBP_GATE_FULL || GATE == HBP_GATE_CHANNEL) w *= gg[c].get(i);
-                if (w_post) w *= wp.get(i);
-                const float wy = w * yy[c].get(i);
-                next[c][i] = hh.get(i) + row_gate * (r1 * wy);
-                const float a = w_pre ? dx[c].get(i) * wq.get(i) : dx[c].get(i);
-                sum[0] += a * next[c][i];
+                float w = n.scale * wp[c].get(i);
+                if constexpr (kFull || kChannel) w *= gg[c].get(i);
+                const float wy = w * yy[c].get(i), next = hh[c].get(i) + row_gate * (r1 * wy), a = dx[c].get(i) * wq[c].get(i);
+                sum[0] += a * next;
                 sum[1] += wy * (dh[c].get(i) + r2 * a);
-                sum[2] += wy * next[c][i];
+                sum[2] += wy * next;
             }
-        }
         block_sums<3, THREADS>(sum, slots[odd]);
         const float along2 = r2 * r2 * r2 * (sum[0] * inverse_width);
         const float through = sum[1] - along2 * sum[2];  // sum of b y, a row's gate left out
@@ -145,33 +154,26 @@ __global__ __launch_bounds__(THREADS) void k_residual_norms_backward(NormBackArg
         if (GATE == HBP_GATE_TOKEN && n.d_gate && threadIdx.x == 0) static_cast<float *>(n.d_gate)[t] = r1 * through;
 #pragma unroll
         for (int c = 0; c < CHUNKS; c++) {
-            const int col = (c * THREADS + threadIdx.x) * 8;
-            const int left = n.width - col;
-            Eight<T> wp, wq, de, dy, dg;
-            if (w_post) wp.load_first(w_post + col, left);
-            if (w_pre) wq.load_first(w_pre + col, left);
+            const int col = (c * THREADS + threadIdx.x) * 8, left = n.width - col;
+            Eight<T> de, dy, dg;
 #pragma unroll
             for (int i = 0; i < 8; i++) {
-                const float yv = yy[c].get(i), xv = dx[c].get(i);
-                const float a = w_pre ? xv * wq.get(i) : xv;
-                const float e = dh[c].get(i) + r2 * a - along2 * next[c][i];
+                const float yv = yy[c].get(i), xv = dx[c].get(i), w_post = wp[c].get(i);
                 float gate = n.scale * row_gate;
-                if constexpr (GATE == HBP_GATE_FULL || GATE == HBP_GATE_CHANNEL) gate *= gg[c].get(i);
-                const float ge = gate * e, unit = yv * r1;
-                const float b = w_post ? ge * wp.get(i) : ge;
+                if constexpr (kFull || kChannel) gate *= gg[c].get(i);
+                const float unit = yv * r1, next = hh[c].get(i) + gate * (unit * w_post);
+                const float e = dh[c].get(i) + r2 * (xv * wq[c].get(i)) - along2 * next;
+                const float ge = gate * e;
                 de.set(i, e);
-                dy.set(i, r1 * b - along1 * yv);
+                dy.set(i, r1 * (ge * w_post) - along1 * yv);
                 sum_post[c][i] += ge * unit;
-                sum_pre[c][i] += xv * (next[c][i] * r2);
-                if constexpr (GATE == HBP_GATE_FULL || GATE == HBP_GATE_CHANNEL) {
-                    const float d = n.scale * e * (w_post ? unit * wp.get(i) : unit);
-                    if constexpr (GATE == HBP_GATE_FULL) dg.set(i, d);
-                    else sum_gate[c][i] += d;
-                }
+                sum_pre[c][i] += xv * (next * r2);
+                if constexpr (kFull) dg.set(i, n.scale * e * (unit * w_post));
+                if constexpr (kChannel) sum_gate[c][i] += n.scale * e * (unit * w_post);
             }
             de.store_first(static_cast<T *>(n.d_h) + t * n.lddh + col, left);
             dy.store_first(static_cast<T *>(n.d_y) + t * n.lddy + col, left);
-            if constexpr (GATE == HBP_GATE_FULL)
+            if constexpr (kFull)
                 if (n.d_gate) dg.store_first(static_cast<T *>(n.d_gate) + t * n.ldg + col, left);
         }
     }
@@ -184,25 +186,40 @@ __global__ __launch_bounds__(THREADS) void k_residual_norms_backward(NormBackArg
             if (col + i < n.width) {
                 mine[col + i] = sum_post[c][i];
                 mine[n.width + col + i] = sum_pre[c][i];
-                if constexpr (GATE == HBP_GATE_CHANNEL) mine[2 * n.width + col + i] = sum_gate[c][i];
+                if constexpr (kChannel) mine[2 * n.width + col + i] = sum_gate[c][i];
             }
     }
 }
 
-// out[which][col] = sum over the workgroups of partial[workgroup][which][col], in ascending order within each quarter
-__global__ __launch_bounds__(256) void k_norm_weight_sums(const float *partial, int32_t workgroups, int32_t width, float *d_w_post, float *d_w_pre,
-                                                          float *d_gate)
+// out[which][col] = sum over the workgroups of partial[workgroup][which][col]: sixteen shares of them, each in ascending order, then the shares
+constexpr int kShares = 16;
+__global__ __launch_bounds__(kShares * 64) void k_norm_weight_sums(const float *partial, int32_t workgroups, int32_t width, float *d_w_post, float *d_w_pre, float *d_gate)
 {
-    __shared__ float quarter[4][64];
-    const int lane = threadIdx.x % 64, part = threadIdx.x / 64, col = blockIdx.x * 64 + lane;
+    __shared__ float shares[kShares][64];
+    const int lane = threadIdx.x % 64, share = threadIdx.x / 64, col = blockIdx.x * 64 + lane;
     float *out = blockIdx.y == 0 ? d_w_post : blockIdx.y == 1 ? d_w_pre : d_gate;
     if (!out) return;
     float sum = 0;
-    if (col < width)
-        for (int b = part; b < workgroups; b += 4) sum += partial[((int64_t)b * 3 + blockIdx.y) * width + col];
-    quarter[part][lane] = sum;
+    if (col < width) {
+        const float *at = partial + (int64_t)blockIdx.y * width + col;
+        const int64_t apart = 3 * (int64_t)width;
+        int b = share;
+        for (; b + 7 * kShares < workgroups; b += 8 * kShares) {
+            float v[8];
+#pragma unroll
+            for (int k = 0; k < 8; k++) v[k] = at[(b + k * kShares) * apart];
+#pragma unroll
+            for (int k = 0; k < 8; k++) sum += v[k];
+        }
+        for (; b < workgroups; b += kShares) sum += at[b * apart];
+    }
+    shares[share][lane] = sum;
     __syncthreads();
-    if (part == 0 && col < width) out[col] = quarter[0][lane] + quarter[1][lane] + quarter[2][lane] + quarter[3][lane];
+    if (share == 0 && col < width) {
+        sum = 0;
+        for (int k = 0; k < kShares; k++) sum += shares[k][lane];
+        out[col] = sum;
+    }
 }
 
 // Threads and chunks for a width: f(threads, chunks) as compile-time constants
@@ -215,6 +232,15 @@ template <typename F> int by_width_forward(int64_t width, F f)
     if (width <= 8192) return f(Int<1024>(), Int<1>());
     return f(Int<1024>(), Int<2>());
 }
+template <typename F> int by_width_backward(int64_t width, F f)
+{
+    if (width <= 512) return f(Int<64>(), Int<1>());
+    if (width <= 1024) return f(Int<128>(), Int<1>());
+    if (width <= 2048) return f(Int<256>(), Int<1>());
+    if (width <= 4096) return f(Int<512>(), Int<1>());
+    if (width <= 8192) return f(Int<512>(), Int<2>());
+    return f(Int<512>(), Int<4>());
+}
 template <typename F> int by_gate(int kind, F f)
 {
     switch (kind) {
@@ -225,11 +251,12 @@ template <typename F> int by_gate(int kind, F f)
     }
 }
 
+// as many as are on the chip at once: 16 wavefronts for each of 256 compute units; no more than there are rows, and of narrow rows four rows each
 int64_t backward_workgroups(int64_t tokens, int64_t width)
 {
-    const int64_t threads = width <= 512 ? 64 : width <= 2048 ? 256 : width <= 4096 ? 512 : 1024;
-    const int64_t most = 256 * 1024 / threads;  // 16 wavefronts for each of 256 compute units
-    return tokens < most ? tokens : most;
+    const int64_t threads = width <= 512 ? 64 : width <= 1024 ? 128 : width <= 2048 ? 256 : 512;
+    const int64_t most = 256 * 1024 / threads, enough = threads < 512 ? (tokens + 3) / 4 : tokens;
+    return enough < most ? enough : most;
 }
 
 int check_norms(const hbp_norms_t *n)
@@ -326,7 +353,7 @@ int hbp_residual_norms_backward(const hbp_norms_t *n, const void *d_h_out, int64
         rc = by_type(n->type, [&](auto type) -> int {
             using T = decltype(type);
             return by_gate(n->gate_kind, [&](auto gate) -> int {
-                return by_width_forward(n->width, [&](auto threads, auto chunks) -> int {
+                return by_width_backward(n->width, [&](auto threads, auto chunks) -> int {
                     constexpr int kThreads = decltype(threads)::value;
                     k_residual_norms_backward<T, kThreads, decltype(chunks)::value, decltype(gate)::value>
                         <<<dim3((unsigned)workgroups), kThreads, 0, st>>>(a);
@@ -339,7 +366,7 @@ int hbp_residual_norms_backward(const hbp_norms_t *n, const void *d_h_out, int64
     }
     float *channel = n->gate_kind == HBP_GATE_CHANNEL ? static_cast<float *>(d_gate) : nullptr;
     if (d_w_post || d_w_pre || channel) {
-        k_norm_weight_sums<<<dim3((unsigned)((n->width + 63) / 64), channel ? 3 : 2), 256, 0, st>>>(
+        k_norm_weight_sums<<<dim3((unsigned)((n->width + 63) / 64), channel ? 3 : 2), kShares * 64, 0, st>>>(
             static_cast<const float *>(workspace), workgroups, (int32_t)n->width, d_w_post, d_w_pre, channel);
         HBP_HIP(hipGetLastError());
     }
