@@ -13,48 +13,71 @@ template <typename S> __device__ __forceinline__ float zero_of(const Q4 &a, int6
     return a.zeros ? to_f32(static_cast<const S *>(a.zeros)[row * a.groups + group]) : 8.0f;
 }
 
-// Packing: a lane takes eight columns, the group's 4 to 64 lanes exchange its extremes.
+// Extremes over the 4 to 64 lanes of a group: over quads and rows of sixteen by the vector unit's own lane exchanges.
+template <typename F> __device__ __forceinline__ float group_reduce(float v, int lanes, F op)
+{
+    auto dpp = [&](auto control) {
+        return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), decltype(control)::value, 0xf, 0xf, true));
+    };
+    v = op(v, dpp(std::integral_constant<int, 0xb1>()));   // quad_perm 1 0 3 2
+    v = op(v, dpp(std::integral_constant<int, 0x4e>()));   // quad_perm 2 3 0 1
+    if (lanes > 4) v = op(v, dpp(std::integral_constant<int, 0x141>()));  // row_half_mirror
+    if (lanes > 8) v = op(v, dpp(std::integral_constant<int, 0x140>()));  // row_mirror
+    for (int d = 16; d < lanes; d *= 2) v = op(v, __shfl_xor(v, d));
+    return v;
+}
+
+// Packing: a lane takes eight columns of kPackRows rows, whose loads are all on their way at once.  Bound: HBM for 16-bit weights, by way of the division: the code is
+// that of the quotient, but a product with the reciprocal, off by a few last bits, gives the same one unless it lies next to a half.
+constexpr int kPackRows = 4;
 template <typename T, typename S> __global__ __launch_bounds__(256) void k_q4_pack(Q4 a, const void *w_, int64_t ldw)
 {
-    const int64_t row = blockIdx.y + (int64_t)blockIdx.z * 32768;
-    if (row >= a.n_rows) return;
+    const int64_t row0 = (blockIdx.y + (int64_t)blockIdx.z * 32768) * kPackRows;
     const int64_t col = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 8;
     const int64_t left = a.n_cols - col;
-    Eight<T> w;
-    w.clear();
-    if (left > 0) w.load_first(static_cast<const T *>(w_) + row * ldw + col, left);
-    float low = 0.0f, high = 0.0f, odd = 0.0f;  // odd: NaN from a value that no scale fits
+    Eight<T> w[kPackRows];
 #pragma unroll
-    for (int i = 0; i < 8; i++) {
-        const float v = w.get(i);
-        low = fminf(low, v);
-        high = fmaxf(high, v);
-        odd += v * 0.0f;
+    for (int r = 0; r < kPackRows; r++) {
+        w[r].clear();
+        if (left > 0 && row0 + r < a.n_rows) w[r].load_first(static_cast<const T *>(w_) + (row0 + r) * ldw + col, left);
     }
     const int lanes = 1 << (a.shift - 3);
-    for (int d = 1; d < lanes; d *= 2) {
-        low = fminf(low, __shfl_xor(low, d));
-        high = fmaxf(high, __shfl_xor(high, d));
-        odd += __shfl_xor(odd, d);
-    }
-    if (col >= a.pitch * 2) return;
-    constexpr float kLargest = std::is_same_v<S, f16> ? 65504.0f : std::is_same_v<S, bf16> ? 3.3895313892515355e38f : 3.4028234663852886e38f;
-    const float wide = a.zeros ? (high - low) * (1.0f / 15.0f) : fmaxf(-low, high) * (1.0f / 7.0f);
-    const S scale = from_f32<S>(fminf(wide, kLargest));
-    const float s = to_f32(scale);
-    const float zero = !a.zeros ? 8.0f : s == 0.0f ? 0.0f : rintf(-low / s);
-    uint32_t word = 0;
 #pragma unroll
-    for (int i = 0; i < 8; i++) {
-        const float q = s == 0.0f ? zero : rintf(w.get(i) / s + zero);
-        const uint32_t code = odd == 0.0f ? (uint32_t)fminf(fmaxf(q, 0.0f), 15.0f) : 8u;
-        if (i < left) word |= code << 4 * i;
-    }
-    *reinterpret_cast<uint32_t *>(const_cast<uint8_t *>(a.codes) + row * a.pitch + col / 2) = word;
-    if ((threadIdx.x & (lanes - 1)) == 0 && left > 0) {
-        const int64_t at = row * a.groups + (col >> a.shift);
-        static_cast<S *>(const_cast<void *>(a.scales))[at] = odd == 0.0f ? scale : from_f32<S>(NAN);
-        if (a.zeros) static_cast<S *>(const_cast<void *>(a.zeros))[at] = from_f32<S>(odd == 0.0f ? zero : 0.0f);
+    for (int r = 0; r < kPackRows; r++) {
+        float low = 0.0f, high = 0.0f, odd = 0.0f;  // odd: NaN from a value that no scale fits
+#pragma unroll
+        for (int i = 0; i < 8; i += 2) {
+            const float v0 = w[r].get(i), v1 = w[r].get(i + 1);
+            asm("v_min3_f32 %0, %1, %2, %0" : "+v"(low) : "v"(v0), "v"(v1));  // (fminf would make each value canonical first)
+            asm("v_max3_f32 %0, %1, %2, %0" : "+v"(high) : "v"(v0), "v"(v1));
+            odd = fmaf(v0, 0.0f, fmaf(v1, 0.0f, odd));
+        }
+        low = group_reduce(low, lanes, [](float x, float y) { return fminf(x, y); });
+        high = group_reduce(high, lanes, [](float x, float y) { return fmaxf(x, y); });
+        odd = group_reduce(odd, lanes, [](float x, float y) { return x + y; });
+        const int64_t row = row0 + r;
+        if (col >= a.pitch * 2 || row >= a.n_rows) continue;
+        constexpr float kLargest = std::is_same_v<S, f16> ? 65504.0f : std::is_same_v<S, bf16> ? 3.3895313892515355e38f : 3.4028234663852886e38f;
+        const float wide = a.zeros ? (high - low) * (1.0f / 15.0f) : fmaxf(-low, high) * (1.0f / 7.0f);
+        const S scale = from_f32<S>(fminf(wide, kLargest));
+        const float s = to_f32(scale), inverse = s == 0.0f ? 0.0f : 1.0f / s;
+        const float zero = !a.zeros ? 8.0f : s == 0.0f ? 0.0f : rintf(-low / s);
+        uint32_t word = 0;
+#pragma unroll
+        for (int i = 0; i < 8; i++) {
+            const float v = w[r].get(i);
+            float q = fmaf(v, inverse, zero);
+            if (!(fabsf(__builtin_amdgcn_fractf(q) - 0.5f) > 1e-4f)) q = s == 0.0f ? zero : v / s + zero;  // (also where the reciprocal is not finite)
+            word |= (uint32_t)__builtin_amdgcn_fmed3f(rintf(q), 0.0f, 15.0f) << 4 * i;
+        }
+        if (odd != 0.0f) word = 0x88888888u;
+        if (left < 8) word = left > 0 ? word & ((1u << 4 * left) - 1) : 0;
+        *reinterpret_cast<uint32_t *>(const_cast<uint8_t *>(a.codes) + row * a.pitch + col / 2) = word;
+        if ((threadIdx.x & (lanes - 1)) == 0 && left > 0) {
+            const int64_t at = row * a.groups + (col >> a.shift);
+            static_cast<S *>(const_cast<void *>(a.scales))[at] = odd == 0.0f ? scale : from_f32<S>(NAN);
+            if (a.zeros) static_cast<S *>(const_cast<void *>(a.zeros))[at] = from_f32<S>(odd == 0.0f ? zero : 0.0f);
+        }
     }
 }
 
@@ -297,7 +320,8 @@ int hbp_q4_pack(const hbp_q4_matrix_t *m, int type, const void *w, int64_t ldw, 
     if (!is_type(type) || !w || !aligned(w, type_bytes(type)) || (m->n_rows > 1 && ldw < m->n_cols)) return HBP_ERR_INVALID_ARGUMENT;
     rc = earlier_error();
     if (rc != HBP_OK) return rc;
-    const dim3 grid((unsigned)((a.pitch * 2 + 2047) / 2048), (unsigned)(a.n_rows < 32768 ? a.n_rows : 32768), (unsigned)((a.n_rows + 32767) / 32768));
+    const int64_t fours = ((int64_t)a.n_rows + kPackRows - 1) / kPackRows;
+    const dim3 grid((unsigned)((a.pitch * 2 + 2047) / 2048), (unsigned)(fours < 32768 ? fours : 32768), (unsigned)((fours + 32767) / 32768));
     return by_type(type, [&](auto t) -> int {
         return by_type(m->scale_type, [&](auto s) -> int {
             k_q4_pack<decltype(t), decltype(s)><<<grid, 256, 0, (hipStream_t)stream>>>(a, w, ldw);
