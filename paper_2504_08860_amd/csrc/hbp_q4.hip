@@ -107,7 +107,7 @@ template <typename T, typename S> __global__ __launch_bounds__(256) void k_q4_un
 // Bound: vector instructions, 1.4 + M a weight (a conversion for each code and an fma for each vector; 39 T lanes/s).  Not by the matrix cores: there the scale, which
 // differs from row to row, would have to go into x, in parts, for every group anew.
 // As in the products, code * (scale x) may be infinite where the sum is not: such results are computed again from the definition.
-constexpr int kTransposedWaves = 8, kTransposedRows = 1024;  // rows whose x lies in LDS at a time
+constexpr int kTransposedWaves = 8, kTransposedRows = 512;  // rows whose x lies in LDS at a time
 // What a lane loads of ROWS rows.
 template <typename S, bool ZERO, int C, int ROWS> struct Rows {
     uint32_t w[ROWS][C / 8];
@@ -135,34 +135,42 @@ template <typename S, bool ZERO, int C, int ROWS> struct Rows {
             if constexpr (ZERO) zeros += more ? apart : 0;
         }
     }
-    template <int M> __device__ __forceinline__ void add(const float *x, int apart, float (&acc)[M][C], float (&taken)[M]) const
+    // x: of the first row's M vectors, then the next one's
+    template <int M> __device__ __forceinline__ void add(const float *x, float (&acc)[M][C], float (&taken)[M]) const
     {
 #pragma unroll
-        for (int i0 = 0; i0 < ROWS; i0 += 4) {
-            float4 x4[M];
+        for (int i = 0; i < ROWS; i++) {
+            const float s = to_f32(scale[i]), z = ZERO ? to_f32(zero[ZERO ? i : 0]) : 1.0f;
+            float f[C], u[M];
+            if constexpr (M % 4 == 0) {
 #pragma unroll
-            for (int m = 0; m < M; m++) x4[m] = *reinterpret_cast<const float4 *>(x + m * apart + i0);
-#pragma unroll
-            for (int k = 0; k < 4; k++) {
-                const int i = i0 + k;
-                const float s = to_f32(scale[i]);
-                float f[C];
-#pragma unroll
-                for (int j = 0; j < C / 8; j++) {
-                    const uint32_t even = w[i][j] & 0x0f0f0f0fu, odd = w[i][j] >> 4 & 0x0f0f0f0fu;
-#pragma unroll
-                    for (int b = 0; b < 4; b++) {
-                        f[8 * j + 2 * b] = (float)(even >> 8 * b & 255u);
-                        f[8 * j + 2 * b + 1] = (float)(odd >> 8 * b & 255u);
-                    }
+                for (int m = 0; m < M; m += 4) {
+                    const float4 four = *reinterpret_cast<const float4 *>(x + i * M + m);
+                    u[m] = s * four.x; u[m + 1] = s * four.y; u[m + 2] = s * four.z; u[m + 3] = s * four.w;
                 }
+            } else if constexpr (M % 2 == 0) {
 #pragma unroll
-                for (int m = 0; m < M; m++) {
-                    const float u = s * (k == 0 ? x4[m].x : k == 1 ? x4[m].y : k == 2 ? x4[m].z : x4[m].w);
-                    taken[m] += ZERO ? u * to_f32(zero[ZERO ? i : 0]) : u;
-#pragma unroll
-                    for (int c = 0; c < C; c++) acc[m][c] += f[c] * u;
+                for (int m = 0; m < M; m += 2) {
+                    const float2 two = *reinterpret_cast<const float2 *>(x + i * M + m);
+                    u[m] = s * two.x; u[m + 1] = s * two.y;
                 }
+            } else {
+                u[0] = s * x[i];
+            }
+#pragma unroll
+            for (int j = 0; j < C / 8; j++) {
+                const uint32_t even = w[i][j] & 0x0f0f0f0fu, odd = w[i][j] >> 4 & 0x0f0f0f0fu;
+#pragma unroll
+                for (int b = 0; b < 4; b++) {
+                    f[8 * j + 2 * b] = (float)(even >> 8 * b & 255u);
+                    f[8 * j + 2 * b + 1] = (float)(odd >> 8 * b & 255u);
+                }
+            }
+#pragma unroll
+            for (int m = 0; m < M; m++) {
+                taken[m] += ZERO ? u[m] * z : u[m];
+#pragma unroll
+                for (int c = 0; c < C; c++) acc[m][c] += f[c] * u[m];
             }
         }
     }
@@ -172,7 +180,7 @@ template <typename T, typename S, bool ZERO, int M, int C, int ROWS>
 __global__ __launch_bounds__(kTransposedWaves * kWave) void k_q4_mv_t(Q4 a, const void *x_, int64_t ldx, float *partial, int64_t vectors, int64_t part)
 {
     extern __shared__ float4 lds4[];
-    float *lds = reinterpret_cast<float *>(lds4);  // x of up to kTransposedRows rows of the part, [M][apart]; then the sums of one vector, [wavefront][64 C]
+    float *lds = reinterpret_cast<float *>(lds4);  // x of up to kTransposedRows rows of the part, [row][M]; then the sums of one vector, [wavefront][64 C]
     const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     const int64_t vector0 = (int64_t)blockIdx.z * M;
     const int64_t part0 = (int64_t)blockIdx.y * part, end = min(part0 + part, (int64_t)a.n_rows);
@@ -191,14 +199,14 @@ __global__ __launch_bounds__(kTransposedWaves * kWave) void k_q4_mv_t(Q4 a, cons
         if (row0 > part0) __syncthreads();
 #pragma unroll
         for (int m = 0; m < M; m++)
-            for (int i = threadIdx.x; i < apart; i += blockDim.x) lds[m * apart + i] = vector0 + m < vectors && i < rows ? to_f32(x[(vector0 + m) * ldx + row0 + i]) : 0.0f;
+            for (int i = threadIdx.x; i < apart; i += blockDim.x) lds[i * M + m] = vector0 + m < vectors && i < rows ? to_f32(x[(vector0 + m) * ldx + row0 + i]) : 0.0f;
         __syncthreads();
         for (; r < rows; r += 2 * kStep) {  // (the next rows' loads are issued before this one's are waited for)
             if (r + kStep < rows) two.load(a, row0, r + kStep, rows, at, scale_at);
-            one.template add<M>(lds + r, apart, acc, taken);
+            one.template add<M>(lds + r * M, acc, taken);
             if (r + kStep < rows) {
                 if (r + 2 * kStep < rows) one.load(a, row0, r + 2 * kStep, rows, at, scale_at);
-                two.template add<M>(lds + r + kStep, apart, acc, taken);
+                two.template add<M>(lds + (r + kStep) * M, acc, taken);
             }
         }
     }
@@ -262,6 +270,7 @@ template <typename T, typename S> __global__ __launch_bounds__(256) void k_q4_su
 
 // How a transposed product is cut: vectors, columns and rows at a time a lane takes, rows of a part.  Enough parts that every compute unit has two
 // workgroups, none of fewer rows than its wavefronts take at a time.
+constexpr int kTransposedVectors[] = {1, 2, 4, 6, 8, 10};
 struct TransposedShape {
     int m, c, rows;
     int64_t part, wide, parts;
@@ -269,11 +278,21 @@ struct TransposedShape {
 TransposedShape transposed_shape(const Q4 &a, int64_t vectors)
 {
     TransposedShape s;
-    s.m = vectors <= 1 ? 1 : vectors <= 2 ? 2 : vectors <= 4 ? 4 : 8;
+    // Vectors at a time: an fma for each of a word's eight codes and each vector, and some 27 instructions besides (a conversion for each code, the word's and the scale's
+    // loads): as few as may be in all.
+    s.m = 1;
+    int64_t least_cost = INT64_MAX;
+    for (int m : kTransposedVectors) {
+        const int64_t cost = (vectors + m - 1) / m * (27 + 9 * m);
+        if (cost < least_cost) {
+            least_cost = cost;
+            s.m = m;
+        }
+    }
     s.c = s.m <= 2 ? 16 : 8;
-    s.rows = 8;
+    s.rows = s.m <= 2 ? 8 : 4;
     s.wide = (a.n_cols + kWave * s.c - 1) / (kWave * s.c);
-    const int64_t passes = (vectors + s.m - 1) / s.m, least = s.rows * kTransposedWaves;
+    const int64_t passes = (vectors + s.m - 1) / s.m, least = 2 * s.rows * kTransposedWaves;
     const int64_t most = (a.n_rows + least - 1) / least, wanted = (512 + s.wide * passes - 1) / (s.wide * (passes > 0 ? passes : 1));
     s.parts = wanted < most ? wanted : most;
     s.part = ((a.n_rows + s.parts - 1) / s.parts + least - 1) / least * least;
@@ -404,17 +423,19 @@ int hbp_q4_mv_t(const hbp_q4_matrix_t *m, int type, const void *x, int64_t ldx, 
                 const size_t bytes = x_bytes > sum_bytes ? x_bytes : sum_bytes;
                 const T *x_at = static_cast<const T *>(x) + first * ldx;
                 auto go = [&](auto kernel) { kernel<<<grid, kTransposedWaves * kWave, bytes, st>>>(a, x_at, ldx, partial, count, s.part); };
-                if (a.zeros) {
-                    if (s.m == 1) go(k_q4_mv_t<T, S, true, 1, 16, 8>);
-                    else if (s.m == 2) go(k_q4_mv_t<T, S, true, 2, 16, 8>);
-                    else if (s.m == 4) go(k_q4_mv_t<T, S, true, 4, 8, 8>);
-                    else go(k_q4_mv_t<T, S, true, 8, 8, 8>);
-                } else {
-                    if (s.m == 1) go(k_q4_mv_t<T, S, false, 1, 16, 8>);
-                    else if (s.m == 2) go(k_q4_mv_t<T, S, false, 2, 16, 8>);
-                    else if (s.m == 4) go(k_q4_mv_t<T, S, false, 4, 8, 8>);
-                    else go(k_q4_mv_t<T, S, false, 8, 8, 8>);
-                }
+                auto by_zeros = [&](auto zeros) {
+                    constexpr bool kZero = decltype(zeros)::value;
+                    switch (s.m) {
+                    case 1: return go(k_q4_mv_t<T, S, kZero, 1, 16, 8>);
+                    case 2: return go(k_q4_mv_t<T, S, kZero, 2, 16, 8>);
+                    case 4: return go(k_q4_mv_t<T, S, kZero, 4, 8, 4>);
+                    case 6: return go(k_q4_mv_t<T, S, kZero, 6, 8, 4>);
+                    case 8: return go(k_q4_mv_t<T, S, kZero, 8, 8, 4>);
+                    default: return go(k_q4_mv_t<T, S, kZero, 10, 8, 4>);
+                    }
+                };
+                if (a.zeros) by_zeros(std::true_type());
+                else by_zeros(std::false_type());
                 HBP_HIP(hipGetLastError());
                 k_q4_sum_parts<T, S><<<dim3((unsigned)((a.n_cols + kWave - 1) / kWave), (unsigned)((count + 3) / 4)), 256, 0, st>>>(
                     a, x_at, ldx, partial, (int)s.parts, count, static_cast<T *>(y) + first * ldy, ldy);
