@@ -331,11 +331,11 @@ typedef enum { HBP_F32 = 0, HBP_F16 = 1, HBP_BF16 = 2 } hbp_type;
 /* A dense matrix of 4-bit codes: W[r][k] = scale[r][k / group] * (code[r][k] - zero[r][k / group]).
  *   codes  DEVICE, 16-byte aligned, n_rows rows of 16 * ceil(n_cols / 32) bytes: byte j of a row holds column 2j in its low four
  *          bits and column 2j+1 in its high ones.  What lies behind column n_cols is not looked at (hbp_q4_pack writes zeros).
- *   scales, zeros  DEVICE [n_rows][ceil(n_cols / group)] of scale_type; zeros NULL: 8 for all.  Both finite.
+ *   scales, zeros  DEVICE [n_rows][ceil(n_cols / group)] of scale_type; zeros NULL: 8 for all.
  *   group  columns that share a scale: 32, 64, 128, 256 or 512; the last group of a row may be shorter. */
 typedef struct {
     void *codes, *scales, *zeros;
-    int64_t n_rows, n_cols;   /* at most 2^31 - 512 and 2^28 */
+    int64_t n_rows, n_cols;   /* at most 2^30 and 2^28 */
     int32_t group, scale_type;
 } hbp_q4_matrix_t;
 

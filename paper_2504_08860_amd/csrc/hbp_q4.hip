@@ -303,7 +303,7 @@ TransposedShape transposed_shape(const Q4 &a, int64_t vectors)
 int view(const hbp_q4_matrix_t *m, Q4 *a)
 {
     if (!m || !m->codes || !m->scales || m->n_rows < 1 || m->n_cols < 1 || !is_type(m->scale_type)) return HBP_ERR_INVALID_ARGUMENT;
-    if (m->n_rows > (int64_t(1) << 31) - 512 || m->n_cols > int64_t(1) << 28) return HBP_ERR_TOO_LARGE;
+    if (m->n_rows > int64_t(1) << 30 || m->n_cols > int64_t(1) << 28) return HBP_ERR_TOO_LARGE;
     int shift = 5;
     while (shift < 9 && (1 << shift) != m->group) shift++;
     const int64_t bytes = type_bytes(m->scale_type);
