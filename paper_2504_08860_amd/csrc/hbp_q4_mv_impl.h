@@ -326,11 +326,11 @@ template <typename T> struct Staging {
 
 // The wavefronts' sums of one tile of 16 rows each are added over the column_waves by LDS and written: [wave][k][i][lane].
 template <typename T, typename S, int SETS, int NR>
-__device__ __forceinline__ void add_up_and_write(const Q4Product &p, const float (&acc)[SETS][NR], float *sums, int64_t first_row, int row_waves, int rows_apart, int64_t vector0,
+__device__ __forceinline__ void add_up_and_write(const Q4Product &p, const float (&acc)[SETS][NR], float *sums, int64_t first_row, int log_row_waves, int rows_apart, int64_t vector0,
                                                  int vectors)
 {
     constexpr int kParts = sizeof(T) == 4 ? 3 : 1;
-    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, column_waves = blockDim.x / kWave / row_waves;
+    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, column_waves = blockDim.x / kWave >> log_row_waves, row_waves = 1 << log_row_waves;
     __syncthreads();
 #pragma unroll
     for (int k = 0; k < SETS; k++)
@@ -340,8 +340,8 @@ __device__ __forceinline__ void add_up_and_write(const Q4Product &p, const float
     const int outputs = 16 * row_waves * vectors;
     for (int i0 = 0; i0 < outputs; i0 += blockDim.x) {
         const int i = i0 + threadIdx.x;
-        const int v = i / (16 * row_waves), rw = i / 16 % row_waves;
-        const int64_t row = first_row + rw * rows_apart + i % 16;
+        const int v = i >> (4 + log_row_waves), rw = (i >> 4) & (row_waves - 1);
+        const int64_t row = first_row + rw * rows_apart + (i & 15);
         const bool mine = i < outputs && row < p.a.n_rows;
         float sum = 0;
         if (mine)
@@ -349,7 +349,7 @@ __device__ __forceinline__ void add_up_and_write(const Q4Product &p, const float
                 const int slot = v * kParts + part;
                 float one = 0;
                 for (int w = 0; w < column_waves; w++)
-                    one += sums[(((w * row_waves + rw) * SETS + (slot >> 4)) * NR + (slot >> 2 & 3)) * kWave + (slot & 3) * 16 + i % 16];
+                    one += sums[(((w * row_waves + rw) * SETS + (slot >> 4)) * NR + (slot >> 2 & 3)) * kWave + (slot & 3) * 16 + (i & 15)];
                 sum += one;
             }
         uint64_t again = __ballot(mine && !(fabsf(sum) < INFINITY));
@@ -357,7 +357,7 @@ __device__ __forceinline__ void add_up_and_write(const Q4Product &p, const float
             const int from = __builtin_ctzll(again);
             again &= again - 1;
             const int j = i0 + (int)(threadIdx.x - lane) + from;
-            const float exact = by_definition<T, S>(p, first_row + j / 16 % row_waves * rows_apart + j % 16, vector0 + j / (16 * row_waves));
+            const float exact = by_definition<T, S>(p, first_row + ((j >> 4) & (row_waves - 1)) * rows_apart + (j & 15), vector0 + (j >> (4 + log_row_waves)));
             if (lane == from) sum = exact;
         }
         if (mine) static_cast<T *>(p.y)[(vector0 + v) * p.ldy + row] = from_f32<T>(sum);
@@ -371,12 +371,12 @@ constexpr int kMostSlots = 64;
 constexpr int kStageBytes = 140 * 1024;  // of LDS, at most
 constexpr int kThreads = 512;
 template <typename T, typename S, bool ZERO, int GM, int SETS, int NR, int RT, int U>
-__global__ __launch_bounds__(kThreads) void k_q4_mv(Q4Product p, int32_t per_pass, int32_t row_waves)
+__global__ __launch_bounds__(kThreads) void k_q4_mv(Q4Product p, int32_t per_pass, int32_t log_row_waves)
 {
     using MT = std::conditional_t<sizeof(T) == 4, bf16, T>;
     constexpr int kParts = sizeof(T) == 4 ? 3 : 1;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), waves = blockDim.x / kWave;
-    const int column_waves = waves / row_waves, row_wave = wave % row_waves, column_wave = wave / row_waves;
+    const int row_waves = 1 << log_row_waves, column_waves = waves >> log_row_waves, row_wave = wave & (row_waves - 1), column_wave = wave >> log_row_waves;
     const int64_t vector0 = (int64_t)blockIdx.y * per_pass;
     const int vectors = (int)min((int64_t)per_pass, p.vectors - vector0), slots = vectors * kParts;
     const int64_t first_row = (int64_t)blockIdx.x * row_waves * (16 * RT), row0 = first_row + row_wave * (16 * RT);
@@ -384,8 +384,8 @@ __global__ __launch_bounds__(kThreads) void k_q4_mv(Q4Product p, int32_t per_pas
 #pragma unroll
     for (int t = 0; t < RT; t++) place[t].at(p.a, row0 + 16 * t);
     const int chunks = (p.a.n_cols + 127) / 128;
-    const int step_chunks = column_waves * U, steps = (chunks + step_chunks - 1) / step_chunks;
-    const int log_eights = __builtin_ctz(step_chunks) + 4;  // (a power of two)
+    const int step_chunks = column_waves * U, log_eights = __builtin_ctz(step_chunks) + 4;  // (a power of two)
+    const int steps = (chunks + step_chunks - 1) >> (log_eights - 4);
     const int stride = step_chunks * 128 + kStagePad, buffer = per_pass * kParts * stride;  // values of a slot and of all in LDS
     uint16_t *const x0 = reinterpret_cast<uint16_t *>(lds) + kZeros / 2, *const x1 = x0 + buffer;
     const uint32_t byte0 = column_wave * U * 256, byte1 = byte0 + buffer * 2;
@@ -418,7 +418,7 @@ __global__ __launch_bounds__(kThreads) void k_q4_mv(Q4Product p, int32_t per_pas
         }
     }
 #pragma unroll
-    for (int t = 0; t < RT; t++) add_up_and_write<T, S>(p, acc[t], reinterpret_cast<float *>(lds), first_row + 16 * t, row_waves, 16 * RT, vector0, vectors);
+    for (int t = 0; t < RT; t++) add_up_and_write<T, S>(p, acc[t], reinterpret_cast<float *>(lds), first_row + 16 * t, log_row_waves, 16 * RT, vector0, vectors);
 }
 
 // Many rows and few slots: x stays in LDS as a whole, and each wavefront walks through tiles of RT times 16 rows by itself, all columns of a tile after one
@@ -548,7 +548,7 @@ template <typename T, typename S, bool ZERO, int GM> int launch_mv(const Q4Produ
         const dim3 grid((unsigned)((tiles + rt * row_waves - 1) / (rt * row_waves)), (unsigned)((q.vectors + per_pass - 1) / per_pass));
         const int rc = [&](auto kernel) -> int {
             if (bytes > 64 * 1024) HBP_HIP(hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, kStageBytes));
-            kernel<<<grid, waves * kWave, bytes, st>>>(q, per_pass, row_waves);
+            kernel<<<grid, waves * kWave, bytes, st>>>(q, per_pass, __builtin_ctz(row_waves));
             HBP_HIP(hipGetLastError());
             return HBP_OK;
         }(slots <= 4  ? (u == 4 ? k_q4_mv<T, S, ZERO, GM, 1, 1, 1, 4> : k_q4_mv<T, S, ZERO, GM, 1, 1, 1, 2>)
