@@ -502,9 +502,9 @@ __global__ __launch_bounds__(kThreads) void k_q4_mv_rows(Q4Product p)
 
 // Which kernel, and its shape.  Measured, us, the shapes in the order RT, U, wavefronts, row_waves (rows: k_q4_mv_rows):
 //   1 to 4 slots: where each wavefront of two workgroups a compute unit has tiles to walk through, rows; 131072 x 4096 58.6 (1 4 4 4: 64.5).  Else few
-//     row_waves, so that a column_wave's way is short: 4096 x 4096 1 4 8 1 6.1, with two row_waves 8.6; 14336 x 4096 (4 vectors) 1 2 8 2 13.1, 1 2 8 4 13.7.  Short rows
+//     row_waves, so that a column_wave's way is short: 4096 x 4096 1 4 8 1 6.1, with two row_waves 8.6; 14336 x 4096 (4 vectors) 1 2 8 2 13.1, 1 4 8 2 16.6; fp32 8192 x 28672 1 4 8 2 39, 1 2 8 2 44.  Short rows
 //     leave eight wavefronts nothing to do: 1000 x 1000 1 2 4 1 4.2, 1 2 8 1 5.0.
-//   5 to 16: 16 x 4096 x 4096 1 1 8 1 8.9, 1 2 8 2 10.2; fp32 5 x 10007 x 7001 1 2 8 4 24.3, 2 2 8 2 24.4, 1 1 4 1 25.2.
+//   5 to 16: 16 x 4096 x 4096 1 1 8 1 8.9, 1 2 8 2 10.2; fp32 5 x 10007 x 7001 1 2 8 4 24.3, 2 2 8 2 24.4, 1 1 4 1 25.2; 12 x 40000 x 4096 1 2 4 4 31, 1 2 8 4 40.
 //   more: as many column_waves as x of a step fits the threads' registers with, and with many rows none; 24 x 8192 x 8192 1 1 8 2 24.8, 2 1 8 2 32.7;
 //     64 x 4096 x 4096 1 1 8 4 31.5, 1 1 8 8 47.8; 48 x 131072 x 4096 2 1 8 8 143, 1 1 8 8 180; 64 x 32768 x 8192 1 1 8 8 103, 2 1 8 8 208 (registers).
 template <typename T, typename S, bool ZERO, int GM> int launch_mv(const Q4Product &p, hipStream_t st)
@@ -525,8 +525,10 @@ template <typename T, typename S, bool ZERO, int GM> int launch_mv(const Q4Produ
     if (slots <= 4) {
         waves = chunks > 8 ? 8 : 4;
         row_waves = tiles >= 512 ? 2 : 1;
-        u = chunks * row_waves >= 4 * waves ? 4 : 2;
+        const int64_t four = 4 * (waves / row_waves);  // chunks of a step with U = 4: of use where they are all there are, or where there are several steps
+        u = (chunks > four / 2 && chunks <= four) || chunks >= 4 * four ? 4 : 2;
     } else if (sets == 1) {
+        waves = tiles >= 2048 ? 4 : 8;
         row_waves = tiles > 512 ? 4 : 1;
         u = tiles > 512 ? 2 : 1;
     } else {
