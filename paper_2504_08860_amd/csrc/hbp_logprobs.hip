@@ -142,7 +142,9 @@ template <typename T> __device__ __forceinline__ void finish_row(const LogprobAr
     }
 }
 
-// One pass over a part of a row: statistics in every lane, eight logits at a time.
+// One pass over a part of a row: statistics in every lane, eight logits at a time.  Bound: HBM; 4096 x 32000 bf16 52 us, 5 TB/s, x 32001 (rows at odd addresses) 64, 79 behind 262 MB of
+// writes; some 100 vector instructions, nine of them exponentials, for a wavefront's 512 logits.  Alternatives: barriers and the selection, 8 us for one row in 32 parts,
+// 15 for 64 rows of 50001 in 13.
 //
 // Alternatives: the threads' eights of one turn are a block.  Whatever is below `least` (as order_of has it) cannot be among the top first ones, so only lanes whose largest
 // of eight is not matter, and after the first block hardly any is.  In a block with such lanes `least` is raised before anything is handed over: to the top'th of
@@ -271,7 +273,7 @@ template <typename T, bool TOP, int UNROLL> __global__ __launch_bounds__(kMostTh
     }
 }
 
-// Joins the parts of a row.  Of the parts' alternatives only those matter that are not behind the last one of any part that has `top` of them, nor behind the
+// Joins the parts of a row: 5 us, the latency of loads, two rounds of ranks and the selection.  Of the parts' alternatives only those matter that are not behind the last one of any part that has `top` of them, nor behind the
 // top'th of the parts' first ones.
 constexpr int kJoinThreads = 256, kMostParts = 64;
 template <typename T> __global__ __launch_bounds__(kJoinThreads) void k_logprobs_join(LogprobArgs p)
@@ -309,6 +311,7 @@ struct LogprobBackArgs {
     void *d_logits;
 };
 
+// The gradient, eight logits a thread.  Bound: HBM; 4096 x 32001 bf16 93 us, 5.6 TB/s read and written.
 template <typename T> __global__ __launch_bounds__(256) void k_logprobs_backward(LogprobBackArgs p)
 {
     const int64_t t = blockIdx.y;
@@ -336,7 +339,7 @@ template <typename T> __global__ __launch_bounds__(256) void k_logprobs_backward
     out.store_first(d + col, left);
 }
 
-// parts of a row: enough workgroups for the chip, none of fewer than 4096 logits
+// parts of a row: enough workgroups for the chip (one block each: 64 x 50001 in 8 parts of two blocks 22 us, in 13 of one 15), none of fewer than 4096 logits
 int64_t parts_of(int64_t tokens, int64_t vocabulary)
 {
     const int64_t most = (vocabulary + 4095) / 4096, wanted = (2048 + tokens - 1) / (tokens > 0 ? tokens : 1);

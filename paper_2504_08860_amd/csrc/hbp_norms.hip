@@ -16,7 +16,7 @@ struct NormArgs {
 };
 
 // Forward.  A row is a workgroup's: THREADS threads with CHUNKS times eight columns each, which stay in registers from the only
-// read to the writes; two sums over the row lie between.
+// read to the writes; two sums over the row lie between.  Bound: HBM; 8192 x 4096 bf16 with a gate for each value 63 us, 5.3 TB/s; one row of 4096 2.6 us.
 template <typename T, int THREADS, int CHUNKS, int GATE>
 __global__ __launch_bounds__(THREADS) void k_residual_norms(NormArgs n)
 {
@@ -97,7 +97,9 @@ struct NormBackArgs {
 // h' is computed again from h, y and the gate, which are read anyway: not the rounded one, and no read more.
 //
 // A workgroup walks through every so many rows and keeps its columns' sums for the weights in registers; workgroups' sums are added by a second kernel, in their
-// order.  Of a row, what was read stays in registers as it came (h' is cheaper to compute twice than to keep), and so do the weights.
+// order.  Of a row, what was read stays in registers as it came (h' is cheaper to compute twice than to keep), and so do the weights.  512 threads at most: with 1024
+// a row of 16384 columns does not fit their 128 registers.  Bound: HBM; 8192 x 4096 bf16 with a gate for each value 113 us, 4.7 TB/s, and 5 for the workgroups' sums (39 with
+// four shares and one load at a time).
 template <typename T, int THREADS, int CHUNKS, int GATE>
 __global__ __launch_bounds__(THREADS) void k_residual_norms_backward(NormBackArgs n)
 {
