@@ -349,7 +349,7 @@ int hbp_q4_pack(const hbp_q4_matrix_t *a, int type, const void *w, int64_t ldw, 
 int hbp_q4_unpack(const hbp_q4_matrix_t *a, int type, void *w, int64_t ldw, void *stream);
 
 /* Products with `vectors` vectors at once (rows of x and y: x [vectors][n_cols], y [vectors][n_rows], both of `type`; x and y must not
- * overlap): y[m][r] = sum over k of W[r][k] x[m][k].  The weights are read once for 64 vectors (fp32: 21).  vectors = 0 does nothing. */
+ * overlap): y[m][r] = sum over k of W[r][k] x[m][k].  The weights are read once for 64 vectors (fp32: 21).  vectors at most 2^24; 0 does nothing. */
 int hbp_q4_mv(const hbp_q4_matrix_t *a, int type, const void *x, int64_t ldx, void *y, int64_t ldy, int64_t vectors, void *stream);
 /* The transposed product, which is the gradient of hbp_q4_mv for its x: y[m][k] = sum over r of W[r][k] x[m][r], x [vectors][n_rows],
  * y [vectors][n_cols]. */

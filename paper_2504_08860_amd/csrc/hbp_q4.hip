@@ -1,6 +1,8 @@
 // Matrices held in 4 bits with group scales: packing, and products with a few vectors (hbp_q4_pack, hbp_q4_unpack, hbp_q4_mv, hbp_q4_mv_t).
 #include "hbp_q4.h"
 
+#include <algorithm>
+
 namespace hbp {
 namespace {
 
@@ -105,7 +107,7 @@ template <typename T, typename S> __global__ __launch_bounds__(256) void k_q4_un
 // are added up by LDS, the parts by a second kernel.
 //
 // Bound: vector instructions, 1.4 + M a weight (a conversion for each code and an fma for each vector), and their latency; us: 1 x 8192 x 8192 fp32 14 + 4 for the
-// sum, 19 x 6001 x 4099 with zero points 39.5 + 4.5, 64 x 8192 x 8192 178 (48 TFLOP/s of the 79 that fp32 fma has here).  Not by the matrix cores: there the scale, which
+// sum, 19 x 6001 x 4099 with zero points 31 + 4.5, 64 x 8192 x 8192 173 (50 TFLOP/s of the 79 that fp32 fma has here).  Not by the matrix cores: there the scale, which
 // differs from row to row, would have to go into x, in parts, for every group anew.
 // As in the products, code * (scale x) may be infinite where the sum is not: such results are computed again from the definition.
 constexpr int kTransposedWaves = 8, kTransposedRows = 512;  // rows whose x lies in LDS at a time
@@ -269,8 +271,7 @@ template <typename T, typename S> __global__ __launch_bounds__(256) void k_q4_su
     if (mine) static_cast<T *>(y)[m * ldy + col] = from_f32<T>(sum);
 }
 
-// How a transposed product is cut: vectors, columns and rows at a time a lane takes, rows of a part.  Enough parts that every compute unit has two
-// workgroups, none of fewer rows than its wavefronts take at a time.
+// How a transposed product is cut: vectors, columns and rows at a time a lane takes, rows of a part, none of fewer rows than its wavefronts take at a time.
 constexpr int kTransposedVectors[] = {1, 2, 4, 6, 8, 10};
 struct TransposedShape {
     int m, c, rows;
@@ -293,9 +294,21 @@ TransposedShape transposed_shape(const Q4 &a, int64_t vectors)
     s.c = s.m <= 2 ? 16 : 8;
     s.rows = s.m <= 2 ? 8 : 4;
     s.wide = (a.n_cols + kWave * s.c - 1) / (kWave * s.c);
-    const int64_t passes = (vectors + s.m - 1) / s.m, least = 2 * s.rows * kTransposedWaves;
-    const int64_t most = (a.n_rows + least - 1) / least, wanted = (512 + s.wide * passes - 1) / (s.wide * (passes > 0 ? passes : 1));
-    s.parts = wanted < most ? wanted : most;
+    // Parts: a workgroup for each place on the chip (256 compute units hold one of more than six vectors, 157 registers, or two), or for several rounds of them; as many as
+    // leave the fewest places empty in the last round.  19 x 6001 x 4099 in 432 workgroups 43.8 us, in 252 35.4; 8 x 8192 x 8192 in 512 38.8, in 256 31.5.
+    const int64_t passes = std::max<int64_t>((vectors + s.m - 1) / s.m, 1), least = 2 * s.rows * kTransposedWaves;
+    const int64_t most = (a.n_rows + least - 1) / least, places = s.m > 6 ? 256 : 512, each = s.wide * passes;
+    const int64_t first = std::max<int64_t>(places / each, 1);
+    double fullest = 0;
+    s.parts = 1;
+    for (int64_t parts = first; parts < first + 8; parts++) {
+        const int64_t all = std::min(parts, most) * each, rounds = (all + places - 1) / places;
+        const double full = (double)all / (double)(rounds * places);
+        if (full > fullest + 0.03) {
+            fullest = full;
+            s.parts = std::min(parts, most);
+        }
+    }
     s.part = ((a.n_rows + s.parts - 1) / s.parts + least - 1) / least * least;
     s.parts = (a.n_rows + s.part - 1) / s.part;
     return s;
@@ -316,13 +329,14 @@ int view(const hbp_q4_matrix_t *m, Q4 *a)
     return HBP_OK;
 }
 
+constexpr int64_t kMostVectors = int64_t(1) << 24;  // (so that a workspace's bytes can be counted)
+
 // checks what both products share
-int check_product(const hbp_q4_matrix_t *m, Q4 *a, int type, const void *x, int64_t ldx, int64_t n_x, const void *y, int64_t ldy, int64_t n_y, int64_t vectors)
+int check_product(int type, const void *x, int64_t ldx, int64_t n_x, const void *y, int64_t ldy, int64_t n_y, int64_t vectors)
 {
     if (!is_type(type) || vectors < 0 || (vectors > 1 && (ldx < n_x || ldy < n_y))) return HBP_ERR_INVALID_ARGUMENT;
-    if (vectors > (int64_t(1) << 31) - 512) return HBP_ERR_TOO_LARGE;
+    if (vectors > kMostVectors) return HBP_ERR_TOO_LARGE;
     if (vectors > 0 && (!x || !y || !aligned(x, type_bytes(type)) || !aligned(y, type_bytes(type)))) return HBP_ERR_INVALID_ARGUMENT;
-    (void)m; (void)a;
     return HBP_OK;
 }
 
@@ -375,7 +389,7 @@ int hbp_q4_mv(const hbp_q4_matrix_t *m, int type, const void *x, int64_t ldx, vo
     using namespace hbp;
     Q4 a;
     int rc = view(m, &a);
-    if (rc == HBP_OK) rc = check_product(m, &a, type, x, ldx, m->n_cols, y, ldy, m->n_rows, vectors);
+    if (rc == HBP_OK) rc = check_product(type, x, ldx, m->n_cols, y, ldy, m->n_rows, vectors);
     if (rc != HBP_OK || vectors == 0) return rc;
     rc = earlier_error();
     if (rc != HBP_OK) return rc;
@@ -392,6 +406,7 @@ int hbp_q4_mv_t_workspace(const hbp_q4_matrix_t *m, int64_t vectors, size_t *byt
     const int rc = view(m, &a);
     if (rc != HBP_OK) return rc;
     if (!bytes || vectors < 0) return HBP_ERR_INVALID_ARGUMENT;
+    if (vectors > kMostVectors) return HBP_ERR_TOO_LARGE;
     *bytes = (size_t)transposed_shape(a, vectors).parts * (size_t)vectors * (size_t)a.n_cols * sizeof(float);
     return HBP_OK;
 }
@@ -403,7 +418,7 @@ int hbp_q4_mv_t(const hbp_q4_matrix_t *m, int type, const void *x, int64_t ldx, 
     Q4 a;
     size_t need = 0;
     int rc = view(m, &a);
-    if (rc == HBP_OK) rc = check_product(m, &a, type, x, ldx, m->n_rows, y, ldy, m->n_cols, vectors);
+    if (rc == HBP_OK) rc = check_product(type, x, ldx, m->n_rows, y, ldy, m->n_cols, vectors);
     if (rc == HBP_OK) rc = hbp_q4_mv_t_workspace(m, vectors, &need);
     if (rc != HBP_OK || vectors == 0) return rc;
     if (need && (!workspace || workspace_bytes < need || !aligned(workspace, 256))) return HBP_ERR_INVALID_ARGUMENT;

@@ -344,10 +344,13 @@ def test_what_the_library_refuses():
         a = good | change
         assert L.hbp_q4_mv(matrix_, a["type"], a["x"], a["ldx"], a["y"], a["ldy"], a["vectors"], None) == -1, change
     assert L.hbp_q4_mv(m(rows=1 << 31), 0, at(4096), 64, at(4096), 1 << 31, 1, None) == -4
+    assert L.hbp_q4_mv(m(cols=(1 << 28) + 1), 0, at(4096), 1 << 29, at(4096), 8, 1, None) == -4
+    assert L.hbp_q4_mv(m(), 0, at(4096), 64, at(8192), 8, (1 << 24) + 1, None) == -4
     assert L.hbp_q4_mv(None, 0, at(4096), 64, at(4096), 8, 1, None) == -1
     assert L.hbp_q4_mv(m(), 0, None, 64, None, 8, 0, None) == 0
     need = ctypes.c_size_t()
     assert L.hbp_q4_mv_t_workspace(m(), 3, need) == 0 and L.hbp_q4_mv_t_workspace(m(), -1, need) == -1 and L.hbp_q4_mv_t_workspace(m(), 3, None) == -1
+    assert L.hbp_q4_mv_t_workspace(m(), (1 << 24) + 1, need) == -4
     for matrix_, change in bad:
         if not change:
             assert L.hbp_q4_pack(matrix_, 0, at(4096), 64, None) == -1
