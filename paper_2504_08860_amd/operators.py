@@ -110,6 +110,7 @@ def _matrix(codes, scales, zeros, n_cols, group, device):
     n_rows = codes.shape[0]
     kind = scales.dtype
     assert kind in _types, "scales: float32, float16 or bfloat16 required"
+    assert group > 0, "group: a number of columns required"
     groups = (n_rows, (n_cols + group - 1) // group)
     return hbp_q4_matrix_t(_whole(codes, "codes", (n_rows, (n_cols + 31) // 32 * 16), _uint8, device), _whole(scales, "scales", groups, kind, device),
                            _whole(zeros, "zeros", groups, kind, device), n_rows, n_cols, group, _types[kind])

@@ -316,7 +316,7 @@ def test_what_the_binding_refuses():
     x, y = torch.zeros(2, 40, device="cuda"), torch.zeros(2, 20, device="cuda")
     wrong = [dict(codes=c[:, :-1]), dict(codes=c.int()), dict(scales=s[:, :1]), dict(scales=s.double()), dict(x=x.double()), dict(x=x.half()),
              dict(x=x.cpu()), dict(x=x[:1]), dict(y=y[:, :-1]), dict(y=y.cpu()), dict(x=x.t().contiguous().t()), dict(x=x[:1].expand(2, 40)),
-             dict(group=64), dict(zeros=s.half()), dict(zeros=s[:-1]), dict(x=x[0])]
+             dict(group=64), dict(group=0), dict(zeros=s.half()), dict(zeros=s[:-1]), dict(x=x[0])]
     for change in wrong:
         a = dict(codes=c, scales=s, x=x, y=y, group=32, zeros=None) | change
         with pytest.raises(AssertionError):
