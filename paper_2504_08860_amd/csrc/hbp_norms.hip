@@ -1,6 +1,8 @@
 // Residual sum, gate and norms between two blocks, and their gradients (hbp_residual_norms, hbp_residual_norms_backward).
 #include "hbp_ops.h"
 
+#include <algorithm>
+
 namespace hbp {
 namespace {
 
@@ -15,13 +17,16 @@ struct NormArgs {
     float *rstd;
 };
 
-// Forward.  A row is a workgroup's: THREADS threads with CHUNKS times eight columns each, which stay in registers from the only
+// Forward.  A row is a workgroup's or, up to 256 columns, that of 8 to 32 lanes of a one-wavefront workgroup (with 64 lanes for every row, most of them without columns,
+// 100000 x 128 with gradients took 144 us, so 80): THREADS threads with CHUNKS times eight columns each, which stay in registers from the only
 // read to the writes; two sums over the row lie between.  Bound: HBM; 8192 x 4096 bf16 with a gate for each value 63 us, 5.3 TB/s; one row of 4096 2.6 us.
 template <typename T, int THREADS, int CHUNKS, int GATE>
-__global__ __launch_bounds__(THREADS) void k_residual_norms(NormArgs n)
+__global__ __launch_bounds__(THREADS < kWave ? kWave : THREADS) void k_residual_norms(NormArgs n)
 {
-    __shared__ float slots[2][THREADS / kWave];
-    const int64_t t = blockIdx.x;
+    __shared__ float slots[2][THREADS < kWave ? 1 : THREADS / kWave];
+    constexpr int kAtOnce = THREADS < kWave ? kWave / THREADS : 1;  // rows of a workgroup
+    const int thread = threadIdx.x % THREADS;
+    const int64_t mine = (int64_t)blockIdx.x * kAtOnce + threadIdx.x / THREADS, t = min(mine, n.tokens - 1);  // (behind the last row it is read again)
     const T *h = static_cast<const T *>(n.h) + t * n.ldh, *y = static_cast<const T *>(n.y) + t * n.ldy;
     const T *g = GATE == HBP_GATE_FULL ? static_cast<const T *>(n.gate) + t * n.ldg : static_cast<const T *>(n.gate);
     const T *w_post = static_cast<const T *>(n.w_post), *w_pre = static_cast<const T *>(n.w_pre);
@@ -30,7 +35,7 @@ __global__ __launch_bounds__(THREADS) void k_residual_norms(NormArgs n)
     if constexpr (GATE == HBP_GATE_TOKEN) row_gate *= to_f32(g[t]);
 #pragma unroll
     for (int c = 0; c < CHUNKS; c++) {
-        const int col = (c * THREADS + threadIdx.x) * 8;
+        const int col = (c * THREADS + thread) * 8;
         yy[c].load_first(y + col, n.width - col);
         hh[c].load_first(h + col, n.width - col);
         if constexpr (GATE == HBP_GATE_FULL || GATE == HBP_GATE_CHANNEL) gg[c].load_first(g + col, n.width - col);
@@ -46,7 +51,7 @@ __global__ __launch_bounds__(THREADS) void k_residual_norms(NormArgs n)
     sum[0] = 0;
 #pragma unroll
     for (int c = 0; c < CHUNKS; c++) {
-        const int col = (c * THREADS + threadIdx.x) * 8;
+        const int col = (c * THREADS + thread) * 8;
         Eight<T> w;
         if (w_post) w.load_first(w_post + col, n.width - col);
 #pragma unroll
@@ -60,10 +65,11 @@ __global__ __launch_bounds__(THREADS) void k_residual_norms(NormArgs n)
     }
     block_sums<1, THREADS>(sum, slots[1]);
     const float r2 = rsqrtf(sum[0] / n.width + n.eps);
+    if (mine != t) return;
     T *h_out = static_cast<T *>(n.h_out) + t * n.ldho, *x_out = static_cast<T *>(n.x_out) + t * n.ldxo;
 #pragma unroll
     for (int c = 0; c < CHUNKS; c++) {
-        const int col = (c * THREADS + threadIdx.x) * 8;
+        const int col = (c * THREADS + thread) * 8;
         Eight<T> w, a, b;
         if (w_pre) w.load_first(w_pre + col, n.width - col);
 #pragma unroll
@@ -75,7 +81,7 @@ __global__ __launch_bounds__(THREADS) void k_residual_norms(NormArgs n)
         a.store_first(h_out + col, n.width - col);
         b.store_first(x_out + col, n.width - col);
     }
-    if (n.rstd && threadIdx.x == 0) {
+    if (n.rstd && thread == 0) {
         n.rstd[2 * t] = r1;
         n.rstd[2 * t + 1] = r2;
     }
@@ -88,7 +94,7 @@ struct NormBackArgs {
     const void *d_h_out, *d_x_out, *h, *y, *w_post, *w_pre, *gate;
     const float *rstd;
     void *d_h, *d_y, *d_gate;
-    float *partial;  // [workgroups][3][width]: d_w_post, d_w_pre, a CHANNEL's d_gate
+    float *partial;  // [workgroups times rows at once][3][width]: d_w_post, d_w_pre, a CHANNEL's d_gate
 };
 
 // Backward.  With a = d_x_out w_pre, e = d_h_out + r2 (a - h' r2^2 mean(a h')) is d_h, and b = scale g w_post e goes through the
@@ -101,14 +107,16 @@ struct NormBackArgs {
 // a row of 16384 columns does not fit their 128 registers.  Bound: HBM; 8192 x 4096 bf16 with a gate for each value 113 us, 4.7 TB/s, and 5 for the workgroups' sums (39 with
 // four shares and one load at a time).
 template <typename T, int THREADS, int CHUNKS, int GATE>
-__global__ __launch_bounds__(THREADS) void k_residual_norms_backward(NormBackArgs n)
+__global__ __launch_bounds__(THREADS < kWave ? kWave : THREADS) void k_residual_norms_backward(NormBackArgs n)
 {
-    __shared__ float slots[2][THREADS / kWave * 3];
+    __shared__ float slots[2][THREADS < kWave ? 1 : THREADS / kWave * 3];
+    constexpr int kAtOnce = THREADS < kWave ? kWave / THREADS : 1;  // rows of a workgroup
+    const int thread = threadIdx.x % THREADS, of_these = threadIdx.x / THREADS;
     constexpr bool kFull = GATE == HBP_GATE_FULL, kChannel = GATE == HBP_GATE_CHANNEL;
     Eight<T> wp[CHUNKS], wq[CHUNKS], gg[CHUNKS];
 #pragma unroll
     for (int c = 0; c < CHUNKS; c++) {
-        const int col = (c * THREADS + threadIdx.x) * 8, left = n.width - col;
+        const int col = (c * THREADS + thread) * 8, left = n.width - col;
 #pragma unroll
         for (int i = 0; i < 8; i++) {
             wp[c].set(i, 1.0f);
@@ -121,14 +129,16 @@ __global__ __launch_bounds__(THREADS) void k_residual_norms_backward(NormBackArg
     float sum_post[CHUNKS][8] = {}, sum_pre[CHUNKS][8] = {}, sum_gate[kChannel ? CHUNKS : 1][8] = {};
     const float inverse_width = 1.0f / n.width;
     int odd = 0;
-    for (int64_t t = blockIdx.x; t < n.tokens; t += gridDim.x, odd ^= 1) {
+    for (int64_t t0 = (int64_t)blockIdx.x * kAtOnce; t0 < n.tokens; t0 += (int64_t)gridDim.x * kAtOnce, odd ^= 1) {
+        const bool mine = t0 + of_these < n.tokens;  // (behind the last row it is read again, for nothing)
+        const int64_t t = mine ? t0 + of_these : n.tokens - 1;
         const T *h = static_cast<const T *>(n.h) + t * n.ldh, *y = static_cast<const T *>(n.y) + t * n.ldy;
         const float r1 = n.rstd[2 * t], r2 = n.rstd[2 * t + 1];
         const float row_gate = GATE == HBP_GATE_TOKEN ? to_f32(static_cast<const T *>(n.gate)[t]) : 1.0f;
         Eight<T> yy[CHUNKS], hh[CHUNKS], dx[CHUNKS], dh[CHUNKS];
 #pragma unroll
         for (int c = 0; c < CHUNKS; c++) {
-            const int col = (c * THREADS + threadIdx.x) * 8, left = n.width - col;
+            const int col = (c * THREADS + thread) * 8, left = n.width - col;
             yy[c].load_first(y + col, left);
             hh[c].load_first(h + col, left);
             dx[c].clear();
@@ -150,13 +160,14 @@ __global__ __launch_bounds__(THREADS) void k_residual_norms_backward(NormBackArg
                 sum[2] += wy * next;
             }
         block_sums<3, THREADS>(sum, slots[odd]);
+        if (!mine) continue;
         const float along2 = r2 * r2 * r2 * (sum[0] * inverse_width);
         const float through = sum[1] - along2 * sum[2];  // sum of b y, a row's gate left out
         const float along1 = r1 * r1 * r1 * (row_gate * through * inverse_width);
-        if (GATE == HBP_GATE_TOKEN && n.d_gate && threadIdx.x == 0) static_cast<float *>(n.d_gate)[t] = r1 * through;
+        if (GATE == HBP_GATE_TOKEN && n.d_gate && thread == 0) static_cast<float *>(n.d_gate)[t] = r1 * through;
 #pragma unroll
         for (int c = 0; c < CHUNKS; c++) {
-            const int col = (c * THREADS + threadIdx.x) * 8, left = n.width - col;
+            const int col = (c * THREADS + thread) * 8, left = n.width - col;
             Eight<T> de, dy, dg;
 #pragma unroll
             for (int i = 0; i < 8; i++) {
@@ -179,16 +190,16 @@ __global__ __launch_bounds__(THREADS) void k_residual_norms_backward(NormBackArg
                 if (n.d_gate) dg.store_first(static_cast<T *>(n.d_gate) + t * n.ldg + col, left);
         }
     }
-    float *mine = n.partial + (int64_t)blockIdx.x * 3 * n.width;
+    float *sums = n.partial + ((int64_t)blockIdx.x * kAtOnce + of_these) * 3 * n.width;
 #pragma unroll
     for (int c = 0; c < CHUNKS; c++) {
-        const int col = (c * THREADS + threadIdx.x) * 8;
+        const int col = (c * THREADS + thread) * 8;
 #pragma unroll
         for (int i = 0; i < 8; i++)
             if (col + i < n.width) {
-                mine[col + i] = sum_post[c][i];
-                mine[n.width + col + i] = sum_pre[c][i];
-                if constexpr (kChannel) mine[2 * n.width + col + i] = sum_gate[c][i];
+                sums[col + i] = sum_post[c][i];
+                sums[n.width + col + i] = sum_pre[c][i];
+                if constexpr (kChannel) sums[2 * n.width + col + i] = sum_gate[c][i];
             }
     }
 }
@@ -228,6 +239,9 @@ __global__ __launch_bounds__(kShares * 64) void k_norm_weight_sums(const float *
 template <int V> struct Int { static constexpr int value = V; };
 template <typename F> int by_width_forward(int64_t width, F f)
 {
+    if (width <= 64) return f(Int<8>(), Int<1>());
+    if (width <= 128) return f(Int<16>(), Int<1>());
+    if (width <= 256) return f(Int<32>(), Int<1>());
     if (width <= 512) return f(Int<64>(), Int<1>());
     if (width <= 2048) return f(Int<256>(), Int<1>());
     if (width <= 4096) return f(Int<512>(), Int<1>());
@@ -236,6 +250,9 @@ template <typename F> int by_width_forward(int64_t width, F f)
 }
 template <typename F> int by_width_backward(int64_t width, F f)
 {
+    if (width <= 64) return f(Int<8>(), Int<1>());
+    if (width <= 128) return f(Int<16>(), Int<1>());
+    if (width <= 256) return f(Int<32>(), Int<1>());
     if (width <= 512) return f(Int<64>(), Int<1>());
     if (width <= 1024) return f(Int<128>(), Int<1>());
     if (width <= 2048) return f(Int<256>(), Int<1>());
@@ -253,11 +270,13 @@ template <typename F> int by_gate(int kind, F f)
     }
 }
 
-// as many as are on the chip at once: 16 wavefronts for each of 256 compute units; no more than there are rows, and of narrow rows four rows each
+int64_t rows_at_once(int64_t width) { return width <= 64 ? 8 : width <= 128 ? 4 : width <= 256 ? 2 : 1; }  // of a workgroup
+
+// as many as are on the chip at once: 16 wavefronts for each of 256 compute units; no more than there are rows, and of narrow rows four turns each
 int64_t backward_workgroups(int64_t tokens, int64_t width)
 {
-    const int64_t threads = width <= 512 ? 64 : width <= 1024 ? 128 : width <= 2048 ? 256 : 512;
-    const int64_t most = 256 * 1024 / threads, enough = threads < 512 ? (tokens + 3) / 4 : tokens;
+    const int64_t threads = width <= 512 ? 64 : width <= 1024 ? 128 : width <= 2048 ? 256 : 512, at_once = rows_at_once(width);
+    const int64_t most = 256 * 1024 / threads / at_once, turns = (tokens + at_once - 1) / at_once, enough = threads < 512 ? (turns + 3) / 4 : turns;
     return enough < most ? enough : most;
 }
 
@@ -305,7 +324,7 @@ int hbp_residual_norms(const hbp_norms_t *n, const void *h, int64_t ldh, const v
             return by_width_forward(n->width, [&](auto threads, auto chunks) -> int {
                 constexpr int kThreads = decltype(threads)::value;
                 k_residual_norms<T, kThreads, decltype(chunks)::value, decltype(gate)::value>
-                    <<<dim3((unsigned)a.tokens), kThreads, 0, (hipStream_t)stream>>>(a);
+                    <<<dim3((unsigned)((a.tokens + rows_at_once(n->width) - 1) / rows_at_once(n->width))), std::max(kThreads, kWave), 0, (hipStream_t)stream>>>(a);
                 HBP_HIP(hipGetLastError());
                 return HBP_OK;
             });
@@ -317,7 +336,7 @@ int hbp_residual_norms_backward_workspace(const hbp_norms_t *n, size_t *bytes)
 {
     const int rc = hbp::check_norms(n);
     if (rc != HBP_OK || !bytes) return rc != HBP_OK ? rc : HBP_ERR_INVALID_ARGUMENT;
-    *bytes = (size_t)(hbp::backward_workgroups(n->tokens, n->width) * 3 * n->width) * sizeof(float);
+    *bytes = (size_t)(hbp::backward_workgroups(n->tokens, n->width) * hbp::rows_at_once(n->width) * 3 * n->width) * sizeof(float);
     return HBP_OK;
 }
 
@@ -358,7 +377,7 @@ int hbp_residual_norms_backward(const hbp_norms_t *n, const void *d_h_out, int64
                 return by_width_backward(n->width, [&](auto threads, auto chunks) -> int {
                     constexpr int kThreads = decltype(threads)::value;
                     k_residual_norms_backward<T, kThreads, decltype(chunks)::value, decltype(gate)::value>
-                        <<<dim3((unsigned)workgroups), kThreads, 0, st>>>(a);
+                        <<<dim3((unsigned)workgroups), std::max(kThreads, kWave), 0, st>>>(a);
                     HBP_HIP(hipGetLastError());
                     return HBP_OK;
                 });
@@ -369,7 +388,7 @@ int hbp_residual_norms_backward(const hbp_norms_t *n, const void *d_h_out, int64
     float *channel = n->gate_kind == HBP_GATE_CHANNEL ? static_cast<float *>(d_gate) : nullptr;
     if (d_w_post || d_w_pre || channel) {
         k_norm_weight_sums<<<dim3((unsigned)((n->width + 63) / 64), channel ? 3 : 2), kShares * 64, 0, st>>>(
-            static_cast<const float *>(workspace), workgroups, (int32_t)n->width, d_w_post, d_w_pre, channel);
+            static_cast<const float *>(workspace), workgroups * (int32_t)rows_at_once(n->width), (int32_t)n->width, d_w_post, d_w_pre, channel);
         HBP_HIP(hipGetLastError());
     }
     return HBP_OK;

@@ -98,23 +98,29 @@ template <typename T> struct Eight {
     }
 };
 
-// op over the 64 lanes, the same result in all of them, by lane exchanges of the vector unit alone (quads, halves of rows, rows, quarters, halves).
-template <typename V, typename F> __device__ __forceinline__ V wave_reduce(V v, F op)
+// op over the LANES (8 to 64) neighbouring lanes that a lane is among, the same result in all of them, by lane exchanges of the vector unit alone (quads, halves of
+// rows, rows, quarters, halves).
+template <int LANES = kWave, typename V, typename F> __device__ __forceinline__ V wave_reduce(V v, F op)
 {
-    static_assert(sizeof(V) == 4, "");
+    static_assert(sizeof(V) == 4 && LANES >= 8, "");
     auto dpp = [&](auto control) {
         return __builtin_bit_cast(V, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), decltype(control)::value, 0xf, 0xf, true));
     };
     v = op(v, dpp(std::integral_constant<int, 0xb1>()));   // quad_perm 1 0 3 2
     v = op(v, dpp(std::integral_constant<int, 0x4e>()));   // quad_perm 2 3 0 1
     v = op(v, dpp(std::integral_constant<int, 0x141>()));  // row_half_mirror
-    v = op(v, dpp(std::integral_constant<int, 0x140>()));  // row_mirror
-    const uint32_t w = __builtin_bit_cast(uint32_t, v);
-    auto a = __builtin_amdgcn_permlane16_swap(w, w, false, false);
-    v = op(__builtin_bit_cast(V, (uint32_t)a[0]), __builtin_bit_cast(V, (uint32_t)a[1]));
-    const uint32_t x = __builtin_bit_cast(uint32_t, v);
-    auto b = __builtin_amdgcn_permlane32_swap(x, x, false, false);
-    return op(__builtin_bit_cast(V, (uint32_t)b[0]), __builtin_bit_cast(V, (uint32_t)b[1]));
+    if constexpr (LANES >= 16) v = op(v, dpp(std::integral_constant<int, 0x140>()));  // row_mirror
+    if constexpr (LANES >= 32) {
+        const uint32_t w = __builtin_bit_cast(uint32_t, v);
+        auto a = __builtin_amdgcn_permlane16_swap(w, w, false, false);
+        v = op(__builtin_bit_cast(V, (uint32_t)a[0]), __builtin_bit_cast(V, (uint32_t)a[1]));
+    }
+    if constexpr (LANES >= 64) {
+        const uint32_t w = __builtin_bit_cast(uint32_t, v);
+        auto a = __builtin_amdgcn_permlane32_swap(w, w, false, false);
+        v = op(__builtin_bit_cast(V, (uint32_t)a[0]), __builtin_bit_cast(V, (uint32_t)a[1]));
+    }
+    return v;
 }
 __device__ __forceinline__ float wave_sum(float v)
 {
@@ -130,12 +136,12 @@ __device__ __forceinline__ uint32_t wave_max(uint32_t v)
     return wave_reduce(v, [](uint32_t a, uint32_t b) { return a > b ? a : b; });
 }
 
-// Sums of N values over the THREADS of a workgroup, the same in every thread. `slots`: LDS, THREADS / 64 * N floats, that no other
-// wavefront still reads (two calls in a row need two arrays).
+// Sums of N values over the THREADS of a workgroup, the same in every thread; with THREADS below 64, over each THREADS neighbouring lanes. `slots`: LDS, THREADS / 64 * N
+// floats, that no other wavefront still reads (two calls in a row need two arrays).
 template <int N, int THREADS> __device__ __forceinline__ void block_sums(float (&v)[N], float *slots)
 {
 #pragma unroll
-    for (int i = 0; i < N; i++) v[i] = wave_sum(v[i]);
+    for (int i = 0; i < N; i++) v[i] = wave_reduce<(THREADS < kWave ? THREADS : kWave)>(v[i], [](float a, float b) { return a + b; });
     if constexpr (THREADS > kWave) {
         const int wave = threadIdx.x / kWave;
         if (threadIdx.x % kWave == 0)

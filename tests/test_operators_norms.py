@@ -90,33 +90,47 @@ def near(got, want, name, what, slack=64.0, size=0.0):
 @pytest.mark.parametrize("gate", GATES)
 @pytest.mark.parametrize("apart", [0, 3])
 def test_forward_and_backward(name, gate, apart):
-    import torch
     for tokens, width in ((1, 1), (2, 7), (5, 64), (3, 511), (40, 513), (7, 2048), (600, 2050), (3, 4097), (2, 8192), (5, 8200), (2, 16384)):
-        for weights in (True, False):
-            print(f"[norms] {tokens} x {width} gate {gate} {name} weights {weights}", flush=True)
-            t = inputs(tokens, width, name, gate, width + tokens, weights)
-            d, f = on_gpu(t, apart), numpy_of(t)
-            given = {k: d[k] for k in ("w_post", "w_pre", "gate")} | {"scale": 0.7}
-            h_out, x_out = torch.empty_like(d["h"]), torch.empty_like(d["h"])
-            rstd = torch.empty(tokens, 2, device="cuda")
-            H.hbp_residual_norms(d["h"], d["y"], h_out, x_out, rstd=rstd, eps=EPS, **given)
-            h2, x2, n, q1, q2 = forward(f, 0.7, EPS)
-            near(h_out, h2, name, "h_out", size=np.abs(f["h"]) + np.abs(h2 - f["h"]))
-            near(x_out, x2, name, "x_out", size=(np.abs(f["h"]) + np.abs(h2 - f["h"])) / q2 * (1.0 if f["w_pre"] is None else np.abs(f["w_pre"])))
-            near(rstd, np.concatenate([1 / q1, 1 / q2], 1), "f32", "rstd")
-            d_h, d_y, f32 = torch.empty_like(d["h"]), torch.empty_like(d["h"]), dict(dtype=torch.float32, device="cuda")
-            d_gate = {"none": None, "channel": torch.full((width,), float("nan"), **f32), "token": torch.full((tokens, 1), float("nan"), **f32),
-                      "full": torch.empty_like(d["gate"]) if gate == "full" else None}[gate]
-            if gate == "token" and width == 1:
-                d_gate = torch.empty_like(d["gate"])     # [tokens, 1] with one column: a full gate
-            if gate == "full" and apart:
-                d_gate = torch.empty_strided(d["gate"].shape, d["gate"].stride(), dtype=d["gate"].dtype, device="cuda")
-            d_wp, d_wq = torch.full((width,), float("nan"), **f32), torch.full((width,), float("nan"), **f32)
-            H.hbp_residual_norms_backward(d["d_h_out"], d["d_x_out"], d["h"], d["y"], rstd, d_h, d_y, d_w_post=d_wp, d_w_pre=d_wq, d_gate=d_gate, **given)
-            want, size = backward(f, 0.7, EPS, gate)
-            for key, got in (("d_h", d_h), ("d_y", d_y), ("d_w_post", d_wp), ("d_w_pre", d_wq), ("d_gate", d_gate)):
-                if got is not None:
-                    near(got, want[key], {torch.float32: "f32", torch.float16: "f16", torch.bfloat16: "bf16"}[got.dtype], key, size=size[key])
+        check_both_ways(tokens, width, name, gate, apart)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("name", TYPES)
+@pytest.mark.parametrize("gate", GATES)
+def test_rows_that_share_a_wavefront(name, gate):
+    """narrow rows: several a workgroup, with some too few in the last one; at most 250 / 4 workgroups' sums of a column, in sixteen shares"""
+    for tokens, width in ((1, 8), (9, 33), (1000, 64), (15, 65), (999, 100), (13, 128), (301, 129), (70, 200), (501, 256), (77, 257)):
+        check_both_ways(tokens, width, name, gate, 0)
+        check_both_ways(tokens, width, name, gate, 5)
+
+
+def check_both_ways(tokens, width, name, gate, apart):
+    import torch
+    for weights in (True, False):
+        print(f"[norms] {tokens} x {width} gate {gate} {name} weights {weights}", flush=True)
+        t = inputs(tokens, width, name, gate, width + tokens, weights)
+        d, f = on_gpu(t, apart), numpy_of(t)
+        given = {k: d[k] for k in ("w_post", "w_pre", "gate")} | {"scale": 0.7}
+        h_out, x_out = torch.empty_like(d["h"]), torch.empty_like(d["h"])
+        rstd = torch.empty(tokens, 2, device="cuda")
+        H.hbp_residual_norms(d["h"], d["y"], h_out, x_out, rstd=rstd, eps=EPS, **given)
+        h2, x2, n, q1, q2 = forward(f, 0.7, EPS)
+        near(h_out, h2, name, "h_out", size=np.abs(f["h"]) + np.abs(h2 - f["h"]))
+        near(x_out, x2, name, "x_out", size=(np.abs(f["h"]) + np.abs(h2 - f["h"])) / q2 * (1.0 if f["w_pre"] is None else np.abs(f["w_pre"])))
+        near(rstd, np.concatenate([1 / q1, 1 / q2], 1), "f32", "rstd")
+        d_h, d_y, f32 = torch.empty_like(d["h"]), torch.empty_like(d["h"]), dict(dtype=torch.float32, device="cuda")
+        d_gate = {"none": None, "channel": torch.full((width,), float("nan"), **f32), "token": torch.full((tokens, 1), float("nan"), **f32),
+                  "full": torch.empty_like(d["gate"]) if gate == "full" else None}[gate]
+        if gate == "token" and width == 1:
+            d_gate = torch.empty_like(d["gate"])     # [tokens, 1] with one column: a full gate
+        if gate == "full" and apart:
+            d_gate = torch.empty_strided(d["gate"].shape, d["gate"].stride(), dtype=d["gate"].dtype, device="cuda")
+        d_wp, d_wq = torch.full((width,), float("nan"), **f32), torch.full((width,), float("nan"), **f32)
+        H.hbp_residual_norms_backward(d["d_h_out"], d["d_x_out"], d["h"], d["y"], rstd, d_h, d_y, d_w_post=d_wp, d_w_pre=d_wq, d_gate=d_gate, **given)
+        want, size = backward(f, 0.7, EPS, gate)
+        for key, got in (("d_h", d_h), ("d_y", d_y), ("d_w_post", d_wp), ("d_w_pre", d_wq), ("d_gate", d_gate)):
+            if got is not None:
+                near(got, want[key], {torch.float32: "f32", torch.float16: "f16", torch.bfloat16: "bf16"}[got.dtype], key, size=size[key])
 
 
 @pytest.mark.gpu
@@ -295,3 +309,20 @@ def test_what_the_library_refuses():
     assert back(n(), need.value - 1) == -1 and back(n(), need.value, ws=None) == -1 and back(n(), need.value, ws=4100) == -1
     for change in (dict(h=None), dict(rstd=None), dict(dh=None), dict(lddy=7), dict(dg=at), dict(dho=4098)):
         assert back(n(), need.value, **change) == -1
+
+
+@pytest.mark.gpu
+def test_narrow_rows_in_place():
+    import torch
+    for tokens, width in ((9, 40), (3, 128), (5, 250)):
+        d = on_gpu(inputs(tokens, width, "f16", "full", 8))
+        given = {k: d[k] for k in ("w_post", "w_pre", "gate")}
+        ho, xo, rstd = torch.empty_like(d["h"]), torch.empty_like(d["h"]), torch.empty(tokens, 2, device="cuda")
+        H.hbp_residual_norms(d["h"], d["y"], ho, xo, rstd=rstd, **given)
+        h, y = d["h"].clone(), d["y"].clone()
+        H.hbp_residual_norms(h, y, h, y, **given)
+        assert torch.equal(h, ho) and torch.equal(y, xo)
+        want, a, b = [torch.empty_like(ho), torch.empty_like(ho)], d["d_h_out"].clone(), d["d_x_out"].clone()
+        H.hbp_residual_norms_backward(a, b, d["h"], d["y"], rstd, *want, **given)
+        H.hbp_residual_norms_backward(a, b, d["h"], d["y"], rstd, a, b, **given)
+        assert torch.equal(a, want[0]) and torch.equal(b, want[1])
