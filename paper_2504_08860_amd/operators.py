@@ -107,6 +107,7 @@ def hbp_q4_shapes(n_rows: int, n_cols: int, group: int = 128):
 
 
 def _matrix(codes, scales, zeros, n_cols, group, device):
+    assert codes.dim() == 2, "codes: uint8 matrix required"
     n_rows = codes.shape[0]
     kind = scales.dtype
     assert kind in _types, "scales: float32, float16 or bfloat16 required"
@@ -157,6 +158,7 @@ def _vectors(x, y, n_x, n_y, device):
 def hbp_q4_mv(codes, scales, x, y, group: int = 128, zeros=None, stream=None) -> None:
     """y = x W^T with the 4-bit matrix W [rows, cols]: ``x`` [cols] and ``y`` [rows], or [vectors, cols] and [vectors, rows]."""
     L, device = _start()
+    assert x.dim(), "x: vector or matrix required"
     m = _matrix(codes, scales, zeros, x.shape[-1], group, device)
     status = L.hbp_q4_mv(m, *_vectors(x, y, m.n_cols, m.n_rows, device), _core._stream_ptr(stream))
     if status:
@@ -175,6 +177,7 @@ def hbp_q4_mv_t(codes, scales, x, y, group: int = 128, zeros=None, workspace=Non
     """y = x W with the 4-bit matrix W [rows, cols], the gradient of hbp_q4_mv for its x: ``x`` [rows] and ``y`` [cols], or [vectors,
     rows] and [vectors, cols]."""
     L, device = _start()
+    assert x.dim() and y.dim(), "x, y: vectors or matrices required"
     m = _matrix(codes, scales, zeros, y.shape[-1], group, device)
     v = _vectors(x, y, m.n_rows, m.n_cols, device)
     at, size, kept = _space(workspace, _mv_t_bytes(m.n_rows, m.n_cols, group, m.scale_type, v[5]), stream, device)
@@ -189,9 +192,10 @@ def _norms(shape, dtype, w_post, w_pre, gate, scale, eps, device):
     assert dtype in _types and len(shape) == 2, "h: matrix of float32, float16 or bfloat16 required"
     kind, at, ldg, wide = GATE_NONE, None, 0, (shape[1],)
     if gate is not None:
-        if gate.dim() == 1:
+        dims = gate.dim()
+        if dims == 1:
             kind, at = GATE_CHANNEL, _whole(gate, "gate", wide, dtype, device)
-        elif gate.shape[1] == 1 and shape[1] != 1:
+        elif dims == 2 and gate.shape[1] == 1 and shape[1] != 1:
             kind, at = GATE_TOKEN, _whole(gate, "gate", (shape[0], 1), dtype, device)
         else:
             kind = GATE_FULL
@@ -273,7 +277,10 @@ def hbp_token_logprobs(logits, tokens, logp=None, entropy=None, lse=None, top_id
     assert dtype in _types and len(shape) == 2, "logits: matrix of float32, float16 or bfloat16 required"
     count, vocabulary = shape
     assert (top_ids is None) == (top_logp is None), "top_ids and top_logp go together"
-    top = 0 if top_ids is None else top_ids.shape[1]
+    top = 0
+    if top_ids is not None:
+        assert top_ids.dim() == 2, "top_ids: int32 matrix required"
+        top = top_ids.shape[1]
     number, each, best = _types[dtype], (count,), (count, top)
     at, size, kept = _space(workspace, _logprobs_bytes(number, count, vocabulary, top), stream, device)
     z_at, ldz = _rows(logits, "logits", shape, dtype, device)

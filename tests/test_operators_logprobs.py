@@ -327,3 +327,12 @@ def test_what_the_library_refuses():
     for bad in (dict(type=9), dict(z=None), dict(ldz=1), dict(ids=None), dict(idb=1), dict(lse=None), dict(ent=None), dict(d=None), dict(ldd=99), dict(d=4097), dict(g=4097)):
         assert back(**bad) == -1, bad
     assert back(n=0) == 0
+
+
+@pytest.mark.gpu
+def test_alternatives_of_other_dimensions_are_refused():
+    import torch
+    z, t, o = torch.zeros(2, 50, device="cuda"), torch.zeros(2, dtype=torch.int64, device="cuda"), torch.zeros(2, device="cuda")
+    for shape in ((), (2,), (2, 5, 1)):
+        with pytest.raises(AssertionError):
+            H.hbp_token_logprobs(z, t, o, top_ids=torch.zeros(shape, dtype=torch.int32, device="cuda"), top_logp=torch.zeros(shape, device="cuda"))

@@ -326,3 +326,12 @@ def test_narrow_rows_in_place():
         H.hbp_residual_norms_backward(a, b, d["h"], d["y"], rstd, *want, **given)
         H.hbp_residual_norms_backward(a, b, d["h"], d["y"], rstd, a, b, **given)
         assert torch.equal(a, want[0]) and torch.equal(b, want[1])
+
+
+@pytest.mark.gpu
+def test_gates_of_other_dimensions_are_refused():
+    import torch
+    h = torch.zeros(4, 32, device="cuda")
+    for gate in (torch.zeros((), device="cuda"), torch.zeros(4, 1, 1, device="cuda"), torch.zeros(1, 4, 32, device="cuda")):
+        with pytest.raises(AssertionError):
+            H.hbp_residual_norms(h, h, torch.empty_like(h), torch.empty_like(h), gate=gate)

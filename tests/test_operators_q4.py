@@ -356,3 +356,16 @@ def test_what_the_library_refuses():
             assert L.hbp_q4_pack(matrix_, 0, at(4096), 64, None) == -1
             assert L.hbp_q4_unpack(matrix_, 0, at(4096), 64, None) == -1
     assert L.hbp_q4_pack(m(), 0, None, 64, None) == -1 and L.hbp_q4_pack(m(), 0, at(4096), 63, None) == -1
+
+
+@pytest.mark.gpu
+def test_tensors_of_other_dimensions_are_refused():
+    import torch
+    c, s, _, _ = matrix(20, 40, 32, "f32", False, 1)
+    x, y, one = torch.zeros(40, device="cuda"), torch.zeros(20, device="cuda"), torch.zeros((), device="cuda")
+    for change in (dict(codes=c[0, 0]), dict(codes=c.flatten()), dict(scales=s.flatten()), dict(x=one), dict(y=one), dict(x=x.view(1, 1, 40))):
+        a = dict(codes=c, scales=s, x=x, y=y, group=32) | change
+        with pytest.raises(AssertionError):
+            H.hbp_q4_mv(**a)
+        with pytest.raises(AssertionError):
+            H.hbp_q4_mv_t(**a | dict(x=a["y"], y=a["x"]))
