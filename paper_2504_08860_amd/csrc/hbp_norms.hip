@@ -97,9 +97,10 @@ struct NormBackArgs {
     float *partial;  // [workgroups times rows at once][3][width]: d_w_post, d_w_pre, a CHANNEL's d_gate
 };
 
-// Backward.  With a = d_x_out w_pre, e = d_h_out + r2 (a - h' r2^2 mean(a h')) is d_h, and b = scale g w_post e goes through the
-// first norm: d_y = r1 (b - y r1^2 mean(b y)).  e in the second mean is spelled out, so that all three sums of a row, of
-// a h', of w y (d_h_out + r2 a) and of w y h' with w = scale g w_post, are taken together: one wait for the others per row.
+// Backward.  With the normed rows u = r1 y and v = r2 h' and a = d_x_out w_pre, e = d_h_out + r2 (a - v mean(a v)) is d_h, and b = scale g w_post e goes through the
+// first norm: d_y = r1 (b - u mean(b u)).  e in the second mean is spelled out, so that all three sums of a row, of
+// a v, of w u (d_h_out + r2 a) and of w u v with w = scale g w_post, are taken together: one wait for the others per row.  The sums are over normed rows, so that no
+// power of r1 or r2 is formed, which may be no fp32 number.
 // h' is computed again from h, y and the gate, which are read anyway: not the rounded one, and no read more.
 //
 // A workgroup walks through every so many rows and keeps its columns' sums for the weights in registers; workgroups' sums are added by a second kernel, in their
@@ -154,17 +155,17 @@ __global__ __launch_bounds__(THREADS < kWave ? kWave : THREADS) void k_residual_
             for (int i = 0; i < 8; i++) {
                 float w = n.scale * wp[c].get(i);
                 if constexpr (kFull || kChannel) w *= gg[c].get(i);
-                const float wy = w * yy[c].get(i), next = hh[c].get(i) + row_gate * (r1 * wy), a = dx[c].get(i) * wq[c].get(i);
-                sum[0] += a * next;
-                sum[1] += wy * (dh[c].get(i) + r2 * a);
-                sum[2] += wy * next;
+                const float wu = w * (yy[c].get(i) * r1), hat = (hh[c].get(i) + row_gate * wu) * r2, a = dx[c].get(i) * wq[c].get(i);
+                sum[0] += a * hat;
+                sum[1] += wu * (dh[c].get(i) + r2 * a);
+                sum[2] += wu * hat;
             }
         block_sums<3, THREADS>(sum, slots[odd]);
         if (!mine) continue;
-        const float along2 = r2 * r2 * r2 * (sum[0] * inverse_width);
-        const float through = sum[1] - along2 * sum[2];  // sum of b y, a row's gate left out
-        const float along1 = r1 * r1 * r1 * (row_gate * through * inverse_width);
-        if (GATE == HBP_GATE_TOKEN && n.d_gate && thread == 0) static_cast<float *>(n.d_gate)[t] = r1 * through;
+        const float along2 = r2 * (sum[0] * inverse_width);
+        const float through = sum[1] - along2 * sum[2];  // sum of b u, a row's gate left out
+        const float along1 = row_gate * through * inverse_width;
+        if (GATE == HBP_GATE_TOKEN && n.d_gate && thread == 0) static_cast<float *>(n.d_gate)[t] = through;
 #pragma unroll
         for (int c = 0; c < CHUNKS; c++) {
             const int col = (c * THREADS + thread) * 8, left = n.width - col;
@@ -174,13 +175,13 @@ __global__ __launch_bounds__(THREADS < kWave ? kWave : THREADS) void k_residual_
                 const float yv = yy[c].get(i), xv = dx[c].get(i), w_post = wp[c].get(i);
                 float gate = n.scale * row_gate;
                 if constexpr (kFull || kChannel) gate *= gg[c].get(i);
-                const float unit = yv * r1, next = hh[c].get(i) + gate * (unit * w_post);
-                const float e = dh[c].get(i) + r2 * (xv * wq[c].get(i)) - along2 * next;
+                const float unit = yv * r1, hat = (hh[c].get(i) + gate * (unit * w_post)) * r2;
+                const float e = dh[c].get(i) + r2 * (xv * wq[c].get(i)) - along2 * hat;
                 const float ge = gate * e;
                 de.set(i, e);
-                dy.set(i, r1 * (ge * w_post) - along1 * yv);
+                dy.set(i, r1 * (ge * w_post - along1 * unit));
                 sum_post[c][i] += ge * unit;
-                sum_pre[c][i] += xv * (next * r2);
+                sum_pre[c][i] += xv * hat;
                 if constexpr (kFull) dg.set(i, n.scale * e * (unit * w_post));
                 if constexpr (kChannel) sum_gate[c][i] += n.scale * e * (unit * w_post);
             }

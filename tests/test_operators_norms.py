@@ -335,3 +335,32 @@ def test_gates_of_other_dimensions_are_refused():
     for gate in (torch.zeros((), device="cuda"), torch.zeros(4, 1, 1, device="cuda"), torch.zeros(1, 4, 32, device="cuda")):
         with pytest.raises(AssertionError):
             H.hbp_residual_norms(h, h, torch.empty_like(h), torch.empty_like(h), gate=gate)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("name", ["f32", "bf16"])
+@pytest.mark.parametrize("gate", GATES)
+def test_gradients_of_large_rows_and_of_rows_of_zeros_with_a_small_eps(name, gate):
+    """Norms' factors from 1e-17 to 1e17 (their cubes are no fp32 numbers), with nothing but the norms' own terms in the gradients, too: the bounds are those of
+    ordinary rows, whose roundings are relative to the terms that are added."""
+    import torch
+    for width in (40, 300, 2050):
+        for size_h, size_y, eps in ((1e14, 1e14, EPS), (1e17, 1.0, EPS), (1.0, 1e17, EPS), (1e17, 1e17, EPS), (0.0, 0.0, 1e-28), (0.0, 0.0, 1e-34), (1.0, 0.0, 1e-28)):
+            print(f"[norms] {width} gate {gate} {name} h {size_h} y {size_y} eps {eps}", flush=True)
+            t = inputs(6, width, name, gate, width)
+            t["h"], t["y"] = t["h"] * size_h, t["y"] * size_y
+            t["h"][5], t["y"][5] = some_x(1, width, name, 77)[0], some_x(1, width, name, 78)[0]    # an ordinary row in the same batch
+            for alone in (False, True):
+                if alone:
+                    t["d_h_out"] = torch.zeros_like(t["d_h_out"])
+                d, f = on_gpu(t), numpy_of(t)
+                given = {k: d[k] for k in ("w_post", "w_pre", "gate")} | {"scale": 0.7}
+                rstd, out = torch.empty(6, 2, device="cuda"), [torch.empty_like(d["h"]) for _ in range(4)]
+                H.hbp_residual_norms(d["h"], d["y"], out[0], out[1], rstd=rstd, eps=eps, **given)
+                d_wp, d_wq = torch.empty(width, device="cuda"), torch.empty(width, device="cuda")
+                d_gate = {"none": None, "channel": torch.empty(width, device="cuda"), "token": torch.empty(6, 1, device="cuda"), "full": torch.empty_like(d["h"])}[gate]
+                H.hbp_residual_norms_backward(d["d_h_out"], d["d_x_out"], d["h"], d["y"], rstd, out[2], out[3], d_w_post=d_wp, d_w_pre=d_wq, d_gate=d_gate, **given)
+                want, size = backward(f, 0.7, eps, gate)
+                for key, got in (("d_h", out[2]), ("d_y", out[3]), ("d_w_post", d_wp), ("d_w_pre", d_wq), ("d_gate", d_gate)):
+                    if got is not None:
+                        near(got, want[key], "bf16" if got.dtype == torch.bfloat16 else "f32", key, size=size[key])
