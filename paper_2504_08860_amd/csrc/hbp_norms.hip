@@ -97,16 +97,64 @@ struct NormBackArgs {
     float *partial;  // [workgroups times rows at once][3][width]: d_w_post, d_w_pre, a CHANNEL's d_gate
 };
 
+// Two sums of each of a thread's columns: in registers or, where a thread has 32 columns and their rows leave no registers for them, in LDS, each thread's own.
+template <int THREADS, int CHUNKS> struct Sums {
+    static constexpr bool kInLds = CHUNKS > 2;
+    static constexpr size_t kBytes = kInLds ? sizeof(float) * 2 * CHUNKS * 8 * THREADS : 0;
+    float v[2][kInLds ? 1 : CHUNKS][8];
+    int thread;
+    static __device__ __forceinline__ float4 *lds()
+    {
+        extern __shared__ float4 sums_in_lds[];
+        return sums_in_lds;
+    }
+    __device__ __forceinline__ float4 &place(int which, int c, int half) const { return lds()[((which * CHUNKS + c) * 2 + half) * THREADS + thread]; }
+    __device__ __forceinline__ Sums(int t) : v{}, thread(t)
+    {
+        if constexpr (kInLds)
+#pragma unroll
+            for (int i = 0; i < 4 * CHUNKS; i++) lds()[i * THREADS + thread] = float4{0, 0, 0, 0};
+    }
+    __device__ __forceinline__ void add(int which, int c, const float (&x)[8])
+    {
+        if constexpr (kInLds) {
+#pragma unroll
+            for (int half = 0; half < 2; half++) {
+                float4 &s = place(which, c, half);
+                s = float4{s.x + x[4 * half], s.y + x[4 * half + 1], s.z + x[4 * half + 2], s.w + x[4 * half + 3]};
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; i++) v[which][c][i] += x[i];
+        }
+    }
+    __device__ __forceinline__ void get(int which, int c, float (&x)[8]) const
+    {
+        if constexpr (kInLds) {
+#pragma unroll
+            for (int half = 0; half < 2; half++) {
+                const float4 s = place(which, c, half);
+                x[4 * half] = s.x; x[4 * half + 1] = s.y; x[4 * half + 2] = s.z; x[4 * half + 3] = s.w;
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; i++) x[i] = v[which][c][i];
+        }
+    }
+};
+
 // Backward.  With the normed rows u = r1 y and v = r2 h' and a = d_x_out w_pre, e = d_h_out + r2 (a - v mean(a v)) is d_h, and b = scale g w_post e goes through the
 // first norm: d_y = r1 (b - u mean(b u)).  e in the second mean is spelled out, so that all three sums of a row, of
 // a v, of w u (d_h_out + r2 a) and of w u v with w = scale g w_post, are taken together: one wait for the others per row.  The sums are over normed rows, so that no
 // power of r1 or r2 is formed, which may be no fp32 number.
 // h' is computed again from h, y and the gate, which are read anyway: not the rounded one, and no read more.
 //
-// A workgroup walks through every so many rows and keeps its columns' sums for the weights in registers; workgroups' sums are added by a second kernel, in their
-// order.  Of a row, what was read stays in registers as it came (h' is cheaper to compute twice than to keep), and so do the weights.  512 threads at most: with 1024
-// a row of 16384 columns does not fit their 128 registers.  Bound: HBM; 8192 x 4096 bf16 with a gate for each value 113 us, 4.7 TB/s, and 5 for the workgroups' sums (39 with
-// four shares and one load at a time).
+// A workgroup walks through every so many rows and keeps its columns' sums for the weights; workgroups' sums are added by a second kernel, in their
+// order.  Of a row, what was read stays in registers as it came (h' is cheaper to compute twice than to keep), and so do, up to 16 columns a thread, the weights.  512 threads at
+// most: with 1024 a row of 16384 columns does not fit their 128 registers.  With 512 it fits their 256 if nothing else is kept there: the sums are in LDS, 128 KB, the weights are read again for each
+// row, from the caches, and the compiler is not to keep what it made of a row from one walk through it to the next.  2048 x 16384 fp32 with a gate for each column 283 us, with all of it in
+// registers, of which 661 were spilled, 606 (still spilled: 19 of fp32 rows with such a gate, 12 with one for each value).
+// Bound: HBM; 8192 x 4096 bf16 with a gate for each value 113 us, 4.7 TB/s, and 5 for the workgroups' sums (39 with four shares and one load at a time).
 template <typename T, int THREADS, int CHUNKS, int GATE>
 __global__ __launch_bounds__(THREADS < kWave ? kWave : THREADS) void k_residual_norms_backward(NormBackArgs n)
 {
@@ -114,20 +162,24 @@ __global__ __launch_bounds__(THREADS < kWave ? kWave : THREADS) void k_residual_
     constexpr int kAtOnce = THREADS < kWave ? kWave / THREADS : 1;  // rows of a workgroup
     const int thread = threadIdx.x % THREADS, of_these = threadIdx.x / THREADS;
     constexpr bool kFull = GATE == HBP_GATE_FULL, kChannel = GATE == HBP_GATE_CHANNEL;
-    Eight<T> wp[CHUNKS], wq[CHUNKS], gg[CHUNKS];
-#pragma unroll
-    for (int c = 0; c < CHUNKS; c++) {
+    constexpr bool kKeep = !Sums<THREADS, CHUNKS>::kInLds;  // the weights
+    constexpr int kWeights = kKeep ? CHUNKS : 1;
+    Eight<T> wp[kWeights], wq[kWeights], gg[kFull ? CHUNKS : kWeights];
+    auto load_weights = [&](int c, int to) {
         const int col = (c * THREADS + thread) * 8, left = n.width - col;
 #pragma unroll
         for (int i = 0; i < 8; i++) {
-            wp[c].set(i, 1.0f);
-            wq[c].set(i, 1.0f);
+            wp[to].set(i, 1.0f);
+            wq[to].set(i, 1.0f);
         }
-        if (n.w_post) wp[c].load_first(static_cast<const T *>(n.w_post) + col, left);
-        if (n.w_pre) wq[c].load_first(static_cast<const T *>(n.w_pre) + col, left);
-        if constexpr (kChannel) gg[c].load_first(static_cast<const T *>(n.gate) + col, left);
-    }
-    float sum_post[CHUNKS][8] = {}, sum_pre[CHUNKS][8] = {}, sum_gate[kChannel ? CHUNKS : 1][8] = {};
+        if (n.w_post) wp[to].load_first(static_cast<const T *>(n.w_post) + col, left);
+        if (n.w_pre) wq[to].load_first(static_cast<const T *>(n.w_pre) + col, left);
+        if constexpr (kChannel) gg[to].load_first(static_cast<const T *>(n.gate) + col, left);
+    };
+    if constexpr (kKeep)
+#pragma unroll
+        for (int c = 0; c < CHUNKS; c++) load_weights(c, c);
+    Sums<THREADS, CHUNKS> sums(thread);
     const float inverse_width = 1.0f / n.width;
     int odd = 0;
     for (int64_t t0 = (int64_t)blockIdx.x * kAtOnce; t0 < n.tokens; t0 += (int64_t)gridDim.x * kAtOnce, odd ^= 1) {
@@ -150,18 +202,28 @@ __global__ __launch_bounds__(THREADS < kWave ? kWave : THREADS) void k_residual_
         }
         float sum[3] = {0, 0, 0};
 #pragma unroll
-        for (int c = 0; c < CHUNKS; c++)
+        for (int c = 0; c < CHUNKS; c++) {
+            const int k = kKeep ? c : 0, kg = kKeep || kFull ? c : 0;
+            if constexpr (!kKeep) load_weights(c, 0);
 #pragma unroll
             for (int i = 0; i < 8; i++) {
-                float w = n.scale * wp[c].get(i);
-                if constexpr (kFull || kChannel) w *= gg[c].get(i);
-                const float wu = w * (yy[c].get(i) * r1), hat = (hh[c].get(i) + row_gate * wu) * r2, a = dx[c].get(i) * wq[c].get(i);
+                float w = n.scale * wp[k].get(i);
+                if constexpr (kFull || kChannel) w *= gg[kg].get(i);
+                const float wu = w * (yy[c].get(i) * r1), hat = (hh[c].get(i) + row_gate * wu) * r2, a = dx[c].get(i) * wq[k].get(i);
                 sum[0] += a * hat;
                 sum[1] += wu * (dh[c].get(i) + r2 * a);
                 sum[2] += wu * hat;
             }
+        }
         block_sums<3, THREADS>(sum, slots[odd]);
         if (!mine) continue;
+        if constexpr (!kKeep)
+#pragma unroll
+            for (int c = 0; c < CHUNKS; c++) {
+                yy[c].forget();
+                hh[c].forget();
+                dx[c].forget();
+            }
         const float along2 = r2 * (sum[0] * inverse_width);
         const float through = sum[1] - along2 * sum[2];  // sum of b u, a row's gate left out
         const float along1 = row_gate * through * inverse_width;
@@ -170,37 +232,45 @@ __global__ __launch_bounds__(THREADS < kWave ? kWave : THREADS) void k_residual_
         for (int c = 0; c < CHUNKS; c++) {
             const int col = (c * THREADS + thread) * 8, left = n.width - col;
             Eight<T> de, dy, dg;
+            float post[8], pre[8];
+            const int k = kKeep ? c : 0, kg = kKeep || kFull ? c : 0;
+            if constexpr (!kKeep) load_weights(c, 0);
 #pragma unroll
             for (int i = 0; i < 8; i++) {
-                const float yv = yy[c].get(i), xv = dx[c].get(i), w_post = wp[c].get(i);
+                const float yv = yy[c].get(i), xv = dx[c].get(i), w_post = wp[k].get(i);
                 float gate = n.scale * row_gate;
-                if constexpr (kFull || kChannel) gate *= gg[c].get(i);
+                if constexpr (kFull || kChannel) gate *= gg[kg].get(i);
                 const float unit = yv * r1, hat = (hh[c].get(i) + gate * (unit * w_post)) * r2;
-                const float e = dh[c].get(i) + r2 * (xv * wq[c].get(i)) - along2 * hat;
-                const float ge = gate * e;
+                const float e = dh[c].get(i) + r2 * (xv * wq[k].get(i)) - along2 * hat;
                 de.set(i, e);
-                dy.set(i, r1 * (ge * w_post - along1 * unit));
-                sum_post[c][i] += ge * unit;
-                sum_pre[c][i] += xv * hat;
+                dy.set(i, r1 * (gate * e * w_post - along1 * unit));
+                post[i] = (kChannel ? n.scale : gate) * e * unit;
+                pre[i] = xv * hat;
                 if constexpr (kFull) dg.set(i, n.scale * e * (unit * w_post));
-                if constexpr (kChannel) sum_gate[c][i] += n.scale * e * (unit * w_post);
             }
+            sums.add(0, c, post);
+            sums.add(1, c, pre);
             de.store_first(static_cast<T *>(n.d_h) + t * n.lddh + col, left);
             dy.store_first(static_cast<T *>(n.d_y) + t * n.lddy + col, left);
             if constexpr (kFull)
                 if (n.d_gate) dg.store_first(static_cast<T *>(n.d_gate) + t * n.ldg + col, left);
         }
     }
-    float *sums = n.partial + ((int64_t)blockIdx.x * kAtOnce + of_these) * 3 * n.width;
+    float *partial = n.partial + ((int64_t)blockIdx.x * kAtOnce + of_these) * 3 * n.width;
 #pragma unroll
     for (int c = 0; c < CHUNKS; c++) {
         const int col = (c * THREADS + thread) * 8;
+        float post[8], pre[8];
+        sums.get(0, c, post);
+        sums.get(1, c, pre);
+        const int k = kKeep ? c : 0;
+        if constexpr (kChannel && !kKeep) load_weights(c, 0);
 #pragma unroll
         for (int i = 0; i < 8; i++)
-            if (col + i < n.width) {
-                sums[col + i] = sum_post[c][i];
-                sums[n.width + col + i] = sum_pre[c][i];
-                if constexpr (kChannel) sums[2 * n.width + col + i] = sum_gate[c][i];
+            if (col + i < n.width) {  // (a CHANNEL's gate and w_post are the same in every row: one sum for both)
+                partial[col + i] = kChannel ? gg[k].get(i) * post[i] : post[i];
+                partial[n.width + col + i] = pre[i];
+                if constexpr (kChannel) partial[2 * n.width + col + i] = wp[k].get(i) * post[i];
             }
     }
 }
@@ -273,11 +343,11 @@ template <typename F> int by_gate(int kind, F f)
 
 int64_t rows_at_once(int64_t width) { return width <= 64 ? 8 : width <= 128 ? 4 : width <= 256 ? 2 : 1; }  // of a workgroup
 
-// as many as are on the chip at once: 16 wavefronts for each of 256 compute units; no more than there are rows, and of narrow rows four turns each
+// as many as are on the chip at once: 16 wavefronts for each of 256 compute units, with sums in LDS 8; no more than there are rows, and of narrow rows four turns each
 int64_t backward_workgroups(int64_t tokens, int64_t width)
 {
     const int64_t threads = width <= 512 ? 64 : width <= 1024 ? 128 : width <= 2048 ? 256 : 512, at_once = rows_at_once(width);
-    const int64_t most = 256 * 1024 / threads / at_once, turns = (tokens + at_once - 1) / at_once, enough = threads < 512 ? (turns + 3) / 4 : turns;
+    const int64_t most = width > 8192 ? 256 : 256 * 1024 / threads / at_once, turns = (tokens + at_once - 1) / at_once, enough = threads < 512 ? (turns + 3) / 4 : turns;
     return enough < most ? enough : most;
 }
 
@@ -377,8 +447,10 @@ int hbp_residual_norms_backward(const hbp_norms_t *n, const void *d_h_out, int64
             return by_gate(n->gate_kind, [&](auto gate) -> int {
                 return by_width_backward(n->width, [&](auto threads, auto chunks) -> int {
                     constexpr int kThreads = decltype(threads)::value;
-                    k_residual_norms_backward<T, kThreads, decltype(chunks)::value, decltype(gate)::value>
-                        <<<dim3((unsigned)workgroups), std::max(kThreads, kWave), 0, st>>>(a);
+                    constexpr size_t kLds = Sums<kThreads, decltype(chunks)::value>::kBytes;
+                    auto kernel = k_residual_norms_backward<T, kThreads, decltype(chunks)::value, decltype(gate)::value>;
+                    if (kLds) HBP_HIP(hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)kLds));
+                    kernel<<<dim3((unsigned)workgroups), std::max(kThreads, kWave), kLds, st>>>(a);
                     HBP_HIP(hipGetLastError());
                     return HBP_OK;
                 });

@@ -64,6 +64,12 @@ template <typename T> struct Eight {
 #pragma unroll
         for (int i = 0; i < kWords; i++) w[i] = 0;
     }
+    // The compiler no longer knows these values: it cannot use again what it has made of them so far.
+    __device__ __forceinline__ void forget()
+    {
+#pragma unroll
+        for (int i = 0; i < kWords; i++) asm("" : "+v"(w[i]));
+    }
     // the first `n` of eight (n >= 8: all); the others are zero, and not read
     __device__ __forceinline__ void load_first(const T *p, int64_t n)
     {
