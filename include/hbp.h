@@ -394,8 +394,10 @@ int hbp_residual_norms_backward_workspace(const hbp_norms_t *n, size_t *bytes);
 int hbp_token_logprobs(int type, const void *logits, int64_t ldz, int64_t tokens, int64_t vocabulary, const void *ids, int id_bytes, float *logp,
                        float *entropy, float *lse, int top, int32_t *top_ids, float *top_logp, void *workspace, size_t workspace_bytes, void *stream);
 int hbp_token_logprobs_workspace(int type, int64_t tokens, int64_t vocabulary, int top, size_t *bytes);
-/* The logits' gradient from g_logp and g_entropy (DEVICE float [tokens], either may be NULL: zero) and the forward call's lse and entropy:
- * d[v] = g_logp ((v is the token) - p_v) - g_entropy p_v (z_v - lse + entropy), of `type`, row stride ldd; d_logits may be the logits. */
+/* The logits' gradient from g_logp and g_entropy (DEVICE float [tokens], either may be NULL: zero) and the forward call's lse and entropy of the same
+ * logits: d[v] = g_logp ((v is the token) - p_v) - g_entropy p_v (z_v - lse + entropy), of `type`, row stride ldd; d_logits may be the logits.  In rows with an
+ * |lse| of 16 or more (results of 16 bits: 64), which fp32 holds too roughly for p = exp(z - lse), differences are taken to the row's largest logit and the
+ * logarithm of its sum, found again: such rows are read twice. */
 int hbp_token_logprobs_backward(int type, const void *logits, int64_t ldz, int64_t tokens, int64_t vocabulary, const void *ids, int id_bytes,
                                 const float *lse, const float *entropy, const float *g_logp, const float *g_entropy, void *d_logits, int64_t ldd,
                                 void *stream);

@@ -311,9 +311,30 @@ struct LogprobBackArgs {
     void *d_logits;
 };
 
-// The gradient, eight logits a thread.  Bound: HBM; 4096 x 32001 bf16 93 us, 5.6 TB/s read and written.
+// The gradient.  p is exp(z - lse), and lse, in 32 bits, is off by half its last place, which p is then off by relative to itself: up to 2^-21, what the other roundings of z - lse
+// come to, for |lse| below 16; for results of 16 bits, which are off by 2^-12 and more themselves, 2^-19 is let pass.  Rows whose lse is larger have their largest logit and its sum taken
+// again, as the forward call took them, and p from those: by the row's first workgroup alone, which then takes all of the row (d_logits may be the logits, so that no other one may read what it writes).
+template <typename T> constexpr float kLseLimit = sizeof(T) == 4 ? 16.0f : 64.0f;
+
+// below(z): z - lse
+template <typename T, typename F>
+__device__ __forceinline__ void logit_gradients(const Eight<T> &v, Eight<T> &out, int64_t col, int64_t id, float u, float w, float entropy, bool none, F below)
+{
+#pragma unroll
+    for (int i = 0; i < 8; i++) {
+        const float lp = below(v.get(i));
+        const float prob = __builtin_amdgcn_exp2f(lp * kPerLog2);
+        float g = prob * (u + (prob > 0.0f ? w * (lp + entropy) : 0.0f));
+        g = col + i == id ? u - g : -g;
+        if (none) g = u == u ? 0.0f : u;
+        out.set(i, g);
+    }
+}
+
+// Eight logits a thread.  Bound: HBM; 4096 x 32001 bf16 93 us, 5.6 TB/s read and written.
 template <typename T> __global__ __launch_bounds__(256) void k_logprobs_backward(LogprobBackArgs p)
 {
+    __shared__ Stats wave_stats[256 / kWave];
     const int64_t t = blockIdx.y;
     const T *z = static_cast<const T *>(p.logits) + t * p.ldz;
     T *d = static_cast<T *>(p.d_logits) + t * p.ldd;
@@ -322,21 +343,36 @@ template <typename T> __global__ __launch_bounds__(256) void k_logprobs_backward
     float u = id >= 0 && p.g_logp ? p.g_logp[t] : 0.0f;
     if (id >= p.vocabulary && p.g_logp) u = NAN;
     const bool none = lse == -INFINITY;
-    const int64_t col = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 8;
-    const int64_t left = p.vocabulary - col;
-    if (left <= 0) return;
+    const int64_t col = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 8, left = p.vocabulary - col;
     Eight<T> v, out;
-    v.load_first(z + col, left);
-#pragma unroll
-    for (int i = 0; i < 8; i++) {
-        const float lp = v.get(i) - lse;
-        const float prob = __builtin_amdgcn_exp2f(lp * kPerLog2);
-        float g = prob * (u + (prob > 0.0f ? w * (lp + entropy) : 0.0f));
-        g = col + i == id ? u - g : -g;
-        if (none) g = u == u ? 0.0f : u;
-        out.set(i, g);
+    v.load_first(z + col, left);  // (on its way while lse is waited for; not used where the row is the first workgroup's)
+    if (none || !(fabsf(lse) >= kLseLimit<T>)) {
+        if (left <= 0) return;
+        logit_gradients(v, out, col, id, u, w, entropy, none, [&](float z) { return z - lse; });
+        out.store_first(d + col, left);
+        return;
     }
-    out.store_first(d + col, left);
+    if (blockIdx.x > 0) return;
+    Stats a{kLowest, 0.0f, 0.0f};
+    for (int64_t col = threadIdx.x * 8; col < p.vocabulary; col += 256 * 8) {
+        v.load_first(z + col, p.vocabulary - col);
+        float f[8];
+#pragma unroll
+        for (int i = 0; i < 8; i++) f[i] = col + i < p.vocabulary ? v.get(i) : -INFINITY;
+        add_eight(a, f);
+    }
+    a = wave_join(a);
+    if (threadIdx.x % kWave == 0) wave_stats[threadIdx.x / kWave] = a;
+    __syncthreads();
+    const int lane = threadIdx.x % kWave;
+    a = wave_join(lane < 256 / kWave ? wave_stats[lane] : Stats{kLowest, 0.0f, 0.0f});
+    const float log_s = logf(a.s);
+    for (int64_t col = threadIdx.x * 8; col < p.vocabulary; col += 256 * 8) {
+        const int64_t left = p.vocabulary - col;
+        v.load_first(z + col, left);
+        logit_gradients(v, out, col, id, u, w, entropy, false, [&](float z) { return z - a.m - log_s; });
+        out.store_first(d + col, left);
+    }
 }
 
 // parts of a row: enough workgroups for the chip (one block each: 64 x 50001 in 8 parts of two blocks 22 us, in 13 of one 15), none of fewer than 4096 logits

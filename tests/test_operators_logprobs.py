@@ -336,3 +336,37 @@ def test_alternatives_of_other_dimensions_are_refused():
     for shape in ((), (2,), (2, 5, 1)):
         with pytest.raises(AssertionError):
             H.hbp_token_logprobs(z, t, o, top_ids=torch.zeros(shape, dtype=torch.int32, device="cuda"), top_logp=torch.zeros(shape, device="cuda"))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("name", TYPES)
+@pytest.mark.parametrize("v", [100, 9000, 40001])
+def test_gradient_of_logits_far_from_zero(name, v):
+    """Logits around a number that lse, in 32 bits, holds only roughly or not at all: a probability is that of the difference to the largest one, whose roundings are
+    relative to itself and to ln v (check_gradient's `size`, not that of the logits), and a row's gradient for its token's logit adds up to zero."""
+    import torch
+    low = float(torch.finfo(dtype(name)).min)
+    for k, at in enumerate([20.0, 30.0, 200.0, -1000.0, 1e4, -6e4] + ([] if name == "f16" else [1e6, 1e8, -1e8, 3e38]) + [low]):
+        for masked in (0.0, 0.4):
+            print(f"[logprobs far] {v} {name} around {at} masked {masked}", flush=True)
+            z = logits_of(4, v, "f32", 50 + k)
+            z = (z + at if at != low else torch.full_like(z, low)).to(dtype(name))
+            gone = torch.from_numpy(np.random.default_rng(k).random((4, v)) < masked)
+            gone[:, 7] = False
+            z[gone] = -INF
+            f, tokens = z.double().numpy(), torch.tensor([7, 3, -1, v - 1])
+            wide = torch.full((4, v + 5), float("nan"), dtype=z.dtype, device="cuda")
+            wide[:, 2:2 + v] = z.cuda()
+            zg = wide[:, 2:2 + v] if k % 2 else z.cuda()
+            out = run(zg, tokens.cuda())
+            u, w = (torch.randn(4, generator=torch.Generator().manual_seed(k + i)) for i in (0, 1))
+            u[2] = 0.0                                 # (no token: nothing comes from there)
+            d = torch.empty_like(zg)
+            H.hbp_token_logprobs_backward(zg, tokens.cuda(), out["lse"], out["entropy"], u.cuda(), w.cuda(), d)
+            check_gradient(d, f, tokens.numpy(), u.numpy(), w.numpy(), name, np.log(v) + 4)
+            if name == "f32":
+                only = torch.empty_like(zg)
+                H.hbp_token_logprobs_backward(zg, tokens.cuda(), out["lse"], out["entropy"], u.cuda(), None, only)
+                assert (only.double().sum(1).abs().cpu() <= 2.0 ** -24 * (8 * (np.log(v) + 4) + 16 + 4) * u.abs().double()).all()
+            H.hbp_token_logprobs_backward(zg, tokens.cuda(), out["lse"], out["entropy"], u.cuda(), w.cuda(), zg)      # in place
+            assert torch.equal(zg, d)
