@@ -210,7 +210,8 @@ template <typename S, bool ZERO, int GM, int RT, int U> struct Batch {
     static __device__ __forceinline__ float of(const Scales<S, N * U> &s, int shift, int u, int g)
     {
         if constexpr (GM < 4 || U == 1) return to_f32(s.v[u * N + g]);
-        else return to_f32(shift == 7 ? s.v[u] : shift == 8 ? s.v[u / 2] : s.v[0]);
+        const float own = to_f32(s.v[u]), of_two = to_f32(s.v[u / 2]), of_all = to_f32(s.v[0]);  // (chosen from as values: from among places in the array, it would be in memory)
+        return shift == 7 ? own : shift == 8 ? of_two : of_all;
     }
 };
 
