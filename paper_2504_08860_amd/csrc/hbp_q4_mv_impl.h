@@ -1,15 +1,20 @@
 // Products y = x W^T with a matrix in 4 bits, on the matrix cores (hbp_q4_mv).
 //
-// A code q becomes the number 16 + q by putting its four bits at the top of the mantissa of 16, in bf16 or fp16, exactly: one shift and one
+// With x of 16 bits a code q becomes the number 16 + q by putting its four bits at the top of the mantissa of 16, in bf16 or fp16, exactly: one shift and one
 // and-or for two codes.  The matrix instruction multiplies them with x and sums in fp32; the 16, and the zero point, are taken out
 // of a group's sum as (16 + zero) times the group's sum of x, which the same instruction gives with a constant for the codes.  Then the group's sum is
-// multiplied by its scale, in fp32: no weight is ever rounded.
+// multiplied by its scale, in fp32: no weight is ever rounded.  On the way stand sums as large as 24 sum x of a group: off, for an x all of one sign, by some 1e-5 of a result,
+// which is a hundredth of what 16 bits of x and of the result are off by.
+//
+// With an fp32 x that would show, and a code becomes q itself as a bf16: as a byte of an fp8 number of four bits of exponent, whose values up to 15 steps of the smallest one lie evenly, it
+// is q steps, and one conversion makes two codes of two of them.  Behind each 32 columns the zero point is taken off with a second instruction, of x with -zero as a bf16, so that
+// nothing larger than those columns' own sum of zero x stands on the way.  What of a zero point eight bits do not hold, if anything, is taken out of a group's sum as above.
 //
 // The instruction's 16 rows on the side of x are "slots".  A vector of fp16 or bf16 takes one; one of fp32 is split into three bf16 parts
 // of 8 bits of the mantissa each, exactly, and takes three, whose sums are added at the end.  The 16 columns on the side of the weights are
 // 16 rows of the matrix.
 //
-// What is larger on the way than in the end: (16 + q) x instead of (q - zero) x, before the scale.  Where that, or a value of x itself, is infinite
+// What is larger on the way than in the end: (16 + q) x or (q - zero) x, before the scale.  Where that, or a value of x itself, is infinite
 // or NaN, the result is not finite, and such a result is computed again from the definition, (scale (q - zero)) x.
 #pragma once
 
@@ -22,6 +27,8 @@ namespace {
 
 typedef float float4_t __attribute__((ext_vector_type(4)));
 typedef uint32_t uint4_t __attribute__((ext_vector_type(4)));
+typedef float float2_t __attribute__((ext_vector_type(2)));
+typedef bf16 bf16x2_t __attribute__((ext_vector_type(2)));
 
 template <typename MT> struct Cores;
 template <> struct Cores<bf16> {
@@ -65,6 +72,18 @@ template <typename MT> __device__ __forceinline__ uint4_t numbers_of(uint32_t w,
     return r;
 }
 
+// Eight codes of a word as they are, in bf16, in the order 0 2 4 6 1 3 5 7 (which an fp32 x is staged in).  512: the steps of an fp8 number of four bits of exponent are 1 / 512.
+__device__ __forceinline__ uint4_t codes_of(uint32_t w)
+{
+    const uint32_t even = w & 0x0f0f0f0fu, odd = w >> 4 & 0x0f0f0f0fu;
+    uint4_t r;
+    r.x = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(even, 512.0f, false));
+    r.y = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(even, 512.0f, true));
+    r.z = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(odd, 512.0f, false));
+    r.w = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(odd, 512.0f, true));
+    return r;
+}
+
 // Four words of each lane, exchanged between the four quarters of a wavefront: word j of quarter q becomes word q of quarter j.
 __device__ __forceinline__ void transpose_quarters(uint4_t &w)
 {
@@ -89,7 +108,7 @@ template <typename T, typename S> __device__ __forceinline__ float by_definition
     return wave_sum(sum);
 }
 
-// Eight values of x on their way into LDS: as one part in the order of numbers_of, or as three.
+// Eight values of x on their way into LDS: as one part in the order of numbers_of, or as three in that of codes_of.
 template <typename T> struct Staged {
     Eight<T> v;
     __device__ __forceinline__ void store(uint32_t *at, int words_to_next_part)
@@ -98,10 +117,10 @@ template <typename T> struct Staged {
         if constexpr (sizeof(T) == 4) {
 #pragma unroll
             for (int part = 0; part < 3; part++) {
-                w.x = (v.w[0] >> 16) | (v.w[4] & 0xffff0000u);
-                w.y = (v.w[1] >> 16) | (v.w[5] & 0xffff0000u);
-                w.z = (v.w[2] >> 16) | (v.w[6] & 0xffff0000u);
-                w.w = (v.w[3] >> 16) | (v.w[7] & 0xffff0000u);
+                w.x = (v.w[0] >> 16) | (v.w[2] & 0xffff0000u);
+                w.y = (v.w[4] >> 16) | (v.w[6] & 0xffff0000u);
+                w.z = (v.w[1] >> 16) | (v.w[3] & 0xffff0000u);
+                w.w = (v.w[5] >> 16) | (v.w[7] & 0xffff0000u);
                 *reinterpret_cast<uint4_t *>(at + part * words_to_next_part) = w;
 #pragma unroll
                 for (int i = 0; i < 8; i++) v.w[i] = __float_as_uint(__uint_as_float(v.w[i]) - __uint_as_float(v.w[i] & 0xffff0000u));
@@ -242,10 +261,17 @@ __device__ __forceinline__ void clear_zeros()
     if (threadIdx.x < kZeros / 16) lds[threadIdx.x] = uint4_t{0, 0, 0, 0};
 }
 
-// Adds what a batch's chunks contribute; byte: of the first one's columns behind a slot's start.
-template <typename MT, typename S, bool ZERO, int GM, int SETS, int NR, int RT, int U>
+// Adds what a batch's chunks contribute; byte: of the first one's columns behind a slot's start.  T: of x.
+template <typename T, typename S, bool ZERO, int GM, int SETS, int NR, int RT, int U>
 __device__ __forceinline__ void add_batch(const Batch<S, ZERO, GM, RT, U> &b, const Side<SETS, NR> &side, int shift, uint32_t byte, Constants constants, float (&acc)[RT][SETS][NR])
 {
+    constexpr bool kCodes = sizeof(T) == 4;  // codes as they are, not as 16 + q
+    // A zero point is taken off as a bf16, which is all of it where it is a code.  The rest of it, if any, as further bf16 numbers where groups are of 32 columns, or else by the group's
+    // sum of x, in fp32; us, fp32: 16 x 16384 x 4096 with groups of 32 and fp16 zero points 47 as numbers, 172 by the sum (registers); 16 x 20000 x 4096 with groups of 128 76 and 68.
+    // (Not by a branch for zero points that are no codes: behind one that it put between a matrix instruction and what reads the result, the compiler left out wait states.)
+    constexpr int kZeroParts = GM > 1 || std::is_same_v<S, bf16> ? 1 : std::is_same_v<S, f16> ? 2 : 3;
+    constexpr bool kTaken = !kCodes || (ZERO && GM > 1 && !std::is_same_v<S, bf16>);
+    using MT = std::conditional_t<kCodes, bf16, T>;
     using C = Cores<MT>;
 #pragma unroll
     for (int u = 0; u < U; u++) {
@@ -266,26 +292,49 @@ __device__ __forceinline__ void add_batch(const Batch<S, ZERO, GM, RT, U> &b, co
 #pragma unroll
                 for (int j = 0; j < GM; j++) {
                     v[j][k] = side.x(k, byte + u * 256, g * GM + j);
-                    taken[k] = C::mul(v[j][k], uint4_t{kept, kept, kept, kept}, taken[k]);
+                    if constexpr (kTaken) taken[k] = C::mul(v[j][k], uint4_t{kept, kept, kept, kept}, taken[k]);
                 }
             }
 #pragma unroll
             for (int t = 0; t < RT; t++) {
+                const float f = b.of(b.scale[t], shift, u, g), zero = ZERO ? b.of(b.zero[ZERO ? t : 0], shift, u, g) : 8.0f;
+                float off = -16.0f - zero;
                 float4_t sum[SETS];
+                if constexpr (kCodes) {
+                    uint32_t minus[ZERO ? kZeroParts : 1];
+                    float rest = -zero;
 #pragma unroll
-                for (int k = 0; k < SETS; k++) sum[k] = ZERO ? float4_t{0, 0, 0, 0} : taken[k];
+                    for (uint32_t &part : minus) {
+                        part = __builtin_bit_cast(uint32_t, __builtin_convertvector(float2_t{rest, rest}, bf16x2_t));
+                        rest -= __uint_as_float(part & 0xffff0000u);
+                    }
+                    off = rest;
 #pragma unroll
-                for (int j = 0; j < GM; j++) {
-                    const uint4_t w = numbers_of<MT>(words[t][g * GM + j], constants);
+                    for (int k = 0; k < SETS; k++) sum[k] = float4_t{0, 0, 0, 0};
 #pragma unroll
-                    for (int k = 0; k < SETS; k++) sum[k] = C::mul(v[j][k], w, sum[k]);
+                    for (int j = 0; j < GM; j++) {
+#pragma unroll
+                        for (int i = (int)(sizeof(minus) / 4) - 1; i >= 0; i--)  // (the small ones while the sum is small)
+#pragma unroll
+                            for (int k = 0; k < SETS; k++) sum[k] = C::mul(v[j][k], uint4_t{minus[i], minus[i], minus[i], minus[i]}, sum[k]);
+                        const uint4_t w = codes_of(words[t][g * GM + j]);
+#pragma unroll
+                        for (int k = 0; k < SETS; k++) sum[k] = C::mul(v[j][k], w, sum[k]);
+                    }
+                } else {
+#pragma unroll
+                    for (int k = 0; k < SETS; k++) sum[k] = ZERO ? float4_t{0, 0, 0, 0} : taken[k];
+#pragma unroll
+                    for (int j = 0; j < GM; j++) {
+                        const uint4_t w = numbers_of<MT>(words[t][g * GM + j], constants);
+#pragma unroll
+                        for (int k = 0; k < SETS; k++) sum[k] = C::mul(v[j][k], w, sum[k]);
+                    }
                 }
-                const float f = b.of(b.scale[t], shift, u, g);
-                const float off = ZERO ? -16.0f - b.of(b.zero[ZERO ? t : 0], shift, u, g) : 0.0f;
 #pragma unroll
                 for (int k = 0; k < SETS; k++)
 #pragma unroll
-                    for (int i = 0; i < NR; i++) acc[t][k][i] += f * (ZERO ? sum[k][i] + off * taken[k][i] : sum[k][i]);
+                    for (int i = 0; i < NR; i++) acc[t][k][i] += f * (ZERO && kTaken ? sum[k][i] + off * taken[k][i] : sum[k][i]);
             }
         }
     }
@@ -409,7 +458,7 @@ __global__ __launch_bounds__(kThreads) void k_q4_mv(Q4Product p, int32_t per_pas
             b.load(p.a, place, (step + 1) * step_chunks + column_wave * U);
         }
         __syncthreads();
-        add_batch<MT>(a, side, p.a.shift, byte0, constants, acc);
+        add_batch<T>(a, side, p.a.shift, byte0, constants, acc);
         if (step + 1 < steps) {
             staging.end(p, vector0, vectors, (step + 1) * step_chunks * 128, log_eights, x1, stride);
             if (step + 2 < steps) {
@@ -417,7 +466,7 @@ __global__ __launch_bounds__(kThreads) void k_q4_mv(Q4Product p, int32_t per_pas
                 a.load(p.a, place, (step + 2) * step_chunks + column_wave * U);
             }
             __syncthreads();
-            add_batch<MT>(b, side, p.a.shift, byte1, constants, acc);
+            add_batch<T>(b, side, p.a.shift, byte1, constants, acc);
         }
     }
 #pragma unroll
@@ -469,7 +518,7 @@ __global__ __launch_bounds__(kThreads) void k_q4_mv_rows(Q4Product p)
     float acc[RT][1][NR] = {};
     int batch = 0;
     auto step = [&](const Batch<S, ZERO, GM, RT, U> &now) {
-        add_batch<MT>(now, side, p.a.shift, batch * (U * 256), constants, acc);
+        add_batch<T>(now, side, p.a.shift, batch * (U * 256), constants, acc);
         if (++batch < batches) return;
         batch = 0;
 #pragma unroll

@@ -369,3 +369,52 @@ def test_tensors_of_other_dimensions_are_refused():
             H.hbp_q4_mv(**a)
         with pytest.raises(AssertionError):
             H.hbp_q4_mv_t(**a | dict(x=a["y"], y=a["x"]))
+
+
+def codes_around_their_zeros(rows, cols, group, scales, zeros, seed):
+    """(codes, scales, zero points or None, values in 64 bits), on the GPU: of every weight its opposite is as likely, so that a sum of them with numbers of one sign
+    is as large as a sum with numbers of either."""
+    import torch
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    shape, of = H.hbp_q4_shapes(rows, cols, group)[1], torch.arange(cols, device="cuda") // group
+    z = torch.randint(4, 12, shape, generator=g, device="cuda") if zeros else torch.full(shape, 8, device="cuda")
+    q = z[:, of] + torch.randint(-4, 5, (rows, cols), generator=g, device="cuda")
+    packed = torch.zeros(rows, (cols + 31) // 32 * 32, dtype=torch.uint8, device="cuda")
+    packed[:, :cols] = q.to(torch.uint8)
+    s = (0.02 * (0.5 + torch.rand(shape, generator=g, device="cuda"))).to(dtype(scales))
+    z = z.to(dtype(scales))
+    if zeros == "broken":                     # zero points between codes
+        z = (z.float() + 0.3).to(dtype(scales))
+    w = s.double()[:, of] * (q.double() - z.double()[:, of])
+    return packed[:, 0::2] | packed[:, 1::2] << 4, s, z if zeros else None, w
+
+
+X_OF_ONE_SIGN = {"positive": lambda n: n.abs(), "cut off": lambda n: n.clamp(min=0), "around 3": lambda n: n.abs() + 3}
+
+
+def near_the_sum(y, x, w, roundings, what):
+    """fp32 sums of products w x (x [vectors, n], w [n, outputs], 64 bits, on the GPU): so many roundings of the size of the sum and of the root of its terms' squares,
+    which is the size of partial sums of terms of either sign."""
+    import torch
+    want, terms = torch.mm(x, w), torch.mm(x.square(), w.square()).sqrt()
+    worst = ((y.double() - want).abs() / (2.0 ** -24 * (want.abs() + terms))).max().item()
+    assert worst <= roundings, f"{what}: {worst:.3g} roundings, {roundings:.3g} allowed"
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kind", list(X_OF_ONE_SIGN))
+@pytest.mark.parametrize("zeros", [False, True, "broken"])
+def test_products_with_an_x_that_is_not_centred(kind, zeros):
+    """Sums over a group, then over groups, of terms that are centred though x is not: sixteen roundings, whichever kernel it is (in a model of the sums, fp32 in pieces of
+    eight columns, it is up to eight)."""
+    import torch
+    for rows, cols in ((300, 4096), (8300, 2048)):
+        for group in (32, 64, 128, 512):
+            c, s, z, w = codes_around_their_zeros(rows, cols, group, "f32" if group == 64 else "f16", zeros, group)
+            wt = w.t().contiguous()
+            for vectors in (1, 5, 9, 21):
+                print(f"[q4 not centred] mv {rows} x {cols} group {group} zeros {zeros} {kind} {vectors}", flush=True)
+                x = X_OF_ONE_SIGN[kind](torch.randn(vectors, cols, generator=torch.Generator(device="cuda").manual_seed(vectors), device="cuda"))
+                y = torch.empty(vectors, rows, device="cuda")
+                H.hbp_q4_mv(c, s, x, y, group=group, zeros=z)
+                near_the_sum(y, x.double(), wt, 16, f"{rows} x {cols} group {group} {vectors} vectors")
