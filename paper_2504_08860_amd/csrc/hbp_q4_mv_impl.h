@@ -560,9 +560,10 @@ __global__ __launch_bounds__(kThreads) void k_q4_mv_rows(Q4Product p)
 //   5 to 16: 16 x 4096 x 4096 1 1 8 1 8.9, 1 2 8 2 10.2; fp32 5 x 10007 x 7001 1 2 8 4 24.3, 2 2 8 2 24.4, 1 1 4 1 25.2; 12 x 40000 x 4096 1 2 4 4 31, 1 2 8 4 40.
 //   more: as many column_waves as x of a step fits the threads' registers with, and with many rows none; 24 x 8192 x 8192 1 1 8 2 24.8, 2 1 8 2 32.7;
 //     64 x 4096 x 4096 1 1 8 4 31.5, 1 1 8 8 47.8; 48 x 131072 x 4096 2 1 8 8 143, 1 1 8 8 180; 64 x 32768 x 8192 1 1 8 8 103, 2 1 8 8 208 (registers).
+//     Two tiles of three sets, four groups a chunk and zero points do not fit the registers (38 to 90 spilled): one; 48 x 20000 x 4096 bf16 47, two 105; 48 x 131072 x 4096 199, two 273.
 template <typename T, typename S, bool ZERO, int GM> int launch_mv(const Q4Product &p, hipStream_t st)
 {
-    constexpr int kParts = sizeof(T) == 4 ? 3 : 1;
+    constexpr int kParts = sizeof(T) == 4 ? 3 : 1, kThreeSetTiles = ZERO && GM == 1 ? 1 : 2;
     const int per_pass = (int)std::min<int64_t>(kMostSlots / kParts, p.vectors);
     const int slots = per_pass * kParts, sets = (slots + 15) / 16;
     const int64_t tiles = (p.a.n_rows + 15) / 16, chunks = (p.a.n_cols + 127) / 128, passes = (p.vectors + per_pass - 1) / per_pass;
@@ -589,7 +590,7 @@ template <typename T, typename S, bool ZERO, int GM> int launch_mv(const Q4Produ
         while (row_waves < 8 && (per_pass * (waves / row_waves) * 16 > kStagedEights * kThreads ||
                                  slots * (waves / row_waves * 128 + kStagePad) * 4 > kStageBytes - kZeros))
             row_waves *= 2;
-        rt = tiles >= 1024 && sets < 4 ? 2 : 1;
+        rt = tiles >= 1024 && sets < 4 ? (sets == 3 ? kThreeSetTiles : 2) : 1;
     }
     const int64_t step = waves / row_waves * u, steps = (chunks + step - 1) / step;
     const size_t bytes = std::max<size_t>(kZeros + (steps > 1 ? 2 : 1) * slots * (step * 128 + kStagePad) * 2, (size_t)waves * sets * (slots <= 4 ? 1 : 4) * kWave * 4);
@@ -609,7 +610,7 @@ template <typename T, typename S, bool ZERO, int GM> int launch_mv(const Q4Produ
         }(slots <= 4  ? (u == 4 ? k_q4_mv<T, S, ZERO, GM, 1, 1, 1, 4> : k_q4_mv<T, S, ZERO, GM, 1, 1, 1, 2>)
           : sets == 1 ? (u == 2 ? k_q4_mv<T, S, ZERO, GM, 1, 4, 1, 2> : k_q4_mv<T, S, ZERO, GM, 1, 4, 1, 1>)
           : sets == 2 ? (rt == 2 ? k_q4_mv<T, S, ZERO, GM, 2, 4, 2, 1> : k_q4_mv<T, S, ZERO, GM, 2, 4, 1, 1>)
-          : sets == 3 ? (rt == 2 ? k_q4_mv<T, S, ZERO, GM, 3, 4, 2, 1> : k_q4_mv<T, S, ZERO, GM, 3, 4, 1, 1>)
+          : sets == 3 ? (rt == 2 ? k_q4_mv<T, S, ZERO, GM, 3, 4, kThreeSetTiles, 1> : k_q4_mv<T, S, ZERO, GM, 3, 4, 1, 1>)
                       : k_q4_mv<T, S, ZERO, GM, 4, 4, 1, 1>);
         if (rc != HBP_OK) return rc;
     }

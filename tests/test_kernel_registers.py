@@ -13,7 +13,7 @@ MOST = 128   # bytes; kernels that have a few values too many for their register
 
 
 @pytest.mark.skipif(READELF is None or OBJDUMP is None, reason="no llvm-readelf")
-@pytest.mark.parametrize("kernels", ["norm", "logprobs"])
+@pytest.mark.parametrize("kernels", ["norm", "logprobs", "q4"])
 def test_scratch_memory(kernels, tmp_path):
     library = tmp_path / "lib.so"
     shutil.copy(H.LIB_PATH, library)
