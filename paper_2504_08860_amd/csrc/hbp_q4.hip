@@ -102,14 +102,14 @@ template <typename T, typename S> __global__ __launch_bounds__(256) void k_q4_un
     out.store_first(static_cast<T *>(w) + row * ldw + col, left);
 }
 
-// y = x W, the transposed product.  A lane takes C neighbouring columns (of one group) and adds code * (scale x) row by row, in fp32, for up to M vectors;
-// what the zero points take away, zero (scale x), is one sum for all C.  A workgroup has 64 C columns of a part of the rows, its wavefronts every eighth batch of ROWS rows; they
+// y = x W, the transposed product.  A lane takes C neighbouring columns (of one group) and adds (code - zero) * (scale x) row by row, in fp32, for up to M vectors
+// (zero (scale x) as a sum of its own, taken off at the end, would be one fma for all C, and leave errors of its own size in a result that is much smaller where x is of one sign).  A workgroup has 64 C columns of a part of the rows, its wavefronts every eighth batch of ROWS rows; they
 // are added up by LDS, the parts by a second kernel.
 //
 // Bound: vector instructions, 1.4 + M a weight (a conversion for each code and an fma for each vector), and their latency; us: 1 x 8192 x 8192 fp32 14 + 4 for the
 // sum, 19 x 6001 x 4099 with zero points 31 + 4.5, 64 x 8192 x 8192 173 (50 TFLOP/s of the 79 that fp32 fma has here).  Not by the matrix cores: there the scale, which
 // differs from row to row, would have to go into x, in parts, for every group anew.
-// As in the products, code * (scale x) may be infinite where the sum is not: such results are computed again from the definition.
+// As in the products, (code - zero) * (scale x) may be infinite where the sum is not: such results are computed again from the definition.
 constexpr int kTransposedWaves = 8, kTransposedRows = 512;  // rows whose x lies in LDS at a time
 // What a lane loads of ROWS rows.
 template <typename S, bool ZERO, int C, int ROWS> struct Rows {
@@ -139,11 +139,11 @@ template <typename S, bool ZERO, int C, int ROWS> struct Rows {
         }
     }
     // x: of the first row's M vectors, then the next one's
-    template <int M> __device__ __forceinline__ void add(const float *x, float (&acc)[M][C], float (&taken)[M]) const
+    template <int M> __device__ __forceinline__ void add(const float *x, float (&acc)[M][C]) const
     {
 #pragma unroll
         for (int i = 0; i < ROWS; i++) {
-            const float s = to_f32(scale[i]), z = ZERO ? to_f32(zero[ZERO ? i : 0]) : 1.0f;
+            const float s = to_f32(scale[i]) * (ZERO ? 1.0f : 16.0f), z = ZERO ? to_f32(zero[ZERO ? i : 0]) : 0.0f;
             float f[C], u[M];
             if constexpr (M % 4 == 0) {
 #pragma unroll
@@ -162,19 +162,26 @@ template <typename S, bool ZERO, int C, int ROWS> struct Rows {
             }
 #pragma unroll
             for (int j = 0; j < C / 8; j++) {
-                const uint32_t even = w[i][j] & 0x0f0f0f0fu, odd = w[i][j] >> 4 & 0x0f0f0f0fu;
+                if constexpr (ZERO) {
+                    const uint32_t even = w[i][j] & 0x0f0f0f0fu, odd = w[i][j] >> 4 & 0x0f0f0f0fu;
 #pragma unroll
-                for (int b = 0; b < 4; b++) {
-                    f[8 * j + 2 * b] = (float)(even >> 8 * b & 255u);
-                    f[8 * j + 2 * b + 1] = (float)(odd >> 8 * b & 255u);
+                    for (int b = 0; b < 4; b++) {
+                        f[8 * j + 2 * b] = (float)(even >> 8 * b & 255u) - z;
+                        f[8 * j + 2 * b + 1] = (float)(odd >> 8 * b & 255u) - z;
+                    }
+                } else {  // with 8 flipped a code is a number of four bits with a sign, of which the instruction makes (code - 8) / 16
+                    const uint32_t even = w[i][j] ^ 0x88888888u, odd = even >> 4;
+#pragma unroll
+                    for (int b = 0; b < 4; b++) {
+                        f[8 * j + 2 * b] = __builtin_amdgcn_cvt_off_f32_i4(even >> 8 * b & 255u);
+                        f[8 * j + 2 * b + 1] = __builtin_amdgcn_cvt_off_f32_i4(odd >> 8 * b & 255u);
+                    }
                 }
             }
 #pragma unroll
-            for (int m = 0; m < M; m++) {
-                taken[m] += ZERO ? u[m] * z : u[m];
+            for (int m = 0; m < M; m++)
 #pragma unroll
                 for (int c = 0; c < C; c++) acc[m][c] += f[c] * u[m];
-            }
         }
     }
 };
@@ -192,7 +199,7 @@ __global__ __launch_bounds__(kTransposedWaves * kWave) void k_q4_mv_t(Q4 a, cons
     const int col = blockIdx.x * (kWave * C) + lane * C;
     const uint32_t at = min(col, (int)(a.pitch * 2) - C) / 2;  // (lanes behind the last column read its codes again)
     const uint32_t scale_at = min(col >> a.shift, a.groups - 1) * sizeof(S);
-    float acc[M][C] = {}, taken[M] = {};
+    float acc[M][C] = {};
     constexpr int kStep = kTransposedWaves * ROWS;
     for (int64_t row0 = part0; row0 < end; row0 += apart) {
         const int rows = (int)min((int64_t)apart, end - row0);
@@ -206,10 +213,10 @@ __global__ __launch_bounds__(kTransposedWaves * kWave) void k_q4_mv_t(Q4 a, cons
         __syncthreads();
         for (; r < rows; r += 2 * kStep) {  // (the next rows' loads are issued before this one's are waited for)
             if (r + kStep < rows) two.load(a, row0, r + kStep, rows, at, scale_at);
-            one.template add<M>(lds + r * M, acc, taken);
+            one.template add<M>(lds + r * M, acc);
             if (r + kStep < rows) {
                 if (r + 2 * kStep < rows) one.load(a, row0, r + 2 * kStep, rows, at, scale_at);
-                two.template add<M>(lds + (r + kStep) * M, acc, taken);
+                two.template add<M>(lds + (r + kStep) * M, acc);
             }
         }
     }
@@ -217,10 +224,8 @@ __global__ __launch_bounds__(kTransposedWaves * kWave) void k_q4_mv_t(Q4 a, cons
     for (int m = 0; m < M; m++) {
         __syncthreads();
 #pragma unroll
-        for (int c = 0; c < C; c += 4) {
-            const float off = ZERO ? taken[m] : 8.0f * taken[m];
-            reinterpret_cast<float4 *>(lds)[(wave * (kWave * C) + lane * C + c) / 4] = float4{acc[m][c] - off, acc[m][c + 1] - off, acc[m][c + 2] - off, acc[m][c + 3] - off};
-        }
+        for (int c = 0; c < C; c += 4)
+            reinterpret_cast<float4 *>(lds)[(wave * (kWave * C) + lane * C + c) / 4] = float4{acc[m][c], acc[m][c + 1], acc[m][c + 2], acc[m][c + 3]};
         __syncthreads();
         if (vector0 + m < vectors)
             for (int c = threadIdx.x; c < kWave * C; c += blockDim.x) {

@@ -418,3 +418,19 @@ def test_products_with_an_x_that_is_not_centred(kind, zeros):
                 y = torch.empty(vectors, rows, device="cuda")
                 H.hbp_q4_mv(c, s, x, y, group=group, zeros=z)
                 near_the_sum(y, x.double(), wt, 16, f"{rows} x {cols} group {group} {vectors} vectors")
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kind", list(X_OF_ONE_SIGN))
+@pytest.mark.parametrize("zeros", [False, True, "broken"])
+def test_transposed_products_with_an_x_that_is_not_centred(kind, zeros):
+    """One row after another in fp32: roundings by the root of the number of rows, half of it and sixteen more are allowed (in a model of the sums it is up to a
+    fifth of the root)."""
+    import torch
+    for rows, cols, group, vectors in ((8192, 300, 128, 1), (8192, 515, 32, 19), (8192, 2048, 64, 640), (1500, 300, 128, 4), (6001, 1000, 512, 2)):
+        print(f"[q4 not centred] mv_t {rows} x {cols} group {group} zeros {zeros} {kind} {vectors}", flush=True)
+        c, s, z, w = codes_around_their_zeros(rows, cols, group, "f32" if group == 64 else "f16", zeros, group)
+        x = X_OF_ONE_SIGN[kind](torch.randn(vectors, rows, generator=torch.Generator(device="cuda").manual_seed(vectors), device="cuda"))
+        y = torch.empty(vectors, cols, device="cuda")
+        H.hbp_q4_mv_t(c, s, x, y, group=group, zeros=z)
+        near_the_sum(y, x.double(), w, 16 + rows ** 0.5 / 2, f"{rows} x {cols} group {group} {vectors} vectors")
