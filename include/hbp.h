@@ -340,8 +340,8 @@ typedef struct {
 } hbp_q4_matrix_t;
 
 /* Rounds a dense matrix w (DEVICE, `type`, row stride ldw) into a's codes, scales and, where a->zeros is not NULL, zero points.  Without
- * zero points: scale = max |w| / 7 over the group, code = rint(w / scale) + 8.  With them: low = min(w, 0), high = max(w, 0), scale =
- * (high - low) / 15, zero = rint(-low / scale) (so that 0 is a code), code = rint(w / scale + zero).  The scale is rounded to its type
+ * zero points: scale = max |w| / 7 over the group, code = rint(w / scale + 8).  With them: low = min(w, 0), high = max(w, 0), scale =
+ * (high - low) / 15, zero = rint(-low / scale), at most 15 (so that 0 is a code), code = rint(w / scale + zero).  The scale is rounded to its type
  * first (at most that type's largest value) and the codes, clamped to 0..15, go by the rounded one; a scale of 0 gives the codes of 0.  A group with a NaN or an infinity gets a NaN
  * scale (and zero point 0, codes 8).  *a HOST. */
 int hbp_q4_pack(const hbp_q4_matrix_t *a, int type, const void *w, int64_t ldw, void *stream);

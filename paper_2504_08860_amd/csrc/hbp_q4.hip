@@ -60,10 +60,11 @@ template <typename T, typename S> __global__ __launch_bounds__(256) void k_q4_pa
         const int64_t row = row0 + r;
         if (col >= a.pitch * 2 || row >= a.n_rows) continue;
         constexpr float kLargest = std::is_same_v<S, f16> ? 65504.0f : std::is_same_v<S, bf16> ? 3.3895313892515355e38f : 3.4028234663852886e38f;
-        const float wide = a.zeros ? (high - low) * (1.0f / 15.0f) : fmaxf(-low, high) * (1.0f / 7.0f);
+        const float span = high - low;  // may be more than the largest number where a fifteenth of it is not
+        const float wide = !a.zeros ? fmaxf(-low, high) * (1.0f / 7.0f) : span < INFINITY ? span * (1.0f / 15.0f) : high * (1.0f / 15.0f) - low * (1.0f / 15.0f);
         const S scale = from_f32<S>(fminf(wide, kLargest));
         const float s = to_f32(scale), inverse = s == 0.0f ? 0.0f : 1.0f / s;
-        const float zero = !a.zeros ? 8.0f : s == 0.0f ? 0.0f : rintf(-low / s);
+        const float zero = !a.zeros ? 8.0f : s == 0.0f ? 0.0f : fminf(rintf(-low / s), 15.0f);
         uint32_t word = 0;
 #pragma unroll
         for (int i = 0; i < 8; i++) {

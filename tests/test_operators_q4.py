@@ -434,3 +434,35 @@ def test_transposed_products_with_an_x_that_is_not_centred(kind, zeros):
         y = torch.empty(vectors, cols, device="cuda")
         H.hbp_q4_mv_t(c, s, x, y, group=group, zeros=z)
         near_the_sum(y, x.double(), w, 16 + rows ** 0.5 / 2, f"{rows} x {cols} group {group} {vectors} vectors")
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("name", ["f32", "bf16"])
+@pytest.mark.parametrize("scales", TYPES)
+def test_pack_with_zero_points_at_the_ends_of_the_range(name, scales):
+    """Groups as wide as the type is (high - low is no fp32 number), larger than a scale can say, and so narrow that the scale is one of the smallest numbers of its type: 0 stays a
+    value of its own, zero points are codes, and what no end of the range cuts off is off by half a step and the roundings of a quotient."""
+    import torch
+    most = 0.98 * float(torch.finfo(dtype(name)).max)      # (so that fifteen steps are a number where the scale is rounded up)
+    smallest = TINY[scales]
+    top = float(torch.finfo(dtype(scales)).max)
+    rows = [(-0.9 * most, 0.9 * most), (-0.99 * most, 0.2 * most), (-0.1 * most, 0.95 * most), (-most, 0.0), (0.0, most)]
+    rows += [(-21.0 * smallest, 0.0), (-22.0 * smallest, 0.5 * smallest), (-8.0 * smallest, 14.4 * smallest)] if scales == "f16" else []
+    w = torch.empty(len(rows), 32, dtype=torch.float64)
+    for r, (low, high) in enumerate(rows):
+        w[r] = torch.linspace(low, high, 32, dtype=torch.float64)
+        w[r, 5] = 0.0
+    w = w.float().to(dtype(name))
+    c = torch.empty(H.hbp_q4_shapes(len(rows), 32, 32)[0], dtype=torch.uint8, device="cuda")
+    s = torch.empty(len(rows), 1, dtype=dtype(scales), device="cuda")
+    z = torch.empty_like(s)
+    H.hbp_q4_pack(w.cuda(), c, s, group=32, zeros=z)
+    back = torch.from_numpy(values(c, s, z, 32, 32))
+    assert torch.equal(H.hbp_q4_unpack(c, s, 32, group=32, zeros=z).cpu(), back.float())   # (half a step beyond the largest number is an infinity)
+    s, z = s.cpu().double(), z.cpu().double()
+    assert ((z >= 0) & (z <= 15) & (z == z.round())).all() and torch.isfinite(s).all() and not back[:, 5].any()
+    wd = w.double()
+    step = torch.stack([(wd[r].max().clamp(min=0) - wd[r].min().clamp(max=0)) / 15 for r in range(len(rows))])[:, None]
+    assert ((s - step.clamp(max=top)).abs() <= UNIT[scales] * s * 1.001 + smallest / 2 + 2.0 ** -22 * s).all()
+    inside = (wd / s + z >= 0) & (wd / s + z <= 15)
+    assert inside[:, 5].all() and ((back - wd).abs()[inside] <= (s * (0.5 + 1e-5)).expand_as(wd)[inside]).all()
