@@ -336,6 +336,8 @@ int view(const hbp_q4_matrix_t *m, Q4 *a)
 }
 
 constexpr int64_t kMostVectors = int64_t(1) << 24;  // (so that a workspace's bytes can be counted)
+// Vectors of one pair of launches: the grids end at 65535 in the dimension of the passes and in that of the sum's fours of vectors.  The workspace is used again by the next pair.
+int64_t vectors_at_once(const TransposedShape &s, int64_t vectors) { return std::min<int64_t>(vectors, 16384 * s.m); }
 
 // checks what both products share
 int check_product(int type, const void *x, int64_t ldx, int64_t n_x, const void *y, int64_t ldy, int64_t n_y, int64_t vectors)
@@ -413,7 +415,8 @@ int hbp_q4_mv_t_workspace(const hbp_q4_matrix_t *m, int64_t vectors, size_t *byt
     if (rc != HBP_OK) return rc;
     if (!bytes || vectors < 0) return HBP_ERR_INVALID_ARGUMENT;
     if (vectors > kMostVectors) return HBP_ERR_TOO_LARGE;
-    *bytes = (size_t)transposed_shape(a, vectors).parts * (size_t)vectors * (size_t)a.n_cols * sizeof(float);
+    const TransposedShape s = transposed_shape(a, vectors);
+    *bytes = (size_t)s.parts * (size_t)vectors_at_once(s, vectors) * (size_t)a.n_cols * sizeof(float);
     return HBP_OK;
 }
 
@@ -437,9 +440,8 @@ int hbp_q4_mv_t(const hbp_q4_matrix_t *m, int type, const void *x, int64_t ldx, 
         return by_type(m->scale_type, [&](auto scale) -> int {
             using T = decltype(t);
             using S = decltype(scale);
-            constexpr int64_t kPasses = 32768;
-            for (int64_t first = 0; first < vectors; first += kPasses * s.m) {  // (the grid's third dimension ends at 65535)
-                const int64_t count = vectors - first < kPasses * s.m ? vectors - first : kPasses * s.m;
+            for (int64_t first = 0; first < vectors;) {
+                const int64_t count = vectors_at_once(s, vectors - first);
                 const dim3 grid((unsigned)s.wide, (unsigned)s.parts, (unsigned)((count + s.m - 1) / s.m));
                 const size_t x_bytes = (size_t)s.m * (s.part < kTransposedRows ? s.part : kTransposedRows) * 4, sum_bytes = (size_t)kTransposedWaves * kWave * s.c * 4;
                 const size_t bytes = x_bytes > sum_bytes ? x_bytes : sum_bytes;
@@ -462,6 +464,7 @@ int hbp_q4_mv_t(const hbp_q4_matrix_t *m, int type, const void *x, int64_t ldx, 
                 k_q4_sum_parts<T, S><<<dim3((unsigned)((a.n_cols + kWave - 1) / kWave), (unsigned)((count + 3) / 4)), 256, 0, st>>>(
                     a, x_at, ldx, partial, (int)s.parts, count, static_cast<T *>(y) + first * ldy, ldy);
                 HBP_HIP(hipGetLastError());
+                first += count;
             }
             return HBP_OK;
         });

@@ -466,3 +466,24 @@ def test_pack_with_zero_points_at_the_ends_of_the_range(name, scales):
     assert ((s - step.clamp(max=top)).abs() <= UNIT[scales] * s * 1.001 + smallest / 2 + 2.0 ** -22 * s).all()
     inside = (wd / s + z >= 0) & (wd / s + z <= 15)
     assert inside[:, 5].all() and ((back - wd).abs()[inside] <= (s * (0.5 + 1e-5)).expand_as(wd)[inside]).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("direction,vectors", [("mv", (1 << 21) + 70), ("mv_t", 262_141), ("mv_t", 327_691)])
+def test_more_vectors_than_a_grid_has_passes(direction, vectors):
+    import torch
+    rows, cols = 3, 5
+    c, s, z, w = matrix(rows, cols, 32, "f16", True, 3)
+    n_in, n_out = (cols, rows) if direction == "mv" else (rows, cols)
+    x = some_x(vectors, n_in, "bf16", 17)
+    y = torch.full((vectors, n_out), float("nan"), dtype=x.dtype, device="cuda")
+    print(f"[q4 vectors] {direction} {vectors}", flush=True)
+    (H.hbp_q4_mv if direction == "mv" else H.hbp_q4_mv_t)(c, s, x.cuda(), y, group=32, zeros=z)
+    agree(y, x.double().numpy() @ (w.T if direction == "mv" else w), x, "bf16")
+
+
+def test_workspace_for_many_vectors_is_that_of_a_launch():
+    need = [ctypes.c_size_t(), ctypes.c_size_t()]
+    for n, vectors in zip(need, (1 << 20, 1 << 24)):
+        assert H.lib().hbp_q4_mv_t_workspace(H.hbp_q4_matrix_t(4096, 4096, None, 64, 4096, 32, 0), vectors, n) == 0
+    assert need[0].value == need[1].value < 4 << 30
