@@ -7,6 +7,7 @@ namespace hbp {
 namespace {
 
 constexpr int64_t kMaxWidth = 16384;
+constexpr int64_t kMostWorkgroups = int64_t(1) << 21;  // of one forward launch: a grid counts its threads, up to 1024 of each, in 32 bits
 
 struct NormArgs {
     int64_t tokens, ldh, ldy, ldho, ldxo, ldg;
@@ -394,9 +395,21 @@ int hbp_residual_norms(const hbp_norms_t *n, const void *h, int64_t ldh, const v
         return by_gate(n->gate_kind, [&](auto gate) -> int {
             return by_width_forward(n->width, [&](auto threads, auto chunks) -> int {
                 constexpr int kThreads = decltype(threads)::value;
-                k_residual_norms<T, kThreads, decltype(chunks)::value, decltype(gate)::value>
-                    <<<dim3((unsigned)((a.tokens + rows_at_once(n->width) - 1) / rows_at_once(n->width))), std::max(kThreads, kWave), 0, (hipStream_t)stream>>>(a);
-                HBP_HIP(hipGetLastError());
+                const int64_t at_once = rows_at_once(n->width);
+                for (int64_t first = 0; first < n->tokens; first += kMostWorkgroups * at_once) {
+                    NormArgs q = a;
+                    q.tokens = std::min(n->tokens - first, kMostWorkgroups * at_once);
+                    q.h = static_cast<const T *>(h) + first * ldh;
+                    q.y = static_cast<const T *>(y) + first * ldy;
+                    q.h_out = static_cast<T *>(h_out) + first * ldho;
+                    q.x_out = static_cast<T *>(x_out) + first * ldxo;
+                    if (n->gate_kind == HBP_GATE_TOKEN) q.gate = static_cast<const T *>(n->gate) + first;
+                    if (n->gate_kind == HBP_GATE_FULL) q.gate = static_cast<const T *>(n->gate) + first * n->ldg;
+                    if (rstd) q.rstd = rstd + 2 * first;
+                    k_residual_norms<T, kThreads, decltype(chunks)::value, decltype(gate)::value>
+                        <<<dim3((unsigned)((q.tokens + at_once - 1) / at_once)), std::max(kThreads, kWave), 0, (hipStream_t)stream>>>(q);
+                    HBP_HIP(hipGetLastError());
+                }
                 return HBP_OK;
             });
         });

@@ -364,3 +364,32 @@ def test_gradients_of_large_rows_and_of_rows_of_zeros_with_a_small_eps(name, gat
                 for key, got in (("d_h", out[2]), ("d_y", out[3]), ("d_w_post", d_wp), ("d_w_pre", d_wq), ("d_gate", d_gate)):
                     if got is not None:
                         near(got, want[key], "bf16" if got.dtype == torch.bfloat16 else "f32", key, size=size[key])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("gate", GATES)
+@pytest.mark.parametrize("tokens,width", [((1 << 24) + 13, 1), ((1 << 21) + 3, 300)])
+def test_more_rows_than_one_launch_takes(tokens, width, gate):
+    import torch
+    g = torch.Generator(device="cuda").manual_seed(1)
+    r = lambda *shape: torch.randn(*shape, generator=g, device="cuda", dtype=torch.bfloat16)  # noqa: E731
+    h, y = r(tokens, width), r(tokens, width)
+    gates = {"none": None, "channel": r(width), "token": r(tokens, 1), "full": r(tokens, width)}[gate]
+    ho, xo, rstd = torch.empty_like(h), torch.empty_like(h), torch.empty(tokens, 2, device="cuda")
+    print(f"[norms] {tokens} x {width} {gate}", flush=True)
+    H.hbp_residual_norms(h, y, ho, xo, rstd=rstd, gate=gates, eps=EPS)
+    for part in (slice(0, 50), slice(tokens - 100, tokens)):
+        cut = None if gates is None else gates if gate == "channel" else gates[part]
+        a, b, factors = torch.empty_like(h[part]), torch.empty_like(h[part]), torch.empty_like(rstd[part])
+        H.hbp_residual_norms(h[part], y[part], a, b, rstd=factors, gate=cut, eps=EPS)
+        assert torch.equal(ho[part], a) and torch.equal(xo[part], b) and torch.equal(rstd[part], factors)
+
+
+@pytest.mark.gpu
+def test_more_threads_than_32_bits_count():
+    import torch
+    tokens = (1 << 29) + 5
+    h, y = torch.ones(tokens, 1, dtype=torch.bfloat16, device="cuda"), torch.ones(tokens, 1, dtype=torch.bfloat16, device="cuda")
+    print("[norms] 2^29 + 5 rows of one column", flush=True)
+    H.hbp_residual_norms(h, y, h, y, eps=EPS)
+    assert (h == 2).all() and (y == 1).all()
