@@ -401,10 +401,20 @@ int hbp_q4_mv(const hbp_q4_matrix_t *m, int type, const void *x, int64_t ldx, vo
     if (rc != HBP_OK || vectors == 0) return rc;
     rc = earlier_error();
     if (rc != HBP_OK) return rc;
-    const Q4Product p{a, x, y, ldx, ldy, vectors, m->scale_type};
     hipStream_t st = (hipStream_t)stream;
-    if (a.zeros) return type == HBP_F32 ? launch_q4_mv_f32_zeros(p, st) : type == HBP_F16 ? launch_q4_mv_f16_zeros(p, st) : launch_q4_mv_bf16_zeros(p, st);
-    return type == HBP_F32 ? launch_q4_mv_f32(p, st) : type == HBP_F16 ? launch_q4_mv_f16(p, st) : launch_q4_mv_bf16(p, st);
+    constexpr int32_t kRows = 1 << 26;  // of one launch: a grid counts its threads, up to sixteen for a row, in 32 bits
+    const int64_t scale_bytes = type_bytes(m->scale_type) * a.groups;
+    for (int64_t first = 0; first < m->n_rows; first += kRows) {
+        Q4Product p{a, x, static_cast<char *>(y) + first * type_bytes(type), ldx, ldy, vectors, m->scale_type};
+        p.a.codes += first * a.pitch;
+        p.a.scales = static_cast<const char *>(a.scales) + first * scale_bytes;
+        if (a.zeros) p.a.zeros = static_cast<const char *>(a.zeros) + first * scale_bytes;
+        p.a.n_rows = (int32_t)std::min<int64_t>(m->n_rows - first, kRows);
+        if (a.zeros) rc = type == HBP_F32 ? launch_q4_mv_f32_zeros(p, st) : type == HBP_F16 ? launch_q4_mv_f16_zeros(p, st) : launch_q4_mv_bf16_zeros(p, st);
+        else rc = type == HBP_F32 ? launch_q4_mv_f32(p, st) : type == HBP_F16 ? launch_q4_mv_f16(p, st) : launch_q4_mv_bf16(p, st);
+        if (rc != HBP_OK) return rc;
+    }
+    return HBP_OK;
 }
 
 int hbp_q4_mv_t_workspace(const hbp_q4_matrix_t *m, int64_t vectors, size_t *bytes)

@@ -101,3 +101,8 @@ def test_infinities_where_rows_are_many(zeros):
                 assert np.isfinite(got).all() and (np.abs(got - want) <= 2.0 ** -7 * np.abs(want)).all()
             if vectors > 1:
                 agree(y[1:, some], x[1:].double().numpy() @ w.T, x[1:], name)
+
+
+@pytest.mark.parametrize("vectors", [1, 5])
+def test_more_rows_than_one_launch_takes(vectors):
+    check((1 << 26) + 133, 32, 32, "f16", True, [("bf16", vectors)], 1)
