@@ -312,8 +312,9 @@ struct LogprobBackArgs {
 };
 
 // The gradient.  p is exp(z - lse), and lse, in 32 bits, is off by half its last place, which p is then off by relative to itself: up to 2^-21, what the other roundings of z - lse
-// come to, for |lse| below 16; for results of 16 bits, which are off by 2^-12 and more themselves, 2^-19 is let pass.  Rows whose lse is larger have their largest logit and its sum taken
-// again, as the forward call took them, and p from those: by the row's first workgroup alone, which then takes all of the row (d_logits may be the logits, so that no other one may read what it writes).
+// come to, for |lse| below 16; for results of 16 bits, which are off by 2^-12 and more themselves, 2^-19 is let pass, for |lse| below 64.  Rows whose lse is larger have their largest logit and
+// its sum taken again, as the forward call took them, and p from those: by one of the row's workgroups, which then takes all of the row (d_logits may be the logits, so that no other one may
+// read what it writes).  us, such rows and others: 4096 x 32001 fp32 374 and 193, bf16 256 and 108; 64 x 50001 fp32 16 and 8; one row of 131072 27 and 8.
 template <typename T> constexpr float kLseLimit = sizeof(T) == 4 ? 16.0f : 64.0f;
 
 // below(z): z - lse
@@ -332,9 +333,9 @@ __device__ __forceinline__ void logit_gradients(const Eight<T> &v, Eight<T> &out
 }
 
 // Eight logits a thread.  Bound: HBM; 4096 x 32001 bf16 93 us, 5.6 TB/s read and written.
-template <typename T> __global__ __launch_bounds__(256) void k_logprobs_backward(LogprobBackArgs p)
+template <typename T, int THREADS> __global__ __launch_bounds__(THREADS) void k_logprobs_backward(LogprobBackArgs p)
 {
-    __shared__ Stats wave_stats[256 / kWave];
+    __shared__ Stats wave_stats[THREADS / kWave];
     const int64_t t = blockIdx.y;
     const T *z = static_cast<const T *>(p.logits) + t * p.ldz;
     T *d = static_cast<T *>(p.d_logits) + t * p.ldd;
@@ -343,35 +344,45 @@ template <typename T> __global__ __launch_bounds__(256) void k_logprobs_backward
     float u = id >= 0 && p.g_logp ? p.g_logp[t] : 0.0f;
     if (id >= p.vocabulary && p.g_logp) u = NAN;
     const bool none = lse == -INFINITY;
-    const int64_t col = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 8, left = p.vocabulary - col;
+    const int64_t col = ((int64_t)blockIdx.x * THREADS + threadIdx.x) * 8, left = p.vocabulary - col;
     Eight<T> v, out;
-    v.load_first(z + col, left);  // (on its way while lse is waited for; not used where the row is the first workgroup's)
+    v.load_first(z + col, left);  // (on its way while lse is waited for; not used where another workgroup has the row)
     if (none || !(fabsf(lse) >= kLseLimit<T>)) {
         if (left <= 0) return;
         logit_gradients(v, out, col, id, u, w, entropy, none, [&](float z) { return z - lse; });
         out.store_first(d + col, left);
         return;
     }
-    if (blockIdx.x > 0) return;
+    if (blockIdx.x != blockIdx.y % gridDim.x) return;  // (not the first one in every row: those may all be of one XCD)
+    constexpr int kAhead = 2, kTurn = THREADS * 8;
     Stats a{kLowest, 0.0f, 0.0f};
-    for (int64_t col = threadIdx.x * 8; col < p.vocabulary; col += 256 * 8) {
-        v.load_first(z + col, p.vocabulary - col);
-        float f[8];
+    for (int64_t col = threadIdx.x * 8; col < p.vocabulary; col += kAhead * kTurn) {
+        Eight<T> some[kAhead];
 #pragma unroll
-        for (int i = 0; i < 8; i++) f[i] = col + i < p.vocabulary ? v.get(i) : -INFINITY;
-        add_eight(a, f);
+        for (int k = 0; k < kAhead; k++) some[k].load_first(z + col + k * kTurn, p.vocabulary - col - k * kTurn);
+#pragma unroll
+        for (int k = 0; k < kAhead; k++) {
+            float f[8];
+#pragma unroll
+            for (int i = 0; i < 8; i++) f[i] = col + k * kTurn + i < p.vocabulary ? some[k].get(i) : -INFINITY;
+            add_eight(a, f);
+        }
     }
     a = wave_join(a);
     if (threadIdx.x % kWave == 0) wave_stats[threadIdx.x / kWave] = a;
     __syncthreads();
     const int lane = threadIdx.x % kWave;
-    a = wave_join(lane < 256 / kWave ? wave_stats[lane] : Stats{kLowest, 0.0f, 0.0f});
+    a = wave_join(lane < THREADS / kWave ? wave_stats[lane] : Stats{kLowest, 0.0f, 0.0f});
     const float log_s = logf(a.s);
-    for (int64_t col = threadIdx.x * 8; col < p.vocabulary; col += 256 * 8) {
-        const int64_t left = p.vocabulary - col;
-        v.load_first(z + col, left);
-        logit_gradients(v, out, col, id, u, w, entropy, false, [&](float z) { return z - a.m - log_s; });
-        out.store_first(d + col, left);
+    for (int64_t col = threadIdx.x * 8; col < p.vocabulary; col += kAhead * kTurn) {
+        Eight<T> some[kAhead];
+#pragma unroll
+        for (int k = 0; k < kAhead; k++) some[k].load_first(z + col + k * kTurn, p.vocabulary - col - k * kTurn);
+#pragma unroll
+        for (int k = 0; k < kAhead; k++) {
+            logit_gradients(some[k], out, col + k * kTurn, id, u, w, entropy, false, [&](float z) { return z - a.m - log_s; });
+            out.store_first(d + col + k * kTurn, p.vocabulary - col - k * kTurn);
+        }
     }
 }
 
@@ -491,7 +502,9 @@ int hbp_token_logprobs_backward(int type, const void *logits, int64_t ldz, int64
             p.lse = lse + at; p.entropy = entropy ? entropy + at : nullptr;
             p.g_logp = g_logp ? g_logp + at : nullptr; p.g_entropy = g_entropy ? g_entropy + at : nullptr;
             p.d_logits = static_cast<T *>(d_logits) + at * ldd;
-            k_logprobs_backward<T><<<dim3((unsigned)((vocabulary + 2047) / 2048), (unsigned)rows), 256, 0, (hipStream_t)stream>>>(p);
+            auto go = [&](auto kernel, int threads) { kernel<<<dim3((unsigned)((vocabulary + threads * 8 - 1) / (threads * 8)), (unsigned)rows), threads, 0, (hipStream_t)stream>>>(p); };
+            if (rows < 256) go(k_logprobs_backward<T, 1024>, 1024);  // (so that a row that is one workgroup's is not a quarter of a compute unit's)
+            else go(k_logprobs_backward<T, 256>, 256);
             HBP_HIP(hipGetLastError());
         }
         return HBP_OK;
