@@ -370,3 +370,23 @@ def test_gradient_of_logits_far_from_zero(name, v):
                 assert (only.double().sum(1).abs().cpu() <= 2.0 ** -24 * (8 * (np.log(v) + 4) + 16 + 4) * u.abs().double()).all()
             H.hbp_token_logprobs_backward(zg, tokens.cuda(), out["lse"], out["entropy"], u.cuda(), w.cuda(), zg)      # in place
             assert torch.equal(zg, d)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("name", TYPES)
+def test_rows_far_from_zero_among_others(name):
+    """Every third row around 10000, more rows than those that workgroups of another size take: gradients as of each row alone, in place, too."""
+    import torch
+    for n, v in ((400, 3000), (257, 20011)):
+        print(f"[logprobs far] {n} x {v} {name} among others", flush=True)
+        z = logits_of(n, v, "f32", n)
+        z[::3] += 1e4
+        z = z.to(dtype(name))
+        tokens = torch.from_numpy(np.random.default_rng(n).integers(0, v, n))
+        out = run(z.cuda(), tokens.cuda())
+        u, w = (torch.randn(n, generator=torch.Generator().manual_seed(i)) for i in (1, 2))
+        d, zg = torch.empty_like(z, device="cuda"), z.cuda()
+        H.hbp_token_logprobs_backward(zg, tokens.cuda(), out["lse"], out["entropy"], u.cuda(), w.cuda(), d)
+        check_gradient(d, z.double().numpy(), tokens.numpy(), u.numpy(), w.numpy(), name, np.log(v) + 4)
+        H.hbp_token_logprobs_backward(zg, tokens.cuda(), out["lse"], out["entropy"], u.cuda(), w.cuda(), zg)
+        assert torch.equal(zg, d)

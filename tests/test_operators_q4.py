@@ -487,3 +487,21 @@ def test_workspace_for_many_vectors_is_that_of_a_launch():
     for n, vectors in zip(need, (1 << 20, 1 << 24)):
         assert H.lib().hbp_q4_mv_t_workspace(H.hbp_q4_matrix_t(4096, 4096, None, 64, 4096, 32, 0), vectors, n) == 0
     assert need[0].value == need[1].value < 4 << 30
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("name", ["f16", "bf16"])
+@pytest.mark.parametrize("zeros", [False, True])
+def test_products_of_16_bit_vectors_that_are_not_centred(name, zeros):
+    """Codes on their way as 16 + q, against a sixteenth of what rounding x to 16 bits is worth: that much of the root of the terms' squares, beside the result's own rounding."""
+    import torch
+    for rows, cols, group, vectors in ((300, 4096, 128, 1), (300, 4096, 32, 4), (300, 4096, 512, 16), (8300, 2048, 64, 40), (66_000, 1000, 128, 2)):
+        for kind, of in X_OF_ONE_SIGN.items():
+            print(f"[q4 not centred] mv {rows} x {cols} group {group} zeros {zeros} {kind} {vectors} of {name}", flush=True)
+            c, s, z, w = codes_around_their_zeros(rows, cols, group, "f32", zeros, group)
+            x = of(torch.randn(vectors, cols, generator=torch.Generator(device="cuda").manual_seed(vectors), device="cuda")).to(dtype(name))
+            y = torch.empty(vectors, rows, dtype=x.dtype, device="cuda")
+            H.hbp_q4_mv(c, s, x, y, group=group, zeros=z)
+            xd, wt = x.double(), w.t().contiguous()
+            want, terms = torch.mm(xd, wt), torch.mm(xd.square(), wt.square()).sqrt()
+            assert ((y.double() - want).abs() <= UNIT[name] * (want.abs() * (1 + 1e-6) + terms / 16)).all()
