@@ -349,7 +349,8 @@ int hbp_q4_pack(const hbp_q4_matrix_t *a, int type, const void *w, int64_t ldw, 
 int hbp_q4_unpack(const hbp_q4_matrix_t *a, int type, void *w, int64_t ldw, void *stream);
 
 /* Products with `vectors` vectors at once (rows of x and y: x [vectors][n_cols], y [vectors][n_rows], both of `type`; x and y must not
- * overlap): y[m][r] = sum over k of W[r][k] x[m][k].  The weights are read once for 64 vectors (fp32: 21).  vectors at most 2^24; 0 does nothing. */
+ * overlap): y[m][r] = sum over k of W[r][k] x[m][k].  The weights are read once for 64 vectors (fp32: 21); for some
+ * 200 bf16 vectors and more, and in the transposed product for some 30 and more, hbp_q4_unpack and a library's dense product take less time.  vectors at most 2^24; 0 does nothing. */
 int hbp_q4_mv(const hbp_q4_matrix_t *a, int type, const void *x, int64_t ldx, void *y, int64_t ldy, int64_t vectors, void *stream);
 /* The transposed product, which is the gradient of hbp_q4_mv for its x: y[m][k] = sum over r of W[r][k] x[m][r], x [vectors][n_rows],
  * y [vectors][n_cols]. */
@@ -363,7 +364,8 @@ int hbp_q4_mv_t_workspace(const hbp_q4_matrix_t *a, int64_t vectors, size_t *byt
  *   x_out = h_out * r2 * w_pre, r2 = (mean h_out^2 + eps)^-1/2    the norm before the next block (h_out before it is rounded)
  * h, y, h_out, x_out and gate of `type`; h_out may be h, x_out may be y.  w_post, w_pre [width] of `type`, or NULL for ones.
  * gate by gate_kind: NONE (1; gate NULL), CHANNEL [width], TOKEN [tokens], FULL [tokens][width] with row stride ldg.
- * rstd DEVICE float [tokens][2] = r1, r2, or NULL (the backward call needs it).  width at most 16384, eps > 0.  tokens = 0 does nothing. */
+ * rstd DEVICE float [tokens][2] = r1, r2, or NULL (the backward call needs it).  width at most 16384, eps > 0.  A row whose sum of squares is no fp32
+ * number (above 3.4e38) is one of infinite length: r = 0.  tokens = 0 does nothing. */
 typedef enum { HBP_GATE_NONE = 0, HBP_GATE_CHANNEL = 1, HBP_GATE_TOKEN = 2, HBP_GATE_FULL = 3 } hbp_gate_kind;
 typedef struct {
     int64_t tokens, width;
@@ -389,7 +391,7 @@ int hbp_residual_norms_backward_workspace(const hbp_norms_t *n, size_t *bytes);
  *   top_ids int32, top_logp float, DEVICE [tokens][top], top = 0..64 and at most vocabulary; top_ids and top_logp may not be NULL where
  *          top > 0: the largest logits in descending order, among equal ones the lowest index first (NaN counts as larger than
  *          any number, -0 equals 0)
- * A logit of -inf is a masked token: p = 0, logp -inf, no part in the entropy, no gradient.  A row with nothing else: lse = -inf, every logp
+ * A logit of -inf is a masked token: p = 0, logp -inf, no part in the entropy, no gradient (but g_logp where it is the row's own token).  A row with nothing else: lse = -inf, every logp
  * -inf, entropy 0, gradient 0.  A row with a NaN or +inf: lse, logp and entropy NaN.  vocabulary at most 2^30.  tokens = 0 does nothing. */
 int hbp_token_logprobs(int type, const void *logits, int64_t ldz, int64_t tokens, int64_t vocabulary, const void *ids, int id_bytes, float *logp,
                        float *entropy, float *lse, int top, int32_t *top_ids, float *top_logp, void *workspace, size_t workspace_bytes, void *stream);

@@ -104,12 +104,12 @@ template <typename T, typename S> __global__ __launch_bounds__(256) void k_q4_un
 }
 
 // y = x W, the transposed product.  A lane takes C neighbouring columns (of one group) and adds (code - zero) * (scale x) row by row, in fp32, for up to M vectors
-// (zero (scale x) as a sum of its own, taken off at the end, would be one fma for all C, and leave errors of its own size in a result that is much smaller where x is of one sign).  A workgroup has 64 C columns of a part of the rows, its wavefronts every eighth batch of ROWS rows; they
-// are added up by LDS, the parts by a second kernel.
+// (zero (scale x) as a sum of its own, taken off at the end, would be one fma for all C, and leave errors of its own size in a result that is much smaller where x is of
+// one sign).  A workgroup has 64 C columns of a part of the rows, its wavefronts every eighth batch of ROWS rows; they are added up by LDS, the parts by a second kernel.
 //
-// Bound: vector instructions, 1.4 + M a weight (a conversion for each code and an fma for each vector), and their latency; us: 1 x 8192 x 8192 fp32 14 + 4 for the
-// sum, 19 x 6001 x 4099 with zero points 31 + 4.5, 64 x 8192 x 8192 173 (50 TFLOP/s of the 79 that fp32 fma has here).  Not by the matrix cores: there the scale, which
-// differs from row to row, would have to go into x, in parts, for every group anew.
+// Bound: vector instructions, 1.4 + M a weight (a conversion for each code, with zero points a subtraction more, and an fma for each vector), and their latency; us: 1 x 8192 x 8192 fp32 14 + 4 for the
+// sum, 19 x 6001 x 4099 with zero points 30 + 4.5, 64 x 8192 x 8192 170 (51 TFLOP/s of the 79 that fp32 fma has here).  For the matrix cores the scale, which
+// differs from row to row, would have to go into x, in two or three parts, once for each group of columns: not tried.
 // As in the products, (code - zero) * (scale x) may be infinite where the sum is not: such results are computed again from the definition.
 constexpr int kTransposedWaves = 8, kTransposedRows = 512;  // rows whose x lies in LDS at a time
 // What a lane loads of ROWS rows.
@@ -300,8 +300,9 @@ TransposedShape transposed_shape(const Q4 &a, int64_t vectors)
     s.c = s.m <= 2 ? 16 : 8;
     s.rows = s.m <= 2 ? 8 : 4;
     s.wide = (a.n_cols + kWave * s.c - 1) / (kWave * s.c);
-    // Parts: a workgroup for each place on the chip (256 compute units hold one of more than six vectors, 157 registers, or two), or for several rounds of them; as many as
-    // leave the fewest places empty in the last round.  19 x 6001 x 4099 in 432 workgroups 43.8 us, in 252 35.4; 8 x 8192 x 8192 in 512 38.8, in 256 31.5.
+    // Parts: a workgroup for each place on the chip (one of more than six vectors a compute unit, or two), or for several rounds of them; as many as
+    // leave the fewest places empty in the last round.  19 x 6001 x 4099 in 432 workgroups 43.8 us, in 252 35.4.  (Ten vectors take 138 registers and more, of which one workgroup fits; eight without
+    // zero points take 120, and two would fit, which is slower for one pass, 8 x 30000 x 2048 34.6 for 32.3, and faster for several, 64 x 8192 x 8192 142 for 170.)
     const int64_t passes = std::max<int64_t>((vectors + s.m - 1) / s.m, 1), least = 2 * s.rows * kTransposedWaves;
     const int64_t most = (a.n_rows + least - 1) / least, places = s.m > 6 ? 256 : 512, each = s.wide * passes;
     const int64_t first = std::max<int64_t>(places / each, 1);

@@ -417,7 +417,7 @@ __device__ __forceinline__ void add_up_and_write(const Q4Product &p, const float
 // A workgroup of row_waves * column_waves wavefronts takes row_waves * RT * 16 rows.  In a step each column_wave takes U chunks of 128 columns; x of
 // the step lies in LDS, that of the next one, and its codes and scales, are on their way into registers meanwhile.  The column_waves are added up at the end.
 // GM: pieces of 32 columns that share a scale (4: 128 columns and more).  SETS: slots / 16, NR: slots of a set / 4, each rounded up (NR to 1 or 4).
-// Bound: latency.  One vector: a chain of load, barrier, sum; 4096 x 4096 bf16 5 to 6 us.  Many: 204 to 256 registers leave one workgroup a compute unit; 48 x 131072 x 4096 fp16 146
+// Bound: latency.  One vector: a chain of load, barrier, sum; 4096 x 4096 bf16 4 to 6 us.  Many: 204 to 256 registers leave one workgroup a compute unit; 48 x 131072 x 4096 fp16 139 to 146
 // us (298 MB, 350 TFLOP/s; vector unit 45 %, matrix cores 20 % busy).  Held to 128 registers it spills (173).
 constexpr int kMostSlots = 64;
 constexpr int kStageBytes = 140 * 1024;  // of LDS, at most
@@ -474,7 +474,7 @@ __global__ __launch_bounds__(kThreads) void k_q4_mv(Q4Product p, int32_t per_pas
 }
 
 // Many rows and few slots: x stays in LDS as a whole, and each wavefront walks through tiles of RT times 16 rows by itself, all columns of a tile after one
-// another, the next U chunks always on their way: no barrier, and nothing to add up but the parts of an fp32 x.  Bound: HBM; 131072 x 4096 bf16, groups of 64, 58.6 us, 4.9 TB/s
+// another, the next U chunks always on their way: no barrier, and nothing to add up but the parts of an fp32 x.  Bound: HBM; 131072 x 4096 bf16, groups of 64, 57.4 us, 4.9 TB/s
 // of 6 that such tiles can be read at (some 60 vector instructions for 16 rows x 128 columns, 28 % of the unit).
 template <typename T, typename S, bool ZERO, int GM, int NR, int RT, int U>
 __global__ __launch_bounds__(kThreads) void k_q4_mv_rows(Q4Product p)
@@ -553,13 +553,14 @@ __global__ __launch_bounds__(kThreads) void k_q4_mv_rows(Q4Product p)
     }
 }
 
-// Which kernel, and its shape.  Measured, us, the shapes in the order RT, U, wavefronts, row_waves (rows: k_q4_mv_rows):
-//   1 to 4 slots: where each wavefront of two workgroups a compute unit has tiles to walk through, rows; 131072 x 4096 58.6 (1 4 4 4: 64.5).  Else few
-//     row_waves, so that a column_wave's way is short: 4096 x 4096 1 4 8 1 6.1, with two row_waves 8.6; 14336 x 4096 (4 vectors) 1 2 8 2 13.1, 1 4 8 2 16.6; fp32 8192 x 28672 1 4 8 2 39, 1 2 8 2 44.  Short rows
-//     leave eight wavefronts nothing to do: 1000 x 1000 1 2 4 1 4.2, 1 2 8 1 5.0.
-//   5 to 16: 16 x 4096 x 4096 1 1 8 1 8.9, 1 2 8 2 10.2; fp32 5 x 10007 x 7001 1 2 8 4 24.3, 2 2 8 2 24.4, 1 1 4 1 25.2; 12 x 40000 x 4096 1 2 4 4 31, 1 2 8 4 40.
-//   more: as many column_waves as x of a step fits the threads' registers with, and with many rows none; 24 x 8192 x 8192 1 1 8 2 24.8, 2 1 8 2 32.7;
-//     64 x 4096 x 4096 1 1 8 4 31.5, 1 1 8 8 47.8; 48 x 131072 x 4096 2 1 8 8 143, 1 1 8 8 180; 64 x 32768 x 8192 1 1 8 8 103, 2 1 8 8 208 (registers).
+// Which kernel, and its shape.  Measured, us (bf16, groups of 128, where nothing else is said), the shapes in the order RT, U, wavefronts, row_waves (rows: k_q4_mv_rows):
+//   1 to 4 slots: where each wavefront of two workgroups a compute unit has tiles to walk through, rows; 131072 x 4096 53.5 (1 4 4 4: 55.4; groups of 64: 57.4 and 57.3).  Else few
+//     row_waves, so that a column_wave's way is short: 4096 x 4096 1 4 8 1 5.5, with two row_waves 6.9.  Four chunks where that is all there are, or in several steps: fp32 8192 x 28672 1 4 8 2 35, 1 2 8 2 39.
+//     Else two: groups of 64, 10000 x 7000 1 2 8 2 17.0, 1 4 8 2 20.3, 4000 x 5000 1 2 8 1 6.3, 1 4 8 1 7.6 (not best where steps of four come out even: 14336 x 4096 1 2 8 2 15.3, 1 4 8 2 13.3).  Short rows
+//     leave eight wavefronts nothing to do: 1000 x 1000 1 2 4 1 3.3, 1 2 8 1 3.7.
+//   5 to 16: 16 x 4096 x 4096 1 1 8 1 8.0, 1 2 8 2 9.1; fp32 5 x 10007 x 7001, groups of 32, 1 2 8 4 25.8, 1 2 8 2 30.4, 1 1 8 4 30.8 (with zero points 32.1, 37.3, 39.0); 12 x 40000 x 4096 1 2 4 4 31, 1 2 8 4 40.
+//   more: as many column_waves as x of a step fits the threads' registers with, and with many rows none; 24 x 8192 x 8192 1 1 8 2 23.2, 2 1 8 2 30.8;
+//     64 x 4096 x 4096 1 1 8 4 28.8, 1 1 8 8 44.6; 48 x 131072 x 4096, groups of 64, 2 1 8 8 138, 1 1 8 8 169; 64 x 32768 x 8192 1 1 8 8 90, 2 1 8 8 about twice that (registers).
 //     Two tiles of three sets, four groups a chunk and zero points do not fit the registers (38 to 90 spilled): one; 48 x 20000 x 4096 bf16 47, two 105; 48 x 131072 x 4096 199, two 273.
 template <typename T, typename S, bool ZERO, int GM> int launch_mv(const Q4Product &p, hipStream_t st)
 {
