@@ -7,6 +7,7 @@ import subprocess
 import pytest
 
 import paper_2504_08860_amd as H
+from paper_2504_08860_amd.build import build_library
 
 READELF, OBJDUMP = (next((p for p in (f"/opt/rocm/llvm/bin/{n}", shutil.which(n) or "") if os.path.exists(p)), None) for n in ("llvm-readelf", "llvm-objdump"))
 MOST = 128   # bytes; kernels that have a few values too many for their registers are not split for them
@@ -16,6 +17,8 @@ MOST = 128   # bytes; kernels that have a few values too many for their register
 @pytest.mark.parametrize("kernels", ["norm", "logprobs", "q4"])
 def test_scratch_memory(kernels, tmp_path):
     library = tmp_path / "lib.so"
+    if not os.path.exists(H.LIB_PATH):
+        build_library()
     shutil.copy(H.LIB_PATH, library)
     subprocess.run([OBJDUMP, "--offloading", str(library)], cwd=tmp_path, check=True, capture_output=True)
     scratch = {}

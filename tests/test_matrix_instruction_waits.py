@@ -11,6 +11,7 @@ import subprocess
 import pytest
 
 import paper_2504_08860_amd as H
+from paper_2504_08860_amd.build import build_library
 
 OBJDUMP = next((p for p in ("/opt/rocm/llvm/bin/llvm-objdump", shutil.which("llvm-objdump") or "") if os.path.exists(p)), None)
 STATES = 8
@@ -80,6 +81,8 @@ def too_early(code):
 @pytest.mark.skipif(OBJDUMP is None, reason="no llvm-objdump")
 def test_nothing_touches_the_results_of_a_matrix_instruction_too_early(tmp_path):
     library = tmp_path / "lib.so"
+    if not os.path.exists(H.LIB_PATH):
+        build_library()
     shutil.copy(H.LIB_PATH, library)
     subprocess.run([OBJDUMP, "--offloading", str(library)], cwd=tmp_path, check=True, capture_output=True)
     found, count = [], 0
