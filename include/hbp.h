@@ -404,6 +404,65 @@ int hbp_token_logprobs_backward(int type, const void *logits, int64_t ldz, int64
                                 const float *lse, const float *entropy, const float *g_logp, const float *g_entropy, void *d_logits, int64_t ldd,
                                 void *stream);
 
+/* A paged cache of keys and values, and the sequences of a batch whose new tokens are appended to it and attend over it.
+ *   keys, values  DEVICE, 16-byte aligned, of `type`: pages of [kv_heads][page_size][head_dim] each, `ldk` and `ldv` values from one page to
+ *          the next (multiples of 8, at least kv_heads * page_size * head_dim), so that both may lie in one array
+ *   table  DEVICE int32 [sequences][table_width], rows ldt apart: the page that holds a sequence's positions i * page_size onwards is
+ *          table[s][i].  A number that is no page (below 0 or from `pages` on) is a page that is not held: nothing is written there, and no query sees
+ *          those positions.  A page may be in several sequences' rows (a shared prefix), for reading; where two rows write to one slot, either one's value is there.
+ *   starts DEVICE int32 [sequences + 1], ascending: the new tokens of sequence s are rows starts[s] .. starts[s + 1] - 1 of every array of
+ *          [tokens] rows; none, or many.  Rows of no sequence are not touched.
+ *   lengths DEVICE int32 [sequences]: positions of sequence s with its new tokens, which are the last ones: row starts[s + 1] - 1 has position
+ *          lengths[s] - 1.  Positions below 0 or from table_width * page_size on are not in the cache.
+ * Read when the kernels run, so a captured graph takes the values that these arrays hold at each replay.
+ * head_dim 8..256, a multiple of 8; page_size 1..65536; pages * page_size below 2^31. */
+typedef struct {
+    void *keys, *values;
+    const int32_t *table, *starts, *lengths;
+    int64_t ldk, ldv, ldt, pages, sequences, table_width;
+    int32_t type, kv_heads, page_size, head_dim;
+} hbp_paged_t;
+
+/* Puts the keys k and the values v [tokens][kv_heads][head_dim] of new tokens into the cache, and rotates keys and queries by their positions on the
+ * way: with the angle a = position * frequencies[i], of the first 2 * pairs values of each head the pair (x, y) of values i and i + pairs
+ * (interleaved: 2 i and 2 i + 1) becomes (x cos a - y sin a, y cos a + x sin a); the others stay.  Angles are held in 64 bits.
+ *   k, v   row strides ldk, ldv (of tokens; the heads of a token lie together), `type` of the cache
+ *   q, q_out  [tokens][heads][head_dim], row strides ldq, ldqo: queries, and where the rotated ones go (may be q); both NULL with heads = 0: none
+ *   frequencies  DEVICE float [pairs], 0 <= pairs <= head_dim / 2; pairs = 0: no rotation
+ * tokens at most 2^30; 0 does nothing. */
+int hbp_paged_append(const hbp_paged_t *cache /* HOST */, int64_t tokens, const void *k, int64_t ldk, const void *v, int64_t ldv, const void *q,
+                     int64_t ldq, int heads, void *q_out, int64_t ldqo, const float *frequencies, int pairs, int interleaved, void *stream);
+
+/* Attention of new tokens over the cache that already holds their own keys and values: for the query of row r and head h, at position p,
+ *   out[r][h] = sum over j of w_j value_j, w = softmax over j of cap(scale q . key_j), j <= p and, with a window > 0, j > p - window,
+ * over the positions that the cache holds, keys and values of head h / (heads / kv_heads); cap(s) = softcap tanh(s / softcap), or s where softcap is 0.  A query that
+ * sees no position, or none with a score above -inf, gives 0.  What lies in slots that a query does not see has no part in its result, whatever it is.
+ *   q, out [tokens][heads][head_dim], row strides ldq, ldo, `type` of the cache; out may be q.  heads a multiple of kv_heads.
+ *   most_new  no sequence has more new tokens than this (rows of one behind it are not computed); 1 for decoding
+ * Scores, the softmax and sums are fp32; the weights of a row, at most some 2^8 times its largest one, are rounded to 16-bit `type`s for their product with the
+ * values.  fp32 products are sums of products of bf16 parts, 2^-22 relative.  tokens * (heads / kv_heads) below 2^31; tokens = 0 does nothing. */
+int hbp_paged_attention(const hbp_paged_t *cache /* HOST */, int64_t tokens, const void *q, int64_t ldq, int heads, void *out, int64_t ldo,
+                        float scale, float softcap, int window, int64_t most_new, void *workspace, size_t workspace_bytes, void *stream);
+int hbp_paged_attention_workspace(const hbp_paged_t *cache, int64_t tokens, int heads, int window, int64_t most_new, size_t *bytes /* HOST */);
+
+/* Which drafted tokens stand, and the token behind them.  Sequence s has rows starts[s] .. starts[s + 1] - 1 of logits [rows][vocabulary] (`type`, row stride
+ * ldz), one for each token that the model was given: the last token that stands, then the drafted ones.  Row r says what follows token r, so draft
+ * d = ids[r + 1] of row r, for all rows of s but the last, is taken in order:
+ *   p = softmax(logits[r] / temperature[s]) (temperature 0: 1 at the largest logit, the lowest index among equal ones)
+ *   d stands if uniforms[r] * q(d) < p(d), q = draft_probs[r], the probabilities that d was drawn from; NULL: q is 1 at d and 0 elsewhere
+ * and behind the first one that does not, or the last one, a new token is drawn: the first v for which sum over j <= v of w_j exceeds
+ * u * (sum of w), u = uniforms of the sequence's last row; w = max(p - q, 0) where a draft did not stand (p, where that is 0 everywhere), w = p of the last row where all do.
+ *   new_ids DEVICE int32 [rows]: the drafts that stand, the new token, then -1; accepted DEVICE int32 [sequences]: how many stand
+ *   starts DEVICE int32 [sequences + 1]; ids DEVICE int32 or int64 (id_bytes 4 or 8) [rows]; uniforms DEVICE float [rows], in [0, 1)
+ *   temperature DEVICE float [sequences], >= 0, or NULL for 1;  draft_probs DEVICE float [rows][vocabulary], row stride ldp; a sequence's last row is not read
+ * p, w and all sums are held in 64 bits.  A logit of -inf is a masked token.  A row with nothing else, with a NaN or with +inf has no p: its draft does not stand and the
+ * new token is -1, as with a temperature below 0 or NaN.  A draft that is no token (below 0, or `vocabulary` or more) does not stand.  A sequence without rows: accepted 0.  Rows of no
+ * sequence are not touched.  vocabulary and rows at most 2^30.  rows = 0 sets accepted to 0. */
+int hbp_verify_drafts(int type, const void *logits, int64_t ldz, int64_t rows, int64_t vocabulary, const void *ids, int id_bytes, const float *uniforms,
+                      const int32_t *starts, int64_t sequences, const float *temperature, const float *draft_probs, int64_t ldp, int32_t *new_ids,
+                      int32_t *accepted, void *workspace, size_t workspace_bytes, void *stream);
+int hbp_verify_drafts_workspace(int64_t rows, int64_t vocabulary, int64_t sequences, size_t *bytes /* HOST */);
+
 const char *hbp_status_string(int status);
 /* hipError_t of the most recent HBP_ERR_HIP on this thread, as int. */
 int hbp_last_hip_error(void);

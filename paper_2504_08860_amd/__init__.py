@@ -46,6 +46,7 @@ EXPORTED_SYMBOLS = (
     # operators beside the sparse products (operators.py)
     "hbp_q4_pack", "hbp_q4_unpack", "hbp_q4_mv", "hbp_q4_mv_t", "hbp_q4_mv_t_workspace", "hbp_residual_norms", "hbp_residual_norms_backward",
     "hbp_residual_norms_backward_workspace", "hbp_token_logprobs", "hbp_token_logprobs_workspace", "hbp_token_logprobs_backward",
+    "hbp_paged_append", "hbp_paged_attention", "hbp_paged_attention_workspace", "hbp_verify_drafts", "hbp_verify_drafts_workspace",
 )
 
 
@@ -309,5 +310,6 @@ def hbp_release_workspace() -> None:
 
 
 from . import operators  # noqa: E402  (which reaches back into this module)
-from .operators import (hbp_norms_t, hbp_q4_matrix_t, hbp_q4_mv, hbp_q4_mv_t, hbp_q4_pack, hbp_q4_shapes, hbp_q4_unpack,  # noqa: E402,F401
-                        hbp_residual_norms, hbp_residual_norms_backward, hbp_token_logprobs, hbp_token_logprobs_backward)
+from .operators import (hbp_norms_t, hbp_paged_append, hbp_paged_attention, hbp_paged_t, hbp_q4_matrix_t, hbp_q4_mv, hbp_q4_mv_t,  # noqa: E402,F401
+                        hbp_q4_pack, hbp_q4_shapes, hbp_q4_unpack, hbp_residual_norms, hbp_residual_norms_backward, hbp_token_logprobs,
+                        hbp_token_logprobs_backward, hbp_verify_drafts)

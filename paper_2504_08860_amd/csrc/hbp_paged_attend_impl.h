@@ -1,0 +1,522 @@
+// Attention of new tokens over a paged cache, on the matrix cores (hbp_paged_attention).
+//
+// Scores are taken as S^T = K Q^T and results as O^T = V^T P^T, so that a lane of a wavefront has one query in both (lane % 16), with its softmax statistics: S^T comes out
+// as four positions a lane, and with the positions of a step of 32 dealt to the instruction's rows as they are here (row r of half a is position 8 (r / 4) + 4 a + r % 4) the eight weights that a
+// lane makes of them are what the second product takes from it, without a word being exchanged.  V is wanted column by column: a lane loads eight positions of D / 16 columns that lie
+// together and turns them in its registers.
+//
+// fp32 is taken as three bf16 parts of 8 bits each, exactly, and a product as the six products of parts that matter (2^-22 of it is left out).
+#pragma once
+
+#include <algorithm>
+
+#include "hbp_paged_attend.h"
+
+namespace hbp {
+namespace {
+
+typedef float float4_t __attribute__((ext_vector_type(4)));
+typedef uint32_t uint4_t __attribute__((ext_vector_type(4)));
+typedef uint16_t ushort2_t __attribute__((ext_vector_type(2)));
+template <typename T, int N> using vec_t = T __attribute__((ext_vector_type(N)));
+
+constexpr float kLowest = -3.4028234663852886e38f;
+
+__device__ __forceinline__ uint32_t low_halves(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x05040100u); }    // a's, then b's
+__device__ __forceinline__ uint32_t high_halves(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x07060302u); }
+
+// Eight values of a lane as an operand of the matrix instruction.
+template <typename T> struct Operand {
+    uint4_t w;
+    static __device__ __forceinline__ Operand of(const uint32_t (&bits)[4]) { return Operand{uint4_t{bits[0], bits[1], bits[2], bits[3]}}; }
+    static __device__ __forceinline__ Operand of(const float (&v)[8])   // rounded
+    {
+        vec_t<T, 8> r;
+#pragma unroll
+        for (int i = 0; i < 8; i++) r[i] = from_f32<T>(v[i]);
+        return Operand{__builtin_bit_cast(uint4_t, r)};
+    }
+};
+template <> struct Operand<float> {
+    uint4_t w[3];
+    static __device__ __forceinline__ Operand of(const float (&v)[8])
+    {
+        Operand r;
+        float rest[8];
+#pragma unroll
+        for (int i = 0; i < 8; i++) rest[i] = v[i];
+#pragma unroll
+        for (int part = 0; part < 3; part++) {
+#pragma unroll
+            for (int i = 0; i < 4; i++) r.w[part][i] = high_halves(__float_as_uint(rest[2 * i]), __float_as_uint(rest[2 * i + 1]));
+            if (part < 2)
+#pragma unroll
+                for (int i = 0; i < 8; i++) rest[i] -= __uint_as_float(__float_as_uint(rest[i]) & 0xffff0000u);
+        }
+        return r;
+    }
+    static __device__ __forceinline__ Operand of(const uint32_t (&bits)[8])
+    {
+        float v[8];
+#pragma unroll
+        for (int i = 0; i < 8; i++) v[i] = __uint_as_float(bits[i]);
+        return of(v);
+    }
+};
+__device__ __forceinline__ float4_t multiply_bf16(uint4_t a, uint4_t b, float4_t c)
+{
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(vec_t<bf16, 8>, a), __builtin_bit_cast(vec_t<bf16, 8>, b), c, 0, 0, 0);
+}
+__device__ __forceinline__ float4_t multiply(const Operand<bf16> &a, const Operand<bf16> &b, float4_t c) { return multiply_bf16(a.w, b.w, c); }
+__device__ __forceinline__ float4_t multiply(const Operand<f16> &a, const Operand<f16> &b, float4_t c)
+{
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(vec_t<f16, 8>, a.w), __builtin_bit_cast(vec_t<f16, 8>, b.w), c, 0, 0, 0);
+}
+__device__ __forceinline__ float4_t multiply(const Operand<float> &a, const Operand<float> &b, float4_t c)
+{
+    c = multiply_bf16(a.w[1], b.w[1], c);
+    c = multiply_bf16(a.w[0], b.w[2], c);
+    c = multiply_bf16(a.w[2], b.w[0], c);
+    c = multiply_bf16(a.w[0], b.w[1], c);
+    c = multiply_bf16(a.w[1], b.w[0], c);
+    return multiply_bf16(a.w[0], b.w[0], c);
+}
+
+// over the four lanes that have the same query
+template <typename F> __device__ __forceinline__ float over_quarters(float v, F op)
+{
+    uint32_t w = __float_as_uint(v);
+    auto a = __builtin_amdgcn_permlane16_swap(w, w, false, false);
+    v = op(__uint_as_float(a[0]), __uint_as_float(a[1]));
+    w = __float_as_uint(v);
+    auto b = __builtin_amdgcn_permlane32_swap(w, w, false, false);
+    return op(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+
+// Exponents of 2 of scores.  tanh x = 1 - 2 / (e^2x + 1), off by some 2^-24 of 1 where x is small, which is 2^-24 of the cap in the exponent.
+__device__ __forceinline__ float exponent_of(const Attend &a, float score)
+{
+    if (a.cap_out == 0.0f) return score * a.per;
+    const float e = __builtin_amdgcn_exp2f(score * a.cap_in);   // (cap_in has 2 / log 2 in it)
+    return a.cap_out - 2.0f * a.cap_out * __builtin_amdgcn_rcpf(e + 1.0f);
+}
+
+// A position's slot: its page (-1: not held) and the place in it
+struct Slot {
+    int32_t page, within;
+};
+__device__ __forceinline__ Slot slot_of(const Paged &c, const int32_t *table, int32_t position)
+{
+    const int32_t which = c.by_page.divide(position);
+    const int32_t page = table[which];
+    return Slot{page >= 0 && page < c.pages ? page : -1, position - which * c.page_size};
+}
+template <typename T> __device__ __forceinline__ const T *row_of(const void *pages, int64_t ld, const Paged &c, int32_t kv_head, Slot s)
+{
+    return static_cast<const T *>(pages) + (int64_t)max(s.page, 0) * ld + (int64_t)(kv_head * c.page_size + s.within) * c.head_dim;
+}
+
+// N values (4 to 16, 8 or more bytes) of a row in the cache: rows are 16-byte aligned
+template <typename T, int N> struct Piece {
+    static constexpr int kWords = N * sizeof(T) / 4;
+    uint32_t w[kWords];
+    __device__ __forceinline__ void load(const T *p)
+    {
+        if constexpr (kWords == 2) {
+            const uint2 v = *reinterpret_cast<const uint2 *>(p);
+            w[0] = v.x; w[1] = v.y;
+        } else {
+#pragma unroll
+            for (int i = 0; i < kWords / 4; i++) {
+                const uint4 v = *reinterpret_cast<const uint4 *>(reinterpret_cast<const char *>(p) + 16 * i);
+                w[4 * i] = v.x; w[4 * i + 1] = v.y; w[4 * i + 2] = v.z; w[4 * i + 3] = v.w;
+            }
+        }
+    }
+};
+
+// Few rows: a workgroup of four wavefronts takes 16 NQ rows, and each wavefront every fourth step of their positions, straight from the cache into registers; the four
+// results are joined in LDS.  The next step's keys are on their way from the scores on, this one's values until the weights are there.
+template <typename T, int D, int NQ, bool ANY_PAGE> __global__ __launch_bounds__(256) void k_attend(Attend a, int64_t first_unit)
+{
+    constexpr int kSteps = D / 32, kTiles = D / 16;   // of 32 columns in Q K^T; of 16 in the result, which a lane holds D / 16 neighbouring columns of
+    constexpr int kPitch = D + 4;
+    __shared__ float joined[4][16][kPitch];
+    __shared__ float2 joined_stats[4][16];
+    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, column = lane % 16, quarter = lane / 16;
+    const int64_t number = first_unit + blockIdx.x;
+    const int32_t unit_number = (int32_t)(number / a.c.kv_heads), kv_head = (int32_t)(number - (int64_t)unit_number * a.c.kv_heads);
+    Unit x;
+    if (!find_unit<false>(a, unit_number, x)) return;
+    const int32_t begin = x.low + x.part * x.size, end = min(begin + x.size, x.high);
+    const int32_t *table = a.c.table + x.sequence * a.c.ldt;
+    const int32_t dim = a.c.head_dim;
+
+    Operand<T> q[NQ][kSteps];
+    int32_t low[NQ], count[NQ];   // the positions that the lane's query sees: low .. low + count - 1
+    int32_t all_low = 0, all_high = 0x7fffffff;
+#pragma unroll
+    for (int n = 0; n < NQ; n++) {
+        const int32_t row = x.tile * a.tile_rows + n * 16 + column;
+        const bool is_row = row < x.rows;
+        const int32_t token = a.by_group.divide(is_row ? row : 0), head = kv_head * a.group + (is_row ? row - token * a.group : 0);
+        const T *from = static_cast<const T *>(a.q) + (int64_t)(x.first_token + token) * a.ldq + (int64_t)head * dim;
+#pragma unroll
+        for (int k = 0; k < kSteps; k++) {
+            const int32_t at = 32 * k + 8 * quarter;
+            Eight<T> v;
+            v.clear();
+            if (is_row && at < dim) v.load(from + at);
+            if (a.negative)
+#pragma unroll
+                for (int i = 0; i < Eight<T>::kWords; i++) v.w[i] ^= sizeof(T) == 4 ? 0x80000000u : 0x80008000u;
+            q[n][k] = Operand<T>::of(v.w);
+        }
+        const int64_t position = x.first_position + token;
+        low[n] = (int32_t)max((int64_t)0, a.window ? position - a.window + 1 : 0);
+        const int32_t high = (int32_t)max((int64_t)0, min(position + 1, (int64_t)end));
+        count[n] = is_row ? max(0, high - low[n]) : 0;
+        if (is_row) {
+            all_low = max(all_low, low[n]);
+            all_high = min(all_high, high);
+        }
+    }
+    all_low = wave_reduce(all_low, [](int32_t p, int32_t q) { return max(p, q); });
+    all_high = wave_reduce(all_high, [](int32_t p, int32_t q) { return min(p, q); });
+    const int32_t least_low = x.low;   // (a multiple of kStep: positions from there to the window's are seen by no row, and their values have to go)
+    int32_t tile_low = 0x7fffffff;
+#pragma unroll
+    for (int n = 0; n < NQ; n++) tile_low = min(tile_low, count[n] ? low[n] : 0x7fffffff);
+    tile_low = max(least_low, wave_reduce(tile_low, [](int32_t p, int32_t q) { return min(p, q); }));
+
+    float m[NQ], l[NQ];
+    float4_t o[NQ][kTiles];
+#pragma unroll
+    for (int n = 0; n < NQ; n++) {
+        m[n] = kLowest;
+        l[n] = 0.0f;
+#pragma unroll
+        for (int j = 0; j < kTiles; j++) o[n][j] = float4_t{0, 0, 0, 0};
+    }
+
+    // what a lane loads of a step: as rows of K, positions 8 (column / 4) + column % 4 and 4 more; as columns of V, 8 quarter + 0..7
+    struct Places {
+        Slot k[ANY_PAGE ? 2 : 1], v[ANY_PAGE ? 8 : 1];
+    };
+    auto places = [&](int32_t step) {   // (of positions moved back before the end: what is read there has no weight)
+        Places r;
+        if constexpr (ANY_PAGE) {
+#pragma unroll
+            for (int h = 0; h < 2; h++) r.k[h] = slot_of(a.c, table, min(step + 8 * (column / 4) + 4 * h + column % 4, end - 1));
+#pragma unroll
+            for (int i = 0; i < 8; i++) r.v[i] = slot_of(a.c, table, min(step + 8 * quarter + i, end - 1));
+        } else {
+            const int32_t last = (end - 1) / 8 * 8;   // (eight positions from a multiple of 8 on are in one page)
+            r.k[0] = slot_of(a.c, table, min(step + 8 * (column / 4), last));
+            r.v[0] = slot_of(a.c, table, min(step + 8 * quarter, last));
+        }
+        return r;
+    };
+    Piece<T, 8> kf[2][kSteps];
+    auto load_keys = [&](const Places &p) {
+#pragma unroll
+        for (int h = 0; h < 2; h++) {
+            const T *from = ANY_PAGE ? row_of<T>(a.c.keys, a.c.ldk, a.c, kv_head, p.k[ANY_PAGE ? h : 0])
+                                     : row_of<T>(a.c.keys, a.c.ldk, a.c, kv_head, p.k[0]) + (4 * h + column % 4) * dim;
+#pragma unroll
+            for (int k = 0; k < kSteps; k++) {
+                const int32_t at = 32 * k + 8 * quarter;
+                kf[h][k].load(from + (at < dim ? at : 0));
+            }
+        }
+    };
+
+    if (begin < end) {
+        int32_t step = begin + wave * kStep;
+        Places now = places(step), next = places(step + 4 * kStep);
+        load_keys(now);
+        for (; step < end; step += 4 * kStep) {
+            // values
+            constexpr int kPieces = kTiles > 8 ? kTiles / 8 : 1, kEach = kTiles > 8 ? 8 : kTiles;
+            Piece<T, kEach> vf[8][kPieces];
+#pragma unroll
+            for (int i = 0; i < 8; i++) {
+                const T *from = ANY_PAGE ? row_of<T>(a.c.values, a.c.ldv, a.c, kv_head, now.v[ANY_PAGE ? i : 0])
+                                         : row_of<T>(a.c.values, a.c.ldv, a.c, kv_head, now.v[0]) + i * dim;
+#pragma unroll
+                for (int c = 0; c < kPieces; c++) {
+                    const int32_t at = kTiles * column + kEach * c;
+                    vf[i][c].load(from + (at < dim ? at : 0));
+                }
+            }
+            // scores
+            float4_t s[NQ][2];
+#pragma unroll
+            for (int n = 0; n < NQ; n++) s[n][0] = s[n][1] = float4_t{0, 0, 0, 0};
+#pragma unroll
+            for (int k = 0; k < kSteps; k++) {
+                const uint32_t there = 32 * k + 8 * quarter < dim ? 0xffffffffu : 0u;
+#pragma unroll
+                for (int h = 0; h < 2; h++) {
+#pragma unroll
+                    for (int i = 0; i < Piece<T, 8>::kWords; i++) kf[h][k].w[i] &= there;
+                    const Operand<T> key = Operand<T>::of(kf[h][k].w);
+#pragma unroll
+                    for (int n = 0; n < NQ; n++) s[n][h] = multiply(key, q[n][k], s[n][h]);
+                }
+            }
+            const Places mine = now;
+            now = next;
+            load_keys(now);
+            next = places(step + 8 * kStep);
+
+            uint32_t held = 0;   // bits of the lane's eight positions that the cache holds
+#pragma unroll
+            for (int i = 0; i < 8; i++) held |= mine.v[ANY_PAGE ? i : 0].page >= 0 ? 1u << i : 0u;
+            const bool whole = step >= all_low && step + kStep <= all_high && __ballot(held != 0xff) == 0;   // every row sees every position
+
+            Operand<T> weights[NQ];
+            float p[NQ][8];
+#pragma unroll
+            for (int n = 0; n < NQ; n++) {
+                float e[8];
+#pragma unroll
+                for (int i = 0; i < 8; i++) e[i] = s[n][i / 4][i % 4];
+                if constexpr (sizeof(T) == 4) {
+                    // Parts of an infinite value, and products of parts that overflow, make NaN of what may be a number or an infinity: from the definition
+                    bool odd = false;
+#pragma unroll
+                    for (int i = 0; i < 8; i++) odd |= !(fabsf(e[i]) < INFINITY);
+                    if (__ballot(odd) != 0 && count[n] > 0) {
+                        const int32_t row = x.tile * a.tile_rows + n * 16 + column, token = a.by_group.divide(row);
+                        const float *query = static_cast<const float *>(a.q) + (int64_t)(x.first_token + token) * a.ldq + (int64_t)(kv_head * a.group + row - token * a.group) * dim;
+                        for (int i = 0; i < 8; i++) {
+                            const int32_t position = min(step + 8 * quarter + i, end - 1);
+                            const float *key = row_of<float>(a.c.keys, a.c.ldk, a.c, kv_head, slot_of(a.c, table, position));
+                            float sum = 0.0f;
+                            for (int d = 0; d < dim; d++) sum += query[d] * key[d];
+                            sum = a.negative ? -sum : sum;
+#pragma unroll
+                            for (int j = 0; j < 8; j++)
+                                if (j == i && !(fabsf(e[j]) < INFINITY)) e[j] = sum;
+                        }
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < 8; i++) e[i] = exponent_of(a, e[i]);
+                if (!whole)
+#pragma unroll
+                    for (int i = 0; i < 8; i++) {
+                        const bool sees = (uint32_t)(step + 8 * quarter + i - low[n]) < (uint32_t)count[n] && (held >> i & 1);
+                        e[i] = sees ? e[i] : -INFINITY;
+                    }
+                float top = e[0];
+#pragma unroll
+                for (int i = 1; i < 8; i++) top = fmaxf(top, e[i]);
+                // The weights are taken relative to an earlier largest exponent while none is more than 8 above it: sums stay far from overflow, and nothing is exchanged.
+                if (__ballot(top > m[n] + 8.0f) != 0) {
+                    const float to = over_quarters(fmaxf(top, m[n]), [](float p, float q) { return fmaxf(p, q); });
+                    const float f = __builtin_amdgcn_exp2f(m[n] - to);
+                    m[n] = to;
+                    l[n] *= f;
+#pragma unroll
+                    for (int j = 0; j < kTiles; j++)
+#pragma unroll
+                        for (int i = 0; i < 4; i++) o[n][j][i] *= f;
+                }
+#pragma unroll
+                for (int i = 0; i < 8; i++) {
+                    p[n][i] = __builtin_amdgcn_exp2f(e[i] - m[n]);
+                    l[n] += p[n][i];
+                }
+                weights[n] = Operand<T>::of(p[n]);
+            }
+
+            // Values that no row sees must not be there at all, not even with a weight of 0, and infinities or NaN among others only for those rows that see them.
+            bool odd = false;
+            if (!whole || sizeof(T) == 4) {
+                uint32_t largest = 0;
+#pragma unroll
+                for (int i = 0; i < 8; i++) {
+                    const int32_t position = step + 8 * quarter + i;
+                    const uint32_t seen = position >= tile_low && position < end && (held >> i & 1) ? 0xffffffffu : 0u;
+#pragma unroll
+                    for (int c = 0; c < kPieces; c++)
+#pragma unroll
+                        for (int w = 0; w < Piece<T, kEach>::kWords; w++) {
+                            vf[i][c].w[w] &= seen;
+                            if constexpr (sizeof(T) == 4) {
+                                largest = max(largest, vf[i][c].w[w] & 0x7fffffffu);
+                            } else {
+                                const ushort2_t v = __builtin_bit_cast(ushort2_t, vf[i][c].w[w] & 0x7fff7fffu), u = __builtin_bit_cast(ushort2_t, largest);
+                                largest = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(v, u));
+                            }
+                        }
+                }
+                constexpr uint32_t kInfinite = sizeof(T) == 4 ? 0x7f800000u : std::is_same_v<T, f16> ? 0x7c00u : 0x7f80u;
+                odd = sizeof(T) == 4 ? largest >= kInfinite : (largest & 0xffffu) >= kInfinite || largest >> 16 >= kInfinite;
+            }
+            if (__ballot(odd) == 0) {
+#pragma unroll
+                for (int j = 0; j < kTiles; j++) {
+                    Operand<T> value;
+                    if constexpr (sizeof(T) == 4) {
+                        float v[8];
+#pragma unroll
+                        for (int i = 0; i < 8; i++) v[i] = __uint_as_float(vf[i][j / kEach].w[j % kEach]);
+                        value = Operand<T>::of(v);
+                    } else {
+                        uint32_t bits[4];
+#pragma unroll
+                        for (int i = 0; i < 4; i++) {
+                            const uint32_t one = vf[2 * i][j / kEach].w[j % kEach / 2], two = vf[2 * i + 1][j / kEach].w[j % kEach / 2];
+                            bits[i] = j & 1 ? high_halves(one, two) : low_halves(one, two);
+                        }
+                        value = Operand<T>::of(bits);
+                    }
+#pragma unroll
+                    for (int n = 0; n < NQ; n++) o[n][j] = multiply(value, weights[n], o[n][j]);
+                }
+            } else {
+                for (int u = 0; u < 4; u++)
+#pragma unroll
+                    for (int i = 0; i < 8; i++) {
+                        const int32_t position = step + 8 * u + i;
+                        if (position < tile_low || position >= end) continue;
+                        const Slot slot = slot_of(a.c, table, position);
+                        if (slot.page < 0) continue;
+                        const T *from = row_of<T>(a.c.values, a.c.ldv, a.c, kv_head, slot);
+#pragma unroll
+                        for (int n = 0; n < NQ; n++) {
+                            const float weight = __shfl(p[n][i], 16 * u + column);
+                            const bool sees = (uint32_t)(position - low[n]) < (uint32_t)count[n];
+#pragma unroll
+                            for (int j = 0; j < kTiles; j++)
+#pragma unroll
+                                for (int k = 0; k < 4; k++) {
+                                    const int32_t d = kTiles * (4 * quarter + k) + j;
+                                    if (sees && d < dim) o[n][j][k] += weight * to_f32(from[d]);
+                                }
+                        }
+                    }
+            }
+        }
+    }
+
+    // the four wavefronts' sums
+#pragma unroll
+    for (int n = 0; n < NQ; n++) {
+        l[n] = over_quarters(l[n], [](float p, float q) { return p + q; });
+        if (n) __syncthreads();
+#pragma unroll
+        for (int k = 0; k < 4; k++)
+#pragma unroll
+            for (int j = 0; j < kTiles; j++) joined[wave][column][kTiles * (4 * quarter + k) + j] = o[n][j][k];
+        if (quarter == 0) joined_stats[wave][column] = float2{m[n], l[n]};
+        __syncthreads();
+        constexpr int kChunks = D / 8;
+        for (int i = threadIdx.x; i < 16 * kChunks; i += 256) {
+            const int r = i / kChunks, at = i % kChunks * 8;
+            const int32_t row = x.tile * a.tile_rows + n * 16 + r;
+            if (row >= x.rows || at >= dim) continue;
+            float top = kLowest, sum = 0.0f, v[8] = {};
+#pragma unroll
+            for (int w = 0; w < 4; w++) top = fmaxf(top, joined_stats[w][r].x);
+#pragma unroll
+            for (int w = 0; w < 4; w++) {
+                const float2 stats = joined_stats[w][r];
+                const float f = __builtin_amdgcn_exp2f(stats.x - top);
+                sum += stats.y * f;
+#pragma unroll
+                for (int k = 0; k < 8; k++) v[k] += joined[w][r][at + k] * f;
+            }
+            if (x.parts == 1) {
+                const int32_t token = a.by_group.divide(row);
+                Eight<T> out;
+                const float inverse = sum == 0.0f ? 0.0f : 1.0f / sum;
+#pragma unroll
+                for (int k = 0; k < 8; k++) out.set(k, sum == 0.0f ? 0.0f : v[k] * inverse);
+                out.store(static_cast<T *>(a.out) + (int64_t)(x.first_token + token) * a.ldo + (int64_t)(kv_head * a.group + row - token * a.group) * dim + at);
+            } else {
+                const int64_t to = ((int64_t)(x.slot + x.part) * a.c.kv_heads + kv_head) * a.tile_rows + n * 16 + r;
+                float4 *sums = reinterpret_cast<float4 *>(a.partial + to * dim + at);
+                sums[0] = float4{v[0], v[1], v[2], v[3]};
+                sums[1] = float4{v[4], v[5], v[6], v[7]};
+                if (at == 0) a.partial_stats[to] = float2{top, sum};
+            }
+        }
+    }
+}
+
+// Joins the parts of tiles that were split: a workgroup sixteen rows of a tile.
+template <typename T> __global__ __launch_bounds__(256) void k_attend_join(Attend a, int64_t first)
+{
+    const int64_t number = first + blockIdx.x;
+    const int32_t groups = a.tile_rows / 16, dim = a.c.head_dim;
+    const int64_t tile_head = number / groups;
+    const int32_t n = (int32_t)(number - tile_head * groups), tile = (int32_t)(tile_head / a.c.kv_heads), kv_head = (int32_t)(tile_head - (int64_t)tile * a.c.kv_heads);
+    Unit x;
+    if (!find_unit<true>(a, tile, x) || x.parts == 1) return;
+    const int32_t span = max(0, x.high - x.low), parts = x.size ? (span + x.size - 1) / x.size : 0;   // (those with positions)
+    const int32_t chunks = dim / 8;
+    for (int i = threadIdx.x; i < 16 * chunks; i += 256) {
+        const int r = i / chunks, at = i % chunks * 8;
+        const int32_t row = x.tile * a.tile_rows + n * 16 + r;
+        if (row >= x.rows) continue;
+        const int64_t from = ((int64_t)x.slot * a.c.kv_heads + kv_head) * a.tile_rows + n * 16 + r, apart = (int64_t)a.c.kv_heads * a.tile_rows;
+        float top = kLowest, sum = 0.0f, v[8] = {};
+#pragma unroll 8
+        for (int p = 0; p < parts; p++) top = fmaxf(top, a.partial_stats[from + p * apart].x);
+#pragma unroll 4
+        for (int p = 0; p < parts; p++) {
+            const float2 stats = a.partial_stats[from + p * apart];
+            const float4 *sums = reinterpret_cast<const float4 *>(a.partial + (from + p * apart) * dim + at);
+            const float4 one = sums[0], two = sums[1];
+            const float f = __builtin_amdgcn_exp2f(stats.x - top);
+            sum += stats.y * f;
+            v[0] += one.x * f; v[1] += one.y * f; v[2] += one.z * f; v[3] += one.w * f;
+            v[4] += two.x * f; v[5] += two.y * f; v[6] += two.z * f; v[7] += two.w * f;
+        }
+        const int32_t token = a.by_group.divide(row);
+        Eight<T> out;
+        const float inverse = 1.0f / sum;
+#pragma unroll
+        for (int k = 0; k < 8; k++) out.set(k, sum == 0.0f ? 0.0f : v[k] * inverse);
+        out.store(static_cast<T *>(a.out) + (int64_t)(x.first_token + token) * a.ldo + (int64_t)(kv_head * a.group + row - token * a.group) * dim + at);
+    }
+}
+
+template <typename T, int D, int NQ, bool ANY_PAGE> int launch_units(const Attend &a, hipStream_t st)
+{
+    constexpr int64_t kMost = int64_t(1) << 23;   // workgroups of one launch: a grid's threads are counted in 32 bits
+    const int64_t units = (a.tiles + a.aim + 1) * a.c.kv_heads;   // (each tile one more than its positions by a part's)
+    for (int64_t at = 0; at < units; at += kMost) {
+        k_attend<T, D, NQ, ANY_PAGE><<<dim3((unsigned)std::min(units - at, kMost)), 256, 0, st>>>(a, at);
+        HBP_HIP(hipGetLastError());
+    }
+    return HBP_OK;
+}
+
+template <typename T> int launch_attend(const Attend &a, hipStream_t st)
+{
+    const bool any = a.c.page_size % 8 != 0;
+    auto by_page = [&](auto d, auto n) -> int {
+        return any ? launch_units<T, decltype(d)::value, 1, true>(a, st) : launch_units<T, decltype(d)::value, decltype(n)::value, false>(a, st);
+    };
+    auto by_rows = [&](auto d) -> int {
+        return a.tile_rows == 16 ? by_page(d, std::integral_constant<int, 1>()) : by_page(d, std::integral_constant<int, 2>());
+    };
+    const int32_t dim = a.c.head_dim;
+    const int rc = dim <= 64 ? by_rows(std::integral_constant<int, 64>()) : dim <= 128 ? by_rows(std::integral_constant<int, 128>()) : by_rows(std::integral_constant<int, 256>());
+    if (rc != HBP_OK || a.slots == 0) return rc;
+    constexpr int64_t kMost = int64_t(1) << 23;
+    const int64_t joins = a.tiles * a.c.kv_heads * (a.tile_rows / 16);
+    for (int64_t at = 0; at < joins; at += kMost) {
+        k_attend_join<T><<<dim3((unsigned)std::min(joins - at, kMost)), 256, 0, st>>>(a, at);
+        HBP_HIP(hipGetLastError());
+    }
+    return HBP_OK;
+}
+
+}  // namespace
+}  // namespace hbp

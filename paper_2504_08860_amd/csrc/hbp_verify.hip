@@ -1,0 +1,461 @@
+// Drafted tokens against the target's probabilities, and the token drawn behind those that stand (hbp_verify_drafts).
+//
+// What comes out are whole numbers: an index is off where a running sum lies on the wrong side of a border, and over a hundred thousand tokens of which each
+// has its border, sums in 32 bits would be so in one of some hundred draws.  So exponentials and sums are held in 64 bits from the logits on.
+#include "hbp_paged.h"
+
+#include <algorithm>
+
+namespace hbp {
+namespace {
+
+// A part of a row: its largest logit (-inf: nothing is left, or NaN), the lowest index of that, and the sum of exp((z - largest) / temperature).
+struct RowPart {
+    double sum;
+    float largest;
+    int32_t first;
+};
+
+constexpr int kThreads = 256, kEach = 16, kPart = kThreads * kEach, kMostParts = kWave;   // (kPart: logits of a part, for up to kMostParts of them; longer rows have longer parts)
+
+struct VerifyArgs {
+    const void *logits;
+    const void *ids;
+    const float *uniforms, *temperature, *draft_probs;
+    const int32_t *starts;
+    int32_t *new_ids, *accepted;
+    RowPart *stats;      // [rows][parts]
+    double *weights;     // [sequences][parts], where there are draft_probs
+    int64_t ldz, ldp;
+    int32_t rows, vocabulary, sequences, id_bytes, parts, part;
+};
+
+// 2^y for y <= 0, to some 2^-42 of it: 2^whole by the exponent's bits, and the series of 2^r = exp(r log 2) for |r| <= 1/2, whose first missing term is (log(2) / 2)^11 / 11! = 2e-13.
+__device__ __forceinline__ double power_of_2(double y)
+{
+    constexpr double c1 = 0.69314718055994531, c2 = c1 * c1 / 2, c3 = c2 * c1 / 3, c4 = c3 * c1 / 4, c5 = c4 * c1 / 5, c6 = c5 * c1 / 6, c7 = c6 * c1 / 7, c8 = c7 * c1 / 8,
+                     c9 = c8 * c1 / 9, c10 = c9 * c1 / 10;
+    y = y < -1100.0 ? -1100.0 : y;   // (0 all the same; NaN stays)
+    const double whole = rint(y), r = y - whole;
+    double v = c10;
+    v = fma(v, r, c9);
+    v = fma(v, r, c8);
+    v = fma(v, r, c7);
+    v = fma(v, r, c6);
+    v = fma(v, r, c5);
+    v = fma(v, r, c4);
+    v = fma(v, r, c3);
+    v = fma(v, r, c2);
+    v = fma(v, r, c1);
+    v = fma(v, r, 1.0);
+    return ldexp(v, (int)whole);
+}
+
+// what a difference of logits is multiplied by to be an exponent of 2: NaN where the temperature is none; 1 / log 2 where it is 0 (that row's sum says whether it has a NaN)
+__device__ __forceinline__ double per_logit(float temperature)
+{
+    constexpr double kPerLog2 = 1.4426950408889634;
+    if (temperature == 0.0f) return kPerLog2;
+    return temperature > 0.0f ? kPerLog2 / (double)temperature : (double)NAN;
+}
+__device__ __forceinline__ double exponential(float z, float largest, double per)
+{
+    return z == -INFINITY ? 0.0 : power_of_2(((double)z - (double)largest) * per);
+}
+
+__device__ __forceinline__ double wave_sum(double v)
+{
+#pragma unroll
+    for (int d = 1; d < kWave; d *= 2) v += __shfl_xor(v, d);
+    return v;
+}
+__device__ __forceinline__ double wave_running_sum(double v)   // of the lanes up to each
+{
+    const int lane = threadIdx.x % kWave;
+#pragma unroll
+    for (int d = 1; d < kWave; d *= 2) {
+        const double below = __shfl_up(v, d);
+        v += lane >= d ? below : 0.0;
+    }
+    return v;
+}
+
+// Eight logits from column `col` on; behind the end -inf.
+template <typename T> __device__ __forceinline__ void load_logits(const T *z, int32_t col, int32_t end, float (&f)[8])
+{
+    Eight<T> v;
+    v.load_first(z + col, end - col);
+#pragma unroll
+    for (int i = 0; i < 8; i++) f[i] = col + i < end ? v.get(i) : -INFINITY;
+}
+
+// Sums over parts of rows: a part's logits stay in registers between its largest one and the sum.
+template <typename T> __global__ __launch_bounds__(kThreads) void k_verify_rows(VerifyArgs a, int32_t first_row)
+{
+    __shared__ float wave_largest[kThreads / kWave];
+    __shared__ int32_t wave_first[kThreads / kWave];
+    __shared__ double wave_sums[kThreads / kWave];
+    const int32_t row = first_row + blockIdx.y, begin = blockIdx.x * a.part, end = min(begin + a.part, a.vocabulary);
+    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+    const T *z = static_cast<const T *>(a.logits) + (int64_t)row * a.ldz;
+    float largest = -INFINITY;
+    int32_t first = a.vocabulary;
+    double sum = 0.0;
+    double per = 1.4426950408889634;
+    for (int32_t from = begin; from < end; from += kPart) {
+        float f[kEach / 8][8];
+#pragma unroll
+        for (int k = 0; k < kEach / 8; k++) load_logits(z, from + (k * kThreads + (int)threadIdx.x) * 8, end, f[k]);
+        if (from == begin && a.temperature) {
+            const int32_t s = sequence_of(a.starts, a.sequences, row);
+            if (s < a.sequences) per = per_logit(a.temperature[s]);
+        }
+        float m = -INFINITY;
+        int32_t at = a.vocabulary;
+#pragma unroll
+        for (int k = 0; k < kEach / 8; k++)
+#pragma unroll
+            for (int i = 0; i < 8; i++)
+                if (f[k][i] > m) {
+                    m = f[k][i];
+                    at = from + (k * kThreads + (int)threadIdx.x) * 8 + i;
+                }
+        const float top = hbp::wave_max(m);
+        const uint32_t index = ~hbp::wave_max(m == top ? ~(uint32_t)at : 0u);   // (the lowest one)
+        __syncthreads();
+        if (lane == 0) {
+            wave_largest[wave] = top;
+            wave_first[wave] = (int32_t)index;
+        }
+        __syncthreads();
+        float block_top = wave_largest[0];
+        int32_t block_first = wave_first[0];
+#pragma unroll
+        for (int w = 1; w < kThreads / kWave; w++)
+            if (wave_largest[w] > block_top || (wave_largest[w] == block_top && wave_first[w] < block_first)) {
+                block_top = wave_largest[w];
+                block_first = wave_first[w];
+            }
+        if (block_top > largest) {
+            sum *= exponential(largest, block_top, per);
+            largest = block_top;
+            first = block_first;
+        }
+#pragma unroll
+        for (int k = 0; k < kEach / 8; k++)
+#pragma unroll
+            for (int i = 0; i < 8; i++) sum += exponential(f[k][i], largest, per);   // (a NaN makes it NaN)
+    }
+    sum = wave_sum(sum);
+    if (lane == 0) wave_sums[wave] = sum;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        sum = 0;
+#pragma unroll
+        for (int w = 0; w < kThreads / kWave; w++) sum += wave_sums[w];
+        a.stats[(int64_t)row * a.parts + blockIdx.x] = RowPart{sum, largest, first};
+    }
+}
+
+// A whole row, from its parts, by a wavefront
+__device__ __forceinline__ RowPart join_parts(const VerifyArgs &a, int32_t row, double per)
+{
+    const int lane = threadIdx.x % kWave;
+    RowPart mine{0.0, -INFINITY, a.vocabulary};
+    if (lane < a.parts) mine = a.stats[(int64_t)row * a.parts + lane];
+    RowPart all;
+    all.largest = hbp::wave_max(mine.largest);
+    all.first = (int32_t)~hbp::wave_max(mine.largest == all.largest ? ~(uint32_t)mine.first : 0u);
+    // (a part whose sum is NaN keeps it, whatever its largest logit is)
+    all.sum = wave_sum(mine.sum == 0.0 ? 0.0 : mine.sum * exponential(mine.largest, all.largest, per) + (mine.sum != mine.sum ? mine.sum : 0.0));
+    return all;
+}
+
+__device__ __forceinline__ int64_t id_of(const VerifyArgs &a, int32_t row)
+{
+    return a.id_bytes == 8 ? static_cast<const int64_t *>(a.ids)[row] : static_cast<const int32_t *>(a.ids)[row];
+}
+
+// p of a token that is one, of a row whose parts are joined: NaN where it has none
+template <typename T> __device__ __forceinline__ double probability(const VerifyArgs &a, int32_t row, int32_t v, const RowPart &all, float temperature, double per)
+{
+    if (!(all.sum > 0.0)) return NAN;
+    if (temperature == 0.0f) return v == all.first ? 1.0 : 0.0;
+    return exponential(to_f32(static_cast<const T *>(a.logits)[(int64_t)row * a.ldz + v]), all.largest, per) / all.sum;
+}
+
+// The first row of begin..end-1 whose draft does not stand (end - 1 where all do), by a workgroup, a wavefront a row; and that row's parts joined, in every thread
+template <typename T>
+__device__ __forceinline__ int32_t first_to_fall(const VerifyArgs &a, int32_t begin, int32_t end, float temperature, double per, RowPart &all, int32_t *wave_falls)
+{
+    const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave;
+    int32_t stop = end - 1;
+    for (int32_t from = begin; from < end - 1; from += kThreads / kWave) {
+        const int32_t row = from + wave;
+        bool stands = true;
+        if (row < end - 1) {
+            const RowPart r = join_parts(a, row, per);
+            const int64_t d = id_of(a, row + 1);
+            stands = false;
+            if (d >= 0 && d < a.vocabulary) {
+                const double q = a.draft_probs ? (double)a.draft_probs[(int64_t)row * a.ldp + d] : 1.0;
+                stands = (double)a.uniforms[row] * q < probability<T>(a, row, (int32_t)d, r, temperature, per);
+            }
+        }
+        __syncthreads();
+        if (lane == 0) wave_falls[wave] = stands ? end : row;
+        __syncthreads();
+        int32_t least = end;
+#pragma unroll
+        for (int w = 0; w < kThreads / kWave; w++) least = min(least, wave_falls[w]);
+        if (least < end) {
+            stop = least;
+            break;
+        }
+    }
+    all = join_parts(a, stop, per);
+    return stop;
+}
+
+// What tokens `col`.. of eight are drawn by: max(p - q, 0), or p (as exponentials, or 1 at the largest) without the draft `d` where there are no draft_probs.
+template <typename T, bool DIFFERENCE>
+__device__ __forceinline__ void weights_of(const VerifyArgs &a, int32_t row, int32_t col, int32_t end, const RowPart &all, float temperature, double per, int64_t d, double (&w)[8])
+{
+    float f[8];
+    load_logits(static_cast<const T *>(a.logits) + (int64_t)row * a.ldz, col, end, f);
+    Eight<float> q;
+    if constexpr (DIFFERENCE) q.load_first(a.draft_probs + (int64_t)row * a.ldp + col, end - col);
+#pragma unroll
+    for (int i = 0; i < 8; i++) {
+        double e = temperature == 0.0f ? (col + i == all.first ? 1.0 : 0.0) : exponential(f[i], all.largest, per);
+        if (col + i >= end || col + i == d) e = 0.0;
+        if constexpr (DIFFERENCE) {
+            const double p = temperature == 0.0f ? e : e / all.sum;
+            e = col + i < end ? fmax(p - (double)q.get(i), 0.0) : 0.0;
+            if (q.get(i) != q.get(i)) e = NAN;
+        }
+        w[i] = e;
+    }
+}
+
+// sum over a part of max(p - q, 0), of the row whose draft does not stand
+template <typename T> __global__ __launch_bounds__(kThreads) void k_verify_differences(VerifyArgs a, int32_t first_sequence)
+{
+    __shared__ int32_t wave_falls[kThreads / kWave];
+    __shared__ double wave_sums[kThreads / kWave];
+    const int32_t s = first_sequence + blockIdx.y, begin = a.starts[s], end = a.starts[s + 1];
+    if (begin < 0 || end <= begin || end > a.rows) return;
+    const float temperature = a.temperature ? a.temperature[s] : 1.0f;
+    const double per = per_logit(temperature);
+    RowPart all;
+    const int32_t row = first_to_fall<T>(a, begin, end, temperature, per, all, wave_falls);
+    if (row == end - 1) return;
+    const int32_t from = blockIdx.x * a.part, to = min(from + a.part, a.vocabulary);
+    double sum = 0.0;
+    for (int32_t col = from + threadIdx.x * 8; col < to; col += kThreads * 8) {
+        double w[8];
+        weights_of<T, true>(a, row, col, to, all, temperature, per, -1, w);
+#pragma unroll
+        for (int i = 0; i < 8; i++) sum += w[i];
+    }
+    sum = wave_sum(sum);
+    if (threadIdx.x % kWave == 0) wave_sums[threadIdx.x / kWave] = sum;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        sum = 0;
+#pragma unroll
+        for (int w = 0; w < kThreads / kWave; w++) sum += wave_sums[w];
+        a.weights[(int64_t)s * a.parts + blockIdx.x] = sum;
+    }
+}
+
+// The drafts that stand and the new token, a workgroup a sequence: the part that the drawn place is in, by the parts' sums, then the token in it.
+template <typename T> __global__ __launch_bounds__(kThreads) void k_verify_draw(VerifyArgs a, int32_t first_sequence)
+{
+    __shared__ int32_t wave_falls[kThreads / kWave];
+    __shared__ double wave_sums[kThreads / kWave];
+    const int32_t s = first_sequence + blockIdx.x, begin = a.starts[s], end = a.starts[s + 1];
+    if (begin < 0 || end <= begin || end > a.rows) {
+        if (threadIdx.x == 0) a.accepted[s] = 0;
+        return;
+    }
+    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+    const float temperature = a.temperature ? a.temperature[s] : 1.0f;
+    const double per = per_logit(temperature);
+    RowPart all;
+    const int32_t row = first_to_fall<T>(a, begin, end, temperature, per, all, wave_falls);
+    const bool fell = row < end - 1;
+    int64_t d = fell && !a.draft_probs ? id_of(a, row + 1) : -1;
+    bool difference = fell && a.draft_probs;
+    // the parts' sums of weights, a lane a part
+    double part = 0.0, total = 0.0;
+    if (difference) {
+        if (lane < a.parts) part = a.weights[(int64_t)s * a.parts + lane];
+        total = wave_sum(part);
+        if (!(total > 0.0)) difference = false;   // (nothing is left of p - q: p)
+    }
+    auto of_p = [&](int64_t without) {
+        const RowPart mine = lane < a.parts ? a.stats[(int64_t)row * a.parts + lane] : RowPart{0.0, -INFINITY, a.vocabulary};
+        const bool has = without >= 0 && without < a.vocabulary && without / a.part == lane;
+        if (temperature == 0.0f) {
+            part = lane == all.first / a.part && all.first != without ? 1.0 : 0.0;
+        } else {
+            part = mine.sum > 0.0 ? mine.sum * exponential(mine.largest, all.largest, per) : 0.0;
+            if (has) part = fmax(part - exponential(to_f32(static_cast<const T *>(a.logits)[(int64_t)row * a.ldz + without]), all.largest, per), 0.0);
+        }
+        total = wave_sum(part);
+    };
+    if (!difference) {
+        of_p(d);
+        if (!(total > 0.0) && d >= 0) {   // (the draft was all there is)
+            d = -1;
+            of_p(-1);
+        }
+    }
+    int32_t token = -1;
+    if (all.sum > 0.0 && total > 0.0) {   // (the same in every thread)
+        const double wanted = (double)a.uniforms[end - 1] * total;
+        const double running = wave_running_sum(part);
+        uint64_t over = __ballot(running > wanted && part > 0.0);
+        const uint64_t some = __ballot(part > 0.0);
+        if (!over) over = 1ull << (63 - __builtin_clzll(some));   // (roundings: the last one with a weight)
+        const int which = __builtin_ctzll(over);
+        const double before = __shfl(running, which) - __shfl(part, which);
+        const double left = wanted - before;
+        const int32_t from = which * a.part, to = min(from + a.part, a.vocabulary);
+        double base = 0.0;
+        int32_t last = -1;   // the last token with a weight so far
+        for (int32_t at = from; at < to && token < 0; at += kThreads * 8) {
+            const int32_t col = at + threadIdx.x * 8;
+            double w[8];
+            if (col < to) {
+                if (difference) weights_of<T, true>(a, row, col, to, all, temperature, per, -1, w);
+                else weights_of<T, false>(a, row, col, to, all, temperature, per, d, w);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 8; i++) w[i] = 0.0;
+            }
+            double mine = 0.0;
+#pragma unroll
+            for (int i = 0; i < 8; i++) mine += w[i];
+            const double upto = wave_running_sum(mine);
+            __syncthreads();
+            if (lane == kWave - 1) wave_sums[wave] = upto;
+            __syncthreads();
+            double below = base + upto - mine;
+#pragma unroll
+            for (int k = 0; k < kThreads / kWave; k++) {
+                if (k < wave) below += wave_sums[k];
+                base += wave_sums[k];
+            }
+            int32_t found = 0x7fffffff, latest = -1;
+#pragma unroll
+            for (int i = 0; i < 8; i++) {
+                below += w[i];
+                if (w[i] > 0.0) {
+                    latest = col + i;
+                    if (below > left) found = min(found, col + i);
+                }
+            }
+            const int32_t wave_found = (int32_t)~hbp::wave_max(~(uint32_t)found), wave_latest = (int32_t)hbp::wave_max((uint32_t)(latest + 1)) - 1;
+            __shared__ int32_t found_by[kThreads / kWave], latest_by[kThreads / kWave];
+            if (lane == 0) {
+                found_by[wave] = wave_found;
+                latest_by[wave] = wave_latest;
+            }
+            __syncthreads();
+            found = 0x7fffffff;
+#pragma unroll
+            for (int k = 0; k < kThreads / kWave; k++) {
+                found = min(found, found_by[k]);
+                last = max(last, latest_by[k]);
+            }
+            if (found != 0x7fffffff) token = found;
+        }
+        if (token < 0) token = last;
+    }
+    for (int32_t r = begin + threadIdx.x; r < end; r += kThreads) a.new_ids[r] = r < row ? (int32_t)id_of(a, r + 1) : r == row ? token : -1;
+    if (threadIdx.x == 0) a.accepted[s] = row - begin;
+}
+
+__global__ void k_verify_nothing(int32_t *accepted, int32_t sequences)
+{
+    for (int32_t s = blockIdx.x * blockDim.x + threadIdx.x; s < sequences; s += gridDim.x * blockDim.x) accepted[s] = 0;
+}
+
+int32_t parts_of(int64_t vocabulary)
+{
+    return (int32_t)std::min<int64_t>((vocabulary + kPart - 1) / kPart, kMostParts);
+}
+
+}  // namespace
+}  // namespace hbp
+
+extern "C" {
+
+int hbp_verify_drafts_workspace(int64_t rows, int64_t vocabulary, int64_t sequences, size_t *bytes)
+{
+    using namespace hbp;
+    if (rows < 0 || vocabulary < 1 || sequences < 0 || !bytes) return HBP_ERR_INVALID_ARGUMENT;
+    if (rows > (int64_t(1) << 30) || vocabulary > (int64_t(1) << 30) || sequences > (int64_t(1) << 24)) return HBP_ERR_TOO_LARGE;
+    *bytes = rows && sequences ? (size_t)parts_of(vocabulary) * ((size_t)rows * sizeof(RowPart) + (size_t)sequences * sizeof(double)) : 0;
+    return HBP_OK;
+}
+
+int hbp_verify_drafts(int type, const void *logits, int64_t ldz, int64_t rows, int64_t vocabulary, const void *ids, int id_bytes, const float *uniforms,
+                      const int32_t *starts, int64_t sequences, const float *temperature, const float *draft_probs, int64_t ldp, int32_t *new_ids,
+                      int32_t *accepted, void *workspace, size_t workspace_bytes, void *stream)
+{
+    using namespace hbp;
+    size_t need = 0;
+    int rc = hbp_verify_drafts_workspace(rows, vocabulary, sequences, &need);
+    if (rc != HBP_OK) return rc;
+    if (!is_type(type)) return HBP_ERR_INVALID_ARGUMENT;
+    if (sequences == 0) return HBP_OK;
+    if (!accepted || !aligned(accepted, 4)) return HBP_ERR_INVALID_ARGUMENT;
+    hipStream_t st = (hipStream_t)stream;
+    if (rows > 0) {
+        if (!logits || !ids || !uniforms || !starts || !new_ids || (id_bytes != 4 && id_bytes != 8)) return HBP_ERR_INVALID_ARGUMENT;
+        if (!aligned(logits, type_bytes(type)) || !aligned(ids, id_bytes)) return HBP_ERR_INVALID_ARGUMENT;
+        for (const void *p : {(const void *)uniforms, (const void *)starts, (const void *)temperature, (const void *)draft_probs, (const void *)new_ids})
+            if (!aligned(p, 4)) return HBP_ERR_INVALID_ARGUMENT;
+        if (rows > 1 && (ldz < vocabulary || (draft_probs && ldp < vocabulary))) return HBP_ERR_INVALID_ARGUMENT;
+        if (!workspace || workspace_bytes < need || !aligned(workspace, 256)) return HBP_ERR_INVALID_ARGUMENT;
+    }
+    rc = earlier_error();
+    if (rc != HBP_OK) return rc;
+    if (rows == 0) {
+        k_verify_nothing<<<dim3((unsigned)std::min<int64_t>((sequences + 255) / 256, 1024)), 256, 0, st>>>(accepted, (int32_t)sequences);
+        HBP_HIP(hipGetLastError());
+        return HBP_OK;
+    }
+    VerifyArgs a{};
+    a.logits = logits; a.ldz = ldz; a.rows = (int32_t)rows; a.vocabulary = (int32_t)vocabulary;
+    a.ids = ids; a.id_bytes = id_bytes; a.uniforms = uniforms; a.starts = starts; a.sequences = (int32_t)sequences;
+    a.temperature = temperature; a.draft_probs = draft_probs; a.ldp = ldp;
+    a.new_ids = new_ids; a.accepted = accepted;
+    a.parts = parts_of(vocabulary);
+    a.part = (int32_t)(((vocabulary + a.parts - 1) / a.parts + 7) / 8 * 8);
+    a.stats = static_cast<RowPart *>(workspace);
+    a.weights = reinterpret_cast<double *>(a.stats + rows * a.parts);
+    return by_type(type, [&](auto t) -> int {
+        using T = decltype(t);
+        constexpr int64_t kMost = 32768;   // of one launch: the grid's second dimension ends at 65535
+        for (int64_t at = 0; at < rows; at += kMost) {
+            k_verify_rows<T><<<dim3((unsigned)a.parts, (unsigned)std::min(rows - at, kMost)), kThreads, 0, st>>>(a, (int32_t)at);
+            HBP_HIP(hipGetLastError());
+        }
+        for (int64_t at = 0; at < sequences; at += kMost) {
+            const unsigned count = (unsigned)std::min(sequences - at, kMost);
+            if (draft_probs) {
+                k_verify_differences<T><<<dim3((unsigned)a.parts, count), kThreads, 0, st>>>(a, (int32_t)at);
+                HBP_HIP(hipGetLastError());
+            }
+            k_verify_draw<T><<<dim3(count), kThreads, 0, st>>>(a, (int32_t)at);
+            HBP_HIP(hipGetLastError());
+        }
+        return HBP_OK;
+    });
+}
+
+}  // extern "C"

@@ -1,4 +1,5 @@
-"""Binding of the operators beside the sparse products (``include/hbp.h``): 4-bit matrices, residual norms, token log probabilities.
+"""Binding of the operators beside the sparse products (``include/hbp.h``): 4-bit matrices, residual norms, token log probabilities, a paged cache
+with its attention, verification of drafted tokens.
 
 Argument marshalling only, as in the package itself, whose names these functions are reached by.  Tensors are checked for device,
 type and shape; rows may lie further apart than they are long (the last dimension is contiguous).  A call runs on torch's current
@@ -27,6 +28,12 @@ class hbp_norms_t(ctypes.Structure):
                 ("scale", ctypes.c_float), ("eps", ctypes.c_float)]
 
 
+class hbp_paged_t(ctypes.Structure):
+    _fields_ = [("keys", ctypes.c_void_p), ("values", ctypes.c_void_p), ("table", ctypes.c_void_p), ("starts", ctypes.c_void_p), ("lengths", ctypes.c_void_p),
+                ("ldk", ctypes.c_int64), ("ldv", ctypes.c_int64), ("ldt", ctypes.c_int64), ("pages", ctypes.c_int64), ("sequences", ctypes.c_int64),
+                ("table_width", ctypes.c_int64), ("type", ctypes.c_int32), ("kv_heads", ctypes.c_int32), ("page_size", ctypes.c_int32), ("head_dim", ctypes.c_int32)]
+
+
 _torch = _uint8 = _i32 = _i64 = _f32 = None
 _types = {}  # the library's numbers of torch's value types; set, as those above, with the library's argument types
 
@@ -49,6 +56,12 @@ def declare(L) -> None:
     L.hbp_token_logprobs.argtypes = [i32, vp, i64, i64, i64, vp, i32, vp, vp, vp, i32, vp, vp, vp, size, vp]
     L.hbp_token_logprobs_workspace.argtypes = [i32, i64, i64, i32, size_out]
     L.hbp_token_logprobs_backward.argtypes = [i32, vp, i64, i64, i64, vp, i32] + [vp] * 5 + [i64, vp]
+    paged, f32 = ctypes.POINTER(hbp_paged_t), ctypes.c_float
+    L.hbp_paged_append.argtypes = [paged, i64, vp, i64, vp, i64, vp, i64, i32, vp, i64, vp, i32, i32, vp]
+    L.hbp_paged_attention.argtypes = [paged, i64, vp, i64, i32, vp, i64, f32, f32, i32, i64, vp, size, vp]
+    L.hbp_paged_attention_workspace.argtypes = [paged, i64, i32, i32, i64, size_out]
+    L.hbp_verify_drafts.argtypes = [i32, vp, i64, i64, i64, vp, i32, vp, vp, i64, vp, vp, i64, vp, vp, vp, size, vp]
+    L.hbp_verify_drafts_workspace.argtypes = [i64, i64, i64, size_out]
 
 
 # (A small operator is 3 to 5 us of GPU time, and these checks are much of what a loop of them waits for.  A tensor's shape, strides, type,
@@ -307,3 +320,127 @@ def hbp_token_logprobs_backward(logits, tokens, lse, entropy, g_logp, g_entropy,
                                            _core._stream_ptr(stream))
     if status:
         raise _core.HbpError(status, "hbp_token_logprobs_backward")
+
+
+# ------------------------------------------------------------------------------------ a paged cache and its attention
+
+def _pages(t, what, shape, dtype, device):
+    """(address, values from one page to the next) of [pages, kv_heads, page_size, head_dim], each page contiguous in itself"""
+    if t.dtype is dtype and t.shape == shape and t.get_device() == device:
+        pages, heads, size, dim = shape
+        apart, of_head, of_row, one = t.stride()
+        if pages < 2:
+            apart = max(apart, heads * size * dim)
+        if one == 1 and (of_row == dim or size < 2) and (of_head == size * dim or heads < 2):
+            return t.data_ptr(), apart
+    raise AssertionError(f"{what}: {dtype} tensor of shape {tuple(shape)} on the current CUDA device required, pages contiguous in themselves")
+
+
+def _heads(t, what, shape, dtype, device):
+    """(address, row stride) of [tokens, heads, head_dim], a token's heads together"""
+    if t.dtype is dtype and t.shape == shape and t.get_device() == device:
+        tokens, heads, dim = shape
+        apart, of_head, one = t.stride()
+        if tokens < 2:
+            apart = heads * dim
+        if one == 1 and (of_head == dim or heads < 2) and apart >= heads * dim:
+            return t.data_ptr(), apart
+    raise AssertionError(f"{what}: {dtype} tensor of shape {tuple(shape)} on the current CUDA device required, a token's heads contiguous")
+
+
+def _cache(keys, values, table, starts, lengths, device):
+    shape, dtype = keys.shape, keys.dtype
+    assert len(shape) == 4 and dtype in _types, "keys: float32, float16 or bfloat16 of [pages, kv_heads, page_size, head_dim] required"
+    assert table.dim() == 2, "table: int32 matrix required"
+    (k_at, ldk), (v_at, ldv) = _pages(keys, "keys", shape, dtype, device), _pages(values, "values", shape, dtype, device)
+    sequences, width = table.shape
+    t_at, ldt = _rows(table, "table", (sequences, width), _i32, device)
+    return hbp_paged_t(k_at, v_at, t_at, _whole(starts, "starts", (sequences + 1,), _i32, device), _whole(lengths, "lengths", (sequences,), _i32, device),
+                       ldk, ldv, ldt, shape[0], sequences, width, _types[dtype], shape[1], shape[2], shape[3])
+
+
+def hbp_paged_append(k, v, keys, values, table, starts, lengths, q=None, q_out=None, frequencies=None, interleaved: bool = False, stream=None) -> None:
+    """Puts new tokens' ``k`` and ``v`` [tokens, kv_heads, head_dim] into the cache (``keys``, ``values`` [pages, kv_heads, page_size, head_dim], ``table``
+    int32 [sequences, pages of one]).  Sequence s has rows ``starts[s]`` .. ``starts[s + 1] - 1`` (int32 [sequences + 1]), the last ones of its ``lengths[s]``
+    (int32) positions.  ``frequencies`` (float32 [pairs]): keys, and queries ``q`` into ``q_out``, are rotated by their positions on the way."""
+    L, device = _start()
+    c = _cache(keys, values, table, starts, lengths, device)
+    dtype, tokens = keys.dtype, k.shape[0]
+    shape = (tokens, c.kv_heads, c.head_dim)
+    k_at, v_at = _heads(k, "k", shape, dtype, device), _heads(v, "v", shape, dtype, device)
+    assert (q is None) == (q_out is None), "q and q_out go together"
+    heads, q_at, o_at = 0, (None, 0), (None, 0)
+    if q is not None:
+        assert q.dim() == 3, "q: [tokens, heads, head_dim] required"
+        heads = q.shape[1]
+        shape = (tokens, heads, c.head_dim)
+        q_at, o_at = _heads(q, "q", shape, dtype, device), _heads(q_out, "q_out", shape, dtype, device)
+    pairs = 0
+    if frequencies is not None:
+        assert frequencies.dim() == 1, "frequencies: float32 vector required"
+        pairs = frequencies.shape[0]
+    status = L.hbp_paged_append(c, tokens, *k_at, *v_at, *q_at, heads, *o_at, _whole(frequencies, "frequencies", (pairs,), _f32, device), pairs,
+                                1 if interleaved else 0, _core._stream_ptr(stream))
+    if status:
+        raise _core.HbpError(status, "hbp_paged_append")
+
+
+@functools.lru_cache(maxsize=1024)
+def _attention_bytes(tokens, heads, window, most_new, pages, sequences, width, dtype_number, kv_heads, page_size, head_dim):
+    need = ctypes.c_size_t()
+    page = kv_heads * page_size * head_dim
+    c = hbp_paged_t(4096, 4096, 4096, 4096, 4096, page, page, width, pages, sequences, width, dtype_number, kv_heads, page_size, head_dim)  # (sizes alone are looked at)
+    _core._check(_core.lib().hbp_paged_attention_workspace(c, tokens, heads, window, most_new, need), "hbp_paged_attention_workspace")
+    return need.value
+
+
+def hbp_paged_attention(q, keys, values, table, starts, lengths, out, scale: float | None = None, softcap: float = 0.0, window: int = 0,
+                        most_new: int | None = None, workspace=None, stream=None) -> None:
+    """Attention of new tokens' queries ``q`` [tokens, heads, head_dim] over the cache that holds their own keys and values already (as hbp_paged_append has
+    them), into ``out``: causal, at most the last ``window`` positions if given, scores times ``scale`` (1 / sqrt(head_dim)) and capped at ``softcap`` if given.
+    ``most_new``: no sequence has more new tokens than this (1 for decoding; without it, tokens)."""
+    L, device = _start()
+    c = _cache(keys, values, table, starts, lengths, device)
+    shape, dtype = q.shape, keys.dtype
+    assert len(shape) == 3 and shape[2] == c.head_dim, "q: [tokens, heads, head_dim] required"
+    tokens, heads, dim = shape
+    q_at, o_at = _heads(q, "q", shape, dtype, device), _heads(out, "out", shape, dtype, device)
+    most = tokens if most_new is None else most_new
+    need = _attention_bytes(tokens, heads, window, most, c.pages, c.sequences, c.table_width, c.type, c.kv_heads, c.page_size, dim)
+    at, size, kept = _space(workspace, need, stream, device)
+    status = L.hbp_paged_attention(c, tokens, *q_at, heads, *o_at, dim ** -0.5 if scale is None else scale, softcap, window, most, at, size,
+                                   _core._stream_ptr(stream))
+    if status:
+        raise _core.HbpError(status, "hbp_paged_attention")
+
+
+# ------------------------------------------------------------------------------------ verification of drafted tokens
+
+@functools.lru_cache(maxsize=1024)
+def _verify_bytes(rows, vocabulary, sequences):
+    need = ctypes.c_size_t()
+    _core._check(_core.lib().hbp_verify_drafts_workspace(rows, vocabulary, sequences, need), "hbp_verify_drafts_workspace")
+    return need.value
+
+
+def hbp_verify_drafts(logits, tokens, uniforms, starts, new_tokens, accepted, draft_probs=None, temperature=None, workspace=None, stream=None) -> None:
+    """Which drafted tokens stand, and the token behind them.  Sequence s has rows ``starts[s]`` .. ``starts[s + 1] - 1`` of ``logits`` [rows, vocabulary] and
+    ``tokens`` (int32 or int64 [rows]): the last token that stands, then the drafts, which were drawn from the ``draft_probs`` (float32 [rows, vocabulary]; None: from
+    nothing) of the row before.  ``uniforms`` float32 [rows], ``temperature`` float32 [sequences] (0: the largest logit).  ``new_tokens`` int32 [rows]: drafts that
+    stand, the new token, then -1; ``accepted`` int32 [sequences]: how many stand."""
+    L, device = _start()
+    shape, dtype = logits.shape, logits.dtype
+    assert dtype in _types and len(shape) == 2, "logits: matrix of float32, float16 or bfloat16 required"
+    rows, vocabulary = shape
+    assert accepted.dim() == 1, "accepted: int32 vector required"
+    assert tokens is not None, "tokens: int32 or int64 required"
+    sequences = accepted.shape[0]
+    z_at, ldz = _rows(logits, "logits", shape, dtype, device)
+    p_at, ldp = (None, 0) if draft_probs is None else _rows(draft_probs, "draft_probs", shape, _f32, device)
+    at, size, kept = _space(workspace, _verify_bytes(rows, vocabulary, sequences), stream, device)
+    status = L.hbp_verify_drafts(_types[dtype], z_at, ldz, rows, vocabulary, *_ids(tokens, rows, device), _whole(uniforms, "uniforms", (rows,), _f32, device),
+                                 _whole(starts, "starts", (sequences + 1,), _i32, device), sequences,
+                                 _whole(temperature, "temperature", (sequences,), _f32, device), p_at, ldp, _whole(new_tokens, "new_tokens", (rows,), _i32, device),
+                                 _whole(accepted, "accepted", (sequences,), _i32, device), at, size, _core._stream_ptr(stream))
+    if status:
+        raise _core.HbpError(status, "hbp_verify_drafts")
