@@ -11,9 +11,9 @@ struct Attend {
     void *out;
     int64_t ldq, ldo;
     int32_t tokens, heads, group, most_new, window;
-    float per;                 // scores to exponents of 2: |scale| / log 2 (of a negative scale, queries change their sign)
+    float per;                 // scores to exponents of 2: |scale| / log 2, 1 where it is 0
     float cap_in, cap_out;     // with a cap: exponents are cap_out tanh(cap_in score); cap_out 0: none
-    int32_t negative;
+    uint32_t keep, flip;       // of queries' bits, in both halves of a word: signs change where scale is negative, a scale of 0 leaves zeros
     Divider by_group, by_kv_heads;
     int32_t tile_rows;         // rows (a token's query heads of one head of keys lie together) that a workgroup takes at once
     int32_t aim, least;        // parts of all tiles of one head of keys, about, and positions that a part has at least

@@ -25,11 +25,13 @@ int plan(const hbp_paged_t *cache, int64_t tokens, int heads, int window, int64_
     a->window = window;
     a->by_group = Divider::of(group);
     a->by_kv_heads = Divider::of(cache->kv_heads);
-    a->tile_rows = most_new * group > 16 && cache->page_size % 8 == 0 && cache->type != HBP_F32 ? 32 : 16;
+    const int64_t most_rows = most_new * group;
+    const bool few = most_rows <= 16 || cache->page_size % 8 || cache->type == HBP_F32, wide = cache->head_dim > 128;
+    a->tile_rows = few ? 16 : most_rows <= 32 && !wide ? 32 : most_rows <= 128 || wide ? 128 : 256;
     const int64_t rows = a->tile_rows;
     a->tiles = std::min(tokens * group / rows + cache->sequences, cache->sequences * ((most_new * group + rows - 1) / rows));
-    a->least = 4 * kStep;
-    a->aim = (int32_t)std::max<int64_t>(1, 2048 / cache->kv_heads);
+    a->least = rows > 32 ? 512 : 4 * kStep;
+    a->aim = (int32_t)std::max<int64_t>(1, (rows > 32 ? 1024 : 2048) / cache->kv_heads);
     // Parts of tiles that are split: each is of more than `length` positions, so that its parts are at most twice its positions by `length`, and in all twice `aim`.
     const int64_t span = window ? std::min<int64_t>(a->c.capacity, (int64_t)window + rows) : a->c.capacity, most_parts = (span + a->least - 1) / a->least;
     a->slots = most_parts < 2 ? 0 : (int32_t)std::min<int64_t>(2 * a->aim + 64, a->tiles * most_parts);
@@ -69,8 +71,9 @@ int hbp_paged_attention(const hbp_paged_t *cache, int64_t tokens, const void *q,
     if (rc != HBP_OK) return rc;
     a.q = q; a.ldq = ldq; a.out = out; a.ldo = ldo;
     constexpr float kPerLog2 = 1.4426950408889634f;
-    a.negative = scale < 0;
-    a.per = std::fabs(scale) * kPerLog2;
+    a.keep = scale == 0 ? 0u : 0xffffffffu;
+    a.flip = scale < 0 ? (cache->type == HBP_F32 ? 0x80000000u : 0x80008000u) : 0u;
+    a.per = scale == 0 ? 1.0f : std::fabs(scale) * kPerLog2;
     if (softcap > 0) {
         a.cap_in = 2 * kPerLog2 * (std::fabs(scale) / softcap);
         a.cap_out = softcap * kPerLog2;

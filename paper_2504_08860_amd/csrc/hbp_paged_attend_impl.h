@@ -116,13 +116,15 @@ template <typename T> __device__ __forceinline__ const T *row_of(const void *pag
     return static_cast<const T *>(pages) + (int64_t)max(s.page, 0) * ld + (int64_t)(kv_head * c.page_size + s.within) * c.head_dim;
 }
 
-// N values (4 to 16, 8 or more bytes) of a row in the cache: rows are 16-byte aligned
+// N values (2 to 16, 4 or more bytes) of a row in the cache: rows are 16-byte aligned
 template <typename T, int N> struct Piece {
     static constexpr int kWords = N * sizeof(T) / 4;
     uint32_t w[kWords];
     __device__ __forceinline__ void load(const T *p)
     {
-        if constexpr (kWords == 2) {
+        if constexpr (kWords == 1) {
+            w[0] = *reinterpret_cast<const uint32_t *>(p);
+        } else if constexpr (kWords == 2) {
             const uint2 v = *reinterpret_cast<const uint2 *>(p);
             w[0] = v.x; w[1] = v.y;
         } else {
@@ -133,7 +135,78 @@ template <typename T, int N> struct Piece {
             }
         }
     }
+    __device__ __forceinline__ float get(int i) const
+    {
+        if constexpr (sizeof(T) == 4) return __uint_as_float(w[i]);
+        else return to_f32(__builtin_bit_cast(T, (uint16_t)(w[i / 2] >> (i & 1) * 16)));
+    }
 };
+
+// Infinities and NaN among 16-bit values, two to a word, or among fp32 values
+__device__ __forceinline__ uint32_t largest_halves(uint32_t a, uint32_t b)
+{
+    return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(ushort2_t, a), __builtin_bit_cast(ushort2_t, b)));
+}
+template <typename T> constexpr uint32_t kInfinite = std::is_same_v<T, float> ? 0x7f800000u : std::is_same_v<T, f16> ? 0x7c00u : 0x7f80u;
+template <typename T> __device__ __forceinline__ bool has_odd(uint32_t w)   // of words without signs
+{
+    return sizeof(T) == 4 ? w >= kInfinite<T> : (w & 0xffffu) >= kInfinite<T> || w >> 16 >= kInfinite<T>;
+}
+template <typename T> __device__ __forceinline__ uint32_t without_odd(uint32_t w)
+{
+    if constexpr (sizeof(T) == 4) return (w & 0x7fffffffu) >= kInfinite<T> ? 0u : w;
+    const uint32_t low = (w & 0x7fffu) >= kInfinite<T> ? 0u : w & 0xffffu, high = (w >> 16 & 0x7fffu) >= kInfinite<T> ? 0u : w & 0xffff0000u;
+    return low | high;
+}
+// The weight of position t of a step for the lane's query, from the lane that has it
+template <typename T> __device__ __forceinline__ float weight_of(const Operand<T> &weights, int t, int column)
+{
+    uint32_t w[3];
+#pragma unroll
+    for (int part = 0; part < (sizeof(T) == 4 ? 3 : 1); part++) {
+        const uint4_t *from = reinterpret_cast<const uint4_t *>(&weights) + part;
+        const uint32_t mine = t / 2 % 4 == 0 ? (*from)[0] : t / 2 % 4 == 1 ? (*from)[1] : t / 2 % 4 == 2 ? (*from)[2] : (*from)[3];
+        w[part] = (uint32_t)__shfl((int)mine, t / 8 * 16 + column) >> (t & 1) * 16 & 0xffffu;
+    }
+    if constexpr (sizeof(T) == 4) return __uint_as_float(w[0] << 16) + __uint_as_float(w[1] << 16) + __uint_as_float(w[2] << 16);
+    else return to_f32(__builtin_bit_cast(T, (uint16_t)w[0]));
+}
+
+// Adds the infinities and NaN among the values of positions from..to - 1 of a step, for the queries that see them.  (Hardly ever called: it is not to cost registers elsewhere.)
+template <typename T, int D, int NQ>
+__device__ __forceinline__ void add_odd(const Attend &a, const int32_t *table, int32_t kv_head, int32_t step, int32_t from, int32_t to, const Operand<T> (&weights)[NQ],
+                                        const int32_t (&low)[NQ], const int32_t (&count)[NQ], float4_t (&o)[NQ][D / 16])
+{
+    constexpr int kTiles = D / 16, kEach = kTiles > 8 ? 8 : kTiles;
+    const int lane = threadIdx.x % kWave, column = lane % 16;
+#pragma unroll 1
+    for (int32_t position = from; position < to; position++) {
+        const Slot slot = slot_of(a.c, table, position);
+        if (slot.page < 0) continue;
+        const T *values = row_of<T>(a.c.values, a.c.ldv, a.c, kv_head, slot);
+        int32_t at = kTiles * 4 * (lane / 16);
+#pragma unroll
+        for (int k = 0; k < 4; k++)
+#pragma unroll
+            for (int c = 0; c < kTiles; c += kEach) {
+                asm volatile("" : "+v"(at) : : "memory");   // (one load after the other, nothing worked out before the loop)
+                Piece<T, kEach> v;
+                const int32_t d = at + kTiles * k + c;
+                if (d >= a.c.head_dim) continue;
+                v.load(values + d);
+#pragma unroll
+                for (int n = 0; n < NQ; n++) {
+                    const float weight = weight_of(weights[n], position - step, column);
+                    const bool sees = (uint32_t)(position - low[n]) < (uint32_t)count[n];
+#pragma unroll
+                    for (int i = 0; i < kEach; i++) {
+                        const float value = v.get(i);
+                        if (sees && !(fabsf(value) < INFINITY)) o[n][c + i][k] += weight * value;
+                    }
+                }
+            }
+    }
+}
 
 // Few rows: a workgroup of four wavefronts takes 16 NQ rows, and each wavefront every fourth step of their positions, straight from the cache into registers; the four
 // results are joined in LDS.  The next step's keys are on their way from the scores on, this one's values until the weights are there.
@@ -167,9 +240,8 @@ template <typename T, int D, int NQ, bool ANY_PAGE> __global__ __launch_bounds__
             Eight<T> v;
             v.clear();
             if (is_row && at < dim) v.load(from + at);
-            if (a.negative)
 #pragma unroll
-                for (int i = 0; i < Eight<T>::kWords; i++) v.w[i] ^= sizeof(T) == 4 ? 0x80000000u : 0x80008000u;
+            for (int i = 0; i < Eight<T>::kWords; i++) v.w[i] = (v.w[i] & a.keep) ^ a.flip;
             q[n][k] = Operand<T>::of(v.w);
         }
         const int64_t position = x.first_position + token;
@@ -276,10 +348,9 @@ template <typename T, int D, int NQ, bool ANY_PAGE> __global__ __launch_bounds__
             const bool whole = step >= all_low && step + kStep <= all_high && __ballot(held != 0xff) == 0;   // every row sees every position
 
             Operand<T> weights[NQ];
-            float p[NQ][8];
 #pragma unroll
             for (int n = 0; n < NQ; n++) {
-                float e[8];
+                float e[8], p[8];
 #pragma unroll
                 for (int i = 0; i < 8; i++) e[i] = s[n][i / 4][i % 4];
                 if constexpr (sizeof(T) == 4) {
@@ -295,7 +366,7 @@ template <typename T, int D, int NQ, bool ANY_PAGE> __global__ __launch_bounds__
                             const float *key = row_of<float>(a.c.keys, a.c.ldk, a.c, kv_head, slot_of(a.c, table, position));
                             float sum = 0.0f;
                             for (int d = 0; d < dim; d++) sum += query[d] * key[d];
-                            sum = a.negative ? -sum : sum;
+                            sum = a.flip ? -sum : sum;
 #pragma unroll
                             for (int j = 0; j < 8; j++)
                                 if (j == i && !(fabsf(e[j]) < INFINITY)) e[j] = sum;
@@ -326,13 +397,14 @@ template <typename T, int D, int NQ, bool ANY_PAGE> __global__ __launch_bounds__
                 }
 #pragma unroll
                 for (int i = 0; i < 8; i++) {
-                    p[n][i] = __builtin_amdgcn_exp2f(e[i] - m[n]);
-                    l[n] += p[n][i];
+                    p[i] = __builtin_amdgcn_exp2f(e[i] - m[n]);
+                    l[n] += p[i];
                 }
-                weights[n] = Operand<T>::of(p[n]);
+                weights[n] = Operand<T>::of(p);
             }
 
-            // Values that no row sees must not be there at all, not even with a weight of 0, and infinities or NaN among others only for those rows that see them.
+            // Values that no row sees must not be there at all, not even with a weight of 0; infinities and NaN are taken out where only some rows see them (in fp32 everywhere:
+            // parts of an infinity make NaN), and added for those rows.
             bool odd = false;
             if (!whole || sizeof(T) == 4) {
                 uint32_t largest = 0;
@@ -345,60 +417,41 @@ template <typename T, int D, int NQ, bool ANY_PAGE> __global__ __launch_bounds__
 #pragma unroll
                         for (int w = 0; w < Piece<T, kEach>::kWords; w++) {
                             vf[i][c].w[w] &= seen;
-                            if constexpr (sizeof(T) == 4) {
-                                largest = max(largest, vf[i][c].w[w] & 0x7fffffffu);
-                            } else {
-                                const ushort2_t v = __builtin_bit_cast(ushort2_t, vf[i][c].w[w] & 0x7fff7fffu), u = __builtin_bit_cast(ushort2_t, largest);
-                                largest = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(v, u));
-                            }
+                            if constexpr (sizeof(T) == 4) largest = max(largest, vf[i][c].w[w] & 0x7fffffffu);
+                            else largest = largest_halves(largest, vf[i][c].w[w] & 0x7fff7fffu);
                         }
                 }
-                constexpr uint32_t kInfinite = sizeof(T) == 4 ? 0x7f800000u : std::is_same_v<T, f16> ? 0x7c00u : 0x7f80u;
-                odd = sizeof(T) == 4 ? largest >= kInfinite : (largest & 0xffffu) >= kInfinite || largest >> 16 >= kInfinite;
+                odd = __ballot(has_odd<T>(largest)) != 0;
+                if (odd)
+#pragma unroll
+                    for (int i = 0; i < 8; i++)
+#pragma unroll
+                        for (int c = 0; c < kPieces; c++)
+#pragma unroll
+                            for (int w = 0; w < Piece<T, kEach>::kWords; w++) vf[i][c].w[w] = without_odd<T>(vf[i][c].w[w]);
             }
-            if (__ballot(odd) == 0) {
 #pragma unroll
-                for (int j = 0; j < kTiles; j++) {
-                    Operand<T> value;
-                    if constexpr (sizeof(T) == 4) {
-                        float v[8];
+            for (int j = 0; j < kTiles; j++) {
+                Operand<T> value;
+                if constexpr (sizeof(T) == 4) {
+                    float v[8];
 #pragma unroll
-                        for (int i = 0; i < 8; i++) v[i] = __uint_as_float(vf[i][j / kEach].w[j % kEach]);
-                        value = Operand<T>::of(v);
-                    } else {
-                        uint32_t bits[4];
+                    for (int i = 0; i < 8; i++) v[i] = __uint_as_float(vf[i][j / kEach].w[j % kEach]);
+                    value = Operand<T>::of(v);
+                } else {
+                    uint32_t bits[4];
 #pragma unroll
-                        for (int i = 0; i < 4; i++) {
-                            const uint32_t one = vf[2 * i][j / kEach].w[j % kEach / 2], two = vf[2 * i + 1][j / kEach].w[j % kEach / 2];
-                            bits[i] = j & 1 ? high_halves(one, two) : low_halves(one, two);
-                        }
-                        value = Operand<T>::of(bits);
+                    for (int i = 0; i < 4; i++) {
+                        const uint32_t one = vf[2 * i][j / kEach].w[j % kEach / 2], two = vf[2 * i + 1][j / kEach].w[j % kEach / 2];
+                        bits[i] = j & 1 ? high_halves(one, two) : low_halves(one, two);
                     }
-#pragma unroll
-                    for (int n = 0; n < NQ; n++) o[n][j] = multiply(value, weights[n], o[n][j]);
+                    value = Operand<T>::of(bits);
                 }
-            } else {
-                for (int u = 0; u < 4; u++)
 #pragma unroll
-                    for (int i = 0; i < 8; i++) {
-                        const int32_t position = step + 8 * u + i;
-                        if (position < tile_low || position >= end) continue;
-                        const Slot slot = slot_of(a.c, table, position);
-                        if (slot.page < 0) continue;
-                        const T *from = row_of<T>(a.c.values, a.c.ldv, a.c, kv_head, slot);
-#pragma unroll
-                        for (int n = 0; n < NQ; n++) {
-                            const float weight = __shfl(p[n][i], 16 * u + column);
-                            const bool sees = (uint32_t)(position - low[n]) < (uint32_t)count[n];
-#pragma unroll
-                            for (int j = 0; j < kTiles; j++)
-#pragma unroll
-                                for (int k = 0; k < 4; k++) {
-                                    const int32_t d = kTiles * (4 * quarter + k) + j;
-                                    if (sees && d < dim) o[n][j][k] += weight * to_f32(from[d]);
-                                }
-                        }
-                    }
+                for (int n = 0; n < NQ; n++) o[n][j] = multiply(value, weights[n], o[n][j]);
+            }
+            if (odd) {
+                add_odd<T, D, NQ>(a, table, kv_head, step, max(tile_low, step), min(end, step + kStep), weights, low, count, o);
             }
         }
     }
@@ -492,27 +545,6 @@ template <typename T, int D, int NQ, bool ANY_PAGE> int launch_units(const Atten
     const int64_t units = (a.tiles + a.aim + 1) * a.c.kv_heads;   // (each tile one more than its positions by a part's)
     for (int64_t at = 0; at < units; at += kMost) {
         k_attend<T, D, NQ, ANY_PAGE><<<dim3((unsigned)std::min(units - at, kMost)), 256, 0, st>>>(a, at);
-        HBP_HIP(hipGetLastError());
-    }
-    return HBP_OK;
-}
-
-template <typename T> int launch_attend(const Attend &a, hipStream_t st)
-{
-    const bool any = a.c.page_size % 8 != 0;
-    auto by_page = [&](auto d, auto n) -> int {
-        return any ? launch_units<T, decltype(d)::value, 1, true>(a, st) : launch_units<T, decltype(d)::value, decltype(n)::value, false>(a, st);
-    };
-    auto by_rows = [&](auto d) -> int {
-        return a.tile_rows == 16 ? by_page(d, std::integral_constant<int, 1>()) : by_page(d, std::integral_constant<int, 2>());
-    };
-    const int32_t dim = a.c.head_dim;
-    const int rc = dim <= 64 ? by_rows(std::integral_constant<int, 64>()) : dim <= 128 ? by_rows(std::integral_constant<int, 128>()) : by_rows(std::integral_constant<int, 256>());
-    if (rc != HBP_OK || a.slots == 0) return rc;
-    constexpr int64_t kMost = int64_t(1) << 23;
-    const int64_t joins = a.tiles * a.c.kv_heads * (a.tile_rows / 16);
-    for (int64_t at = 0; at < joins; at += kMost) {
-        k_attend_join<T><<<dim3((unsigned)std::min(joins - at, kMost)), 256, 0, st>>>(a, at);
         HBP_HIP(hipGetLastError());
     }
     return HBP_OK;

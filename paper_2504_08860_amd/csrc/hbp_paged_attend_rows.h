@@ -1,0 +1,363 @@
+// Attention of many rows over a paged cache (prompts): k_attend_rows, for 16-bit types and pages of whole eights of positions.
+#pragma once
+
+#include "hbp_paged_attend_impl.h"
+
+namespace hbp {
+namespace {
+
+// A workgroup of four wavefronts takes 64 NQ rows, 16 NQ a wavefront, and walks through their positions in turns of 64 (heads wider than 128: 32), which all four read from LDS: keys and values come
+// from the cache into registers two turns ahead, values are turned there (eight positions of one column become a lane's share of an operand), and both lie in LDS as operands of the matrix
+// instruction, lane after lane, so that every read is one of 16 bytes a lane without conflicts.  Three buffers and one barrier a turn.  The scores of the next block of 32 positions are
+// multiplied while this one's become weights.
+template <typename T, int D, int NQ> __global__ __launch_bounds__(256) void k_attend_rows(Attend a, int64_t first_unit)
+{
+    constexpr int kTurn = D > 128 ? 32 : 64, kBlocks = kTurn / kStep, kEights = kTurn / 8;
+    constexpr int kSteps = D / 32, kTiles = D / 16;
+    constexpr int kOperand = 64 * 16;                          // bytes of an operand of a wavefront
+    constexpr int kKeyBytes = kBlocks * 2 * kSteps * kOperand, kBytes = 2 * kKeyBytes;   // (as many of values)
+    constexpr int kChunks = D / 8, kKeyRows = 256 / kChunks, kKeyLoads = kTurn / kKeyRows;   // keys: a thread loads a chunk of eight columns of neighbouring positions
+    constexpr int kColumns = D == 64 ? 2 : 4, kQuads = D / kColumns;                         // values: some columns of eight positions
+    constexpr int kApart = 16 / (kTiles / kColumns);
+    static_assert(kKeyLoads <= 8 && 256 / kQuads == kEights, "");
+    extern __shared__ uint4 lds[];
+    __shared__ uint32_t held_by[3][kEights];   // whether the cache holds eight positions
+    __shared__ int32_t odd_by[3];              // the last turn, and 1, in whose values there are infinities or NaN
+    char *const base = reinterpret_cast<char *>(lds);
+    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, column = lane % 16, quarter = lane / 16;
+    const int64_t number = first_unit + blockIdx.x;
+    const int32_t unit_number = (int32_t)(number / a.c.kv_heads), kv_head = (int32_t)(number - (int64_t)unit_number * a.c.kv_heads);
+    Unit x;
+    if (!find_unit<false>(a, unit_number, x)) return;
+    const int32_t begin = x.low + x.part * x.size, end = min(begin + x.size, x.high);
+    const int32_t *table = a.c.table + x.sequence * a.c.ldt;
+    const int32_t dim = a.c.head_dim;
+    const int32_t first_row = x.tile * a.tile_rows + wave * 16 * NQ;
+
+    Operand<T> q[NQ][kSteps];
+    int32_t low[NQ], count[NQ];
+    int32_t all_low = 0, all_high = 0x7fffffff, some_low = 0x7fffffff, some_high = 0;   // positions that all rows of the wavefront see, and that some do
+#pragma unroll
+    for (int n = 0; n < NQ; n++) {
+        const int32_t row = first_row + n * 16 + column;
+        const bool is_row = row < x.rows;
+        const int32_t token = a.by_group.divide(is_row ? row : 0), head = kv_head * a.group + (is_row ? row - token * a.group : 0);
+        const T *from = static_cast<const T *>(a.q) + (int64_t)(x.first_token + token) * a.ldq + (int64_t)head * dim;
+#pragma unroll
+        for (int k = 0; k < kSteps; k++) {
+            const int32_t at = 32 * k + 8 * quarter;
+            Eight<T> v;
+            v.clear();
+            if (is_row && at < dim) v.load(from + at);
+#pragma unroll
+            for (int i = 0; i < Eight<T>::kWords; i++) v.w[i] = (v.w[i] & a.keep) ^ a.flip;
+            q[n][k] = Operand<T>::of(v.w);
+        }
+        const int64_t position = x.first_position + token;
+        low[n] = (int32_t)max((int64_t)0, a.window ? position - a.window + 1 : 0);
+        const int32_t high = (int32_t)max((int64_t)0, min(position + 1, (int64_t)end));
+        count[n] = is_row ? max(0, high - low[n]) : 0;
+        if (is_row) {
+            all_low = max(all_low, low[n]);
+            all_high = min(all_high, high);
+            if (count[n]) {
+                some_low = min(some_low, low[n]);
+                some_high = max(some_high, high);
+            }
+        }
+    }
+    auto least = [](int32_t p, int32_t q) { return min(p, q); };
+    auto most = [](int32_t p, int32_t q) { return max(p, q); };
+    all_low = wave_reduce(all_low, most);
+    all_high = wave_reduce(all_high, least);
+    some_low = wave_reduce(some_low, least);
+    some_high = wave_reduce(some_high, most);
+    // what the tile's rows see at all, and what all of them do
+    const int32_t last_row = min((x.tile + 1) * a.tile_rows, x.rows) - 1;
+    const int64_t p0 = x.first_position + a.by_group.divide(x.tile * a.tile_rows), p1 = x.first_position + a.by_group.divide(last_row);
+    const int32_t tile_low = (int32_t)max((int64_t)x.low, a.window ? p0 - a.window + 1 : 0);
+    const int64_t tile_all_low = a.window ? p1 - a.window + 1 : 0, tile_all_high = p0 + 1;
+
+    const float per = a.cap_out != 0.0f ? 1.0f : a.per;   // (of what the cap has made of scores)
+    float m[NQ], l[NQ];
+    float4_t o[NQ][kTiles];
+#pragma unroll
+    for (int n = 0; n < NQ; n++) {
+        m[n] = kLowest;
+        l[n] = 0.0f;
+#pragma unroll
+        for (int j = 0; j < kTiles; j++) o[n][j] = float4_t{0, 0, 0, 0};
+    }
+
+    // A turn's keys and values on their way: loaded into registers, then put into LDS as operands.
+    Piece<T, 8> kf[kKeyLoads];
+    Piece<T, kColumns> vf[8];
+    const int key_chunk = threadIdx.x % kChunks, key_row = threadIdx.x / kChunks * kKeyLoads;   // positions key_row ..
+    const int quad = threadIdx.x % kQuads, eight = threadIdx.x / kQuads;
+    struct Places {
+        Slot k, v;
+    };
+    const int32_t last_eight = (end - 1) / 8 * 8;
+    auto places = [&](int32_t turn) {   // (of positions moved back before the end: what is read there has no weight)
+        Places p;
+        p.k = slot_of(a.c, table, min(turn + key_row / 8 * 8, last_eight));
+        p.k.within += key_row % 8;
+        p.v = slot_of(a.c, table, min(turn + 8 * eight, last_eight));
+        return p;
+    };
+    auto load = [&](const Places &p) {
+        const T *keys = row_of<T>(a.c.keys, a.c.ldk, a.c, kv_head, p.k) + (8 * key_chunk < dim ? 8 * key_chunk : 0);
+        const T *values = row_of<T>(a.c.values, a.c.ldv, a.c, kv_head, p.v) + (kColumns * quad < dim ? kColumns * quad : 0);
+#pragma unroll
+        for (int i = 0; i < kKeyLoads; i++) kf[i].load(keys + i * dim);
+#pragma unroll
+        for (int i = 0; i < 8; i++) vf[i].load(values + i * dim);
+    };
+    // row r of half h of a block is its position 8 (r / 4) + 4 h + r % 4; a row's place among 16 changes with the chunk of columns, so that neither side meets a bank twice
+    auto put = [&](int32_t turn, int which, bool held) {
+        char *const keys = base + which * kBytes, *const values = keys + kKeyBytes;
+        const uint32_t there = 8 * key_chunk < dim ? 0xffffffffu : 0u;
+#pragma unroll
+        for (int i = 0; i < kKeyLoads; i++) {
+            const int position = key_row + i, block = position / kStep, h = position / 4 % 2, r = position / 8 % 4 * 4 + position % 4;
+            const int operand = (block * 2 + h) * kSteps + key_chunk / 4;
+            *reinterpret_cast<uint4_t *>(keys + operand * kOperand + (key_chunk % 4 * 16 + (r ^ (key_chunk % 16))) * 16) =
+                uint4_t{kf[i].w[0] & there, kf[i].w[1] & there, kf[i].w[2] & there, kf[i].w[3] & there};
+        }
+        if (quad == 0) held_by[which][eight] = held;
+        // Values that no row sees must not be there at all, not even with a weight of 0; infinities and NaN that only some rows see are taken out, and added for those rows
+        const bool edge = turn < tile_all_low || (int64_t)turn + kTurn > tile_all_high || turn + kTurn > end;   // (the same in all threads)
+        if (edge || !held) {
+            uint32_t largest = 0;
+#pragma unroll
+            for (int i = 0; i < 8; i++) {
+                const int32_t position = turn + 8 * eight + i;
+                const uint32_t seen = held && position >= tile_low && position < end ? 0xffffffffu : 0u;
+#pragma unroll
+                for (int w = 0; w < kColumns / 2; w++) {
+                    vf[i].w[w] &= seen;
+                    largest = largest_halves(largest, vf[i].w[w] & 0x7fff7fffu);
+                }
+            }
+            if (edge && has_odd<T>(largest)) {
+                odd_by[which] = turn + 1;   // (every thread that finds one says the same)
+#pragma unroll
+                for (int i = 0; i < 8; i++)
+#pragma unroll
+                    for (int w = 0; w < kColumns / 2; w++) vf[i].w[w] = without_odd<T>(vf[i].w[w]);
+            }
+        }
+        // column c is row c / kTiles of tile c % kTiles
+#pragma unroll
+        for (int i = 0; i < kColumns; i++) {
+            uint4_t w;
+#pragma unroll
+            for (int k = 0; k < 4; k++) {
+                const uint32_t one = vf[2 * k].w[i / 2], two = vf[2 * k + 1].w[i / 2];
+                w[k] = i & 1 ? high_halves(one, two) : low_halves(one, two);
+            }
+            const int at = kColumns * quad + i, r = at / kTiles, j = at % kTiles;
+            const int operand = eight / 4 * kTiles + j;
+            *reinterpret_cast<uint4_t *>(values + operand * kOperand + (eight % 4 * 16 + (r ^ (j / kColumns * kApart))) * 16) = w;
+        }
+    };
+    // what has been written to LDS is there for all; loads from the cache stay on their way
+    auto barrier = [&] {
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    };
+    const int key_place = quarter * 16, value_place = quarter * 16;
+    auto scores = [&](float4_t (&s)[NQ][2], int which, int b) {
+        const char *const keys = base + which * kBytes;
+#pragma unroll
+        for (int n = 0; n < NQ; n++) s[n][0] = s[n][1] = float4_t{0, 0, 0, 0};
+#pragma unroll
+        for (int k = 0; k < kSteps; k++)
+#pragma unroll
+            for (int h = 0; h < 2; h++) {
+                const Operand<T> key{*reinterpret_cast<const uint4_t *>(keys + ((b * 2 + h) * kSteps + k) * kOperand + (key_place + (column ^ ((4 * k + quarter) % 16))) * 16)};
+#pragma unroll
+                for (int n = 0; n < NQ; n++) s[n][h] = multiply(key, q[n][k], s[n][h]);
+            }
+    };
+
+    if (threadIdx.x < 3) odd_by[threadIdx.x] = 0;
+    if (begin < end) {
+        Places next = places(begin);
+        load(next);
+        bool held_next = next.v.page >= 0;
+        next = places(begin + kTurn);
+        __syncthreads();
+        put(begin, 0, held_next);
+        load(next);
+        held_next = next.v.page >= 0;
+        next = places(begin + 2 * kTurn);
+        barrier();
+        float4_t s[NQ][2];
+        bool ready = false;    // s has the scores of the turn's first block
+        int which = 0;
+        for (int32_t turn = begin; turn < end; turn += kTurn) {
+            const int following = which == 2 ? 0 : which + 1;
+            const bool active = turn < some_high && turn + kTurn > some_low;   // (the same in all lanes)
+            if (active && !ready) scores(s, which, 0);
+            ready = active;
+            uint32_t held = 0;
+#pragma unroll
+            for (int i = 0; i < kEights; i++) held |= held_by[which][i] << i;
+            const bool odd = odd_by[which] == turn + 1;
+#pragma unroll
+            for (int b = 0; b < kBlocks; b++) {
+                if (b == kBlocks - 1) {
+                    if (turn + kTurn < end) put(turn + kTurn, following, held_next);
+                    load(next);
+                    held_next = next.v.page >= 0;
+                    next = places(turn + 3 * kTurn);
+                }
+                const int32_t block = turn + b * kStep;
+                if (active) {
+                    if (a.cap_out != 0.0f) {
+#pragma unroll
+                        for (int n = 0; n < NQ; n++)
+#pragma unroll
+                            for (int i = 0; i < 8; i++) s[n][i / 4][i % 4] = exponent_of(a, s[n][i / 4][i % 4]);
+                    }
+                    if (block < all_low || block + kStep > all_high || (held >> (4 * b) & 0xf) != 0xf) {
+#pragma unroll
+                        for (int n = 0; n < NQ; n++)
+#pragma unroll
+                            for (int i = 0; i < 8; i++) {
+                                const bool sees = (uint32_t)(block + 8 * quarter + i - low[n]) < (uint32_t)count[n] && (held >> (4 * b + quarter) & 1);
+                                if (!sees) s[n][i / 4][i % 4] = -INFINITY;
+                            }
+                    }
+                    float top[NQ];
+                    bool larger = false;
+#pragma unroll
+                    for (int n = 0; n < NQ; n++) {
+                        top[n] = s[n][0][0];
+#pragma unroll
+                        for (int i = 1; i < 8; i++) top[n] = fmaxf(top[n], s[n][i / 4][i % 4]);
+                        top[n] *= per;
+                        larger |= top[n] > m[n] + 8.0f;
+                    }
+                    if (__ballot(larger) != 0) {   // (see k_attend)
+#pragma unroll
+                        for (int n = 0; n < NQ; n++) {
+                            const float to = over_quarters(fmaxf(top[n], m[n]), [](float p, float q) { return fmaxf(p, q); });
+                            const float f = __builtin_amdgcn_exp2f(m[n] - to);
+                            m[n] = to;
+                            l[n] *= f;
+#pragma unroll
+                            for (int j = 0; j < kTiles; j++)
+#pragma unroll
+                                for (int i = 0; i < 4; i++) o[n][j][i] *= f;
+                        }
+                    }
+                }
+                if (b == kBlocks - 1) barrier();   // (the next turn's operands are in LDS; their buffer was read last in the turn before this one)
+                if (active) {
+                    Operand<T> weights[NQ];
+#pragma unroll
+                    for (int n = 0; n < NQ; n++) {
+                        float p[8];
+#pragma unroll
+                        for (int i = 0; i < 8; i++) {
+                            p[i] = __builtin_amdgcn_exp2f(fmaf(s[n][i / 4][i % 4], per, -m[n]));
+                            l[n] += p[i];
+                        }
+                        weights[n] = Operand<T>::of(p);
+                    }
+                    scores(s, b == kBlocks - 1 ? following : which, b == kBlocks - 1 ? 0 : b + 1);   // (behind the last turn of nothing, for nothing)
+                    const char *const values = base + which * kBytes + kKeyBytes;
+#pragma unroll
+                    for (int j = 0; j < kTiles; j++) {
+                        const Operand<T> value{*reinterpret_cast<const uint4_t *>(values + (b * kTiles + j) * kOperand + (value_place + (column ^ (j / kColumns * kApart))) * 16)};
+#pragma unroll
+                        for (int n = 0; n < NQ; n++) o[n][j] = multiply(value, weights[n], o[n][j]);
+                    }
+                    if (odd) {
+                        add_odd<T, D, NQ>(a, table, kv_head, block, max(tile_low, block), min(end, block + kStep), weights, low, count, o);
+                    }
+                }
+            }
+            which = following;
+        }
+    }
+
+#pragma unroll
+    for (int n = 0; n < NQ; n++) {
+        const float sum = over_quarters(l[n], [](float p, float q) { return p + q; });
+        const int32_t row = first_row + n * 16 + column;
+        if (row >= x.rows) continue;
+        if (x.parts == 1) {
+            const int32_t token = a.by_group.divide(row);
+            T *to = static_cast<T *>(a.out) + (int64_t)(x.first_token + token) * a.ldo + (int64_t)(kv_head * a.group + row - token * a.group) * dim;
+            const float inverse = 1.0f / sum;
+#pragma unroll
+            for (int k = 0; k < 4; k++) {
+                // (columns kTiles (4 quarter + k) .. + kTiles - 1)
+#pragma unroll
+                for (int c = 0; c < kTiles; c += 4) {
+                    const int32_t at = kTiles * (4 * quarter + k) + c;
+                    struct __attribute__((packed, aligned(2))) { T v[4]; } four;
+#pragma unroll
+                    for (int i = 0; i < 4; i++) four.v[i] = from_f32<T>(sum == 0.0f ? 0.0f : o[n][c + i][k] * inverse);
+                    if (at < dim) *reinterpret_cast<decltype(four) *>(to + at) = four;
+                }
+            }
+        } else {
+            const int64_t to = ((int64_t)(x.slot + x.part) * a.c.kv_heads + kv_head) * a.tile_rows + wave * 16 * NQ + n * 16 + column;
+#pragma unroll
+            for (int k = 0; k < 4; k++)
+#pragma unroll
+                for (int c = 0; c < kTiles; c += 4) {
+                    const int32_t at = kTiles * (4 * quarter + k) + c;
+                    if (at < dim) *reinterpret_cast<float4_t *>(a.partial + to * dim + at) = float4_t{o[n][c][k], o[n][c + 1][k], o[n][c + 2][k], o[n][c + 3][k]};
+                }
+            if (quarter == 0) a.partial_stats[to] = float2{m[n], sum};
+        }
+    }
+}
+
+template <typename T, int D, int NQ> int launch_rows(const Attend &a, hipStream_t st)
+{
+    constexpr int64_t kMost = int64_t(1) << 23;
+    constexpr size_t kLds = 3 * 2 * (size_t)(D > 128 ? 32 : 64) * D * sizeof(T);
+    auto kernel = k_attend_rows<T, D, NQ>;
+    HBP_HIP(hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)kLds));
+    const int64_t units = (a.tiles + a.aim + 1) * a.c.kv_heads;
+    for (int64_t at = 0; at < units; at += kMost) {
+        kernel<<<dim3((unsigned)std::min(units - at, kMost)), 256, kLds, st>>>(a, at);
+        HBP_HIP(hipGetLastError());
+    }
+    return HBP_OK;
+}
+
+// Few rows by k_attend, many by k_attend_rows, as the tiles have been planned; then what was split.
+template <typename T> int launch_attend(const Attend &a, hipStream_t st)
+{
+    const bool any = a.c.page_size % 8 != 0;
+    auto by_rows = [&](auto d) -> int {
+        constexpr int D = decltype(d)::value;
+        if (any) return launch_units<T, D, 1, true>(a, st);
+        if (a.tile_rows == 16) return launch_units<T, D, 1, false>(a, st);
+        if constexpr (sizeof(T) == 2) {
+            if (a.tile_rows == 128) return launch_rows<T, D, 2>(a, st);
+            if constexpr (D < 256)
+                if (a.tile_rows == 256) return launch_rows<T, D, 4>(a, st);
+        }
+        return launch_units<T, D, 2, false>(a, st);
+    };
+    const int32_t dim = a.c.head_dim;
+    const int rc = dim <= 64 ? by_rows(std::integral_constant<int, 64>()) : dim <= 128 ? by_rows(std::integral_constant<int, 128>()) : by_rows(std::integral_constant<int, 256>());
+    if (rc != HBP_OK || a.slots == 0) return rc;
+    constexpr int64_t kMost = int64_t(1) << 23;
+    const int64_t joins = a.tiles * a.c.kv_heads * (a.tile_rows / 16);
+    for (int64_t at = 0; at < joins; at += kMost) {
+        k_attend_join<T><<<dim3((unsigned)std::min(joins - at, kMost)), 256, 0, st>>>(a, at);
+        HBP_HIP(hipGetLastError());
+    }
+    return HBP_OK;
+}
+
+}  // namespace
+}  // namespace hbp
