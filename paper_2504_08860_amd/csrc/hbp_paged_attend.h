@@ -69,7 +69,7 @@ template <bool BY_TILE> __device__ __forceinline__ bool find_unit(const Attend &
         total += wave_reduce((float)q.tiles * (float)q.span, [](float p, float q) { return p + q; });
     }
     const float share = fminf(ceilf(total / (float)a.aim), 1073741824.0f);
-    const int32_t length = (max(a.least, (int32_t)share) + kStep - 1) / kStep * kStep;
+    const int32_t length = (max(a.least, __builtin_amdgcn_readfirstlane((int32_t)share)) + kStep - 1) / kStep * kStep;
     int32_t units = 0, slots = 0;   // of the sequences before
     for (int32_t from = 0; from < a.c.sequences; from += kWave) {
         if (from) mine = get(from + lane);
@@ -82,7 +82,7 @@ template <bool BY_TILE> __device__ __forceinline__ bool find_unit(const Attend &
             upto += lane >= d ? u : 0;
             slots_upto += lane >= d ? v : 0;
         }
-        const int32_t all = __shfl(upto, kWave - 1);
+        const int32_t all = __builtin_amdgcn_readlane(upto, kWave - 1);
         if (number < units + all) {
             const int at = __builtin_ctzll(__ballot(number < units + upto));
             auto of = [&](int32_t v) { return __builtin_amdgcn_readlane(v, at); };
@@ -106,7 +106,7 @@ template <bool BY_TILE> __device__ __forceinline__ bool find_unit(const Attend &
             return true;
         }
         units += all;
-        slots += __shfl(slots_upto, kWave - 1);
+        slots += __builtin_amdgcn_readlane(slots_upto, kWave - 1);
     }
     return false;
 }

@@ -82,6 +82,10 @@ __device__ __forceinline__ float4_t multiply(const Operand<float> &a, const Oper
     return multiply_bf16(a.w[0], b.w[0], c);
 }
 
+// a value that is the same in all lanes, as one of the wavefront's
+__device__ __forceinline__ int32_t one(int32_t v) { return __builtin_amdgcn_readfirstlane(v); }
+__device__ __forceinline__ uint32_t one(uint32_t v) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)v); }
+
 // over the four lanes that have the same query
 template <typename F> __device__ __forceinline__ float over_quarters(float v, F op)
 {
@@ -210,13 +214,13 @@ __device__ __forceinline__ void add_odd(const Attend &a, const int32_t *table, i
 
 // Few rows: a workgroup of four wavefronts takes 16 NQ rows, and each wavefront every fourth step of their positions, straight from the cache into registers; the four
 // results are joined in LDS.  The next step's keys are on their way from the scores on, this one's values until the weights are there.
-template <typename T, int D, int NQ, bool ANY_PAGE> __global__ __launch_bounds__(256) void k_attend(Attend a, int64_t first_unit)
+template <typename T, int D, int NQ, bool ANY_PAGE> __global__ __launch_bounds__(256, D * sizeof(T) > 256 ? 1 : 2) void k_attend(Attend a, int64_t first_unit)
 {
     constexpr int kSteps = D / 32, kTiles = D / 16;   // of 32 columns in Q K^T; of 16 in the result, which a lane holds D / 16 neighbouring columns of
     constexpr int kPitch = D + 4;
     __shared__ float joined[4][16][kPitch];
     __shared__ float2 joined_stats[4][16];
-    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, column = lane % 16, quarter = lane / 16;
+    const int lane = threadIdx.x % kWave, wave = one((int32_t)threadIdx.x / kWave), column = lane % 16, quarter = lane / 16;
     const int64_t number = first_unit + blockIdx.x;
     const int32_t unit_number = (int32_t)(number / a.c.kv_heads), kv_head = (int32_t)(number - (int64_t)unit_number * a.c.kv_heads);
     Unit x;
@@ -253,13 +257,13 @@ template <typename T, int D, int NQ, bool ANY_PAGE> __global__ __launch_bounds__
             all_high = min(all_high, high);
         }
     }
-    all_low = wave_reduce(all_low, [](int32_t p, int32_t q) { return max(p, q); });
-    all_high = wave_reduce(all_high, [](int32_t p, int32_t q) { return min(p, q); });
+    all_low = one(wave_reduce(all_low, [](int32_t p, int32_t q) { return max(p, q); }));
+    all_high = one(wave_reduce(all_high, [](int32_t p, int32_t q) { return min(p, q); }));
     const int32_t least_low = x.low;   // (a multiple of kStep: positions from there to the window's are seen by no row, and their values have to go)
     int32_t tile_low = 0x7fffffff;
 #pragma unroll
     for (int n = 0; n < NQ; n++) tile_low = min(tile_low, count[n] ? low[n] : 0x7fffffff);
-    tile_low = max(least_low, wave_reduce(tile_low, [](int32_t p, int32_t q) { return min(p, q); }));
+    tile_low = max(least_low, one(wave_reduce(tile_low, [](int32_t p, int32_t q) { return min(p, q); })));
 
     float m[NQ], l[NQ];
     float4_t o[NQ][kTiles];

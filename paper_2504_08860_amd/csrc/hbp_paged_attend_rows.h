@@ -6,25 +6,26 @@
 namespace hbp {
 namespace {
 
-// A workgroup of four wavefronts takes 64 NQ rows, 16 NQ a wavefront, and walks through their positions in turns of 64 (heads wider than 128: 32), which all four read from LDS: keys and values come
+// A workgroup of eight wavefronts takes 128 NQ rows, 16 NQ a wavefront, and walks through their positions in turns of 64 (heads of up to 64: 128, wider ones than 128: 32), which all of them read from LDS: keys and values come
 // from the cache into registers two turns ahead, values are turned there (eight positions of one column become a lane's share of an operand), and both lie in LDS as operands of the matrix
 // instruction, lane after lane, so that every read is one of 16 bytes a lane without conflicts.  Three buffers and one barrier a turn.  The scores of the next block of 32 positions are
 // multiplied while this one's become weights.
-template <typename T, int D, int NQ> __global__ __launch_bounds__(256) void k_attend_rows(Attend a, int64_t first_unit)
+constexpr int kRowThreads = 512;
+template <typename T, int D, int NQ> __global__ __launch_bounds__(kRowThreads) void k_attend_rows(Attend a, int64_t first_unit)
 {
-    constexpr int kTurn = D > 128 ? 32 : 64, kBlocks = kTurn / kStep, kEights = kTurn / 8;
+    constexpr int kTurn = 8192 / D, kBlocks = kTurn / kStep, kEights = kTurn / 8;
     constexpr int kSteps = D / 32, kTiles = D / 16;
     constexpr int kOperand = 64 * 16;                          // bytes of an operand of a wavefront
     constexpr int kKeyBytes = kBlocks * 2 * kSteps * kOperand, kBytes = 2 * kKeyBytes;   // (as many of values)
-    constexpr int kChunks = D / 8, kKeyRows = 256 / kChunks, kKeyLoads = kTurn / kKeyRows;   // keys: a thread loads a chunk of eight columns of neighbouring positions
-    constexpr int kColumns = D == 64 ? 2 : 4, kQuads = D / kColumns;                         // values: some columns of eight positions
+    constexpr int kChunks = D / 8, kKeyRows = kRowThreads / kChunks, kKeyLoads = kTurn / kKeyRows;   // keys: a thread loads a chunk of eight columns of neighbouring positions
+    constexpr int kColumns = 2, kQuads = D / kColumns;                                        // values: two columns of eight positions
     constexpr int kApart = 16 / (kTiles / kColumns);
-    static_assert(kKeyLoads <= 8 && 256 / kQuads == kEights, "");
+    static_assert(kKeyLoads == 2 && kQuads * kEights == kRowThreads, "");
     extern __shared__ uint4 lds[];
     __shared__ uint32_t held_by[3][kEights];   // whether the cache holds eight positions
     __shared__ int32_t odd_by[3];              // the last turn, and 1, in whose values there are infinities or NaN
     char *const base = reinterpret_cast<char *>(lds);
-    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, column = lane % 16, quarter = lane / 16;
+    const int lane = threadIdx.x % kWave, wave = one((int32_t)threadIdx.x / kWave), column = lane % 16, quarter = lane / 16;
     const int64_t number = first_unit + blockIdx.x;
     const int32_t unit_number = (int32_t)(number / a.c.kv_heads), kv_head = (int32_t)(number - (int64_t)unit_number * a.c.kv_heads);
     Unit x;
@@ -68,10 +69,10 @@ template <typename T, int D, int NQ> __global__ __launch_bounds__(256) void k_at
     }
     auto least = [](int32_t p, int32_t q) { return min(p, q); };
     auto most = [](int32_t p, int32_t q) { return max(p, q); };
-    all_low = wave_reduce(all_low, most);
-    all_high = wave_reduce(all_high, least);
-    some_low = wave_reduce(some_low, least);
-    some_high = wave_reduce(some_high, most);
+    all_low = one(wave_reduce(all_low, most));
+    all_high = one(wave_reduce(all_high, least));
+    some_low = one(wave_reduce(some_low, least));
+    some_high = one(wave_reduce(some_high, most));
     // what the tile's rows see at all, and what all of them do
     const int32_t last_row = min((x.tile + 1) * a.tile_rows, x.rows) - 1;
     const int64_t p0 = x.first_position + a.by_group.divide(x.tile * a.tile_rows), p1 = x.first_position + a.by_group.divide(last_row);
@@ -134,7 +135,7 @@ template <typename T, int D, int NQ> __global__ __launch_bounds__(256) void k_at
                 const int32_t position = turn + 8 * eight + i;
                 const uint32_t seen = held && position >= tile_low && position < end ? 0xffffffffu : 0u;
 #pragma unroll
-                for (int w = 0; w < kColumns / 2; w++) {
+                for (int w = 0; w < Piece<T, kColumns>::kWords; w++) {
                     vf[i].w[w] &= seen;
                     largest = largest_halves(largest, vf[i].w[w] & 0x7fff7fffu);
                 }
@@ -144,7 +145,7 @@ template <typename T, int D, int NQ> __global__ __launch_bounds__(256) void k_at
 #pragma unroll
                 for (int i = 0; i < 8; i++)
 #pragma unroll
-                    for (int w = 0; w < kColumns / 2; w++) vf[i].w[w] = without_odd<T>(vf[i].w[w]);
+                    for (int w = 0; w < Piece<T, kColumns>::kWords; w++) vf[i].w[w] = without_odd<T>(vf[i].w[w]);
             }
         }
         // column c is row c / kTiles of tile c % kTiles
@@ -203,7 +204,8 @@ template <typename T, int D, int NQ> __global__ __launch_bounds__(256) void k_at
             uint32_t held = 0;
 #pragma unroll
             for (int i = 0; i < kEights; i++) held |= held_by[which][i] << i;
-            const bool odd = odd_by[which] == turn + 1;
+            held = one(held);
+            const bool odd = one(odd_by[which]) == turn + 1;
 #pragma unroll
             for (int b = 0; b < kBlocks; b++) {
                 if (b == kBlocks - 1) {
@@ -274,9 +276,8 @@ template <typename T, int D, int NQ> __global__ __launch_bounds__(256) void k_at
 #pragma unroll
                         for (int n = 0; n < NQ; n++) o[n][j] = multiply(value, weights[n], o[n][j]);
                     }
-                    if (odd) {
+                    if (odd)
                         add_odd<T, D, NQ>(a, table, kv_head, block, max(tile_low, block), min(end, block + kStep), weights, low, count, o);
-                    }
                 }
             }
             which = following;
@@ -320,13 +321,13 @@ template <typename T, int D, int NQ> __global__ __launch_bounds__(256) void k_at
 
 template <typename T, int D, int NQ> int launch_rows(const Attend &a, hipStream_t st)
 {
-    constexpr int64_t kMost = int64_t(1) << 23;
-    constexpr size_t kLds = 3 * 2 * (size_t)(D > 128 ? 32 : 64) * D * sizeof(T);
+    constexpr int64_t kMost = int64_t(1) << 22;
+    constexpr size_t kLds = 3 * 2 * 8192 * sizeof(T);
     auto kernel = k_attend_rows<T, D, NQ>;
     HBP_HIP(hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)kLds));
     const int64_t units = (a.tiles + a.aim + 1) * a.c.kv_heads;
     for (int64_t at = 0; at < units; at += kMost) {
-        kernel<<<dim3((unsigned)std::min(units - at, kMost)), 256, kLds, st>>>(a, at);
+        kernel<<<dim3((unsigned)std::min(units - at, kMost)), kRowThreads, kLds, st>>>(a, at);
         HBP_HIP(hipGetLastError());
     }
     return HBP_OK;
@@ -341,9 +342,9 @@ template <typename T> int launch_attend(const Attend &a, hipStream_t st)
         if (any) return launch_units<T, D, 1, true>(a, st);
         if (a.tile_rows == 16) return launch_units<T, D, 1, false>(a, st);
         if constexpr (sizeof(T) == 2) {
-            if (a.tile_rows == 128) return launch_rows<T, D, 2>(a, st);
+            if (a.tile_rows == 128) return launch_rows<T, D, 1>(a, st);
             if constexpr (D < 256)
-                if (a.tile_rows == 256) return launch_rows<T, D, 4>(a, st);
+                if (a.tile_rows == 256) return launch_rows<T, D, 2>(a, st);
         }
         return launch_units<T, D, 2, false>(a, st);
     };
