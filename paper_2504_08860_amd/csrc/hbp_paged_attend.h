@@ -16,11 +16,11 @@ struct Attend {
     uint32_t keep, flip;       // of queries' bits, in both halves of a word: signs change where scale is negative, a scale of 0 leaves zeros
     Divider by_group, by_kv_heads;
     int32_t tile_rows;         // rows (a token's query heads of one head of keys lie together) that a workgroup takes at once
-    int32_t aim, least;        // parts of all tiles of one head of keys, about, and positions that a part has at least
+    int32_t places, aim, least, enough;   // how tiles are split, see find_unit; of one head of keys
     int32_t slots;             // places for results of parts, of each head of keys
     float *partial;            // [slots][kv_heads][tile_rows][head_dim], sums of weights times values
     float2 *partial_stats;     // [slots][kv_heads][tile_rows]: the largest exponent, the sum of weights
-    int64_t tiles;             // at most, of one head of keys
+    int64_t tiles, units;      // at most, of one head of keys
 };
 
 constexpr int kStep = 32;   // positions that a matrix instruction takes at once; parts begin at multiples of it
@@ -28,6 +28,20 @@ constexpr int kStep = 32;   // positions that a matrix instruction takes at once
 int launch_attend_f32(const Attend &a, hipStream_t st);
 int launch_attend_f16(const Attend &a, hipStream_t st);
 int launch_attend_bf16(const Attend &a, hipStream_t st);
+
+// sum over the lanes up to each
+__device__ __forceinline__ int32_t wave_running_sum(int32_t v)
+{
+    auto add = [&](auto control, auto rows) { v += __builtin_amdgcn_update_dpp(0, v, decltype(control)::value, decltype(rows)::value, 0xf, false); };
+    using all = std::integral_constant<int, 0xf>;
+    add(std::integral_constant<int, 0x111>(), all());   // row_shr 1, 2, 4, 8: within rows of 16
+    add(std::integral_constant<int, 0x112>(), all());
+    add(std::integral_constant<int, 0x114>(), all());
+    add(std::integral_constant<int, 0x118>(), all());
+    add(std::integral_constant<int, 0x142>(), std::integral_constant<int, 0xa>());   // the last of a row to the next one, for rows 1 and 3
+    add(std::integral_constant<int, 0x143>(), std::integral_constant<int, 0xc>());   // that of row 1 to rows 2 and 3
+    return v;
+}
 
 // A part of a tile: the rows and the positions that a workgroup takes.
 struct Unit {
@@ -37,11 +51,16 @@ struct Unit {
     int32_t low, high, size;                     // positions that the tile's rows see, from a multiple of kStep on; a part's share
 };
 
-// Finds a unit (or, BY_TILE, a tile) by its number among those of one head of keys: every wavefront for itself, a lane a sequence.  How tiles are split is
-// decided here, from the lengths that the device holds: into parts of about the same length, as many in all as `aim` says, and none of fewer than `least` positions.
-template <bool BY_TILE> __device__ __forceinline__ bool find_unit(const Attend &a, int32_t number, Unit &x)
+// Finds a unit (or, BY_TILE, a tile) by its number among those of one head of keys: by the whole workgroup, some neighbouring sequences a thread.  How tiles are split is
+// decided here, from the lengths that the device holds: into parts of about the same length.  There are to be as many as the chip has places for at once (`places`), so that all of them are busy, but
+// for that none is cut shorter than `least`; beyond `enough` positions they are cut finer, into up to `aim`, which evens out what the places get.
+// Up to 64 sequences each wavefront finds its own, a lane a sequence; more are dealt to the workgroup's threads.  (256 sequences, 64 of them at a time, by each wavefront: 8 us, of loads that wait for
+// each other.)
+template <bool BY_TILE, int THREADS> __device__ __forceinline__ bool find_unit(const Attend &a, int32_t number, Unit &x)
 {
-    const int lane = threadIdx.x % kWave;
+    constexpr int kWaves = THREADS / kWave;
+    __shared__ int32_t work_of[kWaves][3], units_of[kWaves], slots_of[kWaves], found[9];
+    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
     struct Sequence {
         int32_t first, count, taken, length, tiles, span;
     };
@@ -62,53 +81,105 @@ template <bool BY_TILE> __device__ __forceinline__ bool find_unit(const Attend &
         }
         return q;
     };
-    Sequence mine = get(lane);
-    float total = wave_reduce((float)mine.tiles * (float)mine.span, [](float p, float q) { return p + q; });
-    for (int32_t from = kWave; from < a.c.sequences; from += kWave) {
-        const Sequence q = get(from + lane);
-        total += wave_reduce((float)q.tiles * (float)q.span, [](float p, float q) { return p + q; });
+    const bool few = a.c.sequences <= kWave;
+    const int32_t each = few ? 1 : (a.c.sequences + THREADS - 1) / THREADS, mine = few ? lane : (int32_t)threadIdx.x * each;
+    const Sequence own = get(mine);
+    int64_t work = (int64_t)own.tiles * own.span;
+    for (int32_t i = 1; i < each; i++) {
+        const Sequence q = get(mine + i);
+        work += (int64_t)q.tiles * q.span;
     }
-    const float share = fminf(ceilf(total / (float)a.aim), 1073741824.0f);
-    const int32_t length = (max(a.least, __builtin_amdgcn_readfirstlane((int32_t)share)) + kStep - 1) / kStep * kStep;
-    int32_t units = 0, slots = 0;   // of the sequences before
-    for (int32_t from = 0; from < a.c.sequences; from += kWave) {
-        if (from) mine = get(from + lane);
-        const int32_t parts = max(1, (int32_t)((mine.span + length - 1) / length));
-        const int32_t my_units = BY_TILE ? mine.tiles : mine.tiles * parts, my_slots = parts > 1 ? mine.tiles * parts : 0;
-        int32_t upto = my_units, slots_upto = my_slots;
+    // the sum in three pieces of 24 bits, so that it is the same in every kernel in whatever order it is added
+    int32_t piece[3] = {(int32_t)(work & 0xffffff), (int32_t)(work >> 24 & 0xffffff), (int32_t)(work >> 48)};
 #pragma unroll
-        for (int d = 1; d < kWave; d *= 2) {
-            const int32_t u = __shfl_up(upto, d), v = __shfl_up(slots_upto, d);
-            upto += lane >= d ? u : 0;
-            slots_upto += lane >= d ? v : 0;
+    for (int i = 0; i < 3; i++) piece[i] = wave_reduce(piece[i], [](int32_t p, int32_t q) { return p + q; });
+    if (!few) {
+        if (lane == 0)
+#pragma unroll
+            for (int i = 0; i < 3; i++) work_of[wave][i] = piece[i];
+        if (threadIdx.x == 0) found[0] = -1;
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < 3; i++) {
+            piece[i] = 0;
+#pragma unroll
+            for (int w = 0; w < kWaves; w++) piece[i] += work_of[w][i];
         }
-        const int32_t all = __builtin_amdgcn_readlane(upto, kWave - 1);
-        if (number < units + all) {
-            const int at = __builtin_ctzll(__ballot(number < units + upto));
-            auto of = [&](int32_t v) { return __builtin_amdgcn_readlane(v, at); };
-            const int32_t local = number - units - (of(upto) - of(my_units));
-            x.sequence = from + at;
-            x.parts = of(parts);
-            x.tile = BY_TILE ? local : local / x.parts;
-            x.part = BY_TILE ? 0 : local - x.tile * x.parts;
-            // (the latest tiles of a prompt see the most and are taken first)
-            x.tile = of(mine.tiles) - 1 - x.tile;
-            x.slot = slots + of(slots_upto) - of(my_slots) + x.tile * x.parts;
-            x.first_token = of(mine.first);
-            x.rows = of(mine.taken) * a.group;
-            x.first_position = (int64_t)of(mine.length) - of(mine.count);
-            const int32_t row = x.tile * a.tile_rows, last = min(row + a.tile_rows, x.rows) - 1;
-            const int64_t p0 = x.first_position + a.by_group.divide(row), p1 = x.first_position + a.by_group.divide(last);
-            x.low = (int32_t)max((int64_t)0, a.window ? p0 - a.window + 1 : 0) / kStep * kStep;
-            x.high = (int32_t)max((int64_t)0, min(p1 + 1, (int64_t)a.c.capacity));
-            const int32_t span = max(0, x.high - x.low);
-            x.size = ((span + x.parts - 1) / x.parts + kStep - 1) / kStep * kStep;
-            return true;
-        }
-        units += all;
-        slots += __builtin_amdgcn_readlane(slots_upto, kWave - 1);
     }
-    return false;
+    const double total = piece[0] + 16777216.0 * piece[1] + 281474976710656.0 * piece[2];
+    const double share = fmax(fmax(ceil(total / a.aim), fmin(ceil(total / a.places), (double)a.enough)), (double)a.least);
+    const int32_t length = ((int32_t)fmin(share, 1073741824.0) + kStep - 1) / kStep * kStep;
+    auto parts_of = [&](const Sequence &q) { return max(1, (int32_t)((q.span + length - 1) / length)); };
+    auto add = [&](const Sequence &q, int32_t &units, int32_t &slots) {
+        const int32_t parts = parts_of(q);
+        units += BY_TILE ? q.tiles : q.tiles * parts;
+        slots += parts > 1 ? q.tiles * parts : 0;
+    };
+    int32_t units = 0, slots = 0;
+    add(own, units, slots);
+    for (int32_t i = 1; i < each; i++) add(get(mine + i), units, slots);
+    const int32_t upto = wave_running_sum(units), slots_upto = wave_running_sum(slots);
+    int32_t before = upto - units, slots_before = slots_upto - slots;
+    if (!few) {
+        if (lane == kWave - 1) {
+            units_of[wave] = upto;
+            slots_of[wave] = slots_upto;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < kWaves; w++)
+            if (w < wave) {
+                before += units_of[w];
+                slots_before += slots_of[w];
+            }
+    }
+    const bool is_mine = number >= before && number < before + units;
+    Sequence q = own;
+    int32_t at = mine;
+    if (!few && is_mine) {
+        int32_t next = 0, next_slots = 0;
+        add(q, next, next_slots);
+        while (number >= before + next) {
+            before += next;
+            slots_before += next_slots;
+            q = get(++at);
+            next = next_slots = 0;
+            add(q, next, next_slots);
+        }
+    }
+    const int32_t parts = parts_of(q), local = number - before;
+    const int32_t tile = q.tiles - 1 - (BY_TILE ? local : local / parts);   // (the latest tiles of a prompt see the most and are taken first)
+    int32_t values[9] = {at, tile, BY_TILE ? 0 : local % parts, parts, slots_before + tile * parts, q.first, q.taken, q.length, q.count};
+    if (few) {
+        const uint64_t lanes = __ballot(is_mine);
+        if (!lanes) return false;
+        const int owner = __builtin_ctzll(lanes);
+#pragma unroll
+        for (int i = 0; i < 9; i++) values[i] = __builtin_amdgcn_readlane(values[i], owner);
+    } else {
+        if (is_mine)
+#pragma unroll
+            for (int i = 0; i < 9; i++) found[i] = values[i];
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < 9; i++) values[i] = __builtin_amdgcn_readfirstlane(found[i]);
+        if (values[0] < 0) return false;
+    }
+    x.sequence = values[0];
+    x.tile = values[1];
+    x.part = values[2];
+    x.parts = values[3];
+    x.slot = values[4];
+    x.first_token = values[5];
+    x.rows = values[6] * a.group;
+    x.first_position = (int64_t)values[7] - values[8];
+    const int32_t row = x.tile * a.tile_rows, last = min(row + a.tile_rows, x.rows) - 1;
+    const int64_t p0 = x.first_position + a.by_group.divide(row), p1 = x.first_position + a.by_group.divide(last);
+    x.low = (int32_t)max((int64_t)0, a.window ? p0 - a.window + 1 : 0) / kStep * kStep;
+    x.high = (int32_t)max((int64_t)0, min(p1 + 1, (int64_t)a.c.capacity));
+    const int32_t span = max(0, x.high - x.low);
+    x.size = ((span + x.parts - 1) / x.parts + kStep - 1) / kStep * kStep;
+    return true;
 }
 
 }  // namespace hbp

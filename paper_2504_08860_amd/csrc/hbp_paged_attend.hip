@@ -31,10 +31,13 @@ int plan(const hbp_paged_t *cache, int64_t tokens, int heads, int window, int64_
     const int64_t rows = a->tile_rows;
     a->tiles = std::min(tokens * group / rows + cache->sequences, cache->sequences * ((most_new * group + rows - 1) / rows));
     a->least = rows > 32 ? 512 : 4 * kStep;
-    a->aim = (int32_t)std::max<int64_t>(1, (rows > 32 ? 1024 : 2048) / cache->kv_heads);
+    a->enough = rows > 32 ? 2048 : 512;
+    a->places = (int32_t)std::max<int64_t>(1, (rows > 32 ? 256 : 512) / cache->kv_heads);
+    a->aim = (int32_t)std::max<int64_t>(1, (rows > 32 ? 512 : 1024) / cache->kv_heads);
     // Parts of tiles that are split: each is of more than `length` positions, so that its parts are at most twice its positions by `length`, and in all twice `aim`.
     const int64_t span = window ? std::min<int64_t>(a->c.capacity, (int64_t)window + rows) : a->c.capacity, most_parts = (span + a->least - 1) / a->least;
     a->slots = most_parts < 2 ? 0 : (int32_t)std::min<int64_t>(2 * a->aim + 64, a->tiles * most_parts);
+    a->units = std::min(a->tiles + a->aim + 1, a->tiles * std::max<int64_t>(most_parts, 1));   // (each tile one more than its positions by a part's)
     *bytes = (size_t)a->slots * cache->kv_heads * rows * (cache->head_dim * sizeof(float) + sizeof(float2));
     return HBP_OK;
 }

@@ -224,7 +224,7 @@ template <typename T, int D, int NQ, bool ANY_PAGE> __global__ __launch_bounds__
     const int64_t number = first_unit + blockIdx.x;
     const int32_t unit_number = (int32_t)(number / a.c.kv_heads), kv_head = (int32_t)(number - (int64_t)unit_number * a.c.kv_heads);
     Unit x;
-    if (!find_unit<false>(a, unit_number, x)) return;
+    if (!find_unit<false, 256>(a, unit_number, x)) return;
     const int32_t begin = x.low + x.part * x.size, end = min(begin + x.size, x.high);
     const int32_t *table = a.c.table + x.sequence * a.c.ldt;
     const int32_t dim = a.c.head_dim;
@@ -505,35 +505,70 @@ template <typename T, int D, int NQ, bool ANY_PAGE> __global__ __launch_bounds__
     }
 }
 
-// Joins the parts of tiles that were split: a workgroup sixteen rows of a tile.
-template <typename T> __global__ __launch_bounds__(256) void k_attend_join(Attend a, int64_t first)
+// Joins the parts of tiles that were split: a workgroup sixteen rows of a tile, a wavefront a row, LANES lanes a part of it with eight columns each.
+template <typename T, int LANES> __global__ __launch_bounds__(256) void k_attend_join(Attend a, int64_t first)
 {
+    constexpr int kAtOnce = kWave / LANES, kAhead = 4;   // parts side by side, and one behind the other on their way
     const int64_t number = first + blockIdx.x;
     const int32_t groups = a.tile_rows / 16, dim = a.c.head_dim;
     const int64_t tile_head = number / groups;
     const int32_t n = (int32_t)(number - tile_head * groups), tile = (int32_t)(tile_head / a.c.kv_heads), kv_head = (int32_t)(tile_head - (int64_t)tile * a.c.kv_heads);
     Unit x;
-    if (!find_unit<true>(a, tile, x) || x.parts == 1) return;
+    if (!find_unit<true, 256>(a, tile, x) || x.parts == 1) return;
     const int32_t span = max(0, x.high - x.low), parts = x.size ? (span + x.size - 1) / x.size : 0;   // (those with positions)
-    const int32_t chunks = dim / 8;
-    for (int i = threadIdx.x; i < 16 * chunks; i += 256) {
-        const int r = i / chunks, at = i % chunks * 8;
+    const int lane = threadIdx.x % kWave, wave = one((int32_t)threadIdx.x / kWave), which = lane / LANES, at = lane % LANES * 8;
+    const bool mine = at < dim;
+    const int64_t apart = (int64_t)a.c.kv_heads * a.tile_rows;
+    for (int r = wave; r < 16; r += 4) {
         const int32_t row = x.tile * a.tile_rows + n * 16 + r;
-        if (row >= x.rows) continue;
-        const int64_t from = ((int64_t)x.slot * a.c.kv_heads + kv_head) * a.tile_rows + n * 16 + r, apart = (int64_t)a.c.kv_heads * a.tile_rows;
+        if (row >= x.rows) break;
+        const int64_t from = ((int64_t)x.slot * a.c.kv_heads + kv_head) * a.tile_rows + n * 16 + r;
         float top = kLowest, sum = 0.0f, v[8] = {};
-#pragma unroll 8
-        for (int p = 0; p < parts; p++) top = fmaxf(top, a.partial_stats[from + p * apart].x);
-#pragma unroll 4
-        for (int p = 0; p < parts; p++) {
-            const float2 stats = a.partial_stats[from + p * apart];
-            const float4 *sums = reinterpret_cast<const float4 *>(a.partial + (from + p * apart) * dim + at);
-            const float4 one = sums[0], two = sums[1];
-            const float f = __builtin_amdgcn_exp2f(stats.x - top);
-            sum += stats.y * f;
-            v[0] += one.x * f; v[1] += one.y * f; v[2] += one.z * f; v[3] += one.w * f;
-            v[4] += two.x * f; v[5] += two.y * f; v[6] += two.z * f; v[7] += two.w * f;
+        for (int32_t p0 = which; p0 < parts; p0 += kAtOnce * kAhead) {
+            float2 stats[kAhead];
+            float4 one[kAhead], two[kAhead];
+#pragma unroll
+            for (int k = 0; k < kAhead; k++) {
+                const int32_t p = p0 + k * kAtOnce;
+                stats[k] = float2{kLowest, 0.0f};
+                one[k] = two[k] = float4{0, 0, 0, 0};
+                if (p < parts) {
+                    stats[k] = a.partial_stats[from + p * apart];
+                    const float4 *sums = reinterpret_cast<const float4 *>(a.partial + (from + p * apart) * dim + (mine ? at : 0));
+                    one[k] = sums[0];
+                    two[k] = sums[1];
+                }
+            }
+            float higher = top;
+#pragma unroll
+            for (int k = 0; k < kAhead; k++) higher = fmaxf(higher, stats[k].x);
+            const float f = __builtin_amdgcn_exp2f(top - higher);
+            top = higher;
+            sum *= f;
+#pragma unroll
+            for (int i = 0; i < 8; i++) v[i] *= f;
+#pragma unroll
+            for (int k = 0; k < kAhead; k++) {
+                const float g = __builtin_amdgcn_exp2f(stats[k].x - top);
+                sum += stats[k].y * g;
+                v[0] += one[k].x * g; v[1] += one[k].y * g; v[2] += one[k].z * g; v[3] += one[k].w * g;
+                v[4] += two[k].x * g; v[5] += two[k].y * g; v[6] += two[k].z * g; v[7] += two[k].w * g;
+            }
         }
+        float higher = top;
+#pragma unroll
+        for (int d = LANES; d < kWave; d *= 2) higher = fmaxf(higher, __shfl_xor(higher, d));
+        const float f = __builtin_amdgcn_exp2f(top - higher);
+        sum *= f;
+#pragma unroll
+        for (int i = 0; i < 8; i++) v[i] *= f;
+#pragma unroll
+        for (int d = LANES; d < kWave; d *= 2) {
+            sum += __shfl_xor(sum, d);
+#pragma unroll
+            for (int i = 0; i < 8; i++) v[i] += __shfl_xor(v[i], d);
+        }
+        if (which || !mine) continue;
         const int32_t token = a.by_group.divide(row);
         Eight<T> out;
         const float inverse = 1.0f / sum;
@@ -546,7 +581,7 @@ template <typename T> __global__ __launch_bounds__(256) void k_attend_join(Atten
 template <typename T, int D, int NQ, bool ANY_PAGE> int launch_units(const Attend &a, hipStream_t st)
 {
     constexpr int64_t kMost = int64_t(1) << 23;   // workgroups of one launch: a grid's threads are counted in 32 bits
-    const int64_t units = (a.tiles + a.aim + 1) * a.c.kv_heads;   // (each tile one more than its positions by a part's)
+    const int64_t units = a.units * a.c.kv_heads;
     for (int64_t at = 0; at < units; at += kMost) {
         k_attend<T, D, NQ, ANY_PAGE><<<dim3((unsigned)std::min(units - at, kMost)), 256, 0, st>>>(a, at);
         HBP_HIP(hipGetLastError());

@@ -29,7 +29,7 @@ template <typename T, int D, int NQ> __global__ __launch_bounds__(kRowThreads) v
     const int64_t number = first_unit + blockIdx.x;
     const int32_t unit_number = (int32_t)(number / a.c.kv_heads), kv_head = (int32_t)(number - (int64_t)unit_number * a.c.kv_heads);
     Unit x;
-    if (!find_unit<false>(a, unit_number, x)) return;
+    if (!find_unit<false, kRowThreads>(a, unit_number, x)) return;
     const int32_t begin = x.low + x.part * x.size, end = min(begin + x.size, x.high);
     const int32_t *table = a.c.table + x.sequence * a.c.ldt;
     const int32_t dim = a.c.head_dim;
@@ -325,7 +325,7 @@ template <typename T, int D, int NQ> int launch_rows(const Attend &a, hipStream_
     constexpr size_t kLds = 3 * 2 * 8192 * sizeof(T);
     auto kernel = k_attend_rows<T, D, NQ>;
     HBP_HIP(hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)kLds));
-    const int64_t units = (a.tiles + a.aim + 1) * a.c.kv_heads;
+    const int64_t units = a.units * a.c.kv_heads;
     for (int64_t at = 0; at < units; at += kMost) {
         kernel<<<dim3((unsigned)std::min(units - at, kMost)), kRowThreads, kLds, st>>>(a, at);
         HBP_HIP(hipGetLastError());
@@ -354,7 +354,10 @@ template <typename T> int launch_attend(const Attend &a, hipStream_t st)
     constexpr int64_t kMost = int64_t(1) << 23;
     const int64_t joins = a.tiles * a.c.kv_heads * (a.tile_rows / 16);
     for (int64_t at = 0; at < joins; at += kMost) {
-        k_attend_join<T><<<dim3((unsigned)std::min(joins - at, kMost)), 256, 0, st>>>(a, at);
+        const dim3 grid((unsigned)std::min(joins - at, kMost));
+        if (dim <= 64) k_attend_join<T, 8><<<grid, 256, 0, st>>>(a, at);
+        else if (dim <= 128) k_attend_join<T, 16><<<grid, 256, 0, st>>>(a, at);
+        else k_attend_join<T, 32><<<grid, 256, 0, st>>>(a, at);
         HBP_HIP(hipGetLastError());
     }
     return HBP_OK;
