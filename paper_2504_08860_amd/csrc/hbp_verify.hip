@@ -17,6 +17,7 @@ struct RowPart {
 };
 
 constexpr int kThreads = 256, kEach = 16, kPart = kThreads * kEach, kMostParts = kWave;   // (kPart: logits of a part, for up to kMostParts of them; longer rows have longer parts)
+constexpr int kDrawThreads = 512;
 
 struct VerifyArgs {
     const void *logits;
@@ -25,42 +26,44 @@ struct VerifyArgs {
     const int32_t *starts;
     int32_t *new_ids, *accepted;
     RowPart *stats;      // [rows][parts]
-    double *weights;     // [sequences][parts], where there are draft_probs
+    RowPart *decided;    // [sequences], where there are draft_probs: the row that the new token is drawn from, its parts joined
+    int32_t *decided_row;
+    double *weights;     // [sequences][parts], the same
     int64_t ldz, ldp;
     int32_t rows, vocabulary, sequences, id_bytes, parts, part;
 };
 
-// 2^y for y <= 0, to some 2^-42 of it: 2^whole by the exponent's bits, and the series of 2^r = exp(r log 2) for |r| <= 1/2, whose first missing term is (log(2) / 2)^11 / 11! = 2e-13.
-__device__ __forceinline__ double power_of_2(double y)
-{
-    constexpr double c1 = 0.69314718055994531, c2 = c1 * c1 / 2, c3 = c2 * c1 / 3, c4 = c3 * c1 / 4, c5 = c4 * c1 / 5, c6 = c5 * c1 / 6, c7 = c6 * c1 / 7, c8 = c7 * c1 / 8,
-                     c9 = c8 * c1 / 9, c10 = c9 * c1 / 10;
-    y = y < -1100.0 ? -1100.0 : y;   // (0 all the same; NaN stays)
-    const double whole = rint(y), r = y - whole;
-    double v = c10;
-    v = fma(v, r, c9);
-    v = fma(v, r, c8);
-    v = fma(v, r, c7);
-    v = fma(v, r, c6);
-    v = fma(v, r, c5);
-    v = fma(v, r, c4);
-    v = fma(v, r, c3);
-    v = fma(v, r, c2);
-    v = fma(v, r, c1);
-    v = fma(v, r, 1.0);
-    return ldexp(v, (int)whole);
-}
+// 2^(y / 16) for y <= 0, to some 2^-42 of it: y is a whole number of sixteenths, of which the last four bits choose one of sixteen powers (in LDS; they lie in sixteen banks) and the others are the
+// exponent, and a rest x log 2 of at most log 2 / 32, of whose series the first missing term is 1.4e-13.  The whole number comes out of the last bits of a sum with 3 * 2^51.
+struct Powers {
+    double of[16];
+    __device__ __forceinline__ void set()   // (a barrier follows)
+    {
+        if (threadIdx.x < 16) of[threadIdx.x] = exp2(threadIdx.x * 0.0625);
+    }
+    __device__ __forceinline__ double power(double y) const
+    {
+        constexpr double c1 = 0.69314718055994531 / 16, c2 = c1 * c1 / 2, c3 = c2 * c1 / 3, c4 = c3 * c1 / 4, c5 = c4 * c1 / 5, kWhole = 6755399441055744.0;
+        y = fmax(y, -17600.0);   // (0 all the same; passes over NaN)
+        const double sum = y + kWhole, r = y - (sum - kWhole);
+        const int32_t whole = (int32_t)__builtin_bit_cast(uint64_t, sum);
+        const double v = fma(fma(fma(fma(fma(c5, r, c4), r, c3), r, c2), r, c1), r, 1.0);
+        return ldexp(v * of[whole & 15], whole >> 4);
+    }
+};
 
-// what a difference of logits is multiplied by to be an exponent of 2: NaN where the temperature is none; 1 / log 2 where it is 0 (that row's sum says whether it has a NaN)
+// what a difference of logits is multiplied by to be sixteenths of an exponent of 2: NaN where the temperature is none
 __device__ __forceinline__ double per_logit(float temperature)
 {
-    constexpr double kPerLog2 = 1.4426950408889634;
+    constexpr double kPerLog2 = 16 * 1.4426950408889634;
     if (temperature == 0.0f) return kPerLog2;
     return temperature > 0.0f ? kPerLog2 / (double)temperature : (double)NAN;
 }
-__device__ __forceinline__ double exponential(float z, float largest, double per)
+// exp((z - largest) / temperature); per is a number, and NaN is looked for elsewhere
+__device__ __forceinline__ double exponential(const Powers &powers, float z, float largest, double per)
 {
-    return z == -INFINITY ? 0.0 : power_of_2(((double)z - (double)largest) * per);
+    const double e = powers.power(((double)z - (double)largest) * per);
+    return z == -INFINITY ? 0.0 : e;   // (per may be 0)
 }
 
 __device__ __forceinline__ double wave_sum(double v)
@@ -89,76 +92,89 @@ template <typename T> __device__ __forceinline__ void load_logits(const T *z, in
     for (int i = 0; i < 8; i++) f[i] = col + i < end ? v.get(i) : -INFINITY;
 }
 
-// Sums over parts of rows: a part's logits stay in registers between its largest one and the sum.
+// Sums over parts of rows: a part's logits stay in registers between its largest one and the sum.  Bound: the vector unit, some 18 instructions, 13 of them in 64 bits, a logit.
 template <typename T> __global__ __launch_bounds__(kThreads) void k_verify_rows(VerifyArgs a, int32_t first_row)
 {
-    __shared__ float wave_largest[kThreads / kWave];
-    __shared__ int32_t wave_first[kThreads / kWave];
-    __shared__ double wave_sums[kThreads / kWave];
+    constexpr int kWaves = kThreads / kWave;
+    __shared__ float wave_largest[kWaves];
+    __shared__ int32_t wave_first[kWaves];
+    __shared__ double wave_sums[kWaves];
+    __shared__ Powers powers;
     const int32_t row = first_row + blockIdx.y, begin = blockIdx.x * a.part, end = min(begin + a.part, a.vocabulary);
     const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
     const T *z = static_cast<const T *>(a.logits) + (int64_t)row * a.ldz;
-    float largest = -INFINITY;
+    powers.set();
+    float largest = -INFINITY, temperature = 1.0f;
     int32_t first = a.vocabulary;
     double sum = 0.0;
-    double per = 1.4426950408889634;
+    bool odd = false;   // NaN
     for (int32_t from = begin; from < end; from += kPart) {
         float f[kEach / 8][8];
 #pragma unroll
         for (int k = 0; k < kEach / 8; k++) load_logits(z, from + (k * kThreads + (int)threadIdx.x) * 8, end, f[k]);
         if (from == begin && a.temperature) {
             const int32_t s = sequence_of(a.starts, a.sequences, row);
-            if (s < a.sequences) per = per_logit(a.temperature[s]);
+            if (s < a.sequences) temperature = a.temperature[s];
         }
         float m = -INFINITY;
-        int32_t at = a.vocabulary;
 #pragma unroll
         for (int k = 0; k < kEach / 8; k++)
 #pragma unroll
-            for (int i = 0; i < 8; i++)
-                if (f[k][i] > m) {
-                    m = f[k][i];
-                    at = from + (k * kThreads + (int)threadIdx.x) * 8 + i;
-                }
+            for (int i = 0; i < 8; i++) {
+                m = fmaxf(m, f[k][i]);
+                odd |= f[k][i] != f[k][i];
+            }
         const float top = hbp::wave_max(m);
-        const uint32_t index = ~hbp::wave_max(m == top ? ~(uint32_t)at : 0u);   // (the lowest one)
+        int32_t at = a.vocabulary;
+        if (temperature == 0.0f) {
+#pragma unroll
+            for (int k = kEach / 8 - 1; k >= 0; k--)
+#pragma unroll
+                for (int i = 7; i >= 0; i--) at = f[k][i] == top ? from + (k * kThreads + (int)threadIdx.x) * 8 + i : at;
+            at = (int32_t)~hbp::wave_max(top > -INFINITY ? ~(uint32_t)at : ~(uint32_t)a.vocabulary);   // (the lowest one)
+        }
         __syncthreads();
         if (lane == 0) {
             wave_largest[wave] = top;
-            wave_first[wave] = (int32_t)index;
+            wave_first[wave] = at;
         }
         __syncthreads();
         float block_top = wave_largest[0];
         int32_t block_first = wave_first[0];
 #pragma unroll
-        for (int w = 1; w < kThreads / kWave; w++)
+        for (int w = 1; w < kWaves; w++)
             if (wave_largest[w] > block_top || (wave_largest[w] == block_top && wave_first[w] < block_first)) {
                 block_top = wave_largest[w];
                 block_first = wave_first[w];
             }
+        if (temperature != 0.0f) {
+            const double per = per_logit(temperature);
+            if (block_top > largest) sum *= exponential(powers, largest, block_top, per);
+#pragma unroll
+            for (int k = 0; k < kEach / 8; k++)
+#pragma unroll
+                for (int i = 0; i < 8; i++) sum += exponential(powers, f[k][i], fmaxf(block_top, largest), per);
+        }
         if (block_top > largest) {
-            sum *= exponential(largest, block_top, per);
             largest = block_top;
             first = block_first;
         }
-#pragma unroll
-        for (int k = 0; k < kEach / 8; k++)
-#pragma unroll
-            for (int i = 0; i < 8; i++) sum += exponential(f[k][i], largest, per);   // (a NaN makes it NaN)
     }
-    sum = wave_sum(sum);
+    sum = wave_sum(odd ? (double)NAN : sum);
     if (lane == 0) wave_sums[wave] = sum;
     __syncthreads();
     if (threadIdx.x == 0) {
         sum = 0;
 #pragma unroll
-        for (int w = 0; w < kThreads / kWave; w++) sum += wave_sums[w];
+        for (int w = 0; w < kWaves; w++) sum += wave_sums[w];
+        if (temperature == 0.0f && sum == 0.0) sum = largest > -INFINITY ? 1.0 : 0.0;
+        if (largest == INFINITY || !(temperature >= 0.0f)) sum = NAN;
         a.stats[(int64_t)row * a.parts + blockIdx.x] = RowPart{sum, largest, first};
     }
 }
 
 // A whole row, from its parts, by a wavefront
-__device__ __forceinline__ RowPart join_parts(const VerifyArgs &a, int32_t row, double per)
+__device__ __forceinline__ RowPart join_parts(const VerifyArgs &a, const Powers &powers, int32_t row, double per)
 {
     const int lane = threadIdx.x % kWave;
     RowPart mine{0.0, -INFINITY, a.vocabulary};
@@ -167,7 +183,7 @@ __device__ __forceinline__ RowPart join_parts(const VerifyArgs &a, int32_t row, 
     all.largest = hbp::wave_max(mine.largest);
     all.first = (int32_t)~hbp::wave_max(mine.largest == all.largest ? ~(uint32_t)mine.first : 0u);
     // (a part whose sum is NaN keeps it, whatever its largest logit is)
-    all.sum = wave_sum(mine.sum == 0.0 ? 0.0 : mine.sum * exponential(mine.largest, all.largest, per) + (mine.sum != mine.sum ? mine.sum : 0.0));
+    all.sum = wave_sum(mine.sum == 0.0 ? 0.0 : mine.sum * exponential(powers, mine.largest, all.largest, per) + (mine.sum != mine.sum ? mine.sum : 0.0));
     return all;
 }
 
@@ -176,63 +192,64 @@ __device__ __forceinline__ int64_t id_of(const VerifyArgs &a, int32_t row)
     return a.id_bytes == 8 ? static_cast<const int64_t *>(a.ids)[row] : static_cast<const int32_t *>(a.ids)[row];
 }
 
-// p of a token that is one, of a row whose parts are joined: NaN where it has none
-template <typename T> __device__ __forceinline__ double probability(const VerifyArgs &a, int32_t row, int32_t v, const RowPart &all, float temperature, double per)
-{
-    if (!(all.sum > 0.0)) return NAN;
-    if (temperature == 0.0f) return v == all.first ? 1.0 : 0.0;
-    return exponential(to_f32(static_cast<const T *>(a.logits)[(int64_t)row * a.ldz + v]), all.largest, per) / all.sum;
-}
-
 // The first row of begin..end-1 whose draft does not stand (end - 1 where all do), by a workgroup, a wavefront a row; and that row's parts joined, in every thread
-template <typename T>
-__device__ __forceinline__ int32_t first_to_fall(const VerifyArgs &a, int32_t begin, int32_t end, float temperature, double per, RowPart &all, int32_t *wave_falls)
+template <typename T, int THREADS>
+__device__ __forceinline__ int32_t first_to_fall(const VerifyArgs &a, const Powers &powers, int32_t begin, int32_t end, float temperature, double per, RowPart &all)
 {
+    constexpr int kWaves = THREADS / kWave;
+    __shared__ int32_t falls[kWaves];
+    __shared__ RowPart joined[kWaves];
     const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave;
-    int32_t stop = end - 1;
-    for (int32_t from = begin; from < end - 1; from += kThreads / kWave) {
+    for (int32_t from = begin;; from += kWaves) {
         const int32_t row = from + wave;
         bool stands = true;
-        if (row < end - 1) {
-            const RowPart r = join_parts(a, row, per);
-            const int64_t d = id_of(a, row + 1);
-            stands = false;
-            if (d >= 0 && d < a.vocabulary) {
+        RowPart r{0.0, -INFINITY, 0};
+        if (row < end) {
+            const int64_t d = row + 1 < end ? id_of(a, row + 1) : -1;
+            r = join_parts(a, powers, row, per);
+            stands = false;   // (the last row's draft, which is none, never does)
+            if (d >= 0 && d < a.vocabulary && r.sum > 0.0) {
                 const double q = a.draft_probs ? (double)a.draft_probs[(int64_t)row * a.ldp + d] : 1.0;
-                stands = (double)a.uniforms[row] * q < probability<T>(a, row, (int32_t)d, r, temperature, per);
+                const double p = temperature == 0.0f ? (d == r.first ? 1.0 : 0.0)
+                                                     : exponential(powers, to_f32(static_cast<const T *>(a.logits)[(int64_t)row * a.ldz + d]), r.largest, per) / r.sum;
+                stands = (double)a.uniforms[row] * q < p;
             }
         }
         __syncthreads();
-        if (lane == 0) wave_falls[wave] = stands ? end : row;
+        if (lane == 0) {
+            falls[wave] = stands ? end : row;
+            joined[wave] = r;
+        }
         __syncthreads();
         int32_t least = end;
 #pragma unroll
-        for (int w = 0; w < kThreads / kWave; w++) least = min(least, wave_falls[w]);
+        for (int w = 0; w < kWaves; w++) least = min(least, falls[w]);
         if (least < end) {
-            stop = least;
-            break;
+            all = joined[least - from];
+            return least;
         }
     }
-    all = join_parts(a, stop, per);
-    return stop;
 }
 
 // What tokens `col`.. of eight are drawn by: max(p - q, 0), or p (as exponentials, or 1 at the largest) without the draft `d` where there are no draft_probs.
 template <typename T, bool DIFFERENCE>
-__device__ __forceinline__ void weights_of(const VerifyArgs &a, int32_t row, int32_t col, int32_t end, const RowPart &all, float temperature, double per, int64_t d, double (&w)[8])
+__device__ __forceinline__ void weights_of(const VerifyArgs &a, const Powers &powers, int32_t row, int32_t col, int32_t end, const RowPart &all, double inverse, float temperature, double per,
+                                           int64_t d, double (&w)[8])
 {
     float f[8];
     load_logits(static_cast<const T *>(a.logits) + (int64_t)row * a.ldz, col, end, f);
     Eight<float> q;
     if constexpr (DIFFERENCE) q.load_first(a.draft_probs + (int64_t)row * a.ldp + col, end - col);
+    const int32_t gone = d >= col && d < col + 8 ? (int32_t)(d - col) : -1;
 #pragma unroll
     for (int i = 0; i < 8; i++) {
-        double e = temperature == 0.0f ? (col + i == all.first ? 1.0 : 0.0) : exponential(f[i], all.largest, per);
-        if (col + i >= end || col + i == d) e = 0.0;
+        double e = temperature == 0.0f ? (col + i == all.first ? 1.0 : 0.0) : exponential(powers, f[i], all.largest, per);
         if constexpr (DIFFERENCE) {
-            const double p = temperature == 0.0f ? e : e / all.sum;
+            const double p = temperature == 0.0f ? e : e * inverse;
             e = col + i < end ? fmax(p - (double)q.get(i), 0.0) : 0.0;
             if (q.get(i) != q.get(i)) e = NAN;
+        } else if (col + i >= end || i == gone) {
+            e = 0.0;
         }
         w[i] = e;
     }
@@ -241,20 +258,27 @@ __device__ __forceinline__ void weights_of(const VerifyArgs &a, int32_t row, int
 // sum over a part of max(p - q, 0), of the row whose draft does not stand
 template <typename T> __global__ __launch_bounds__(kThreads) void k_verify_differences(VerifyArgs a, int32_t first_sequence)
 {
-    __shared__ int32_t wave_falls[kThreads / kWave];
     __shared__ double wave_sums[kThreads / kWave];
+    __shared__ Powers powers;
     const int32_t s = first_sequence + blockIdx.y, begin = a.starts[s], end = a.starts[s + 1];
     if (begin < 0 || end <= begin || end > a.rows) return;
+    powers.set();
     const float temperature = a.temperature ? a.temperature[s] : 1.0f;
     const double per = per_logit(temperature);
+    __syncthreads();
     RowPart all;
-    const int32_t row = first_to_fall<T>(a, begin, end, temperature, per, all, wave_falls);
+    const int32_t row = first_to_fall<T, kThreads>(a, powers, begin, end, temperature, per, all);
+    if (blockIdx.x == 0 && threadIdx.x == 0) {
+        a.decided[s] = all;
+        a.decided_row[s] = row;
+    }
     if (row == end - 1) return;
     const int32_t from = blockIdx.x * a.part, to = min(from + a.part, a.vocabulary);
+    const double inverse = 1.0 / all.sum;
     double sum = 0.0;
     for (int32_t col = from + threadIdx.x * 8; col < to; col += kThreads * 8) {
         double w[8];
-        weights_of<T, true>(a, row, col, to, all, temperature, per, -1, w);
+        weights_of<T, true>(a, powers, row, col, to, all, inverse, temperature, per, -1, w);
 #pragma unroll
         for (int i = 0; i < 8; i++) sum += w[i];
     }
@@ -270,20 +294,30 @@ template <typename T> __global__ __launch_bounds__(kThreads) void k_verify_diffe
 }
 
 // The drafts that stand and the new token, a workgroup a sequence: the part that the drawn place is in, by the parts' sums, then the token in it.
-template <typename T> __global__ __launch_bounds__(kThreads) void k_verify_draw(VerifyArgs a, int32_t first_sequence)
+template <typename T> __global__ __launch_bounds__(kDrawThreads) void k_verify_draw(VerifyArgs a, int32_t first_sequence)
 {
-    __shared__ int32_t wave_falls[kThreads / kWave];
-    __shared__ double wave_sums[kThreads / kWave];
+    constexpr int kWaves = kDrawThreads / kWave;
+    __shared__ double wave_sums[kWaves];
+    __shared__ int32_t found_by[kWaves], latest_by[kWaves];
+    __shared__ Powers powers;
     const int32_t s = first_sequence + blockIdx.x, begin = a.starts[s], end = a.starts[s + 1];
     if (begin < 0 || end <= begin || end > a.rows) {
         if (threadIdx.x == 0) a.accepted[s] = 0;
         return;
     }
+    powers.set();
     const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
     const float temperature = a.temperature ? a.temperature[s] : 1.0f;
     const double per = per_logit(temperature);
+    __syncthreads();
     RowPart all;
-    const int32_t row = first_to_fall<T>(a, begin, end, temperature, per, all, wave_falls);
+    int32_t row;
+    if (a.draft_probs) {
+        all = a.decided[s];
+        row = a.decided_row[s];
+    } else {
+        row = first_to_fall<T, kDrawThreads>(a, powers, begin, end, temperature, per, all);
+    }
     const bool fell = row < end - 1;
     int64_t d = fell && !a.draft_probs ? id_of(a, row + 1) : -1;
     bool difference = fell && a.draft_probs;
@@ -300,8 +334,8 @@ template <typename T> __global__ __launch_bounds__(kThreads) void k_verify_draw(
         if (temperature == 0.0f) {
             part = lane == all.first / a.part && all.first != without ? 1.0 : 0.0;
         } else {
-            part = mine.sum > 0.0 ? mine.sum * exponential(mine.largest, all.largest, per) : 0.0;
-            if (has) part = fmax(part - exponential(to_f32(static_cast<const T *>(a.logits)[(int64_t)row * a.ldz + without]), all.largest, per), 0.0);
+            part = mine.sum > 0.0 ? mine.sum * exponential(powers, mine.largest, all.largest, per) : 0.0;
+            if (has) part = fmax(part - exponential(powers, to_f32(static_cast<const T *>(a.logits)[(int64_t)row * a.ldz + without]), all.largest, per), 0.0);
         }
         total = wave_sum(part);
     };
@@ -321,16 +355,16 @@ template <typename T> __global__ __launch_bounds__(kThreads) void k_verify_draw(
         if (!over) over = 1ull << (63 - __builtin_clzll(some));   // (roundings: the last one with a weight)
         const int which = __builtin_ctzll(over);
         const double before = __shfl(running, which) - __shfl(part, which);
-        const double left = wanted - before;
+        const double left = wanted - before, inverse = 1.0 / all.sum;
         const int32_t from = which * a.part, to = min(from + a.part, a.vocabulary);
         double base = 0.0;
         int32_t last = -1;   // the last token with a weight so far
-        for (int32_t at = from; at < to && token < 0; at += kThreads * 8) {
+        for (int32_t at = from; at < to && token < 0; at += kDrawThreads * 8) {
             const int32_t col = at + threadIdx.x * 8;
             double w[8];
             if (col < to) {
-                if (difference) weights_of<T, true>(a, row, col, to, all, temperature, per, -1, w);
-                else weights_of<T, false>(a, row, col, to, all, temperature, per, d, w);
+                if (difference) weights_of<T, true>(a, powers, row, col, to, all, inverse, temperature, per, -1, w);
+                else weights_of<T, false>(a, powers, row, col, to, all, inverse, temperature, per, d, w);
             } else {
 #pragma unroll
                 for (int i = 0; i < 8; i++) w[i] = 0.0;
@@ -344,7 +378,7 @@ template <typename T> __global__ __launch_bounds__(kThreads) void k_verify_draw(
             __syncthreads();
             double below = base + upto - mine;
 #pragma unroll
-            for (int k = 0; k < kThreads / kWave; k++) {
+            for (int k = 0; k < kWaves; k++) {
                 if (k < wave) below += wave_sums[k];
                 base += wave_sums[k];
             }
@@ -358,7 +392,6 @@ template <typename T> __global__ __launch_bounds__(kThreads) void k_verify_draw(
                 }
             }
             const int32_t wave_found = (int32_t)~hbp::wave_max(~(uint32_t)found), wave_latest = (int32_t)hbp::wave_max((uint32_t)(latest + 1)) - 1;
-            __shared__ int32_t found_by[kThreads / kWave], latest_by[kThreads / kWave];
             if (lane == 0) {
                 found_by[wave] = wave_found;
                 latest_by[wave] = wave_latest;
@@ -366,7 +399,7 @@ template <typename T> __global__ __launch_bounds__(kThreads) void k_verify_draw(
             __syncthreads();
             found = 0x7fffffff;
 #pragma unroll
-            for (int k = 0; k < kThreads / kWave; k++) {
+            for (int k = 0; k < kWaves; k++) {
                 found = min(found, found_by[k]);
                 last = max(last, latest_by[k]);
             }
@@ -374,7 +407,7 @@ template <typename T> __global__ __launch_bounds__(kThreads) void k_verify_draw(
         }
         if (token < 0) token = last;
     }
-    for (int32_t r = begin + threadIdx.x; r < end; r += kThreads) a.new_ids[r] = r < row ? (int32_t)id_of(a, r + 1) : r == row ? token : -1;
+    for (int32_t r = begin + threadIdx.x; r < end; r += kDrawThreads) a.new_ids[r] = r < row ? (int32_t)id_of(a, r + 1) : r == row ? token : -1;
     if (threadIdx.x == 0) a.accepted[s] = row - begin;
 }
 
@@ -398,7 +431,7 @@ int hbp_verify_drafts_workspace(int64_t rows, int64_t vocabulary, int64_t sequen
     using namespace hbp;
     if (rows < 0 || vocabulary < 1 || sequences < 0 || !bytes) return HBP_ERR_INVALID_ARGUMENT;
     if (rows > (int64_t(1) << 30) || vocabulary > (int64_t(1) << 30) || sequences > (int64_t(1) << 24)) return HBP_ERR_TOO_LARGE;
-    *bytes = rows && sequences ? (size_t)parts_of(vocabulary) * ((size_t)rows * sizeof(RowPart) + (size_t)sequences * sizeof(double)) : 0;
+    *bytes = rows && sequences ? (size_t)parts_of(vocabulary) * ((size_t)rows * sizeof(RowPart) + (size_t)sequences * sizeof(double)) + (size_t)sequences * (sizeof(RowPart) + sizeof(int32_t)) : 0;
     return HBP_OK;
 }
 
@@ -437,7 +470,9 @@ int hbp_verify_drafts(int type, const void *logits, int64_t ldz, int64_t rows, i
     a.parts = parts_of(vocabulary);
     a.part = (int32_t)(((vocabulary + a.parts - 1) / a.parts + 7) / 8 * 8);
     a.stats = static_cast<RowPart *>(workspace);
-    a.weights = reinterpret_cast<double *>(a.stats + rows * a.parts);
+    a.decided = a.stats + rows * a.parts;
+    a.weights = reinterpret_cast<double *>(a.decided + sequences);
+    a.decided_row = reinterpret_cast<int32_t *>(a.weights + sequences * a.parts);
     return by_type(type, [&](auto t) -> int {
         using T = decltype(t);
         constexpr int64_t kMost = 32768;   // of one launch: the grid's second dimension ends at 65535
@@ -451,7 +486,7 @@ int hbp_verify_drafts(int type, const void *logits, int64_t ldz, int64_t rows, i
                 k_verify_differences<T><<<dim3((unsigned)a.parts, count), kThreads, 0, st>>>(a, (int32_t)at);
                 HBP_HIP(hipGetLastError());
             }
-            k_verify_draw<T><<<dim3(count), kThreads, 0, st>>>(a, (int32_t)at);
+            k_verify_draw<T><<<dim3(count), kDrawThreads, 0, st>>>(a, (int32_t)at);
             HBP_HIP(hipGetLastError());
         }
         return HBP_OK;
