@@ -16,8 +16,8 @@ struct RowPart {
     int32_t first;
 };
 
-constexpr int kThreads = 256, kEach = 16, kPart = kThreads * kEach, kMostParts = kWave;   // (kPart: logits of a part, for up to kMostParts of them; longer rows have longer parts)
-constexpr int kDrawThreads = 512;
+constexpr int kThreads = 256, kWaves = kThreads / kWave, kDrawThreads = 512;
+constexpr int kTurn = 16 * kWave, kPart = 2 * kTurn, kMostParts = kWave;   // logits that a wavefront takes at once, and of a part; rows of more than kMostParts such have longer parts
 
 struct VerifyArgs {
     const void *logits;
@@ -33,37 +33,59 @@ struct VerifyArgs {
     int32_t rows, vocabulary, sequences, id_bytes, parts, part;
 };
 
-// 2^(y / 16) for y <= 0, to some 2^-42 of it: y is a whole number of sixteenths, of which the last four bits choose one of sixteen powers (in LDS; they lie in sixteen banks) and the others are the
-// exponent, and a rest x log 2 of at most log 2 / 32, of whose series the first missing term is 1.4e-13.  The whole number comes out of the last bits of a sum with 3 * 2^51.
+// 2^(y / 64) for y <= 0, to some 2^-44 of it: y is a whole number of sixty-fourths, of which the last six bits choose one of sixty-four powers (in LDS) and the others are the
+// exponent, and a rest x log 2 of at most log 2 / 128, of whose series the first missing term is 4e-14.  The whole number comes out of the last bits of a sum with 3 * 2^51.
+constexpr double kFar = -64000.0;   // 2^-1000, and 0 for what is further down
+struct Table {
+    double of[64];
+    constexpr Table() : of{}
+    {
+        for (int i = 0; i < 64; i++) {
+            const double x = i * (0.69314718055994531 / 64);
+            double term = 1.0, sum = 0.0;
+            for (int k = 1; k < 30; k++) {
+                sum += term;
+                term *= x / k;
+            }
+            of[i] = sum;
+        }
+    }
+};
+__device__ const Table kTable;
 struct Powers {
-    double of[16];
+    double of[64];
     __device__ __forceinline__ void set()   // (a barrier follows)
     {
-        if (threadIdx.x < 16) of[threadIdx.x] = exp2(threadIdx.x * 0.0625);
+        if (threadIdx.x < 64) of[threadIdx.x] = kTable.of[threadIdx.x];
     }
-    __device__ __forceinline__ double power(double y) const
+    __device__ __forceinline__ double power_near(double y) const   // y > kFar, or NaN, which stays
     {
-        constexpr double c1 = 0.69314718055994531 / 16, c2 = c1 * c1 / 2, c3 = c2 * c1 / 3, c4 = c3 * c1 / 4, c5 = c4 * c1 / 5, kWhole = 6755399441055744.0;
-        y = fmax(y, -17600.0);   // (0 all the same; passes over NaN)
+        constexpr double c1 = 0.69314718055994531 / 64, c2 = c1 * c1 / 2, c3 = c2 * c1 / 3, c4 = c3 * c1 / 4, kWhole = 6755399441055744.0;
         const double sum = y + kWhole, r = y - (sum - kWhole);
         const int32_t whole = (int32_t)__builtin_bit_cast(uint64_t, sum);
-        const double v = fma(fma(fma(fma(fma(c5, r, c4), r, c3), r, c2), r, c1), r, 1.0);
-        return ldexp(v * of[whole & 15], whole >> 4);
+        const double v = fma(fma(fma(fma(c4, r, c3), r, c2), r, c1), r, 1.0) * of[whole & 63];
+        const uint64_t bits = __builtin_bit_cast(uint64_t, v);
+        const uint32_t high = (uint32_t)(bits >> 32) + ((uint32_t)(whole & ~63) << 14);   // (the exponent's bits begin at 20 of these; a NaN's sum ends in zeros)
+        return __builtin_bit_cast(double, (uint64_t)high << 32 | (uint32_t)bits);
+    }
+    __device__ __forceinline__ double power(double y) const   // NaN gives 0
+    {
+        const double e = power_near(y);
+        return y > kFar ? e : 0.0;
     }
 };
 
-// what a difference of logits is multiplied by to be sixteenths of an exponent of 2: NaN where the temperature is none
+// what a difference of logits is multiplied by to be sixty-fourths of an exponent of 2: NaN where the temperature is none
 __device__ __forceinline__ double per_logit(float temperature)
 {
-    constexpr double kPerLog2 = 16 * 1.4426950408889634;
+    constexpr double kPerLog2 = 64 * 1.4426950408889634;
     if (temperature == 0.0f) return kPerLog2;
     return temperature > 0.0f ? kPerLog2 / (double)temperature : (double)NAN;
 }
 // exp((z - largest) / temperature); per is a number, and NaN is looked for elsewhere
 __device__ __forceinline__ double exponential(const Powers &powers, float z, float largest, double per)
 {
-    const double e = powers.power(((double)z - (double)largest) * per);
-    return z == -INFINITY ? 0.0 : e;   // (per may be 0)
+    return powers.power(((double)z - (double)largest) * per);   // (0 for a masked one, also where per is 0)
 }
 
 __device__ __forceinline__ double wave_sum(double v)
@@ -92,84 +114,94 @@ template <typename T> __device__ __forceinline__ void load_logits(const T *z, in
     for (int i = 0; i < 8; i++) f[i] = col + i < end ? v.get(i) : -INFINITY;
 }
 
-// Sums over parts of rows: a part's logits stay in registers between its largest one and the sum.  Bound: the vector unit, some 18 instructions, 13 of them in 64 bits, a logit.
+// Sums over parts of rows, a wavefront a part: its logits stay in registers between the largest one and the sum, the next ones on their way.  Bound: the vector unit, 11 instructions in 64 bits
+// and 8 others a logit where all of a turn's logits are near enough to the largest to count and none is behind the end; and what a wavefront does beside that, which was as much with 16 logits a lane.
 template <typename T> __global__ __launch_bounds__(kThreads) void k_verify_rows(VerifyArgs a, int32_t first_row)
 {
-    constexpr int kWaves = kThreads / kWave;
-    __shared__ float wave_largest[kWaves];
-    __shared__ int32_t wave_first[kWaves];
-    __shared__ double wave_sums[kWaves];
+    constexpr int kEights = kTurn / kWave / 8;
     __shared__ Powers powers;
-    const int32_t row = first_row + blockIdx.y, begin = blockIdx.x * a.part, end = min(begin + a.part, a.vocabulary);
-    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+    const int lane = threadIdx.x % kWave;
+    const int32_t row = first_row + blockIdx.y, part = __builtin_amdgcn_readfirstlane(blockIdx.x * kWaves + threadIdx.x / kWave);
+    const int32_t begin = min(part * a.part, a.vocabulary), end = min(begin + a.part, a.vocabulary);
     const T *z = static_cast<const T *>(a.logits) + (int64_t)row * a.ldz;
+    Eight<T> next[kEights];
+    auto load = [&](int32_t from) {
+#pragma unroll
+        for (int k = 0; k < kEights; k++) {
+            const int32_t col = from + (k * kWave + lane) * 8;
+            if (from + kTurn <= end) next[k].load(z + col);
+            else next[k].load_first(z + col, end - col);
+        }
+    };
+    load(begin);
     powers.set();
-    float largest = -INFINITY, temperature = 1.0f;
+    float temperature = 1.0f;
+    if (a.temperature) {
+        const int32_t s = __builtin_amdgcn_readfirstlane(sequence_of(a.starts, a.sequences, row));
+        if (s < a.sequences) temperature = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(a.temperature[s])));
+    }
+    const double per = per_logit(temperature);
+    __syncthreads();   // (the powers)
+    float largest = -INFINITY;
     int32_t first = a.vocabulary;
     double sum = 0.0;
     bool odd = false;   // NaN
-    for (int32_t from = begin; from < end; from += kPart) {
-        float f[kEach / 8][8];
+    for (int32_t from = begin; from < end; from += kTurn) {
+        float f[kEights][8], m = largest, low = INFINITY;
 #pragma unroll
-        for (int k = 0; k < kEach / 8; k++) load_logits(z, from + (k * kThreads + (int)threadIdx.x) * 8, end, f[k]);
-        if (from == begin && a.temperature) {
-            const int32_t s = sequence_of(a.starts, a.sequences, row);
-            if (s < a.sequences) temperature = a.temperature[s];
-        }
-        float m = -INFINITY;
+        for (int k = 0; k < kEights; k++)
 #pragma unroll
-        for (int k = 0; k < kEach / 8; k++)
+            for (int i = 0; i < 8; i++) f[k][i] = next[k].get(i);
+        if (from + kTurn > end)
 #pragma unroll
-            for (int i = 0; i < 8; i++) {
-                m = fmaxf(m, f[k][i]);
-                odd |= f[k][i] != f[k][i];
+            for (int k = 0; k < kEights; k++)
+#pragma unroll
+                for (int i = 0; i < 8; i++) f[k][i] = from + (k * kWave + lane) * 8 + i < end ? f[k][i] : -INFINITY;
+        if (from + kTurn < end) load(from + kTurn);
+#pragma unroll
+        for (int k = 0; k < kEights; k++)
+#pragma unroll
+            for (int i = 0; i < 8; i += 2) {
+                asm("v_max3_f32 %0, %1, %2, %0" : "+v"(m) : "v"(f[k][i]), "v"(f[k][i + 1]));   // (fmaxf would make each value canonical first; NaN is passed over)
+                asm("v_min3_f32 %0, %1, %2, %0" : "+v"(low) : "v"(f[k][i]), "v"(f[k][i + 1]));
             }
         const float top = hbp::wave_max(m);
-        int32_t at = a.vocabulary;
         if (temperature == 0.0f) {
+            int32_t at = a.vocabulary;
 #pragma unroll
-            for (int k = kEach / 8 - 1; k >= 0; k--)
+            for (int k = kEights - 1; k >= 0; k--)
 #pragma unroll
-                for (int i = 7; i >= 0; i--) at = f[k][i] == top ? from + (k * kThreads + (int)threadIdx.x) * 8 + i : at;
-            at = (int32_t)~hbp::wave_max(top > -INFINITY ? ~(uint32_t)at : ~(uint32_t)a.vocabulary);   // (the lowest one)
-        }
-        __syncthreads();
-        if (lane == 0) {
-            wave_largest[wave] = top;
-            wave_first[wave] = at;
-        }
-        __syncthreads();
-        float block_top = wave_largest[0];
-        int32_t block_first = wave_first[0];
+                for (int i = 7; i >= 0; i--) {
+                    odd |= f[k][i] != f[k][i];
+                    at = f[k][i] == top ? from + (k * kWave + lane) * 8 + i : at;
+                }
+            at = (int32_t)~hbp::wave_max(~(uint32_t)at);   // (the lowest one)
+            if (top > largest) first = at;
+        } else {
+            if (top > largest) sum *= exponential(powers, largest, top, per);
+            const bool near = ((double)low - (double)top) * per > kFar;
+            if (__ballot(!near) == 0) {
 #pragma unroll
-        for (int w = 1; w < kWaves; w++)
-            if (wave_largest[w] > block_top || (wave_largest[w] == block_top && wave_first[w] < block_first)) {
-                block_top = wave_largest[w];
-                block_first = wave_first[w];
+                for (int k = 0; k < kEights; k++)
+#pragma unroll
+                    for (int i = 0; i < 8; i++) sum += powers.power_near(((double)f[k][i] - (double)top) * per);
+            } else {
+#pragma unroll
+                for (int k = 0; k < kEights; k++)
+#pragma unroll
+                    for (int i = 0; i < 8; i++) {
+                        odd |= f[k][i] != f[k][i];
+                        sum += exponential(powers, f[k][i], top, per);
+                    }
             }
-        if (temperature != 0.0f) {
-            const double per = per_logit(temperature);
-            if (block_top > largest) sum *= exponential(powers, largest, block_top, per);
-#pragma unroll
-            for (int k = 0; k < kEach / 8; k++)
-#pragma unroll
-                for (int i = 0; i < 8; i++) sum += exponential(powers, f[k][i], fmaxf(block_top, largest), per);
         }
-        if (block_top > largest) {
-            largest = block_top;
-            first = block_first;
-        }
+        largest = top;
     }
     sum = wave_sum(odd ? (double)NAN : sum);
-    if (lane == 0) wave_sums[wave] = sum;
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        sum = 0;
-#pragma unroll
-        for (int w = 0; w < kWaves; w++) sum += wave_sums[w];
+    if (lane == 0 && part < a.parts) {
         if (temperature == 0.0f && sum == 0.0) sum = largest > -INFINITY ? 1.0 : 0.0;
         if (largest == INFINITY || !(temperature >= 0.0f)) sum = NAN;
-        a.stats[(int64_t)row * a.parts + blockIdx.x] = RowPart{sum, largest, first};
+        a.stats[(int64_t)row * a.parts + part] = RowPart{sum, largest, first};
     }
 }
 
@@ -255,10 +287,9 @@ __device__ __forceinline__ void weights_of(const VerifyArgs &a, const Powers &po
     }
 }
 
-// sum over a part of max(p - q, 0), of the row whose draft does not stand
+// sums over parts of max(p - q, 0), of the row whose draft does not stand, a wavefront a part
 template <typename T> __global__ __launch_bounds__(kThreads) void k_verify_differences(VerifyArgs a, int32_t first_sequence)
 {
-    __shared__ double wave_sums[kThreads / kWave];
     __shared__ Powers powers;
     const int32_t s = first_sequence + blockIdx.y, begin = a.starts[s], end = a.starts[s + 1];
     if (begin < 0 || end <= begin || end > a.rows) return;
@@ -272,33 +303,28 @@ template <typename T> __global__ __launch_bounds__(kThreads) void k_verify_diffe
         a.decided[s] = all;
         a.decided_row[s] = row;
     }
-    if (row == end - 1) return;
-    const int32_t from = blockIdx.x * a.part, to = min(from + a.part, a.vocabulary);
+    const int32_t part = blockIdx.x * kWaves + threadIdx.x / kWave;
+    if (row == end - 1 || part >= a.parts) return;
     const double inverse = 1.0 / all.sum;
+    const int32_t from = part * a.part, to = min(from + a.part, a.vocabulary);
     double sum = 0.0;
-    for (int32_t col = from + threadIdx.x * 8; col < to; col += kThreads * 8) {
+#pragma unroll 2
+    for (int32_t col = from + threadIdx.x % kWave * 8; col < to; col += kWave * 8) {
         double w[8];
         weights_of<T, true>(a, powers, row, col, to, all, inverse, temperature, per, -1, w);
 #pragma unroll
         for (int i = 0; i < 8; i++) sum += w[i];
     }
     sum = wave_sum(sum);
-    if (threadIdx.x % kWave == 0) wave_sums[threadIdx.x / kWave] = sum;
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        sum = 0;
-#pragma unroll
-        for (int w = 0; w < kThreads / kWave; w++) sum += wave_sums[w];
-        a.weights[(int64_t)s * a.parts + blockIdx.x] = sum;
-    }
+    if (threadIdx.x % kWave == 0) a.weights[(int64_t)s * a.parts + part] = sum;
 }
 
 // The drafts that stand and the new token, a workgroup a sequence: the part that the drawn place is in, by the parts' sums, then the token in it.
 template <typename T> __global__ __launch_bounds__(kDrawThreads) void k_verify_draw(VerifyArgs a, int32_t first_sequence)
 {
-    constexpr int kWaves = kDrawThreads / kWave;
-    __shared__ double wave_sums[kWaves];
-    __shared__ int32_t found_by[kWaves], latest_by[kWaves];
+    constexpr int kDrawWaves = kDrawThreads / kWave;
+    __shared__ double wave_sums[kDrawWaves];
+    __shared__ int32_t found_by[kDrawWaves], latest_by[kDrawWaves];
     __shared__ Powers powers;
     const int32_t s = first_sequence + blockIdx.x, begin = a.starts[s], end = a.starts[s + 1];
     if (begin < 0 || end <= begin || end > a.rows) {
@@ -378,7 +404,7 @@ template <typename T> __global__ __launch_bounds__(kDrawThreads) void k_verify_d
             __syncthreads();
             double below = base + upto - mine;
 #pragma unroll
-            for (int k = 0; k < kWaves; k++) {
+            for (int k = 0; k < kDrawWaves; k++) {
                 if (k < wave) below += wave_sums[k];
                 base += wave_sums[k];
             }
@@ -399,7 +425,7 @@ template <typename T> __global__ __launch_bounds__(kDrawThreads) void k_verify_d
             __syncthreads();
             found = 0x7fffffff;
 #pragma unroll
-            for (int k = 0; k < kWaves; k++) {
+            for (int k = 0; k < kDrawWaves; k++) {
                 found = min(found, found_by[k]);
                 last = max(last, latest_by[k]);
             }
@@ -416,10 +442,13 @@ __global__ void k_verify_nothing(int32_t *accepted, int32_t sequences)
     for (int32_t s = blockIdx.x * blockDim.x + threadIdx.x; s < sequences; s += gridDim.x * blockDim.x) accepted[s] = 0;
 }
 
-int32_t parts_of(int64_t vocabulary)
+// logits of a part: whole turns, so that only the last part of a row ends inside one
+int32_t part_of(int64_t vocabulary)
 {
-    return (int32_t)std::min<int64_t>((vocabulary + kPart - 1) / kPart, kMostParts);
+    const int64_t part = ((vocabulary + kMostParts - 1) / kMostParts + kTurn - 1) / kTurn * kTurn;
+    return (int32_t)std::max<int64_t>(part, kPart);
 }
+int32_t parts_of(int64_t vocabulary) { return (int32_t)((vocabulary + part_of(vocabulary) - 1) / part_of(vocabulary)); }
 
 }  // namespace
 }  // namespace hbp
@@ -468,22 +497,23 @@ int hbp_verify_drafts(int type, const void *logits, int64_t ldz, int64_t rows, i
     a.temperature = temperature; a.draft_probs = draft_probs; a.ldp = ldp;
     a.new_ids = new_ids; a.accepted = accepted;
     a.parts = parts_of(vocabulary);
-    a.part = (int32_t)(((vocabulary + a.parts - 1) / a.parts + 7) / 8 * 8);
+    a.part = part_of(vocabulary);
     a.stats = static_cast<RowPart *>(workspace);
     a.decided = a.stats + rows * a.parts;
     a.weights = reinterpret_cast<double *>(a.decided + sequences);
     a.decided_row = reinterpret_cast<int32_t *>(a.weights + sequences * a.parts);
     return by_type(type, [&](auto t) -> int {
         using T = decltype(t);
+        const unsigned across = (unsigned)((a.parts + kWaves - 1) / kWaves);
         constexpr int64_t kMost = 32768;   // of one launch: the grid's second dimension ends at 65535
         for (int64_t at = 0; at < rows; at += kMost) {
-            k_verify_rows<T><<<dim3((unsigned)a.parts, (unsigned)std::min(rows - at, kMost)), kThreads, 0, st>>>(a, (int32_t)at);
+            k_verify_rows<T><<<dim3(across, (unsigned)std::min(rows - at, kMost)), kThreads, 0, st>>>(a, (int32_t)at);
             HBP_HIP(hipGetLastError());
         }
         for (int64_t at = 0; at < sequences; at += kMost) {
             const unsigned count = (unsigned)std::min(sequences - at, kMost);
             if (draft_probs) {
-                k_verify_differences<T><<<dim3((unsigned)a.parts, count), kThreads, 0, st>>>(a, (int32_t)at);
+                k_verify_differences<T><<<dim3(across, count), kThreads, 0, st>>>(a, (int32_t)at);
                 HBP_HIP(hipGetLastError());
             }
             k_verify_draw<T><<<dim3(count), kDrawThreads, 0, st>>>(a, (int32_t)at);
