@@ -108,7 +108,15 @@ template <bool BY_TILE, int THREADS> __device__ __forceinline__ bool find_unit(c
     }
     const double total = piece[0] + 16777216.0 * piece[1] + 281474976710656.0 * piece[2];
     const double share = fmax(fmax(ceil(total / a.aim), fmin(ceil(total / a.places), (double)a.enough)), (double)a.least);
-    const int32_t length = ((int32_t)fmin(share, 1073741824.0) + kStep - 1) / kStep * kStep;
+    int32_t length = ((int32_t)fmin(share, 1073741824.0) + kStep - 1) / kStep * kStep;
+    // (what the last part of each tile is shorter by makes them more than the places: a second turn of the chip for a few)
+    if (few && length < a.enough)
+        for (int i = 0; i < 4; i++) {
+            const int32_t all = wave_reduce(own.tiles * max(1, (own.span + length - 1) / length), [](int32_t p, int32_t q) { return p + q; });
+            const int64_t longer = ((int64_t)length * all / a.places + kStep) / kStep * kStep;
+            if (all <= a.places || longer > a.enough) break;
+            length = (int32_t)longer;
+        }
     auto parts_of = [&](const Sequence &q) { return max(1, (int32_t)((q.span + length - 1) / length)); };
     auto add = [&](const Sequence &q, int32_t &units, int32_t &slots) {
         const int32_t parts = parts_of(q);

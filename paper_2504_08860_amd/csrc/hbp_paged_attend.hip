@@ -26,8 +26,8 @@ int plan(const hbp_paged_t *cache, int64_t tokens, int heads, int window, int64_
     a->by_group = Divider::of(group);
     a->by_kv_heads = Divider::of(cache->kv_heads);
     const int64_t most_rows = most_new * group;
-    const bool few = most_rows <= 16 || cache->page_size % 8 || cache->type == HBP_F32, wide = cache->head_dim > 128;
-    a->tile_rows = few ? 16 : most_rows <= 32 && !wide ? 32 : most_rows <= 128 || wide ? 128 : 256;
+    const bool wide = cache->head_dim * type_bytes(cache->type) > 256;
+    a->tile_rows = most_rows <= 16 || cache->page_size % 8 ? 16 : most_rows <= 32 && cache->type != HBP_F32 && !wide ? 32 : most_rows <= 128 || wide ? 128 : 256;
     const int64_t rows = a->tile_rows;
     a->tiles = std::min(tokens * group / rows + cache->sequences, cache->sequences * ((most_new * group + rows - 1) / rows));
     a->least = rows > 32 ? 512 : 4 * kStep;

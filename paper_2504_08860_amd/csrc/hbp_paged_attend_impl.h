@@ -176,6 +176,30 @@ template <typename T> __device__ __forceinline__ float weight_of(const Operand<T
     else return to_f32(__builtin_bit_cast(T, (uint16_t)w[0]));
 }
 
+// fp32: parts of an infinite value, and products of parts that overflow, make NaN of what may be a number or an infinity.  Scores of a lane's eight positions of a step that are not finite are computed again.
+__device__ __forceinline__ void by_definition(const Attend &a, const Unit &x, const int32_t *table, int32_t kv_head, int32_t row, bool is_row, int32_t step, int32_t end, float (&e)[8])
+{
+    bool odd = false;
+#pragma unroll
+    for (int i = 0; i < 8; i++) odd |= !(fabsf(e[i]) < INFINITY);
+    if (__ballot(odd) == 0) return;
+    if (!is_row) return;
+    const int32_t token = a.by_group.divide(row);
+    const float *query = static_cast<const float *>(a.q) + (int64_t)(x.first_token + token) * a.ldq + (int64_t)(kv_head * a.group + row - token * a.group) * a.c.head_dim;
+#pragma unroll 1
+    for (int i = 0; i < 8; i++) {
+        const int32_t position = min(step + 8 * ((int)threadIdx.x % kWave / 16) + i, end - 1);
+        const float *key = row_of<float>(a.c.keys, a.c.ldk, a.c, kv_head, slot_of(a.c, table, position));
+        float sum = 0.0f;
+#pragma unroll 1
+        for (int d = 0; d < a.c.head_dim; d++) sum += query[d] * key[d];
+        sum = a.flip ? -sum : sum;
+#pragma unroll
+        for (int j = 0; j < 8; j++)
+            if (j == i && !(fabsf(e[j]) < INFINITY)) e[j] = sum;
+    }
+}
+
 // Adds the infinities and NaN among the values of positions from..to - 1 of a step, for the queries that see them.  (Hardly ever called: it is not to cost registers elsewhere.)
 template <typename T, int D, int NQ>
 __device__ __forceinline__ void add_odd(const Attend &a, const int32_t *table, int32_t kv_head, int32_t step, int32_t from, int32_t to, const Operand<T> (&weights)[NQ],
@@ -357,26 +381,7 @@ template <typename T, int D, int NQ, bool ANY_PAGE> __global__ __launch_bounds__
                 float e[8], p[8];
 #pragma unroll
                 for (int i = 0; i < 8; i++) e[i] = s[n][i / 4][i % 4];
-                if constexpr (sizeof(T) == 4) {
-                    // Parts of an infinite value, and products of parts that overflow, make NaN of what may be a number or an infinity: from the definition
-                    bool odd = false;
-#pragma unroll
-                    for (int i = 0; i < 8; i++) odd |= !(fabsf(e[i]) < INFINITY);
-                    if (__ballot(odd) != 0 && count[n] > 0) {
-                        const int32_t row = x.tile * a.tile_rows + n * 16 + column, token = a.by_group.divide(row);
-                        const float *query = static_cast<const float *>(a.q) + (int64_t)(x.first_token + token) * a.ldq + (int64_t)(kv_head * a.group + row - token * a.group) * dim;
-                        for (int i = 0; i < 8; i++) {
-                            const int32_t position = min(step + 8 * quarter + i, end - 1);
-                            const float *key = row_of<float>(a.c.keys, a.c.ldk, a.c, kv_head, slot_of(a.c, table, position));
-                            float sum = 0.0f;
-                            for (int d = 0; d < dim; d++) sum += query[d] * key[d];
-                            sum = a.flip ? -sum : sum;
-#pragma unroll
-                            for (int j = 0; j < 8; j++)
-                                if (j == i && !(fabsf(e[j]) < INFINITY)) e[j] = sum;
-                        }
-                    }
-                }
+                if constexpr (sizeof(T) == 4) by_definition(a, x, table, kv_head, x.tile * a.tile_rows + n * 16 + column, count[n] > 0, step, end, e);
 #pragma unroll
                 for (int i = 0; i < 8; i++) e[i] = exponent_of(a, e[i]);
                 if (!whole)

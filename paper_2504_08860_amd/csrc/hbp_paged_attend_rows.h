@@ -1,4 +1,4 @@
-// Attention of many rows over a paged cache (prompts): k_attend_rows, for 16-bit types and pages of whole eights of positions.
+// Attention of many rows over a paged cache (prompts): k_attend_rows, for pages of whole eights of positions.
 #pragma once
 
 #include "hbp_paged_attend_impl.h"
@@ -11,19 +11,23 @@ namespace {
 // instruction, lane after lane, so that every read is one of 16 bytes a lane without conflicts.  Three buffers and one barrier a turn.  The scores of the next block of 32 positions are
 // multiplied while this one's become weights.
 constexpr int kRowThreads = 512;
+template <typename T, int D> constexpr int row_turn() { return sizeof(T) == 4 ? (D == 64 ? 64 : 32) : 8192 / D; }
+template <typename T, int D> constexpr int row_buffers() { return sizeof(T) == 4 && D > 128 ? 1 : 3; }   // (as LDS has room for)
+template <typename T, int D> constexpr size_t row_lds() { return row_buffers<T, D>() * 2 * (size_t)row_turn<T, D>() * D * (sizeof(T) == 4 ? 6 : 2); }
 template <typename T, int D, int NQ> __global__ __launch_bounds__(kRowThreads) void k_attend_rows(Attend a, int64_t first_unit)
 {
-    constexpr int kTurn = 8192 / D, kBlocks = kTurn / kStep, kEights = kTurn / 8;
+    constexpr int kParts = sizeof(T) == 4 ? 3 : 1;             // of an operand, see Operand
+    constexpr int kTurn = row_turn<T, D>(), kBuffers = row_buffers<T, D>(), kBlocks = kTurn / kStep, kEights = kTurn / 8;
     constexpr int kSteps = D / 32, kTiles = D / 16;
-    constexpr int kOperand = 64 * 16;                          // bytes of an operand of a wavefront
+    constexpr int kOperand = 64 * 16 * kParts;                 // bytes of an operand of a wavefront
     constexpr int kKeyBytes = kBlocks * 2 * kSteps * kOperand, kBytes = 2 * kKeyBytes;   // (as many of values)
     constexpr int kChunks = D / 8, kKeyRows = kRowThreads / kChunks, kKeyLoads = kTurn / kKeyRows;   // keys: a thread loads a chunk of eight columns of neighbouring positions
-    constexpr int kColumns = 2, kQuads = D / kColumns;                                        // values: two columns of eight positions
+    constexpr int kColumns = D * kEights / kRowThreads, kQuads = D / kColumns;                       // values: one or two columns of eight positions
     constexpr int kApart = 16 / (kTiles / kColumns);
-    static_assert(kKeyLoads == 2 && kQuads * kEights == kRowThreads, "");
+    static_assert(kKeyLoads >= 1 && 8 % kKeyLoads == 0 && kColumns >= 1 && kQuads * kEights == kRowThreads, "");
     extern __shared__ uint4 lds[];
-    __shared__ uint32_t held_by[3][kEights];   // whether the cache holds eight positions
-    __shared__ int32_t odd_by[3];              // the last turn, and 1, in whose values there are infinities or NaN
+    __shared__ uint32_t held_by[kBuffers][kEights];   // whether the cache holds eight positions
+    __shared__ int32_t odd_by[kBuffers];              // the last turn, and 1, in whose values there are infinities or NaN
     char *const base = reinterpret_cast<char *>(lds);
     const int lane = threadIdx.x % kWave, wave = one((int32_t)threadIdx.x / kWave), column = lane % 16, quarter = lane / 16;
     const int64_t number = first_unit + blockIdx.x;
@@ -118,17 +122,24 @@ template <typename T, int D, int NQ> __global__ __launch_bounds__(kRowThreads) v
     auto put = [&](int32_t turn, int which, bool held) {
         char *const keys = base + which * kBytes, *const values = keys + kKeyBytes;
         const uint32_t there = 8 * key_chunk < dim ? 0xffffffffu : 0u;
+        auto store = [](char *to, const Operand<T> &v) {
+            const uint4_t *parts = reinterpret_cast<const uint4_t *>(&v);
+#pragma unroll
+            for (int k = 0; k < kParts; k++) *reinterpret_cast<uint4_t *>(to + k * 64 * 16) = parts[k];
+        };
 #pragma unroll
         for (int i = 0; i < kKeyLoads; i++) {
             const int position = key_row + i, block = position / kStep, h = position / 4 % 2, r = position / 8 % 4 * 4 + position % 4;
             const int operand = (block * 2 + h) * kSteps + key_chunk / 4;
-            *reinterpret_cast<uint4_t *>(keys + operand * kOperand + (key_chunk % 4 * 16 + (r ^ (key_chunk % 16))) * 16) =
-                uint4_t{kf[i].w[0] & there, kf[i].w[1] & there, kf[i].w[2] & there, kf[i].w[3] & there};
+#pragma unroll
+            for (int w = 0; w < Piece<T, 8>::kWords; w++) kf[i].w[w] &= there;
+            store(keys + operand * kOperand + (key_chunk % 4 * 16 + (r ^ (key_chunk % 16))) * 16, Operand<T>::of(kf[i].w));
         }
         if (quad == 0) held_by[which][eight] = held;
-        // Values that no row sees must not be there at all, not even with a weight of 0; infinities and NaN that only some rows see are taken out, and added for those rows
+        // Values that no row sees must not be there at all, not even with a weight of 0; infinities and NaN are taken out where only some rows see them (in fp32 everywhere: parts of an
+        // infinity make NaN), and added for those rows
         const bool edge = turn < tile_all_low || (int64_t)turn + kTurn > tile_all_high || turn + kTurn > end;   // (the same in all threads)
-        if (edge || !held) {
+        if (edge || !held || sizeof(T) == 4) {
             uint32_t largest = 0;
 #pragma unroll
             for (int i = 0; i < 8; i++) {
@@ -137,10 +148,11 @@ template <typename T, int D, int NQ> __global__ __launch_bounds__(kRowThreads) v
 #pragma unroll
                 for (int w = 0; w < Piece<T, kColumns>::kWords; w++) {
                     vf[i].w[w] &= seen;
-                    largest = largest_halves(largest, vf[i].w[w] & 0x7fff7fffu);
+                    if constexpr (sizeof(T) == 4) largest = max(largest, vf[i].w[w] & 0x7fffffffu);
+                    else largest = largest_halves(largest, vf[i].w[w] & 0x7fff7fffu);
                 }
             }
-            if (edge && has_odd<T>(largest)) {
+            if ((edge || sizeof(T) == 4) && has_odd<T>(largest)) {
                 odd_by[which] = turn + 1;   // (every thread that finds one says the same)
 #pragma unroll
                 for (int i = 0; i < 8; i++)
@@ -151,22 +163,33 @@ template <typename T, int D, int NQ> __global__ __launch_bounds__(kRowThreads) v
         // column c is row c / kTiles of tile c % kTiles
 #pragma unroll
         for (int i = 0; i < kColumns; i++) {
-            uint4_t w;
+            uint32_t w[sizeof(T) * 2];
+            if constexpr (sizeof(T) == 4) {
 #pragma unroll
-            for (int k = 0; k < 4; k++) {
-                const uint32_t one = vf[2 * k].w[i / 2], two = vf[2 * k + 1].w[i / 2];
-                w[k] = i & 1 ? high_halves(one, two) : low_halves(one, two);
+                for (int k = 0; k < 8; k++) w[k] = vf[k].w[i];
+            } else {
+#pragma unroll
+                for (int k = 0; k < 4; k++) {
+                    const uint32_t one = vf[2 * k].w[i / 2], two = vf[2 * k + 1].w[i / 2];
+                    w[k] = i & 1 ? high_halves(one, two) : low_halves(one, two);
+                }
             }
             const int at = kColumns * quad + i, r = at / kTiles, j = at % kTiles;
             const int operand = eight / 4 * kTiles + j;
-            *reinterpret_cast<uint4_t *>(values + operand * kOperand + (eight % 4 * 16 + (r ^ (j / kColumns * kApart))) * 16) = w;
+            store(values + operand * kOperand + (eight % 4 * 16 + (r ^ (j / kColumns * kApart))) * 16, Operand<T>::of(w));
         }
     };
     // what has been written to LDS is there for all; loads from the cache stay on their way
     auto barrier = [&] {
         asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
     };
-    const int key_place = quarter * 16, value_place = quarter * 16;
+    auto operand_at = [](const char *from) {
+        Operand<T> v;
+        uint4_t *parts = reinterpret_cast<uint4_t *>(&v);
+#pragma unroll
+        for (int k = 0; k < kParts; k++) parts[k] = *reinterpret_cast<const uint4_t *>(from + k * 64 * 16);
+        return v;
+    };
     auto scores = [&](float4_t (&s)[NQ][2], int which, int b) {
         const char *const keys = base + which * kBytes;
 #pragma unroll
@@ -175,31 +198,41 @@ template <typename T, int D, int NQ> __global__ __launch_bounds__(kRowThreads) v
         for (int k = 0; k < kSteps; k++)
 #pragma unroll
             for (int h = 0; h < 2; h++) {
-                const Operand<T> key{*reinterpret_cast<const uint4_t *>(keys + ((b * 2 + h) * kSteps + k) * kOperand + (key_place + (column ^ ((4 * k + quarter) % 16))) * 16)};
+                const Operand<T> key = operand_at(keys + ((b * 2 + h) * kSteps + k) * kOperand + (quarter * 16 + (column ^ ((4 * k + quarter) % 16))) * 16);
 #pragma unroll
                 for (int n = 0; n < NQ; n++) s[n][h] = multiply(key, q[n][k], s[n][h]);
             }
     };
 
-    if (threadIdx.x < 3) odd_by[threadIdx.x] = 0;
+    if (threadIdx.x < kBuffers) odd_by[threadIdx.x] = 0;
     if (begin < end) {
         Places next = places(begin);
         load(next);
         bool held_next = next.v.page >= 0;
         next = places(begin + kTurn);
-        __syncthreads();
-        put(begin, 0, held_next);
-        load(next);
-        held_next = next.v.page >= 0;
-        next = places(begin + 2 * kTurn);
-        barrier();
+        if constexpr (kBuffers > 1) {
+            __syncthreads();
+            put(begin, 0, held_next);
+            load(next);
+            held_next = next.v.page >= 0;
+            next = places(begin + 2 * kTurn);
+            barrier();
+        }
         float4_t s[NQ][2];
         bool ready = false;    // s has the scores of the turn's first block
         int which = 0;
         for (int32_t turn = begin; turn < end; turn += kTurn) {
-            const int following = which == 2 ? 0 : which + 1;
+            const int following = kBuffers == 1 || which == 2 ? 0 : which + 1;
+            if constexpr (kBuffers == 1) {
+                __syncthreads();   // (nobody reads the turn before this one's operands any more)
+                put(turn, 0, held_next);
+                load(next);
+                held_next = next.v.page >= 0;
+                next = places(turn + 2 * kTurn);
+                barrier();
+            }
             const bool active = turn < some_high && turn + kTurn > some_low;   // (the same in all lanes)
-            if (active && !ready) scores(s, which, 0);
+            if (active && (!ready || kBuffers == 1)) scores(s, which, 0);
             ready = active;
             uint32_t held = 0;
 #pragma unroll
@@ -208,7 +241,7 @@ template <typename T, int D, int NQ> __global__ __launch_bounds__(kRowThreads) v
             const bool odd = one(odd_by[which]) == turn + 1;
 #pragma unroll
             for (int b = 0; b < kBlocks; b++) {
-                if (b == kBlocks - 1) {
+                if (kBuffers > 1 && b == kBlocks - 1) {
                     if (turn + kTurn < end) put(turn + kTurn, following, held_next);
                     load(next);
                     held_next = next.v.page >= 0;
@@ -216,6 +249,16 @@ template <typename T, int D, int NQ> __global__ __launch_bounds__(kRowThreads) v
                 }
                 const int32_t block = turn + b * kStep;
                 if (active) {
+                    if constexpr (sizeof(T) == 4)
+#pragma unroll
+                        for (int n = 0; n < NQ; n++) {
+                            float e[8];
+#pragma unroll
+                            for (int i = 0; i < 8; i++) e[i] = s[n][i / 4][i % 4];
+                            by_definition(a, x, table, kv_head, first_row + n * 16 + column, count[n] > 0, block, end, e);
+#pragma unroll
+                            for (int i = 0; i < 8; i++) s[n][i / 4][i % 4] = e[i];
+                        }
                     if (a.cap_out != 0.0f) {
 #pragma unroll
                         for (int n = 0; n < NQ; n++)
@@ -255,7 +298,7 @@ template <typename T, int D, int NQ> __global__ __launch_bounds__(kRowThreads) v
                         }
                     }
                 }
-                if (b == kBlocks - 1) barrier();   // (the next turn's operands are in LDS; their buffer was read last in the turn before this one)
+                if (kBuffers > 1 && b == kBlocks - 1) barrier();   // (the next turn's operands are in LDS; their buffer was read last in the turn before this one)
                 if (active) {
                     Operand<T> weights[NQ];
 #pragma unroll
@@ -268,11 +311,11 @@ template <typename T, int D, int NQ> __global__ __launch_bounds__(kRowThreads) v
                         }
                         weights[n] = Operand<T>::of(p);
                     }
-                    scores(s, b == kBlocks - 1 ? following : which, b == kBlocks - 1 ? 0 : b + 1);   // (behind the last turn of nothing, for nothing)
+                    if (kBuffers > 1 || b < kBlocks - 1) scores(s, b == kBlocks - 1 ? following : which, b == kBlocks - 1 ? 0 : b + 1);   // (behind the last turn of nothing, for nothing)
                     const char *const values = base + which * kBytes + kKeyBytes;
 #pragma unroll
                     for (int j = 0; j < kTiles; j++) {
-                        const Operand<T> value{*reinterpret_cast<const uint4_t *>(values + (b * kTiles + j) * kOperand + (value_place + (column ^ (j / kColumns * kApart))) * 16)};
+                        const Operand<T> value = operand_at(values + (b * kTiles + j) * kOperand + (quarter * 16 + (column ^ (j / kColumns * kApart))) * 16);
 #pragma unroll
                         for (int n = 0; n < NQ; n++) o[n][j] = multiply(value, weights[n], o[n][j]);
                     }
@@ -322,7 +365,7 @@ template <typename T, int D, int NQ> __global__ __launch_bounds__(kRowThreads) v
 template <typename T, int D, int NQ> int launch_rows(const Attend &a, hipStream_t st)
 {
     constexpr int64_t kMost = int64_t(1) << 22;
-    constexpr size_t kLds = 3 * 2 * 8192 * sizeof(T);
+    constexpr size_t kLds = row_lds<T, D>();
     auto kernel = k_attend_rows<T, D, NQ>;
     HBP_HIP(hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)kLds));
     const int64_t units = a.units * a.c.kv_heads;
@@ -341,12 +384,11 @@ template <typename T> int launch_attend(const Attend &a, hipStream_t st)
         constexpr int D = decltype(d)::value;
         if (any) return launch_units<T, D, 1, true>(a, st);
         if (a.tile_rows == 16) return launch_units<T, D, 1, false>(a, st);
-        if constexpr (sizeof(T) == 2) {
-            if (a.tile_rows == 128) return launch_rows<T, D, 1>(a, st);
-            if constexpr (D < 256)
-                if (a.tile_rows == 256) return launch_rows<T, D, 2>(a, st);
-        }
-        return launch_units<T, D, 2, false>(a, st);
+        if (a.tile_rows == 128) return launch_rows<T, D, 1>(a, st);
+        if constexpr (D * sizeof(T) < 512)
+            if (a.tile_rows == 256) return launch_rows<T, D, 2>(a, st);
+        if constexpr (D * sizeof(T) <= 256 && sizeof(T) == 2) return launch_units<T, D, 2, false>(a, st);
+        return HBP_ERR_INVALID_ARGUMENT;   // (no such plan)
     };
     const int32_t dim = a.c.head_dim;
     const int rc = dim <= 64 ? by_rows(std::integral_constant<int, 64>()) : dim <= 128 ? by_rows(std::integral_constant<int, 128>()) : by_rows(std::integral_constant<int, 256>());
