@@ -67,19 +67,17 @@ __device__ __forceinline__ float4_t multiply_bf16(uint4_t a, uint4_t b, float4_t
 {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(vec_t<bf16, 8>, a), __builtin_bit_cast(vec_t<bf16, 8>, b), c, 0, 0, 0);
 }
-__device__ __forceinline__ float4_t multiply(const Operand<bf16> &a, const Operand<bf16> &b, float4_t c) { return multiply_bf16(a.w, b.w, c); }
-__device__ __forceinline__ float4_t multiply(const Operand<f16> &a, const Operand<f16> &b, float4_t c)
+__device__ __forceinline__ float4_t multiply(const Operand<bf16> &a, const Operand<bf16> &b, float4_t c, int) { return multiply_bf16(a.w, b.w, c); }
+__device__ __forceinline__ float4_t multiply(const Operand<f16> &a, const Operand<f16> &b, float4_t c, int)
 {
     return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(vec_t<f16, 8>, a.w), __builtin_bit_cast(vec_t<f16, 8>, b.w), c, 0, 0, 0);
 }
-__device__ __forceinline__ float4_t multiply(const Operand<float> &a, const Operand<float> &b, float4_t c)
+// the products of parts that make an fp32 product, small ones first; one of them waits for the sum of the one before, so that several sums are taken in turn
+template <typename T> constexpr int kProducts = sizeof(T) == 4 ? 6 : 1;
+__device__ __forceinline__ float4_t multiply(const Operand<float> &a, const Operand<float> &b, float4_t c, int product)
 {
-    c = multiply_bf16(a.w[1], b.w[1], c);
-    c = multiply_bf16(a.w[0], b.w[2], c);
-    c = multiply_bf16(a.w[2], b.w[0], c);
-    c = multiply_bf16(a.w[0], b.w[1], c);
-    c = multiply_bf16(a.w[1], b.w[0], c);
-    return multiply_bf16(a.w[0], b.w[0], c);
+    constexpr int of_a[6] = {1, 0, 2, 0, 1, 0}, of_b[6] = {1, 2, 0, 1, 0, 0};
+    return multiply_bf16(a.w[of_a[product]], b.w[of_b[product]], c);
 }
 
 // a value that is the same in all lanes, as one of the wavefront's
@@ -241,7 +239,7 @@ __device__ __forceinline__ void add_odd(const Attend &a, const int32_t *table, i
 template <typename T, int D, int NQ, bool ANY_PAGE> __global__ __launch_bounds__(256, D * sizeof(T) > 256 ? 1 : 2) void k_attend(Attend a, int64_t first_unit)
 {
     constexpr int kSteps = D / 32, kTiles = D / 16;   // of 32 columns in Q K^T; of 16 in the result, which a lane holds D / 16 neighbouring columns of
-    constexpr int kPitch = D + 4;
+    constexpr int kPitch = D + 4, kSums = sizeof(T) == 4 ? 2 : 1;   // sums taken in turn
     __shared__ float joined[4][16][kPitch];
     __shared__ float2 joined_stats[4][16];
     const int lane = threadIdx.x % kWave, wave = one((int32_t)threadIdx.x / kWave), column = lane % 16, quarter = lane / 16;
@@ -356,14 +354,19 @@ template <typename T, int D, int NQ, bool ANY_PAGE> __global__ __launch_bounds__
 #pragma unroll
             for (int k = 0; k < kSteps; k++) {
                 const uint32_t there = 32 * k + 8 * quarter < dim ? 0xffffffffu : 0u;
+                Operand<T> key[2];
 #pragma unroll
                 for (int h = 0; h < 2; h++) {
 #pragma unroll
                     for (int i = 0; i < Piece<T, 8>::kWords; i++) kf[h][k].w[i] &= there;
-                    const Operand<T> key = Operand<T>::of(kf[h][k].w);
-#pragma unroll
-                    for (int n = 0; n < NQ; n++) s[n][h] = multiply(key, q[n][k], s[n][h]);
+                    key[h] = Operand<T>::of(kf[h][k].w);
                 }
+#pragma unroll
+                for (int product = 0; product < kProducts<T>; product++)
+#pragma unroll
+                    for (int h = 0; h < 2; h++)
+#pragma unroll
+                        for (int n = 0; n < NQ; n++) s[n][h] = multiply(key[h], q[n][k], s[n][h], product);
             }
             const Places mine = now;
             now = next;
@@ -440,24 +443,32 @@ template <typename T, int D, int NQ, bool ANY_PAGE> __global__ __launch_bounds__
                             for (int w = 0; w < Piece<T, kEach>::kWords; w++) vf[i][c].w[w] = without_odd<T>(vf[i][c].w[w]);
             }
 #pragma unroll
-            for (int j = 0; j < kTiles; j++) {
-                Operand<T> value;
-                if constexpr (sizeof(T) == 4) {
-                    float v[8];
+            for (int j = 0; j < kTiles; j += kSums) {
+                Operand<T> value[kSums];
 #pragma unroll
-                    for (int i = 0; i < 8; i++) v[i] = __uint_as_float(vf[i][j / kEach].w[j % kEach]);
-                    value = Operand<T>::of(v);
-                } else {
-                    uint32_t bits[4];
+                for (int c = 0; c < kSums; c++) {
+                    const int at = j + c;
+                    if constexpr (sizeof(T) == 4) {
+                        float v[8];
 #pragma unroll
-                    for (int i = 0; i < 4; i++) {
-                        const uint32_t one = vf[2 * i][j / kEach].w[j % kEach / 2], two = vf[2 * i + 1][j / kEach].w[j % kEach / 2];
-                        bits[i] = j & 1 ? high_halves(one, two) : low_halves(one, two);
+                        for (int i = 0; i < 8; i++) v[i] = __uint_as_float(vf[i][at / kEach].w[at % kEach]);
+                        value[c] = Operand<T>::of(v);
+                    } else {
+                        uint32_t bits[4];
+#pragma unroll
+                        for (int i = 0; i < 4; i++) {
+                            const uint32_t one = vf[2 * i][at / kEach].w[at % kEach / 2], two = vf[2 * i + 1][at / kEach].w[at % kEach / 2];
+                            bits[i] = at & 1 ? high_halves(one, two) : low_halves(one, two);
+                        }
+                        value[c] = Operand<T>::of(bits);
                     }
-                    value = Operand<T>::of(bits);
                 }
 #pragma unroll
-                for (int n = 0; n < NQ; n++) o[n][j] = multiply(value, weights[n], o[n][j]);
+                for (int product = 0; product < kProducts<T>; product++)
+#pragma unroll
+                    for (int c = 0; c < kSums; c++)
+#pragma unroll
+                        for (int n = 0; n < NQ; n++) o[n][j + c] = multiply(value[c], weights[n], o[n][j + c], product);
             }
             if (odd) {
                 add_odd<T, D, NQ>(a, table, kv_head, step, max(tile_low, step), min(end, step + kStep), weights, low, count, o);

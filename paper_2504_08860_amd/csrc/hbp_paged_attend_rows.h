@@ -23,7 +23,7 @@ template <typename T, int D, int NQ> __global__ __launch_bounds__(kRowThreads) v
     constexpr int kKeyBytes = kBlocks * 2 * kSteps * kOperand, kBytes = 2 * kKeyBytes;   // (as many of values)
     constexpr int kChunks = D / 8, kKeyRows = kRowThreads / kChunks, kKeyLoads = kTurn / kKeyRows;   // keys: a thread loads a chunk of eight columns of neighbouring positions
     constexpr int kColumns = D * kEights / kRowThreads, kQuads = D / kColumns;                       // values: one or two columns of eight positions
-    constexpr int kApart = 16 / (kTiles / kColumns);
+    constexpr int kApart = 16 / (kTiles / kColumns), kSums = sizeof(T) == 4 ? 2 : 1;   // kSums: sums taken in turn
     static_assert(kKeyLoads >= 1 && 8 % kKeyLoads == 0 && kColumns >= 1 && kQuads * kEights == kRowThreads, "");
     extern __shared__ uint4 lds[];
     __shared__ uint32_t held_by[kBuffers][kEights];   // whether the cache holds eight positions
@@ -195,13 +195,17 @@ template <typename T, int D, int NQ> __global__ __launch_bounds__(kRowThreads) v
 #pragma unroll
         for (int n = 0; n < NQ; n++) s[n][0] = s[n][1] = float4_t{0, 0, 0, 0};
 #pragma unroll
-        for (int k = 0; k < kSteps; k++)
+        for (int k = 0; k < kSteps; k++) {
+            Operand<T> key[2];
 #pragma unroll
-            for (int h = 0; h < 2; h++) {
-                const Operand<T> key = operand_at(keys + ((b * 2 + h) * kSteps + k) * kOperand + (quarter * 16 + (column ^ ((4 * k + quarter) % 16))) * 16);
+            for (int h = 0; h < 2; h++) key[h] = operand_at(keys + ((b * 2 + h) * kSteps + k) * kOperand + (quarter * 16 + (column ^ ((4 * k + quarter) % 16))) * 16);
 #pragma unroll
-                for (int n = 0; n < NQ; n++) s[n][h] = multiply(key, q[n][k], s[n][h]);
-            }
+            for (int product = 0; product < kProducts<T>; product++)
+#pragma unroll
+                for (int h = 0; h < 2; h++)
+#pragma unroll
+                    for (int n = 0; n < NQ; n++) s[n][h] = multiply(key[h], q[n][k], s[n][h], product);
+        }
     };
 
     if (threadIdx.x < kBuffers) odd_by[threadIdx.x] = 0;
@@ -314,10 +318,17 @@ template <typename T, int D, int NQ> __global__ __launch_bounds__(kRowThreads) v
                     if (kBuffers > 1 || b < kBlocks - 1) scores(s, b == kBlocks - 1 ? following : which, b == kBlocks - 1 ? 0 : b + 1);   // (behind the last turn of nothing, for nothing)
                     const char *const values = base + which * kBytes + kKeyBytes;
 #pragma unroll
-                    for (int j = 0; j < kTiles; j++) {
-                        const Operand<T> value = operand_at(values + (b * kTiles + j) * kOperand + (quarter * 16 + (column ^ (j / kColumns * kApart))) * 16);
+                    for (int j = 0; j < kTiles; j += kSums) {
+                        Operand<T> value[kSums];
 #pragma unroll
-                        for (int n = 0; n < NQ; n++) o[n][j] = multiply(value, weights[n], o[n][j]);
+                        for (int c = 0; c < kSums; c++)
+                            value[c] = operand_at(values + (b * kTiles + j + c) * kOperand + (quarter * 16 + (column ^ ((j + c) / kColumns * kApart))) * 16);
+#pragma unroll
+                        for (int product = 0; product < kProducts<T>; product++)
+#pragma unroll
+                            for (int c = 0; c < kSums; c++)
+#pragma unroll
+                                for (int n = 0; n < NQ; n++) o[n][j + c] = multiply(value[c], weights[n], o[n][j + c], product);
                     }
                     if (odd)
                         add_odd<T, D, NQ>(a, table, kv_head, block, max(tile_low, block), min(end, block + kStep), weights, low, count, o);
