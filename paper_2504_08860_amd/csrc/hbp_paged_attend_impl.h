@@ -521,10 +521,11 @@ template <typename T, int D, int NQ, bool ANY_PAGE> __global__ __launch_bounds__
     }
 }
 
-// Joins the parts of tiles that were split: a workgroup sixteen rows of a tile, a wavefront a row, LANES lanes a part of it with eight columns each.
-template <typename T, int LANES> __global__ __launch_bounds__(256) void k_attend_join(Attend a, int64_t first)
+// Joins the parts of tiles that were split: a workgroup sixteen rows of a tile, LANES lanes a part of a row with eight columns each.  A wavefront has ROWS rows at once, or one with as many parts
+// on their way: what it waits for is the latency of loads.
+template <typename T, int LANES, int ROWS> __global__ __launch_bounds__(256) void k_attend_join(Attend a, int64_t first)
 {
-    constexpr int kAtOnce = kWave / LANES, kAhead = 4;   // parts side by side, and one behind the other on their way
+    constexpr int kAtOnce = kWave / LANES, kAhead = 4 / ROWS;   // parts side by side, and one behind the other on their way
     const int64_t number = first + blockIdx.x;
     const int32_t groups = a.tile_rows / 16, dim = a.c.head_dim;
     const int64_t tile_head = number / groups;
@@ -535,62 +536,79 @@ template <typename T, int LANES> __global__ __launch_bounds__(256) void k_attend
     const int lane = threadIdx.x % kWave, wave = one((int32_t)threadIdx.x / kWave), which = lane / LANES, at = lane % LANES * 8;
     const bool mine = at < dim;
     const int64_t apart = (int64_t)a.c.kv_heads * a.tile_rows;
-    for (int r = wave; r < 16; r += 4) {
-        const int32_t row = x.tile * a.tile_rows + n * 16 + r;
-        if (row >= x.rows) break;
-        const int64_t from = ((int64_t)x.slot * a.c.kv_heads + kv_head) * a.tile_rows + n * 16 + r;
-        float top = kLowest, sum = 0.0f, v[8] = {};
-        for (int32_t p0 = which; p0 < parts; p0 += kAtOnce * kAhead) {
-            float2 stats[kAhead];
-            float4 one[kAhead], two[kAhead];
+    const int32_t tile_row = n * 16, left = x.rows - x.tile * a.tile_rows - tile_row;   // (rows from there on that the sequence has)
+    for (int r0 = wave; r0 < min(16, left); r0 += 4 * ROWS) {
+        float top[ROWS], sum[ROWS], v[ROWS][8];
+        int64_t from[ROWS];
 #pragma unroll
-            for (int k = 0; k < kAhead; k++) {
-                const int32_t p = p0 + k * kAtOnce;
-                stats[k] = float2{kLowest, 0.0f};
-                one[k] = two[k] = float4{0, 0, 0, 0};
-                if (p < parts) {
-                    stats[k] = a.partial_stats[from + p * apart];
-                    const float4 *sums = reinterpret_cast<const float4 *>(a.partial + (from + p * apart) * dim + (mine ? at : 0));
-                    one[k] = sums[0];
-                    two[k] = sums[1];
+        for (int q = 0; q < ROWS; q++) {
+            from[q] = ((int64_t)x.slot * a.c.kv_heads + kv_head) * a.tile_rows + tile_row + min(r0 + 4 * q, left - 1);   // (rows that are not there are read as the last one, for nothing)
+            top[q] = kLowest;
+            sum[q] = 0.0f;
+#pragma unroll
+            for (int i = 0; i < 8; i++) v[q][i] = 0.0f;
+        }
+        for (int32_t p0 = which; p0 < parts; p0 += kAtOnce * kAhead) {
+            float2 stats[ROWS][kAhead];
+            float4 part[ROWS][kAhead][2];
+#pragma unroll
+            for (int q = 0; q < ROWS; q++)
+#pragma unroll
+                for (int k = 0; k < kAhead; k++) {
+                    const int32_t p = p0 + k * kAtOnce;
+                    stats[q][k] = float2{kLowest, 0.0f};
+                    part[q][k][0] = part[q][k][1] = float4{0, 0, 0, 0};
+                    if (p < parts) {
+                        stats[q][k] = a.partial_stats[from[q] + p * apart];
+                        const float4 *sums = reinterpret_cast<const float4 *>(a.partial + (from[q] + p * apart) * dim + (mine ? at : 0));
+                        part[q][k][0] = sums[0];
+                        part[q][k][1] = sums[1];
+                    }
+                }
+#pragma unroll
+            for (int q = 0; q < ROWS; q++) {
+                float higher = top[q];
+#pragma unroll
+                for (int k = 0; k < kAhead; k++) higher = fmaxf(higher, stats[q][k].x);
+                const float f = __builtin_amdgcn_exp2f(top[q] - higher);
+                top[q] = higher;
+                sum[q] *= f;
+#pragma unroll
+                for (int i = 0; i < 8; i++) v[q][i] *= f;
+#pragma unroll
+                for (int k = 0; k < kAhead; k++) {
+                    const float g = __builtin_amdgcn_exp2f(stats[q][k].x - higher);
+                    sum[q] += stats[q][k].y * g;
+                    const float4 one = part[q][k][0], two = part[q][k][1];
+                    v[q][0] += one.x * g; v[q][1] += one.y * g; v[q][2] += one.z * g; v[q][3] += one.w * g;
+                    v[q][4] += two.x * g; v[q][5] += two.y * g; v[q][6] += two.z * g; v[q][7] += two.w * g;
                 }
             }
-            float higher = top;
+        }
 #pragma unroll
-            for (int k = 0; k < kAhead; k++) higher = fmaxf(higher, stats[k].x);
-            const float f = __builtin_amdgcn_exp2f(top - higher);
-            top = higher;
-            sum *= f;
+        for (int q = 0; q < ROWS; q++) {
+            float higher = top[q];
 #pragma unroll
-            for (int i = 0; i < 8; i++) v[i] *= f;
+            for (int d = LANES; d < kWave; d *= 2) higher = fmaxf(higher, __shfl_xor(higher, d));
+            const float f = __builtin_amdgcn_exp2f(top[q] - higher);
+            sum[q] *= f;
 #pragma unroll
-            for (int k = 0; k < kAhead; k++) {
-                const float g = __builtin_amdgcn_exp2f(stats[k].x - top);
-                sum += stats[k].y * g;
-                v[0] += one[k].x * g; v[1] += one[k].y * g; v[2] += one[k].z * g; v[3] += one[k].w * g;
-                v[4] += two[k].x * g; v[5] += two[k].y * g; v[6] += two[k].z * g; v[7] += two[k].w * g;
+            for (int i = 0; i < 8; i++) v[q][i] *= f;
+#pragma unroll
+            for (int d = LANES; d < kWave; d *= 2) {
+                sum[q] += __shfl_xor(sum[q], d);
+#pragma unroll
+                for (int i = 0; i < 8; i++) v[q][i] += __shfl_xor(v[q][i], d);
             }
+            const int r = r0 + 4 * q;
+            if (which || !mine || r >= min(16, left)) continue;
+            const int32_t row = x.tile * a.tile_rows + tile_row + r, token = a.by_group.divide(row);
+            Eight<T> out;
+            const float inverse = 1.0f / sum[q];
+#pragma unroll
+            for (int k = 0; k < 8; k++) out.set(k, sum[q] == 0.0f ? 0.0f : v[q][k] * inverse);
+            out.store(static_cast<T *>(a.out) + (int64_t)(x.first_token + token) * a.ldo + (int64_t)(kv_head * a.group + row - token * a.group) * dim + at);
         }
-        float higher = top;
-#pragma unroll
-        for (int d = LANES; d < kWave; d *= 2) higher = fmaxf(higher, __shfl_xor(higher, d));
-        const float f = __builtin_amdgcn_exp2f(top - higher);
-        sum *= f;
-#pragma unroll
-        for (int i = 0; i < 8; i++) v[i] *= f;
-#pragma unroll
-        for (int d = LANES; d < kWave; d *= 2) {
-            sum += __shfl_xor(sum, d);
-#pragma unroll
-            for (int i = 0; i < 8; i++) v[i] += __shfl_xor(v[i], d);
-        }
-        if (which || !mine) continue;
-        const int32_t token = a.by_group.divide(row);
-        Eight<T> out;
-        const float inverse = 1.0f / sum;
-#pragma unroll
-        for (int k = 0; k < 8; k++) out.set(k, sum == 0.0f ? 0.0f : v[k] * inverse);
-        out.store(static_cast<T *>(a.out) + (int64_t)(x.first_token + token) * a.ldo + (int64_t)(kv_head * a.group + row - token * a.group) * dim + at);
     }
 }
 

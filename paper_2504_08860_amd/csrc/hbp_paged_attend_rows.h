@@ -408,9 +408,13 @@ template <typename T> int launch_attend(const Attend &a, hipStream_t st)
     const int64_t joins = a.tiles * a.c.kv_heads * (a.tile_rows / 16);
     for (int64_t at = 0; at < joins; at += kMost) {
         const dim3 grid((unsigned)std::min(joins - at, kMost));
-        if (dim <= 64) k_attend_join<T, 8><<<grid, 256, 0, st>>>(a, at);
-        else if (dim <= 128) k_attend_join<T, 16><<<grid, 256, 0, st>>>(a, at);
-        else k_attend_join<T, 32><<<grid, 256, 0, st>>>(a, at);
+        auto join = [&](auto lanes) {
+            if (a.tile_rows == 16) k_attend_join<T, decltype(lanes)::value, 1><<<grid, 256, 0, st>>>(a, at);
+            else k_attend_join<T, decltype(lanes)::value, 4><<<grid, 256, 0, st>>>(a, at);
+        };
+        if (dim <= 64) join(std::integral_constant<int, 8>());
+        else if (dim <= 128) join(std::integral_constant<int, 16>());
+        else join(std::integral_constant<int, 32>());
         HBP_HIP(hipGetLastError());
     }
     return HBP_OK;

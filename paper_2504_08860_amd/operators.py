@@ -11,6 +11,7 @@ from __future__ import annotations
 import contextlib
 import ctypes
 import functools
+import struct
 
 import paper_2504_08860_amd as _core
 
@@ -60,6 +61,9 @@ def declare(L) -> None:
     L.hbp_paged_append.argtypes = [paged, i64, vp, i64, vp, i64, vp, i64, i32, vp, i64, vp, i32, i32, vp]
     L.hbp_paged_attention.argtypes = [paged, i64, vp, i64, i32, vp, i64, f32, f32, i32, i64, vp, size, vp]
     L.hbp_paged_attention_workspace.argtypes = [paged, i64, i32, i32, i64, size_out]
+    for name in ("append", "attention"):
+        call = _paged_calls[name] = L["hbp_paged_" + name]
+        call.argtypes, call.restype = [ctypes.c_char_p] + getattr(L, "hbp_paged_" + name).argtypes[1:], ctypes.c_int
     L.hbp_verify_drafts.argtypes = [i32, vp, i64, i64, i64, vp, i32, vp, vp, i64, vp, vp, i64, vp, vp, vp, size, vp]
     L.hbp_verify_drafts_workspace.argtypes = [i64, i64, i64, size_out]
 
@@ -324,39 +328,60 @@ def hbp_token_logprobs_backward(logits, tokens, lse, entropy, g_logp, g_entropy,
 
 # ------------------------------------------------------------------------------------ a paged cache and its attention
 
-def _pages(t, what, shape, dtype, device):
-    """(address, values from one page to the next) of [pages, kv_heads, page_size, head_dim], each page contiguous in itself"""
-    if t.dtype is dtype and t.shape == shape and t.get_device() == device:
-        pages, heads, size, dim = shape
-        apart, of_head, of_row, one = t.stride()
-        if pages < 2:
-            apart = max(apart, heads * size * dim)
-        if one == 1 and (of_row == dim or size < 2) and (of_head == size * dim or heads < 2):
-            return t.data_ptr(), apart
-    raise AssertionError(f"{what}: {dtype} tensor of shape {tuple(shape)} on the current CUDA device required, pages contiguous in themselves")
+# (As above: a call of one token is 3 us of GPU time.  Two tensors that go together are asked side by side, the second one's strides only where they differ, and the
+# struct of the cache is packed, which takes a quarter of the time that building a ctypes one does.)
+def _pages(shape, strides):
+    """Whether pages [kv_heads, page_size, head_dim] are contiguous in themselves."""
+    pages, heads, size, dim = shape
+    apart, of_head, of_row, one = strides
+    return one == 1 and (of_row == dim or size < 2) and (of_head == size * dim or heads < 2)
 
 
-def _heads(t, what, shape, dtype, device):
-    """(address, row stride) of [tokens, heads, head_dim], a token's heads together"""
-    if t.dtype is dtype and t.shape == shape and t.get_device() == device:
+def _heads(a, b, a_what, b_what, shape, dtype, device):
+    """(address, row stride) of two tensors [tokens, heads, head_dim], a token's heads together"""
+    if a.dtype is dtype and b.dtype is dtype and a.shape == shape and b.shape == shape and a.get_device() == device and b.get_device() == device:
         tokens, heads, dim = shape
-        apart, of_head, one = t.stride()
-        if tokens < 2:
-            apart = heads * dim
-        if one == 1 and (of_head == dim or heads < 2) and apart >= heads * dim:
-            return t.data_ptr(), apart
-    raise AssertionError(f"{what}: {dtype} tensor of shape {tuple(shape)} on the current CUDA device required, a token's heads contiguous")
+        a_strides, b_strides = a.stride(), b.stride()
+        a_apart, of_head, one = a_strides
+        if one == 1 and (of_head == dim or heads < 2) and (a_apart >= heads * dim or tokens < 2):
+            b_apart = a_apart
+            if b_strides != a_strides:
+                b_apart, of_head, one = b_strides
+            if one == 1 and (of_head == dim or heads < 2) and (b_apart >= heads * dim or tokens < 2):
+                return a.data_ptr(), a_apart, b.data_ptr(), b_apart
+    raise AssertionError(f"{a_what}, {b_what}: {dtype} tensors of shape {tuple(shape)} on the current CUDA device required, a token's heads contiguous")
+
+
+_pack_paged = struct.Struct("5P6q4i").pack   # an hbp_paged_t
+_paged_calls = {}                            # the entry points, with a packed one for their struct
 
 
 def _cache(keys, values, table, starts, lengths, device):
-    shape, dtype = keys.shape, keys.dtype
+    """(a packed hbp_paged_t, keys' type, kv_heads, head_dim, what the workspace's size goes by)"""
+    shape, dtype, strides = keys.shape, keys.dtype, keys.stride()
     assert len(shape) == 4 and dtype in _types, "keys: float32, float16 or bfloat16 of [pages, kv_heads, page_size, head_dim] required"
+    if not (values.dtype is dtype and values.shape == shape and keys.get_device() == device and values.get_device() == device and _pages(shape, strides)):
+        raise AssertionError(f"keys, values: {dtype} tensors of one shape on the current CUDA device required, pages contiguous in themselves")
+    others = values.stride()
+    assert others == strides or _pages(shape, others), "values: pages contiguous in themselves required"
+    pages, heads, size, dim = shape
+    ldk, ldv = strides[0], others[0]
+    if pages < 2:
+        ldk, ldv = max(ldk, heads * size * dim), max(ldv, heads * size * dim)
     assert table.dim() == 2, "table: int32 matrix required"
-    (k_at, ldk), (v_at, ldv) = _pages(keys, "keys", shape, dtype, device), _pages(values, "values", shape, dtype, device)
     sequences, width = table.shape
-    t_at, ldt = _rows(table, "table", (sequences, width), _i32, device)
-    return hbp_paged_t(k_at, v_at, t_at, _whole(starts, "starts", (sequences + 1,), _i32, device), _whole(lengths, "lengths", (sequences,), _i32, device),
-                       ldk, ldv, ldt, shape[0], sequences, width, _types[dtype], shape[1], shape[2], shape[3])
+    ldt, step = table.stride()
+    if sequences < 2:
+        ldt = width
+    if not (table.dtype is _i32 and table.get_device() == device and ldt >= width and (step == 1 or width < 2)):
+        raise AssertionError("table: int32 matrix on the current CUDA device required, rows contiguous in themselves")
+    if not (starts.dtype is _i32 and lengths.dtype is _i32 and starts.shape == (sequences + 1,) and lengths.shape == (sequences,) and starts.get_device() == device
+            and lengths.get_device() == device and starts.is_contiguous() and lengths.is_contiguous()):
+        raise AssertionError(f"starts, lengths: contiguous int32 vectors of {sequences + 1} and {sequences} on the current CUDA device required")
+    number = _types[dtype]
+    packed = _pack_paged(keys.data_ptr(), values.data_ptr(), table.data_ptr(), starts.data_ptr(), lengths.data_ptr(), ldk, ldv, ldt, pages, sequences, width, number,
+                         heads, size, dim)
+    return packed, dtype, heads, dim, (pages, sequences, width, number, heads, size, dim)
 
 
 def hbp_paged_append(k, v, keys, values, table, starts, lengths, q=None, q_out=None, frequencies=None, interleaved: bool = False, stream=None) -> None:
@@ -364,23 +389,21 @@ def hbp_paged_append(k, v, keys, values, table, starts, lengths, q=None, q_out=N
     int32 [sequences, pages of one]).  Sequence s has rows ``starts[s]`` .. ``starts[s + 1] - 1`` (int32 [sequences + 1]), the last ones of its ``lengths[s]``
     (int32) positions.  ``frequencies`` (float32 [pairs]): keys, and queries ``q`` into ``q_out``, are rotated by their positions on the way."""
     L, device = _start()
-    c = _cache(keys, values, table, starts, lengths, device)
-    dtype, tokens = keys.dtype, k.shape[0]
-    shape = (tokens, c.kv_heads, c.head_dim)
-    k_at, v_at = _heads(k, "k", shape, dtype, device), _heads(v, "v", shape, dtype, device)
+    packed, dtype, kv_heads, dim, _ = _cache(keys, values, table, starts, lengths, device)
+    tokens = k.shape[0]
+    kv = _heads(k, v, "k", "v", (tokens, kv_heads, dim), dtype, device)
     assert (q is None) == (q_out is None), "q and q_out go together"
-    heads, q_at, o_at = 0, (None, 0), (None, 0)
+    heads, q_at, ldq, o_at, ldo = 0, None, 0, None, 0
     if q is not None:
         assert q.dim() == 3, "q: [tokens, heads, head_dim] required"
         heads = q.shape[1]
-        shape = (tokens, heads, c.head_dim)
-        q_at, o_at = _heads(q, "q", shape, dtype, device), _heads(q_out, "q_out", shape, dtype, device)
-    pairs = 0
+        q_at, ldq, o_at, ldo = _heads(q, q_out, "q", "q_out", (tokens, heads, dim), dtype, device)
+    f_at, pairs = None, 0
     if frequencies is not None:
         assert frequencies.dim() == 1, "frequencies: float32 vector required"
         pairs = frequencies.shape[0]
-    status = L.hbp_paged_append(c, tokens, *k_at, *v_at, *q_at, heads, *o_at, _whole(frequencies, "frequencies", (pairs,), _f32, device), pairs,
-                                1 if interleaved else 0, _core._stream_ptr(stream))
+        f_at = _whole(frequencies, "frequencies", (pairs,), _f32, device)
+    status = _paged_calls["append"](packed, tokens, *kv, q_at, ldq, heads, o_at, ldo, f_at, pairs, 1 if interleaved else 0, _core._stream_ptr(stream))
     if status:
         raise _core.HbpError(status, "hbp_paged_append")
 
@@ -400,16 +423,15 @@ def hbp_paged_attention(q, keys, values, table, starts, lengths, out, scale: flo
     them), into ``out``: causal, at most the last ``window`` positions if given, scores times ``scale`` (1 / sqrt(head_dim)) and capped at ``softcap`` if given.
     ``most_new``: no sequence has more new tokens than this (1 for decoding; without it, tokens)."""
     L, device = _start()
-    c = _cache(keys, values, table, starts, lengths, device)
-    shape, dtype = q.shape, keys.dtype
-    assert len(shape) == 3 and shape[2] == c.head_dim, "q: [tokens, heads, head_dim] required"
-    tokens, heads, dim = shape
-    q_at, o_at = _heads(q, "q", shape, dtype, device), _heads(out, "out", shape, dtype, device)
+    packed, dtype, kv_heads, dim, sizes = _cache(keys, values, table, starts, lengths, device)
+    shape = q.shape
+    assert len(shape) == 3 and shape[2] == dim, "q: [tokens, heads, head_dim] required"
+    tokens, heads, _ = shape
+    q_at, ldq, o_at, ldo = _heads(q, out, "q", "out", shape, dtype, device)
     most = tokens if most_new is None else most_new
-    need = _attention_bytes(tokens, heads, window, most, c.pages, c.sequences, c.table_width, c.type, c.kv_heads, c.page_size, dim)
-    at, size, kept = _space(workspace, need, stream, device)
-    status = L.hbp_paged_attention(c, tokens, *q_at, heads, *o_at, dim ** -0.5 if scale is None else scale, softcap, window, most, at, size,
-                                   _core._stream_ptr(stream))
+    at, size, kept = _space(workspace, _attention_bytes(tokens, heads, window, most, *sizes), stream, device)
+    status = _paged_calls["attention"](packed, tokens, q_at, ldq, heads, o_at, ldo, dim ** -0.5 if scale is None else scale, softcap, window, most, at, size,
+                                       _core._stream_ptr(stream))
     if status:
         raise _core.HbpError(status, "hbp_paged_attention")
 
