@@ -14,7 +14,7 @@ constexpr int kRowThreads = 512;
 template <typename T, int D> constexpr int row_turn() { return sizeof(T) == 4 ? (D == 64 ? 64 : 32) : 8192 / D; }
 template <typename T, int D> constexpr int row_buffers() { return sizeof(T) == 4 && D > 128 ? 1 : 3; }   // (as LDS has room for)
 template <typename T, int D> constexpr size_t row_lds() { return row_buffers<T, D>() * 2 * (size_t)row_turn<T, D>() * D * (sizeof(T) == 4 ? 6 : 2); }
-template <typename T, int D, int NQ> __global__ __launch_bounds__(kRowThreads) void k_attend_rows(Attend a, int64_t first_unit)
+template <typename T, int D, int NQ, bool WHOLE> __global__ __launch_bounds__(kRowThreads) void k_attend_rows(Attend a, int64_t first_unit)
 {
     constexpr int kParts = sizeof(T) == 4 ? 3 : 1;             // of an operand, see Operand
     constexpr int kTurn = row_turn<T, D>(), kBuffers = row_buffers<T, D>(), kBlocks = kTurn / kStep, kEights = kTurn / 8;
@@ -26,7 +26,8 @@ template <typename T, int D, int NQ> __global__ __launch_bounds__(kRowThreads) v
     constexpr int kApart = 16 / (kTiles / kColumns), kSums = sizeof(T) == 4 ? 2 : 1;   // kSums: sums taken in turn
     static_assert(kKeyLoads >= 1 && 8 % kKeyLoads == 0 && kColumns >= 1 && kQuads * kEights == kRowThreads, "");
     extern __shared__ uint4 lds[];
-    __shared__ uint32_t held_by[kBuffers][kEights];   // whether the cache holds eight positions
+    __shared__ int64_t keys_at[4][kEights], values_at[4][kEights];   // of four turns: where eight positions' rows begin, in values; odd: the cache does not hold them
+    __shared__ uint32_t held_by[4];                                  // bits of the eights that it holds
     __shared__ int32_t odd_by[kBuffers];              // the last turn, and 1, in whose values there are infinities or NaN
     char *const base = reinterpret_cast<char *>(lds);
     const int lane = threadIdx.x % kWave, wave = one((int32_t)threadIdx.x / kWave), column = lane % 16, quarter = lane / 16;
@@ -36,7 +37,7 @@ template <typename T, int D, int NQ> __global__ __launch_bounds__(kRowThreads) v
     if (!find_unit<false, kRowThreads>(a, unit_number, x)) return;
     const int32_t begin = x.low + x.part * x.size, end = min(begin + x.size, x.high);
     const int32_t *table = a.c.table + x.sequence * a.c.ldt;
-    const int32_t dim = a.c.head_dim;
+    const int32_t dim = WHOLE ? D : a.c.head_dim;   // (WHOLE: loads of neighbouring rows have one address and offsets in their instructions, and nothing is behind the last column)
     const int32_t first_row = x.tile * a.tile_rows + wave * 16 * NQ;
 
     Operand<T> q[NQ][kSteps];
@@ -99,29 +100,48 @@ template <typename T, int D, int NQ> __global__ __launch_bounds__(kRowThreads) v
     Piece<T, kColumns> vf[8];
     const int key_chunk = threadIdx.x % kChunks, key_row = threadIdx.x / kChunks * kKeyLoads;   // positions key_row ..
     const int quad = threadIdx.x % kQuads, eight = threadIdx.x / kQuads;
-    struct Places {
-        Slot k, v;
-    };
+    // Where a turn's rows are is looked up once for each eight positions, by a thread of the first wavefront, two turns before they are loaded: the table's entry in one turn, the addresses in the next.
     const int32_t last_eight = (end - 1) / 8 * 8;
-    auto places = [&](int32_t turn) {   // (of positions moved back before the end: what is read there has no weight)
-        Places p;
-        p.k = slot_of(a.c, table, min(turn + key_row / 8 * 8, last_eight));
-        p.k.within += key_row % 8;
-        p.v = slot_of(a.c, table, min(turn + 8 * eight, last_eight));
-        return p;
+    int32_t entry = 0, entry_position = 0;
+    auto look_up = [&](int32_t turn, int i) {   // (of positions moved back before the end: what is read there has no weight)
+        entry_position = min(turn + 8 * i, last_eight);
+        entry = table[a.c.by_page.divide(entry_position)];
     };
-    auto load = [&](const Places &p) {
-        const T *keys = row_of<T>(a.c.keys, a.c.ldk, a.c, kv_head, p.k) + (8 * key_chunk < dim ? 8 * key_chunk : 0);
-        const T *values = row_of<T>(a.c.values, a.c.ldv, a.c, kv_head, p.v) + (kColumns * quad < dim ? kColumns * quad : 0);
+    auto tell = [&](int which, int i) {
+        const bool held = entry >= 0 && entry < a.c.pages;
+        const int64_t page = held ? entry : 0, row = (int64_t)(kv_head * a.c.page_size + entry_position - a.c.by_page.divide(entry_position) * a.c.page_size) * dim;
+        keys_at[which][i] = (page * a.c.ldk + row) | !held;   // (rows are of whole eights of values)
+        values_at[which][i] = (page * a.c.ldv + row) | !held;
+        return held;
+    };
+    bool held_next = true;
+    const int32_t key_offset = key_row % 8 * dim + (8 * key_chunk < dim ? 8 * key_chunk : 0), value_offset = kColumns * quad < dim ? kColumns * quad : 0;
+    auto load = [&](int turn_number) {
+        const int64_t key_at = keys_at[turn_number % 4][key_row / 8], value_at = values_at[turn_number % 4][eight];
+        held_next = !(value_at & 1);
+        const T *keys = static_cast<const T *>(a.c.keys) + (key_at & ~(int64_t)1) + key_offset;
+        const T *values = static_cast<const T *>(a.c.values) + (value_at & ~(int64_t)1) + value_offset;
 #pragma unroll
         for (int i = 0; i < kKeyLoads; i++) kf[i].load(keys + i * dim);
 #pragma unroll
         for (int i = 0; i < 8; i++) vf[i].load(values + i * dim);
     };
+    auto look_ahead = [&](int turn_number) {   // in turn `turn_number`
+        if (wave == 0) {
+            bool held = true;
+            if (lane < kEights) {
+                held = tell((turn_number + 3) % 4, lane);
+                look_up(begin + (turn_number + 4) * kTurn, lane);
+            }
+            const uint64_t bits = __ballot(held);
+            if (lane == 0) held_by[(turn_number + 3) % 4] = (uint32_t)bits;
+        }
+    };
     // row r of half h of a block is its position 8 (r / 4) + 4 h + r % 4; a row's place among 16 changes with the chunk of columns, so that neither side meets a bank twice
-    auto put = [&](int32_t turn, int which, bool held) {
+    auto put = [&](int32_t turn, int which) {
         char *const keys = base + which * kBytes, *const values = keys + kKeyBytes;
-        const uint32_t there = 8 * key_chunk < dim ? 0xffffffffu : 0u;
+        const bool held = held_next;
+        const uint32_t there = WHOLE || 8 * key_chunk < dim ? 0xffffffffu : 0u;
         auto store = [](char *to, const Operand<T> &v) {
             const uint4_t *parts = reinterpret_cast<const uint4_t *>(&v);
 #pragma unroll
@@ -135,7 +155,6 @@ template <typename T, int D, int NQ> __global__ __launch_bounds__(kRowThreads) v
             for (int w = 0; w < Piece<T, 8>::kWords; w++) kf[i].w[w] &= there;
             store(keys + operand * kOperand + (key_chunk % 4 * 16 + (r ^ (key_chunk % 16))) * 16, Operand<T>::of(kf[i].w));
         }
-        if (quad == 0) held_by[which][eight] = held;
         // Values that no row sees must not be there at all, not even with a weight of 0; infinities and NaN are taken out where only some rows see them (in fp32 everywhere: parts of an
         // infinity make NaN), and added for those rows
         const bool edge = turn < tile_all_low || (int64_t)turn + kTurn > tile_all_high || turn + kTurn > end;   // (the same in all threads)
@@ -210,46 +229,49 @@ template <typename T, int D, int NQ> __global__ __launch_bounds__(kRowThreads) v
 
     if (threadIdx.x < kBuffers) odd_by[threadIdx.x] = 0;
     if (begin < end) {
-        Places next = places(begin);
-        load(next);
-        bool held_next = next.v.page >= 0;
-        next = places(begin + kTurn);
+        const int eights = 3 * kEights;
+        for (int i = threadIdx.x; i < eights; i += kRowThreads) {
+            look_up(begin, i);
+            tell(i / kEights, i % kEights);
+        }
+        __syncthreads();
+        if (wave == 0) {
+            if (lane < 3) {
+                uint32_t bits = 0;
+                for (int i = 0; i < kEights; i++) bits |= (uint32_t)!(values_at[lane][i] & 1) << i;
+                held_by[lane] = bits;
+            }
+            if (lane < kEights) look_up(begin + 3 * kTurn, lane);
+        }
+        load(0);
         if constexpr (kBuffers > 1) {
-            __syncthreads();
-            put(begin, 0, held_next);
-            load(next);
-            held_next = next.v.page >= 0;
-            next = places(begin + 2 * kTurn);
+            put(begin, 0);
+            load(1);
             barrier();
         }
         float4_t s[NQ][2];
         bool ready = false;    // s has the scores of the turn's first block
-        int which = 0;
-        for (int32_t turn = begin; turn < end; turn += kTurn) {
+        int which = 0, turn_number = 0;
+        for (int32_t turn = begin; turn < end; turn += kTurn, turn_number++) {
             const int following = kBuffers == 1 || which == 2 ? 0 : which + 1;
             if constexpr (kBuffers == 1) {
                 __syncthreads();   // (nobody reads the turn before this one's operands any more)
-                put(turn, 0, held_next);
-                load(next);
-                held_next = next.v.page >= 0;
-                next = places(turn + 2 * kTurn);
+                put(turn, 0);
+                load(turn_number + 1);
+                look_ahead(turn_number);
                 barrier();
             }
             const bool active = turn < some_high && turn + kTurn > some_low;   // (the same in all lanes)
             if (active && (!ready || kBuffers == 1)) scores(s, which, 0);
             ready = active;
-            uint32_t held = 0;
-#pragma unroll
-            for (int i = 0; i < kEights; i++) held |= held_by[which][i] << i;
-            held = one(held);
+            const uint32_t held = one(held_by[turn_number % 4]);
             const bool odd = one(odd_by[which]) == turn + 1;
 #pragma unroll
             for (int b = 0; b < kBlocks; b++) {
                 if (kBuffers > 1 && b == kBlocks - 1) {
-                    if (turn + kTurn < end) put(turn + kTurn, following, held_next);
-                    load(next);
-                    held_next = next.v.page >= 0;
-                    next = places(turn + 3 * kTurn);
+                    if (turn + kTurn < end) put(turn + kTurn, following);
+                    load(turn_number + 2);
+                    look_ahead(turn_number);
                 }
                 const int32_t block = turn + b * kStep;
                 if (active) {
@@ -373,11 +395,11 @@ template <typename T, int D, int NQ> __global__ __launch_bounds__(kRowThreads) v
     }
 }
 
-template <typename T, int D, int NQ> int launch_rows(const Attend &a, hipStream_t st)
+template <typename T, int D, int NQ, bool WHOLE> int launch_rows(const Attend &a, hipStream_t st)
 {
     constexpr int64_t kMost = int64_t(1) << 22;
     constexpr size_t kLds = row_lds<T, D>();
-    auto kernel = k_attend_rows<T, D, NQ>;
+    auto kernel = k_attend_rows<T, D, NQ, WHOLE>;
     HBP_HIP(hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)kLds));
     const int64_t units = a.units * a.c.kv_heads;
     for (int64_t at = 0; at < units; at += kMost) {
@@ -395,9 +417,10 @@ template <typename T> int launch_attend(const Attend &a, hipStream_t st)
         constexpr int D = decltype(d)::value;
         if (any) return launch_units<T, D, 1, true>(a, st);
         if (a.tile_rows == 16) return launch_units<T, D, 1, false>(a, st);
-        if (a.tile_rows == 128) return launch_rows<T, D, 1>(a, st);
+        const bool whole = a.c.head_dim == D;
+        if (a.tile_rows == 128) return whole ? launch_rows<T, D, 1, true>(a, st) : launch_rows<T, D, 1, false>(a, st);
         if constexpr (D * sizeof(T) < 512)
-            if (a.tile_rows == 256) return launch_rows<T, D, 2>(a, st);
+            if (a.tile_rows == 256) return whole ? launch_rows<T, D, 2, true>(a, st) : launch_rows<T, D, 2, false>(a, st);
         if constexpr (D * sizeof(T) <= 256 && sizeof(T) == 2) return launch_units<T, D, 2, false>(a, st);
         return HBP_ERR_INVALID_ARGUMENT;   // (no such plan)
     };
