@@ -236,10 +236,11 @@ __device__ __forceinline__ void add_odd(const Attend &a, const int32_t *table, i
 
 // Few rows: a workgroup of four wavefronts takes 16 NQ rows, and each wavefront every fourth step of their positions, straight from the cache into registers; the four
 // results are joined in LDS.  The next step's keys are on their way from the scores on, this one's values until the weights are there.
-template <typename T, int D, int NQ, bool ANY_PAGE> __global__ __launch_bounds__(256, D * sizeof(T) > 256 ? 1 : 2) void k_attend(Attend a, int64_t first_unit)
+template <typename T, int D, int NQ, bool ANY_PAGE> __global__ __launch_bounds__(256, sizeof(T) == 4 && D > 64 ? 1 : 2) void k_attend(Attend a, int64_t first_unit)
 {
     constexpr int kSteps = D / 32, kTiles = D / 16;   // of 32 columns in Q K^T; of 16 in the result, which a lane holds D / 16 neighbouring columns of
-    constexpr int kPitch = D + 4, kSums = sizeof(T) == 4 ? 2 : 1;   // sums taken in turn
+    constexpr int kPitch = D + 4, kSums = sizeof(T) == 4 && D < 256 ? 2 : 1;   // sums taken in turn
+    constexpr bool kAhead = D <= 128;   // whether the next step's keys are on their way beside this one's values: with wider heads they would take the registers of a second wavefront (16 bits: 171 and 166 us for 24 x 5 x 4096)
     __shared__ float joined[4][16][kPitch];
     __shared__ float2 joined_stats[4][16];
     const int lane = threadIdx.x % kWave, wave = one((int32_t)threadIdx.x / kWave), column = lane % 16, quarter = lane / 16;
@@ -332,21 +333,24 @@ template <typename T, int D, int NQ, bool ANY_PAGE> __global__ __launch_bounds__
     if (begin < end) {
         int32_t step = begin + wave * kStep;
         Places now = places(step), next = places(step + 4 * kStep);
-        load_keys(now);
+        if constexpr (kAhead) load_keys(now);
         for (; step < end; step += 4 * kStep) {
-            // values
             constexpr int kPieces = kTiles > 8 ? kTiles / 8 : 1, kEach = kTiles > 8 ? 8 : kTiles;
             Piece<T, kEach> vf[8][kPieces];
+            auto load_values = [&](const Places &p) {
 #pragma unroll
-            for (int i = 0; i < 8; i++) {
-                const T *from = ANY_PAGE ? row_of<T>(a.c.values, a.c.ldv, a.c, kv_head, now.v[ANY_PAGE ? i : 0])
-                                         : row_of<T>(a.c.values, a.c.ldv, a.c, kv_head, now.v[0]) + i * dim;
+                for (int i = 0; i < 8; i++) {
+                    const T *from = ANY_PAGE ? row_of<T>(a.c.values, a.c.ldv, a.c, kv_head, p.v[ANY_PAGE ? i : 0])
+                                             : row_of<T>(a.c.values, a.c.ldv, a.c, kv_head, p.v[0]) + i * dim;
 #pragma unroll
-                for (int c = 0; c < kPieces; c++) {
-                    const int32_t at = kTiles * column + kEach * c;
-                    vf[i][c].load(from + (at < dim ? at : 0));
+                    for (int c = 0; c < kPieces; c++) {
+                        const int32_t at = kTiles * column + kEach * c;
+                        vf[i][c].load(from + (at < dim ? at : 0));
+                    }
                 }
-            }
+            };
+            if constexpr (kAhead) load_values(now);
+            else load_keys(now);
             // scores
             float4_t s[NQ][2];
 #pragma unroll
@@ -370,7 +374,8 @@ template <typename T, int D, int NQ, bool ANY_PAGE> __global__ __launch_bounds__
             }
             const Places mine = now;
             now = next;
-            load_keys(now);
+            if constexpr (kAhead) load_keys(now);
+            else load_values(mine);
             next = places(step + 8 * kStep);
 
             uint32_t held = 0;   // bits of the lane's eight positions that the cache holds

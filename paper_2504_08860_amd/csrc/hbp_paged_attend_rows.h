@@ -23,7 +23,7 @@ template <typename T, int D, int NQ, bool WHOLE> __global__ __launch_bounds__(kR
     constexpr int kKeyBytes = kBlocks * 2 * kSteps * kOperand, kBytes = 2 * kKeyBytes;   // (as many of values)
     constexpr int kChunks = D / 8, kKeyRows = kRowThreads / kChunks, kKeyLoads = kTurn / kKeyRows;   // keys: a thread loads a chunk of eight columns of neighbouring positions
     constexpr int kColumns = D * kEights / kRowThreads, kQuads = D / kColumns;                       // values: one or two columns of eight positions
-    constexpr int kApart = 16 / (kTiles / kColumns), kSums = sizeof(T) == 4 ? 2 : 1;   // kSums: sums taken in turn
+    constexpr int kApart = 16 / (kTiles / kColumns), kSums = sizeof(T) == 4 && D < 256 ? 2 : 1;   // kSums: sums taken in turn
     static_assert(kKeyLoads >= 1 && 8 % kKeyLoads == 0 && kColumns >= 1 && kQuads * kEights == kRowThreads, "");
     extern __shared__ uint4 lds[];
     __shared__ int64_t keys_at[4][kEights], values_at[4][kEights];   // of four turns: where eight positions' rows begin, in values; odd: the cache does not hold them
@@ -158,15 +158,20 @@ template <typename T, int D, int NQ, bool WHOLE> __global__ __launch_bounds__(kR
         // Values that no row sees must not be there at all, not even with a weight of 0; infinities and NaN are taken out where only some rows see them (in fp32 everywhere: parts of an
         // infinity make NaN), and added for those rows
         const bool edge = turn < tile_all_low || (int64_t)turn + kTurn > tile_all_high || turn + kTurn > end;   // (the same in all threads)
-        if (edge || !held || sizeof(T) == 4) {
-            uint32_t largest = 0;
+        if (edge || !held)
 #pragma unroll
             for (int i = 0; i < 8; i++) {
                 const int32_t position = turn + 8 * eight + i;
                 const uint32_t seen = held && position >= tile_low && position < end ? 0xffffffffu : 0u;
 #pragma unroll
+                for (int w = 0; w < Piece<T, kColumns>::kWords; w++) vf[i].w[w] &= seen;
+            }
+        if (edge || !held || sizeof(T) == 4) {
+            uint32_t largest = 0;
+#pragma unroll
+            for (int i = 0; i < 8; i++) {
+#pragma unroll
                 for (int w = 0; w < Piece<T, kColumns>::kWords; w++) {
-                    vf[i].w[w] &= seen;
                     if constexpr (sizeof(T) == 4) largest = max(largest, vf[i].w[w] & 0x7fffffffu);
                     else largest = largest_halves(largest, vf[i].w[w] & 0x7fff7fffu);
                 }
