@@ -65,7 +65,7 @@ int hbp_paged_attention(const hbp_paged_t *cache, int64_t tokens, const void *q,
     size_t need = 0;
     int rc = plan(cache, tokens, heads, window, most_new, &a, &need);
     if (rc != HBP_OK) return rc;
-    if (!std::isfinite(scale) || !std::isfinite(softcap) || softcap < 0) return HBP_ERR_INVALID_ARGUMENT;
+    if (!std::isfinite(scale) || !std::isfinite(softcap) || softcap < 0 || (softcap > 0 && !std::isfinite(scale / softcap * 3.0f))) return HBP_ERR_INVALID_ARGUMENT;
     if (a.tokens == 0) return HBP_OK;
     const int64_t bytes = type_bytes(cache->type), row = (int64_t)heads * cache->head_dim;
     if (!q || !out || !aligned(q, bytes) || !aligned(out, bytes) || (tokens > 1 && (ldq < row || ldo < row))) return HBP_ERR_INVALID_ARGUMENT;
@@ -78,7 +78,7 @@ int hbp_paged_attention(const hbp_paged_t *cache, int64_t tokens, const void *q,
     a.flip = scale < 0 ? (cache->type == HBP_F32 ? 0x80000000u : 0x80008000u) : 0u;
     a.per = scale == 0 ? 1.0f : std::fabs(scale) * kPerLog2;
     if (softcap > 0) {
-        a.cap_in = 2 * kPerLog2 * (std::fabs(scale) / softcap);
+        a.cap_in = std::fabs(scale) / softcap;
         a.cap_out = softcap * kPerLog2;
     }
     const int64_t places = (int64_t)a.slots * cache->kv_heads * a.tile_rows;

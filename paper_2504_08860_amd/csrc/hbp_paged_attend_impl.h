@@ -95,11 +95,11 @@ template <typename F> __device__ __forceinline__ float over_quarters(float v, F 
     return op(__uint_as_float(b[0]), __uint_as_float(b[1]));
 }
 
-// Exponents of 2 of scores.  tanh x = 1 - 2 / (e^2x + 1), off by some 2^-24 of 1 where x is small, which is 2^-24 of the cap in the exponent.
-__device__ __forceinline__ float exponent_of(const Attend &a, float score)
+// Exponents of 2 of scores with a cap.  tanh x = 1 - 2 / (e^2x + 1), off by some 2^-24 of 1 where x is small, which is 2^-24 of the cap in the exponent; fp32 results would show it.
+template <typename T> __device__ __forceinline__ float capped(const Attend &a, float score)
 {
-    if (a.cap_out == 0.0f) return score * a.per;
-    const float e = __builtin_amdgcn_exp2f(score * a.cap_in);   // (cap_in has 2 / log 2 in it)
+    if constexpr (sizeof(T) == 4) return a.cap_out * tanhf(score * a.cap_in);
+    const float e = __builtin_amdgcn_exp2f(score * (a.cap_in * (2.0f * 1.4426950408889634f)));
     return a.cap_out - 2.0f * a.cap_out * __builtin_amdgcn_rcpf(e + 1.0f);
 }
 
@@ -288,6 +288,7 @@ template <typename T, int D, int NQ, bool ANY_PAGE> __global__ __launch_bounds__
     for (int n = 0; n < NQ; n++) tile_low = min(tile_low, count[n] ? low[n] : 0x7fffffff);
     tile_low = max(least_low, one(wave_reduce(tile_low, [](int32_t p, int32_t q) { return min(p, q); })));
 
+    const float per = a.cap_out != 0.0f ? 1.0f : a.per;   // (of what the cap has made of scores)
     float m[NQ], l[NQ];
     float4_t o[NQ][kTiles];
 #pragma unroll
@@ -390,8 +391,9 @@ template <typename T, int D, int NQ, bool ANY_PAGE> __global__ __launch_bounds__
 #pragma unroll
                 for (int i = 0; i < 8; i++) e[i] = s[n][i / 4][i % 4];
                 if constexpr (sizeof(T) == 4) by_definition(a, x, table, kv_head, x.tile * a.tile_rows + n * 16 + column, count[n] > 0, step, end, e);
+                if (a.cap_out != 0.0f)
 #pragma unroll
-                for (int i = 0; i < 8; i++) e[i] = exponent_of(a, e[i]);
+                    for (int i = 0; i < 8; i++) e[i] = capped<T>(a, e[i]);
                 if (!whole)
 #pragma unroll
                     for (int i = 0; i < 8; i++) {
@@ -401,6 +403,7 @@ template <typename T, int D, int NQ, bool ANY_PAGE> __global__ __launch_bounds__
                 float top = e[0];
 #pragma unroll
                 for (int i = 1; i < 8; i++) top = fmaxf(top, e[i]);
+                top *= per;
                 // The weights are taken relative to an earlier largest exponent while none is more than 8 above it: sums stay far from overflow, and nothing is exchanged.
                 if (__ballot(top > m[n] + 8.0f) != 0) {
                     const float to = over_quarters(fmaxf(top, m[n]), [](float p, float q) { return fmaxf(p, q); });
@@ -414,7 +417,7 @@ template <typename T, int D, int NQ, bool ANY_PAGE> __global__ __launch_bounds__
                 }
 #pragma unroll
                 for (int i = 0; i < 8; i++) {
-                    p[i] = __builtin_amdgcn_exp2f(e[i] - m[n]);
+                    p[i] = __builtin_amdgcn_exp2f(fmaf(e[i], per, -m[n]));   // (the exponent is rounded as a difference to the largest one)
                     l[n] += p[i];
                 }
                 weights[n] = Operand<T>::of(p);

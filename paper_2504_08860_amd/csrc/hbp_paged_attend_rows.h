@@ -294,7 +294,7 @@ template <typename T, int D, int NQ, bool WHOLE> __global__ __launch_bounds__(kR
 #pragma unroll
                         for (int n = 0; n < NQ; n++)
 #pragma unroll
-                            for (int i = 0; i < 8; i++) s[n][i / 4][i % 4] = exponent_of(a, s[n][i / 4][i % 4]);
+                            for (int i = 0; i < 8; i++) s[n][i / 4][i % 4] = capped<T>(a, s[n][i / 4][i % 4]);
                     }
                     if (block < all_low || block + kStep > all_high || (held >> (4 * b) & 0xf) != 0xf) {
 #pragma unroll
