@@ -37,7 +37,7 @@ template <typename T, int U> struct Values {
 
 // One workgroup a token at a time.  The token's cosines and sines are made once, for all heads, in LDS.  A thread's unit is U pairs of a head of keys or queries (both values of
 // a pair in one thread, so that queries may be rotated in place), U values behind the rotated ones, or U values of a head of values.  The first kAhead units are loaded before the
-// position is known.
+// position is known.  Bound: HBM; 10000 tokens of 40 + 8 + 8 heads of 80 fp32 values 71 us, 4.2 TB/s read and written; one token of 32 + 8 + 8 heads of 128 2.4 us, a chain of loads.
 constexpr int kThreads = 256, kAhead = 2;
 template <typename T, int U> __global__ __launch_bounds__(kThreads) void k_paged_append(AppendArgs a)
 {
@@ -190,7 +190,9 @@ extern "C" int hbp_paged_append(const hbp_paged_t *cache, int64_t tokens, const 
             HBP_HIP(hipGetLastError());
             return HBP_OK;
         };
-        if (pairs % 8 == 0) return go(std::integral_constant<int, 8>());
+        // (16 bytes a load: 10000 tokens of fp32 with eight values 75.6 us, with four 71.4; 16-bit types the other way round)
+        if constexpr (sizeof(T) == 2)
+            if (pairs % 8 == 0) return go(std::integral_constant<int, 8>());
         if (pairs % 4 == 0) return go(std::integral_constant<int, 4>());
         return go(std::integral_constant<int, 1>());
     });

@@ -14,7 +14,7 @@ struct Attend {
     float per;                 // scores to exponents of 2: |scale| / log 2, 1 where it is 0
     float cap_in, cap_out;     // with a cap: exponents are cap_out tanh(cap_in score); cap_out 0: none
     uint32_t keep, flip;       // of queries' bits, in both halves of a word: signs change where scale is negative, a scale of 0 leaves zeros
-    Divider by_group, by_kv_heads;
+    Divider by_group;
     int32_t tile_rows;         // rows (a token's query heads of one head of keys lie together) that a workgroup takes at once
     int32_t places, aim, least, enough;   // how tiles are split, see find_unit; of one head of keys
     int32_t slots;             // places for results of parts, of each head of keys

@@ -24,7 +24,6 @@ int plan(const hbp_paged_t *cache, int64_t tokens, int heads, int window, int64_
     a->most_new = (int32_t)most_new;
     a->window = window;
     a->by_group = Divider::of(group);
-    a->by_kv_heads = Divider::of(cache->kv_heads);
     const int64_t most_rows = most_new * group;
     const bool wide = cache->head_dim * type_bytes(cache->type) > 256;
     a->tile_rows = most_rows <= 16 || cache->page_size % 8 ? 16 : most_rows <= 32 && cache->type != HBP_F32 && !wide ? 32 : most_rows <= 128 || wide ? 128 : 256;
@@ -36,7 +35,7 @@ int plan(const hbp_paged_t *cache, int64_t tokens, int heads, int window, int64_
     a->aim = (int32_t)std::max<int64_t>(1, (rows > 32 ? 512 : 1024) / cache->kv_heads);
     // Parts of tiles that are split: each is of more than `length` positions, so that its parts are at most twice its positions by `length`, and in all twice `aim`.
     const int64_t span = window ? std::min<int64_t>(a->c.capacity, (int64_t)window + rows) : a->c.capacity, most_parts = (span + a->least - 1) / a->least;
-    a->slots = most_parts < 2 ? 0 : (int32_t)std::min<int64_t>(2 * a->aim + 64, a->tiles * most_parts);
+    a->slots = most_parts < 2 ? 0 : (int32_t)std::min<int64_t>(2 * a->aim + 2, a->tiles * most_parts);
     a->units = std::min(a->tiles + a->aim + 1, a->tiles * std::max<int64_t>(most_parts, 1));   // (each tile one more than its positions by a part's)
     *bytes = (size_t)a->slots * cache->kv_heads * rows * (cache->head_dim * sizeof(float) + sizeof(float2));
     return HBP_OK;

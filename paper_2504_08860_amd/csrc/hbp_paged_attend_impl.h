@@ -174,27 +174,29 @@ template <typename T> __device__ __forceinline__ float weight_of(const Operand<T
     else return to_f32(__builtin_bit_cast(T, (uint16_t)w[0]));
 }
 
-// fp32: parts of an infinite value, and products of parts that overflow, make NaN of what may be a number or an infinity.  Scores of a lane's eight positions of a step that are not finite are computed again.
-__device__ __forceinline__ void by_definition(const Attend &a, const Unit &x, const int32_t *table, int32_t kv_head, int32_t row, bool is_row, int32_t step, int32_t end, float (&e)[8])
+// fp32: parts of an infinite value, and products of parts that overflow, make NaN of what may be a number or an infinity.  Scores of a lane's eight positions of a step that are not finite are computed
+// again where its query sees them (`held`: bits of those that the cache holds).
+__device__ __forceinline__ void by_definition(const Attend &a, const Unit &x, const int32_t *table, int32_t kv_head, int32_t row, int32_t step, int32_t low, int32_t count, uint32_t held, float (&e)[8])
 {
-    bool odd = false;
+    uint32_t odd = 0;
 #pragma unroll
-    for (int i = 0; i < 8; i++) odd |= !(fabsf(e[i]) < INFINITY);
-    if (__ballot(odd) == 0) return;
-    if (!is_row) return;
+    for (int i = 0; i < 8; i++) odd |= !(fabsf(e[i]) < INFINITY) ? 1u << i : 0u;
+    if (__ballot(odd != 0) == 0) return;
+    const int32_t first = step + 8 * ((int)threadIdx.x % kWave / 16);
+    odd &= held;
+    if (odd == 0 || count <= 0) return;
     const int32_t token = a.by_group.divide(row);
     const float *query = static_cast<const float *>(a.q) + (int64_t)(x.first_token + token) * a.ldq + (int64_t)(kv_head * a.group + row - token * a.group) * a.c.head_dim;
 #pragma unroll 1
     for (int i = 0; i < 8; i++) {
-        const int32_t position = min(step + 8 * ((int)threadIdx.x % kWave / 16) + i, end - 1);
-        const float *key = row_of<float>(a.c.keys, a.c.ldk, a.c, kv_head, slot_of(a.c, table, position));
+        if (!(odd >> i & 1) || (uint32_t)(first + i - low) >= (uint32_t)count) continue;
+        const float *key = row_of<float>(a.c.keys, a.c.ldk, a.c, kv_head, slot_of(a.c, table, first + i));
         float sum = 0.0f;
 #pragma unroll 1
-        for (int d = 0; d < a.c.head_dim; d++) sum += query[d] * key[d];
+        for (int d = 0; d < a.c.head_dim && sum == sum; d++) sum += query[d] * key[d];
         sum = a.flip ? -sum : sum;
 #pragma unroll
-        for (int j = 0; j < 8; j++)
-            if (j == i && !(fabsf(e[j]) < INFINITY)) e[j] = sum;
+        for (int j = 0; j < 8; j++) e[j] = j == i ? sum : e[j];
     }
 }
 
@@ -390,7 +392,7 @@ template <typename T, int D, int NQ, bool ANY_PAGE> __global__ __launch_bounds__
                 float e[8], p[8];
 #pragma unroll
                 for (int i = 0; i < 8; i++) e[i] = s[n][i / 4][i % 4];
-                if constexpr (sizeof(T) == 4) by_definition(a, x, table, kv_head, x.tile * a.tile_rows + n * 16 + column, count[n] > 0, step, end, e);
+                if constexpr (sizeof(T) == 4) by_definition(a, x, table, kv_head, x.tile * a.tile_rows + n * 16 + column, step, low[n], count[n], held, e);
                 if (a.cap_out != 0.0f)
 #pragma unroll
                     for (int i = 0; i < 8; i++) e[i] = capped<T>(a, e[i]);

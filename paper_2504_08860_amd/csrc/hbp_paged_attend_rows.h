@@ -286,7 +286,7 @@ template <typename T, int D, int NQ, bool WHOLE> __global__ __launch_bounds__(kR
                             float e[8];
 #pragma unroll
                             for (int i = 0; i < 8; i++) e[i] = s[n][i / 4][i % 4];
-                            by_definition(a, x, table, kv_head, first_row + n * 16 + column, count[n] > 0, block, end, e);
+                            by_definition(a, x, table, kv_head, first_row + n * 16 + column, block, low[n], count[n], held >> (4 * b + quarter) & 1 ? 0xffu : 0u, e);
 #pragma unroll
                             for (int i = 0; i < 8; i++) s[n][i / 4][i % 4] = e[i];
                         }

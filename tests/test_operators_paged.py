@@ -302,6 +302,21 @@ def test_attention_of_extreme_scores(name):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("name", TYPES)
+def test_queries_that_are_no_numbers(name):
+    """NaN and infinities in one row's query are that row's alone."""
+    import torch
+    for sizes, page in (([(3, 300), (1, 40)], 16), ([(3, 300), (1, 40)], 5), ([(50, 300), (1, 40)], 16)):
+        b = Batch(sizes, name, 1, 2, 64, page, seed=2)
+        want = b.attend()
+        b.q[1, 0, 5], b.q[2, 1, 7] = float("nan"), INF
+        got = b.attend()
+        rows = [i for i in range(b.tokens) if i not in (1, 2)]
+        assert torch.equal(got[rows], want[rows]) and torch.equal(got[1, 1], want[1, 1]) and torch.equal(got[2, 0], want[2, 0])
+        assert torch.isnan(got[1, 0]).all() and torch.isnan(got[2, 1]).all()
+
+
+@pytest.mark.gpu
 def test_infinite_visible_values_of_fp32():
     """Infinities that a row does see: scores of -inf have no weight, infinite values give infinities."""
     import torch
@@ -469,7 +484,7 @@ def test_what_the_library_refuses():
     assert append(tokens=(1 << 30) + 1) == -4
     nan = float("nan")
     for bad in (dict(q=None), dict(q=4097), dict(out=None), dict(out=4097), dict(ldq=511), dict(ldo=511), dict(heads=0), dict(heads=7), dict(scale=nan), dict(scale=INF), dict(cap=-1.0),
-                dict(cap=nan), dict(cap=INF), dict(window=-1), dict(most=-1)):
+                dict(cap=nan), dict(cap=INF), dict(cap=1e-44), dict(window=-1), dict(most=-1)):
         assert attend(**bad) == -1, bad
     assert attend(tokens=1 << 30) == -4 and attend(most=0) == 0
     need, long = ctypes.c_size_t(), cache_of(pages=1 << 20, table_width=1 << 19, ldt=1 << 19)

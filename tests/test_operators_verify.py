@@ -88,7 +88,11 @@ class Case:
         self.args = dict(logits=spaced(self.logits), tokens=t(self.ids.astype(np.int64 if self.wide_ids else np.int32)), uniforms=t(self.uniforms), starts=t(self.starts),
                          new_tokens=new, accepted=accepted, draft_probs=None if self.q is None else spaced(torch.from_numpy(self.q)),
                          temperature=None if self.temperature is None else t(self.temperature)) | how
+        if "stream" in how:
+            torch.cuda.synchronize()   # (the other stream waits for what was made on this one, and this one for it)
         H.hbp_verify_drafts(**self.args)
+        if "stream" in how:
+            how["stream"].synchronize()
         return new.cpu().numpy(), accepted.cpu().numpy()
 
     def want(self):
@@ -209,7 +213,6 @@ def test_streams_and_graphs():
     c = Case([4] * 20, 20_000, "bf16", True, (0.0, 0.9, 1.0), seed=6)
     want = c.check()
     side = torch.cuda.Stream()
-    torch.cuda.synchronize()
     new, accepted = c.run(stream=side)
     assert np.array_equal(new, want[0]) and np.array_equal(accepted, want[1])
     a = dict(c.args)
