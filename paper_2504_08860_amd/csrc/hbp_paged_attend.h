@@ -16,7 +16,7 @@ struct Attend {
     uint32_t keep, flip;       // of queries' bits, in both halves of a word: signs change where scale is negative, a scale of 0 leaves zeros
     Divider by_group;
     int32_t tile_rows;         // rows (a token's query heads of one head of keys lie together) that a workgroup takes at once
-    int32_t places, aim, least, enough;   // how tiles are split, see find_unit; of one head of keys
+    int32_t places, aim, least, enough, whole;   // how tiles are split, see find_unit; of one head of keys
     int32_t slots;             // places for results of parts, of each head of keys
     float *partial;            // [slots][kv_heads][tile_rows][head_dim], sums of weights times values
     float2 *partial_stats;     // [slots][kv_heads][tile_rows]: the largest exponent, the sum of weights
@@ -53,7 +53,8 @@ struct Unit {
 
 // Finds a unit (or, BY_TILE, a tile) by its number among those of one head of keys: by the whole workgroup, some neighbouring sequences a thread.  How tiles are split is
 // decided here, from the lengths that the device holds: into parts of about the same length.  There are to be as many as the chip has places for at once (`places`), so that all of them are busy, but
-// for that none is cut shorter than `least`; beyond `enough` positions they are cut finer, into up to `aim`, which evens out what the places get.
+// for that none is cut shorter than `least`; beyond `enough` positions they are cut finer, into up to `aim`, which evens out what the places get.  Tiles of up to
+// `whole` positions are not split: joining their parts takes as long.
 // Up to 64 sequences each wavefront finds its own, a lane a sequence; more are dealt to the workgroup's threads.  (256 sequences, 64 of them at a time, by each wavefront: 8 us, of loads that wait for
 // each other.)
 template <bool BY_TILE, int THREADS> __device__ __forceinline__ bool find_unit(const Attend &a, int32_t number, Unit &x)
@@ -112,12 +113,12 @@ template <bool BY_TILE, int THREADS> __device__ __forceinline__ bool find_unit(c
     // (what the last part of each tile is shorter by makes them more than the places: a second turn of the chip for a few)
     if (few && length < a.enough)
         for (int i = 0; i < 4; i++) {
-            const int32_t all = wave_reduce(own.tiles * max(1, (own.span + length - 1) / length), [](int32_t p, int32_t q) { return p + q; });
+            const int32_t all = wave_reduce(own.tiles * (own.span <= a.whole ? 1 : max(1, (own.span + length - 1) / length)), [](int32_t p, int32_t q) { return p + q; });
             const int64_t longer = ((int64_t)length * all / a.places + kStep) / kStep * kStep;
             if (all <= a.places || longer > a.enough) break;
             length = (int32_t)longer;
         }
-    auto parts_of = [&](const Sequence &q) { return max(1, (int32_t)((q.span + length - 1) / length)); };
+    auto parts_of = [&](const Sequence &q) { return q.span <= a.whole ? 1 : max(1, (int32_t)((q.span + length - 1) / length)); };
     auto add = [&](const Sequence &q, int32_t &units, int32_t &slots) {
         const int32_t parts = parts_of(q);
         units += BY_TILE ? q.tiles : q.tiles * parts;

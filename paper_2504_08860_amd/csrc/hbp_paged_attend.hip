@@ -24,17 +24,21 @@ int plan(const hbp_paged_t *cache, int64_t tokens, int heads, int window, int64_
     a->most_new = (int32_t)most_new;
     a->window = window;
     a->by_group = Divider::of(group);
-    const int64_t most_rows = most_new * group;
-    const bool wide = cache->head_dim * type_bytes(cache->type) > 256;
-    a->tile_rows = most_rows <= 16 || cache->page_size % 8 ? 16 : most_rows <= 32 && cache->type != HBP_F32 && !wide ? 32 : most_rows <= 128 || wide ? 128 : 256;
+    // Rows of a tile.  16 or 32 by k_attend, whose wavefronts share the rows and not the positions: best where the cache's bytes bound it; more by k_attend_rows, whose wavefronts have 16 rows or 32,
+    // and 32 where that leaves enough to do for the chip's 256 places, parts of 512 positions counted (4 x 60 tokens of 4 heads: 21.1 us, with 16 16.2; 512 tokens over 30000 305 and 396).
+    const int64_t most_rows = most_new * group, span = window ? std::min<int64_t>(a->c.capacity, (int64_t)window + most_new) : a->c.capacity;
+    const bool wide = cache->head_dim * type_bytes(cache->type) > 256, any_page = cache->page_size % 8 != 0;
+    const bool plenty = (tokens * group / 256 + cache->sequences) * cache->kv_heads * ((span + 511) / 512) >= 256;
+    a->tile_rows = most_rows <= 16 || any_page ? 16 : most_rows <= 32 && cache->type != HBP_F32 && !wide ? 32 : most_rows <= 128 || wide || !plenty ? 128 : 256;
     const int64_t rows = a->tile_rows;
     a->tiles = std::min(tokens * group / rows + cache->sequences, cache->sequences * ((most_new * group + rows - 1) / rows));
     a->least = rows > 32 ? 512 : 4 * kStep;
     a->enough = rows > 32 ? 2048 : 512;
+    a->whole = a->tiles * cache->kv_heads < 128 ? 512 : 1024;   // (16 x 8 tiles of 1000 positions in two parts 20.9 us, whole 17.6; 8 of them 13.2 and 16.8)
     a->places = (int32_t)std::max<int64_t>(1, (rows > 32 ? 256 : 512) / cache->kv_heads);
     a->aim = (int32_t)std::max<int64_t>(1, (rows > 32 ? 512 : 1024) / cache->kv_heads);
     // Parts of tiles that are split: each is of more than `length` positions, so that its parts are at most twice its positions by `length`, and in all twice `aim`.
-    const int64_t span = window ? std::min<int64_t>(a->c.capacity, (int64_t)window + rows) : a->c.capacity, most_parts = (span + a->least - 1) / a->least;
+    const int64_t most_span = window ? std::min<int64_t>(a->c.capacity, (int64_t)window + rows) : a->c.capacity, most_parts = most_span <= a->whole ? 1 : (most_span + a->least - 1) / a->least;
     a->slots = most_parts < 2 ? 0 : (int32_t)std::min<int64_t>(2 * a->aim + 2, a->tiles * most_parts);
     a->units = std::min(a->tiles + a->aim + 1, a->tiles * std::max<int64_t>(most_parts, 1));   // (each tile one more than its positions by a part's)
     *bytes = (size_t)a->slots * cache->kv_heads * rows * (cache->head_dim * sizeof(float) + sizeof(float2));
