@@ -16,7 +16,7 @@ struct RowPart {
     int32_t first;
 };
 
-constexpr int kThreads = 256, kWaves = kThreads / kWave, kDrawThreads = 512;
+constexpr int kThreads = 256, kWaves = kThreads / kWave, kDrawThreads = 256;
 constexpr int kTurn = 16 * kWave, kPart = 2 * kTurn, kMostParts = kWave;   // logits that a wavefront takes at once, and of a part; rows of more than kMostParts such have longer parts
 
 struct VerifyArgs {
