@@ -180,6 +180,7 @@ template <bool BY_TILE, int THREADS> __device__ __forceinline__ bool find_unit(c
     x.parts = values[3];
     x.slot = values[4];
     x.first_token = values[5];
+    if (x.parts > 1 && (x.slot < 0 || x.slot > a.slots - x.parts)) return false;   // (more than the host counted: only where `starts` does not ascend)
     x.rows = values[6] * a.group;
     x.first_position = (int64_t)values[7] - values[8];
     const int32_t row = x.tile * a.tile_rows, last = min(row + a.tile_rows, x.rows) - 1;

@@ -32,7 +32,7 @@ int plan(const hbp_paged_t *cache, int64_t tokens, int heads, int window, int64_
     a->tile_rows = most_rows <= 16 || any_page ? 16 : most_rows <= 32 && cache->type != HBP_F32 && !wide ? 32 : most_rows <= 128 || wide || !plenty ? 128 : 256;
     const int64_t rows = a->tile_rows;
     a->tiles = std::min(tokens * group / rows + cache->sequences, cache->sequences * ((most_new * group + rows - 1) / rows));
-    a->least = rows > 32 ? 512 : 4 * kStep;
+    a->least = rows <= 32 ? 4 * kStep : cache->type == HBP_F32 ? 512 : 256;   // (4 x 60 tokens of 32 heads over 1000 positions: 29.3 us, with 512 32.3; 7 x 37 in fp32 over ragged 3000 49.7 and 47.7)
     a->enough = rows > 32 ? 2048 : 512;
     a->whole = a->tiles * cache->kv_heads < 128 ? 512 : 1024;   // (16 x 8 tiles of 1000 positions in two parts 20.9 us, whole 17.6; 8 of them 13.2 and 16.8)
     a->places = (int32_t)std::max<int64_t>(1, (rows > 32 ? 256 : 512) / cache->kv_heads);
