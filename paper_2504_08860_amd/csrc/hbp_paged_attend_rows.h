@@ -9,7 +9,10 @@ namespace {
 // A workgroup of eight wavefronts takes 128 NQ rows, 16 NQ a wavefront, and walks through their positions in turns of 64 (heads of up to 64: 128, wider ones than 128: 32), which all of them read from LDS: keys and values come
 // from the cache into registers two turns ahead, values are turned there (eight positions of one column become a lane's share of an operand), and both lie in LDS as operands of the matrix
 // instruction, lane after lane, so that every read is one of 16 bytes a lane without conflicts.  Three buffers and one barrier a turn.  The scores of the next block of 32 positions are
-// multiplied while this one's become weights.
+// multiplied when this one's have become weights, or while they do.  Bound: the matrix cores (515 cycles a block of a wavefront with 2 x 16 rows of heads of 128) and the vector unit (some 80 instructions and 16 exponentials)
+// in turn; 4 x 2048 bf16 tokens over up to 6000 positions, 32 heads of 128, 8 of keys: 730 us, 840 TFLOP/s; one prompt of 16384: 2.25 ms, 980 TFLOP/s.  With 32 rows a wavefront an operand that
+// has been read is multiplied twice; 64 would need accumulation registers, and copies from them (1356 us where this was 818); workgroups of four wavefronts, two on a compute unit, take 1.05 to 1.25 times as
+// long; the two wavefronts of a SIMD in opposite phases, held there by barriers, 1.15 times.
 constexpr int kRowThreads = 512;
 template <typename T, int D> constexpr int row_turn() { return sizeof(T) == 4 ? (D == 64 ? 64 : 32) : 8192 / D; }
 template <typename T, int D> constexpr int row_buffers() { return sizeof(T) == 4 && D > 128 ? 1 : 3; }   // (as LDS has room for)
@@ -24,6 +27,8 @@ template <typename T, int D, int NQ, bool WHOLE> __global__ __launch_bounds__(kR
     constexpr int kChunks = D / 8, kKeyRows = kRowThreads / kChunks, kKeyLoads = kTurn / kKeyRows;   // keys: a thread loads a chunk of eight columns of neighbouring positions
     constexpr int kColumns = D * kEights / kRowThreads, kQuads = D / kColumns;                       // values: one or two columns of eight positions
     constexpr int kApart = 16 / (kTiles / kColumns), kSums = sizeof(T) == 4 && D < 256 ? 2 : 1;   // kSums: sums taken in turn
+    constexpr bool kOrdered = sizeof(T) == 2 && (NQ == 2 || D == 256);   // weights first, then both products in an order that is given, see below (16 rows of 128: 4 x 60 tokens over 400 22.1 us, and 20.0 without)
+    constexpr int kHead = kOrdered ? 2 : 0, kAtOnce = 8;       // key steps whose operands are read before weights are made; operands on their way
     static_assert(kKeyLoads >= 1 && 8 % kKeyLoads == 0 && kColumns >= 1 && kQuads * kEights == kRowThreads, "");
     extern __shared__ uint4 lds[];
     __shared__ int64_t keys_at[4][kEights], values_at[4][kEights];   // of four turns: where eight positions' rows begin, in values; odd: the cache does not hold them
@@ -214,15 +219,22 @@ template <typename T, int D, int NQ, bool WHOLE> __global__ __launch_bounds__(kR
         for (int k = 0; k < kParts; k++) parts[k] = *reinterpret_cast<const uint4_t *>(from + k * 64 * 16);
         return v;
     };
-    auto scores = [&](float4_t (&s)[NQ][2], int which, int b) {
-        const char *const keys = base + which * kBytes;
+    auto key_at = [&](int which, int b, int k, int h) {
+        return operand_at(base + which * kBytes + ((b * 2 + h) * kSteps + k) * kOperand + (quarter * 16 + (column ^ ((4 * k + quarter) % 16))) * 16);
+    };
+    Operand<T> head[kHead ? 2 * kHead : 1];
+    auto read_head = [&](int which, int b) {
+#pragma unroll
+        for (int i = 0; i < 2 * kHead; i++) head[i] = key_at(which, b, i / 2, i % 2);
+    };
+    auto scores = [&](float4_t (&s)[NQ][2], int which, int b) {   // (after read_head)
 #pragma unroll
         for (int n = 0; n < NQ; n++) s[n][0] = s[n][1] = float4_t{0, 0, 0, 0};
 #pragma unroll
         for (int k = 0; k < kSteps; k++) {
             Operand<T> key[2];
 #pragma unroll
-            for (int h = 0; h < 2; h++) key[h] = operand_at(keys + ((b * 2 + h) * kSteps + k) * kOperand + (quarter * 16 + (column ^ ((4 * k + quarter) % 16))) * 16);
+            for (int h = 0; h < 2; h++) key[h] = k < kHead ? head[k < kHead ? 2 * k + h : 0] : key_at(which, b, k, h);
 #pragma unroll
             for (int product = 0; product < kProducts<T>; product++)
 #pragma unroll
@@ -267,13 +279,16 @@ template <typename T, int D, int NQ, bool WHOLE> __global__ __launch_bounds__(kR
                 barrier();
             }
             const bool active = turn < some_high && turn + kTurn > some_low;   // (the same in all lanes)
-            if (active && (!ready || kBuffers == 1)) scores(s, which, 0);
+            if (active && (!ready || kBuffers == 1)) {
+                read_head(which, 0);
+                scores(s, which, 0);
+            }
             ready = active;
             const uint32_t held = one(held_by[turn_number % 4]);
             const bool odd = one(odd_by[which]) == turn + 1;
 #pragma unroll
             for (int b = 0; b < kBlocks; b++) {
-                if (kBuffers > 1 && b == kBlocks - 1) {
+                if (kBuffers > 1 && b == (kOrdered ? 0 : kBlocks - 1)) {
                     if (turn + kTurn < end) put(turn + kTurn, following);
                     load(turn_number + 2);
                     look_ahead(turn_number);
@@ -331,6 +346,11 @@ template <typename T, int D, int NQ, bool WHOLE> __global__ __launch_bounds__(kR
                 }
                 if (kBuffers > 1 && b == kBlocks - 1) barrier();   // (the next turn's operands are in LDS; their buffer was read last in the turn before this one)
                 if (active) {
+                    const int next_which = b == kBlocks - 1 ? following : which, next_block = b == kBlocks - 1 ? 0 : b + 1;
+                    if constexpr (kOrdered) {
+                        read_head(next_which, next_block);
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
                     Operand<T> weights[NQ];
 #pragma unroll
                     for (int n = 0; n < NQ; n++) {
@@ -342,7 +362,8 @@ template <typename T, int D, int NQ, bool WHOLE> __global__ __launch_bounds__(kR
                         }
                         weights[n] = Operand<T>::of(p);
                     }
-                    if (kBuffers > 1 || b < kBlocks - 1) scores(s, b == kBlocks - 1 ? following : which, b == kBlocks - 1 ? 0 : b + 1);   // (behind the last turn of nothing, for nothing)
+                    if constexpr (kOrdered) __builtin_amdgcn_sched_barrier(0);
+                    if (kBuffers > 1 || b < kBlocks - 1) scores(s, next_which, next_block);   // (behind the last turn of nothing, for nothing)
                     const char *const values = base + which * kBytes + kKeyBytes;
 #pragma unroll
                     for (int j = 0; j < kTiles; j += kSums) {
@@ -356,6 +377,18 @@ template <typename T, int D, int NQ, bool WHOLE> __global__ __launch_bounds__(kR
                             for (int c = 0; c < kSums; c++)
 #pragma unroll
                                 for (int n = 0; n < NQ; n++) o[n][j + c] = multiply(value[c], weights[n], o[n][j + c], product);
+                    }
+                    if constexpr (kOrdered) {
+                        // kAtOnce operands on their way, two more for each two that have been multiplied (the compiler's own order has four, and waits for LDS: 747 us instead of 730, 895 instead of 861 with heads of 256)
+                        constexpr int kReads = 2 * kSteps + kTiles;
+                        __builtin_amdgcn_sched_group_barrier(0x100, kAtOnce - 2 * kHead, 0);
+#pragma unroll
+                        for (int i = 0; i < (kReads - kAtOnce) / 2; i++) {
+                            __builtin_amdgcn_sched_group_barrier(0x008, 2 * NQ, 0);
+                            __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+                        }
+                        __builtin_amdgcn_sched_group_barrier(0x008, kAtOnce * NQ, 0);
+                        __builtin_amdgcn_sched_barrier(0);
                     }
                     if (odd)
                         add_odd<T, D, NQ>(a, table, kv_head, block, max(tile_low, block), min(end, block + kStep), weights, low, count, o);
