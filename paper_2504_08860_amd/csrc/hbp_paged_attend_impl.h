@@ -534,7 +534,7 @@ template <typename T, int D, int NQ, bool ANY_PAGE> __global__ __launch_bounds__
 }
 
 // Joins the parts of tiles that were split: a workgroup sixteen rows of a tile, LANES lanes a part of a row with eight columns each.  A wavefront has ROWS rows at once, or one with as many parts
-// on their way: what it waits for is the latency of loads: 4.3 us for one token over 4096 positions, 24.6 for the 1024 tiles of 4 x 2048 tokens over up to 8000.
+// on their way: what it waits for is the latency of loads: 4.3 us for one token over 4096 positions, 29 for the 1024 tiles of 4 x 2048 tokens over up to 8000, 136 MB of parts.
 template <typename T, int LANES, int ROWS> __global__ __launch_bounds__(256) void k_attend_join(Attend a, int64_t first)
 {
     constexpr int kAtOnce = kWave / LANES, kAhead = 4 / ROWS;   // parts side by side, and one behind the other on their way
