@@ -232,6 +232,44 @@ def test_attention_in_parts(name):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("name", TYPES)
+@pytest.mark.parametrize("dim", [40, 64, 96, 128, 136])
+def test_many_rows_of_long_tables(name, dim):
+    """Tables with room for many positions, so that tiles are the largest ones: rows that fill them and do not, infinities and NaN behind texts and before windows, a page that
+    is not held, and a new token's value that only later rows see."""
+    import torch
+    for k, (sizes, kv_heads, group, page, how) in enumerate([
+            ([(150, 700), (0, 5), (65, 65), (257, 900), (1, 333)], 1, 2, 16, {}),
+            ([(100, 160), (90, 1300), (3, 50)], 2, 4, 64, {"softcap": 20.0}),
+            ([(200, 600), (129, 129)], 52, 3, 8, {"window": 75})]):
+        print(f"[long tables] {name} dim {dim} case {k}", flush=True)
+        b = Batch(sizes, name, kv_heads, group, dim, page, seed=dim + k, wide=32768 // page)
+        if k == 0:
+            b.table[0, 3] = -1
+            b.args[0] = b.on(b.table)
+        want = b.check(f"case {k}", **how)
+        window, unseen = how.get("window", 0), torch.ones(b.pages, page, dtype=torch.bool)
+        for s, (n, length) in enumerate(sizes):
+            at, place = b.slots(s, np.arange(max(0, length - n - window + 1) if window else 0, length))
+            unseen[at[at >= 0], place[at >= 0]] = False
+        for bad in (float("nan"), INF):
+            keys, values = b.keys.clone(), b.values.clone()
+            b.keys.masked_fill_(unseen.cuda()[:, None, :, None], bad)
+            b.values.masked_fill_(unseen.cuda()[:, None, :, None], bad)
+            n, length = sizes[0]
+            (at,), (place,) = b.slots(0, np.array([length - 9]))
+            b.values[at, :, place, 5] = bad
+            got = b.attend(**how)
+            rows = np.ones(b.tokens, bool)
+            rows[n - 9:n] = False
+            assert torch.equal(got[rows], want[rows])
+            assert not torch.isfinite(got[~rows][:, :, 5]).any()
+            others = np.arange(dim) != 5
+            assert torch.equal(got[~rows][:, :, others], want[~rows][:, :, others])
+            b.keys.copy_(keys), b.values.copy_(values)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("name", TYPES)
 @pytest.mark.parametrize("page", [16, 5])
 def test_what_a_query_does_not_see(name, page):
     """NaN and infinities in slots behind a text, in pages of no one, before a window, and in new tokens that only later rows see."""
