@@ -212,6 +212,9 @@ __device__ __forceinline__ void add_odd(const Attend &a, const int32_t *table, i
         const Slot slot = slot_of(a.c, table, position);
         if (slot.page < 0) continue;
         const T *values = row_of<T>(a.c.values, a.c.ldv, a.c, kv_head, slot);
+        float weight[NQ];   // (of all lanes, before some of them leave: a lane that is switched off has nothing to give)
+#pragma unroll
+        for (int n = 0; n < NQ; n++) weight[n] = weight_of(weights[n], position - step, column);
         int32_t at = kTiles * 4 * (lane / 16);
 #pragma unroll
         for (int k = 0; k < 4; k++)
@@ -224,12 +227,11 @@ __device__ __forceinline__ void add_odd(const Attend &a, const int32_t *table, i
                 v.load(values + d);
 #pragma unroll
                 for (int n = 0; n < NQ; n++) {
-                    const float weight = weight_of(weights[n], position - step, column);
                     const bool sees = (uint32_t)(position - low[n]) < (uint32_t)count[n];
 #pragma unroll
                     for (int i = 0; i < kEach; i++) {
                         const float value = v.get(i);
-                        if (sees && !(fabsf(value) < INFINITY)) o[n][c + i][k] += weight * value;
+                        if (sees && !(fabsf(value) < INFINITY)) o[n][c + i][k] += weight[n] * value;
                     }
                 }
             }
