@@ -21,6 +21,9 @@ typedef uint16_t ushort2_t __attribute__((ext_vector_type(2)));
 template <typename T, int N> using vec_t = T __attribute__((ext_vector_type(N)));
 
 constexpr float kLowest = -3.4028234663852886e38f;
+// From here on an exponent's own rounding would count: the largest one, score times `per` in fp32, is off by up to half a place (an eighth below 2^22, 64 at 2^31), and a weight that is exp2 of the exact
+// product less that would be as many powers of 2 too large or too small, until the largest one overflows or vanishes.
+constexpr float kFarExponent = 4194304.0f;
 
 __device__ __forceinline__ uint32_t low_halves(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x05040100u); }    // a's, then b's
 __device__ __forceinline__ uint32_t high_halves(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x07060302u); }
@@ -160,6 +163,31 @@ template <typename T> __device__ __forceinline__ uint32_t without_odd(uint32_t w
     const uint32_t low = (w & 0x7fffu) >= kInfinite<T> ? 0u : w & 0xffffu, high = (w >> 16 & 0x7fffu) >= kInfinite<T> ? 0u : w & 0xffff0000u;
     return low | high;
 }
+// Rows whose largest exponent m is far from 0 have exponents rounded as m was: their scores become those that `per` makes differences to m of, without m (less); or the weights that
+// have been made of them are made again.
+__device__ __forceinline__ void far_scores(float (&e)[8], float m, float per, float &less)
+{
+    if (!(fabsf(m) >= kFarExponent)) return;
+    less = 0.0f;
+    const float inverse = 1.0f / per;
+#pragma unroll
+    for (int i = 0; i < 8; i++) {
+#pragma clang fp contract(off)
+        const float exponent = e[i] * per;
+        e[i] = (exponent - m) * inverse;
+    }
+}
+__device__ __forceinline__ void far_weights(float (&p)[8], const float (&e)[8], float m, float per)
+{
+    const bool far = fabsf(m) >= kFarExponent;
+#pragma unroll
+    for (int i = 0; i < 8; i++) {
+#pragma clang fp contract(off)
+        const float exponent = e[i] * per;
+        p[i] = far ? __builtin_amdgcn_exp2f(exponent - m) : p[i];
+    }
+}
+
 // The weight of position t of a step for the lane's query, from the lane that has it
 template <typename T> __device__ __forceinline__ float weight_of(const Operand<T> &weights, int t, int column)
 {
@@ -297,10 +325,12 @@ template <typename T, int D, int NQ, bool ANY_PAGE> __global__ __launch_bounds__
     const float per = a.cap_out != 0.0f ? 1.0f : a.per;   // (of what the cap has made of scores)
     float m[NQ], l[NQ];
     float4_t o[NQ][kTiles];
+    int32_t far[NQ];   // whether a row's largest exponent is far from 0 (the same in all lanes)
 #pragma unroll
     for (int n = 0; n < NQ; n++) {
         m[n] = kLowest;
         l[n] = 0.0f;
+        far[n] = 0;
 #pragma unroll
         for (int j = 0; j < kTiles; j++) o[n][j] = float4_t{0, 0, 0, 0};
     }
@@ -410,11 +440,12 @@ template <typename T, int D, int NQ, bool ANY_PAGE> __global__ __launch_bounds__
 #pragma unroll
                 for (int i = 1; i < 8; i++) top = fmaxf(top, e[i]);
                 top *= per;
-                // The weights are taken relative to an earlier largest exponent while none is more than 8 above it: sums stay far from overflow, and nothing is exchanged.
-                if (__ballot(top > m[n] + 8.0f) != 0) {
+                // The weights are taken relative to an earlier largest exponent while none is more than 8 above it (by the difference, which is exact): sums stay far from overflow, and nothing is exchanged.
+                if (__ballot(top - m[n] > 8.0f) != 0) {
                     const float to = over_quarters(fmaxf(top, m[n]), [](float p, float q) { return fmaxf(p, q); });
                     const float f = __builtin_amdgcn_exp2f(m[n] - to);
                     m[n] = to;
+                    far[n] = __ballot(fabsf(to) >= kFarExponent && to > kLowest) != 0;
                     l[n] *= f;
 #pragma unroll
                     for (int j = 0; j < kTiles; j++)
@@ -422,10 +453,10 @@ template <typename T, int D, int NQ, bool ANY_PAGE> __global__ __launch_bounds__
                         for (int i = 0; i < 4; i++) o[n][j][i] *= f;
                 }
 #pragma unroll
-                for (int i = 0; i < 8; i++) {
-                    p[i] = __builtin_amdgcn_exp2f(fmaf(e[i], per, -m[n]));   // (the exponent is rounded as a difference to the largest one)
-                    l[n] += p[i];
-                }
+                for (int i = 0; i < 8; i++) p[i] = __builtin_amdgcn_exp2f(fmaf(e[i], per, -m[n]));   // (the exponent is rounded as a difference to the largest one)
+                if (one(far[n])) far_weights(p, e, m[n], per);
+#pragma unroll
+                for (int i = 0; i < 8; i++) l[n] += p[i];
                 weights[n] = Operand<T>::of(p);
             }
 

@@ -92,6 +92,7 @@ template <typename T, int D, int NQ, bool WHOLE> __global__ __launch_bounds__(kR
     const float per = a.cap_out != 0.0f ? 1.0f : a.per;   // (of what the cap has made of scores)
     float m[NQ], l[NQ];
     float4_t o[NQ][kTiles];
+    int32_t far = 0;   // whether some row's largest exponent is far from 0 (the same in all lanes)
 #pragma unroll
     for (int n = 0; n < NQ; n++) {
         m[n] = kLowest;
@@ -294,6 +295,7 @@ template <typename T, int D, int NQ, bool WHOLE> __global__ __launch_bounds__(kR
                     look_ahead(turn_number);
                 }
                 const int32_t block = turn + b * kStep;
+                float less[NQ];
                 if (active) {
                     if constexpr (sizeof(T) == 4)
 #pragma unroll
@@ -328,20 +330,38 @@ template <typename T, int D, int NQ, bool WHOLE> __global__ __launch_bounds__(kR
 #pragma unroll
                         for (int i = 1; i < 8; i++) top[n] = fmaxf(top[n], s[n][i / 4][i % 4]);
                         top[n] *= per;
-                        larger |= top[n] > m[n] + 8.0f;
+                        larger |= top[n] - m[n] > 8.0f;
                     }
                     if (__ballot(larger) != 0) {   // (see k_attend)
+                        far = 0;
 #pragma unroll
                         for (int n = 0; n < NQ; n++) {
                             const float to = over_quarters(fmaxf(top[n], m[n]), [](float p, float q) { return fmaxf(p, q); });
                             const float f = __builtin_amdgcn_exp2f(m[n] - to);
                             m[n] = to;
+                            far |= __ballot(fabsf(to) >= kFarExponent && to > kLowest) != 0;
                             l[n] *= f;
 #pragma unroll
                             for (int j = 0; j < kTiles; j++)
 #pragma unroll
                                 for (int i = 0; i < 4; i++) o[n][j][i] *= f;
                         }
+                    }
+                    // (far rows' scores are changed here, or their weights below where the order is given: 16-bit prompts of heads of 128 735 us, and 812 with scores changed; fp32 prompts the other way
+                    // round, 224 and 232)
+                    if constexpr (!kOrdered) {
+#pragma unroll
+                        for (int n = 0; n < NQ; n++) less[n] = m[n];
+                        if (one(far))
+#pragma unroll
+                            for (int n = 0; n < NQ; n++) {
+                                float e[8];
+#pragma unroll
+                                for (int i = 0; i < 8; i++) e[i] = s[n][i / 4][i % 4];
+                                far_scores(e, m[n], per, less[n]);
+#pragma unroll
+                                for (int i = 0; i < 8; i++) s[n][i / 4][i % 4] = e[i];
+                            }
                     }
                 }
                 if (kBuffers > 1 && b == kBlocks - 1) barrier();   // (the next turn's operands are in LDS; their buffer was read last in the turn before this one)
@@ -352,15 +372,25 @@ template <typename T, int D, int NQ, bool WHOLE> __global__ __launch_bounds__(kR
                         __builtin_amdgcn_sched_barrier(0);
                     }
                     Operand<T> weights[NQ];
+                    float p[NQ][8];
+#pragma unroll
+                    for (int n = 0; n < NQ; n++)
+#pragma unroll
+                        for (int i = 0; i < 8; i++) p[n][i] = __builtin_amdgcn_exp2f(fmaf(s[n][i / 4][i % 4], per, -(kOrdered ? m[n] : less[n])));
+                    if constexpr (kOrdered)
+                        if (one(far))
+#pragma unroll
+                            for (int n = 0; n < NQ; n++) {
+                                float e[8];
+#pragma unroll
+                                for (int i = 0; i < 8; i++) e[i] = s[n][i / 4][i % 4];
+                                far_weights(p[n], e, m[n], per);
+                            }
 #pragma unroll
                     for (int n = 0; n < NQ; n++) {
-                        float p[8];
 #pragma unroll
-                        for (int i = 0; i < 8; i++) {
-                            p[i] = __builtin_amdgcn_exp2f(fmaf(s[n][i / 4][i % 4], per, -m[n]));
-                            l[n] += p[i];
-                        }
-                        weights[n] = Operand<T>::of(p);
+                        for (int i = 0; i < 8; i++) l[n] += p[n][i];
+                        weights[n] = Operand<T>::of(p[n]);
                     }
                     if constexpr (kOrdered) __builtin_amdgcn_sched_barrier(0);
                     if (kBuffers > 1 || b < kBlocks - 1) scores(s, next_which, next_block);   // (behind the last turn of nothing, for nothing)

@@ -36,3 +36,38 @@ def test_infinite_values_that_all_rows_see(name, dim):
                 assert (got[..., columns[k]] == signs[k]).all(), f"{how}: column {columns[k]}, eight {k}"
                 got[..., columns[k]] = torch.from_numpy(want[..., columns[k]]).to(got)
             agree(got, want, off + UNIT[name] * np.abs(want), f"{how} turn {turn}")
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("name", TYPES)
+def test_scores_whose_differences_are_large(name):
+    """Whole multiples of 2^10 to 2^100 as scores, exact in fp32, of which any two are equal or far apart: the result is the value at the largest one, or the mean of two values where there are two."""
+    import torch
+    rng = np.random.default_rng(7)
+    for sizes, page in (([(3, 300), (1, 40)], 16), ([(2, 300)], 5), ([(50, 300)], 16), ([(1, 9000)], 16), ([(50, 9000)], 16)):
+        for power in (10, 15, 16, 17, 18, 19, 20, 22, 26) if name == "f16" else (10, 18, 20, 26, 34, 60, 100):
+            b = Batch(sizes, name, 1, 2, 64, page, seed=power)
+            # scores are n 2^power with whole numbers n up to 251, of 16 columns of queries times 16 of keys
+            of_q = 2.0 ** min(power // 2 + 1, 14)
+            of_k = 2.0 ** (power - 4) / of_q
+            b.q[:], b.keys[:] = 0.0, 0.0
+            b.q[..., :16] = of_q
+            for scale in (1.0, -0.7, 0.3, 0.0517):
+                for ties in (False, True):
+                    tops = []
+                    for s, (n, length) in enumerate(sizes):
+                        numbers = rng.integers(0, 250, length)
+                        tops.append(rng.choice(length - n + 1, 2 if ties else 1, replace=False))
+                        numbers[tops[-1]] = 251
+                        at, place = b.slots(s, np.arange(length))
+                        b.keys[at, 0, place, :16] = b.on(np.sign(scale) * numbers[:, None] * of_k).to(b.keys.dtype).expand(-1, 16)
+                    assert torch.isfinite(b.keys).all()
+                    print(f"[large scores] {name} {sizes} page {page} 2^{power} scale {scale} ties {ties}", flush=True)
+                    got = b.attend(scale=scale).double().cpu().numpy()
+                    for s, (n, length) in enumerate(sizes):
+                        at, place = b.slots(s, tops[s])
+                        v = b.values[at, 0, place].double().cpu().numpy()
+                        # One weight times a value, or two equal ones: a 16-bit type's weights are rounded for the product and not for the sum, half a step; products, sums and their quotient are off
+                        # by 8 roundings of fp32 at most, and the result is rounded once.
+                        off = (8 * 2.0 ** -24 + (2 if name != "f32" else 1) * UNIT[name]) * np.abs(v).mean(0) + TINY[name]
+                        rows = got[b.starts[s]:b.starts[s] + n]
+                        assert (np.abs(rows - v.mean(0)) <= off).all(), f"{sizes} page {page} 2^{power} scale {scale} ties {ties}: {np.abs(rows - v.mean(0)).max()}"
