@@ -163,6 +163,11 @@ template <typename T> __device__ __forceinline__ uint32_t without_odd(uint32_t w
     const uint32_t low = (w & 0x7fffu) >= kInfinite<T> ? 0u : w & 0xffffu, high = (w >> 16 & 0x7fffu) >= kInfinite<T> ? 0u : w & 0xffff0000u;
     return low | high;
 }
+// Weights of a row are taken relative to an earlier largest exponent until one is kSlack above it.  In fp16 it is taken 7 less: weights are then 2^7 where they are largest, 2^15 at most, and
+// small ones are rounded to multiples of 2^-24, at most 2^-31 of the largest one and not 2^-24 of it (of a long tail of weights of 2^-25.1 nothing would be left in the result, and 0.3 % in the sum).
+template <typename T> constexpr float kUp = std::is_same_v<T, f16> ? 7.0f : 0.0f;
+template <typename T> constexpr float kSlack = 8.0f + kUp<T>;
+
 // Rows whose largest exponent m is far from 0 have exponents rounded as m was: their scores become those that `per` makes differences to m of, without m (less); or the weights that
 // have been made of them are made again.
 __device__ __forceinline__ void far_scores(float (&e)[8], float m, float per, float &less)
@@ -440,9 +445,9 @@ template <typename T, int D, int NQ, bool ANY_PAGE> __global__ __launch_bounds__
 #pragma unroll
                 for (int i = 1; i < 8; i++) top = fmaxf(top, e[i]);
                 top *= per;
-                // The weights are taken relative to an earlier largest exponent while none is more than 8 above it (by the difference, which is exact): sums stay far from overflow, and nothing is exchanged.
-                if (__ballot(top - m[n] > 8.0f) != 0) {
-                    const float to = over_quarters(fmaxf(top, m[n]), [](float p, float q) { return fmaxf(p, q); });
+                // The weights are taken relative to an earlier largest exponent while none is more than kSlack above it (by the difference, which is exact): sums stay far from overflow, and nothing is exchanged.
+                if (__ballot(top - m[n] > kSlack<T>) != 0) {
+                    const float to = over_quarters(fmaxf(top - kUp<T>, m[n]), [](float p, float q) { return fmaxf(p, q); });
                     const float f = __builtin_amdgcn_exp2f(m[n] - to);
                     m[n] = to;
                     far[n] = __ballot(fabsf(to) >= kFarExponent && to > kLowest) != 0;

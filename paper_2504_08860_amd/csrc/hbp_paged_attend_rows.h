@@ -330,13 +330,13 @@ template <typename T, int D, int NQ, bool WHOLE> __global__ __launch_bounds__(kR
 #pragma unroll
                         for (int i = 1; i < 8; i++) top[n] = fmaxf(top[n], s[n][i / 4][i % 4]);
                         top[n] *= per;
-                        larger |= top[n] - m[n] > 8.0f;
+                        larger |= top[n] - m[n] > kSlack<T>;
                     }
                     if (__ballot(larger) != 0) {   // (see k_attend)
                         far = 0;
 #pragma unroll
                         for (int n = 0; n < NQ; n++) {
-                            const float to = over_quarters(fmaxf(top[n], m[n]), [](float p, float q) { return fmaxf(p, q); });
+                            const float to = over_quarters(fmaxf(top[n] - kUp<T>, m[n]), [](float p, float q) { return fmaxf(p, q); });
                             const float f = __builtin_amdgcn_exp2f(m[n] - to);
                             m[n] = to;
                             far |= __ballot(fabsf(to) >= kFarExponent && to > kLowest) != 0;

@@ -71,3 +71,38 @@ def test_scores_whose_differences_are_large(name):
                         off = (8 * 2.0 ** -24 + (2 if name != "f32" else 1) * UNIT[name]) * np.abs(v).mean(0) + TINY[name]
                         rows = got[b.starts[s]:b.starts[s] + n]
                         assert (np.abs(rows - v.mean(0)) <= off).all(), f"{sizes} page {page} 2^{power} scale {scale} ties {ties}: {np.abs(rows - v.mean(0)).max()}"
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("name", TYPES)
+@pytest.mark.parametrize("new", [1, 40])
+def test_one_position_that_outweighs_a_long_tail(name, new):
+    """One position with a score of 0 and 122879 of about -17.4: weights of 2^-25.1 of the largest one, which are 0.3 % of the sum together.  As many heads of keys as keep texts whole."""
+    import torch
+    size, times, heads, dim = 4096, 30, 512, 8
+    length = size * times
+    g = torch.Generator(device="cuda").manual_seed(new)
+    keys, values = (torch.zeros(2, heads, size, dim, dtype=dtype(name), device="cuda") for _ in range(2))
+    keys[..., 0] = -17.40625      # (as a number of the type, which is taken below)
+    keys[0, :, 5, 0] = 0.0
+    values.copy_(1 + 0.1 * torch.randn(values.shape, generator=g, device="cuda"))
+    values[0, :, 5, :4] = 0.0
+    q = torch.zeros(new, heads, dim, dtype=dtype(name), device="cuda")
+    q[..., 0] = 1.0
+    table = torch.tensor([[0] + [1] * (times - 1)], dtype=torch.int32, device="cuda")
+    args = table, torch.tensor([0, new], dtype=torch.int32, device="cuda"), torch.tensor([length], dtype=torch.int32, device="cuda")
+    out = torch.full_like(q, float("nan"))
+    H.hbp_paged_attention(q, keys, values, *args, out, scale=1.0)
+    v, weight = values.double(), np.exp(float(keys[1, 0, 0, 0]))
+    whole = v[0].sum(1) - v[0, :, 5] + (times - 2) * v[1].sum(1)
+    for i in range(new):
+        seen = size - new + i + 1      # of the last page
+        tail, count = whole + v[1, :, :seen].sum(1), length - size + seen - 1
+        sums = 1 + weight * count
+        want = (v[0, :, 5] + weight * tail) / sums
+        # Of scores with one term an exponent is off by 4 roundings of its size (25).  Weights of 16-bit types are off by half a step, and those of fp16, where they are small, by 2^-32 of the largest one
+        # (which is held as 2^7 or more; 2^-25 is half the smallest step).  Sums of 122880 terms in fp32, of 8 lanes' and instructions' sums each: at most 15360 roundings, all of one sign, of half a step.
+        most = UNIT[name] if name != "f32" else 0.0
+        tiny = 2.0 ** -32 * tail / sums if name == "f16" else 0.0
+        off = (most + (4 * 25 * 0.7 + 2 * 15360) * 2.0 ** -24) * want + tiny + UNIT[name] * want + TINY[name]
+        worst = ((out[i].double() - want).abs() / off).max().item()
+        assert worst <= 1, f"row {i}: {worst:.3g} times what is allowed"
