@@ -98,12 +98,33 @@ template <typename F> __device__ __forceinline__ float over_quarters(float v, F 
     return op(__uint_as_float(b[0]), __uint_as_float(b[1]));
 }
 
-// Exponents of 2 of scores with a cap.  tanh x = 1 - 2 / (e^2x + 1), off by some 2^-24 of 1 where x is small, which is 2^-24 of the cap in the exponent; fp32 results would show it.
+// Exponents of 2 of scores with a cap.  tanh x = 1 - 2 / (e^2x + 1) is off by some 2^-22 of 1 also where x is small, which is as much of the cap in the exponent: fp32 results would show it, and those of 16-bit types
+// with caps above kNearCap (up to there it is 3e-5 of a weight, a sixteenth of fp16's half step).
+constexpr float kNearCap = 128.0f, kPerLog2 = 1.4426950408889634f;
 template <typename T> __device__ __forceinline__ float capped(const Attend &a, float score)
 {
     if constexpr (sizeof(T) == 4) return a.cap_out * tanhf(score * a.cap_in);
-    const float e = __builtin_amdgcn_exp2f(score * (a.cap_in * (2.0f * 1.4426950408889634f)));
+    const float e = __builtin_amdgcn_exp2f(score * (a.cap_in * (2.0f * kPerLog2)));
     return a.cap_out - 2.0f * a.cap_out * __builtin_amdgcn_rcpf(e + 1.0f);
+}
+template <typename T> __host__ __device__ __forceinline__ bool has_far_cap(const Attend &a) { return sizeof(T) == 2 && a.cap_out > kNearCap * kPerLog2; }
+// The same of a lane's eight scores, off relative to what comes out, for 16-bit types and any cap: x below 3/8 by tanh's series, whose first term left out is 3e-8 of it there, and the others by their magnitude, 7e-7
+// of it at the most.  One score after the other: it is not to cost room in the loops that it stands in.
+__device__ __forceinline__ void far_capped(const Attend &a, float (&e)[8])
+{
+#pragma unroll 1
+    for (int i = 0; i < 8; i++) {
+        float score = e[0];
+#pragma unroll
+        for (int j = 1; j < 8; j++) score = j == i ? e[j] : score;
+        const float x = score * a.cap_in, y = x * x;
+        const float near = fmaf(fmaf(fmaf(fmaf(fmaf(-1382.0f / 155925.0f, y, 62.0f / 2835.0f), y, -17.0f / 315.0f), y, 2.0f / 15.0f), y, -1.0f / 3.0f), y * x, x);
+        const float power = __builtin_amdgcn_exp2f(fabsf(x) * (2.0f * kPerLog2));
+        const float other = copysignf(fmaf(-2.0f, __builtin_amdgcn_rcpf(power + 1.0f), 1.0f), x);
+        score = a.cap_out * (fabsf(x) < 0.375f ? near : other);
+#pragma unroll
+        for (int j = 0; j < 8; j++) e[j] = j == i ? score : e[j];
+    }
 }
 
 // A position's slot: its page (-1: not held) and the place in it
@@ -432,9 +453,13 @@ template <typename T, int D, int NQ, bool ANY_PAGE> __global__ __launch_bounds__
 #pragma unroll
                 for (int i = 0; i < 8; i++) e[i] = s[n][i / 4][i % 4];
                 if constexpr (sizeof(T) == 4) by_definition(a, x, table, kv_head, x.tile * a.tile_rows + n * 16 + column, step, low[n], count[n], held, e);
-                if (a.cap_out != 0.0f)
+                if (a.cap_out != 0.0f) {
+                    if (has_far_cap<T>(a))
+                        far_capped(a, e);
+                    else
 #pragma unroll
-                    for (int i = 0; i < 8; i++) e[i] = capped<T>(a, e[i]);
+                        for (int i = 0; i < 8; i++) e[i] = capped<T>(a, e[i]);
+                }
                 if (!whole)
 #pragma unroll
                     for (int i = 0; i < 8; i++) {

@@ -17,7 +17,7 @@ constexpr int kRowThreads = 512;
 template <typename T, int D> constexpr int row_turn() { return sizeof(T) == 4 ? (D == 64 ? 64 : 32) : 8192 / D; }
 template <typename T, int D> constexpr int row_buffers() { return sizeof(T) == 4 && D > 128 ? 1 : 3; }   // (as LDS has room for)
 template <typename T, int D> constexpr size_t row_lds() { return row_buffers<T, D>() * 2 * (size_t)row_turn<T, D>() * D * (sizeof(T) == 4 ? 6 : 2); }
-template <typename T, int D, int NQ, bool WHOLE> __global__ __launch_bounds__(kRowThreads) void k_attend_rows(Attend a, int64_t first_unit)
+template <typename T, int D, int NQ, bool WHOLE, bool FAR_CAP> __global__ __launch_bounds__(kRowThreads) void k_attend_rows(Attend a, int64_t first_unit)
 {
     constexpr int kParts = sizeof(T) == 4 ? 3 : 1;             // of an operand, see Operand
     constexpr int kTurn = row_turn<T, D>(), kBuffers = row_buffers<T, D>(), kBlocks = kTurn / kStep, kEights = kTurn / 8;
@@ -309,9 +309,19 @@ template <typename T, int D, int NQ, bool WHOLE> __global__ __launch_bounds__(kR
                         }
                     if (a.cap_out != 0.0f) {
 #pragma unroll
-                        for (int n = 0; n < NQ; n++)
+                        for (int n = 0; n < NQ; n++) {
+                            if constexpr (FAR_CAP) {
+                                float e[8];
 #pragma unroll
-                            for (int i = 0; i < 8; i++) s[n][i / 4][i % 4] = capped<T>(a, s[n][i / 4][i % 4]);
+                                for (int i = 0; i < 8; i++) e[i] = s[n][i / 4][i % 4];
+                                far_capped(a, e);
+#pragma unroll
+                                for (int i = 0; i < 8; i++) s[n][i / 4][i % 4] = e[i];
+                            } else {
+#pragma unroll
+                                for (int i = 0; i < 8; i++) s[n][i / 4][i % 4] = capped<T>(a, s[n][i / 4][i % 4]);
+                            }
+                        }
                     }
                     if (block < all_low || block + kStep > all_high || (held >> (4 * b) & 0xf) != 0xf) {
 #pragma unroll
@@ -463,11 +473,11 @@ template <typename T, int D, int NQ, bool WHOLE> __global__ __launch_bounds__(kR
     }
 }
 
-template <typename T, int D, int NQ, bool WHOLE> int launch_rows(const Attend &a, hipStream_t st)
+template <typename T, int D, int NQ, bool WHOLE, bool FAR_CAP = false> int launch_rows(const Attend &a, hipStream_t st)
 {
     constexpr int64_t kMost = int64_t(1) << 22;
     constexpr size_t kLds = row_lds<T, D>();
-    auto kernel = k_attend_rows<T, D, NQ, WHOLE>;
+    auto kernel = k_attend_rows<T, D, NQ, WHOLE, FAR_CAP>;
     HBP_HIP(hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)kLds));
     const int64_t units = a.units * a.c.kv_heads;
     for (int64_t at = 0; at < units; at += kMost) {
@@ -486,6 +496,13 @@ template <typename T> int launch_attend(const Attend &a, hipStream_t st)
         if (any) return launch_units<T, D, 1, true>(a, st);
         if (a.tile_rows == 16) return launch_units<T, D, 1, false>(a, st);
         const bool whole = a.c.head_dim == D;
+        // (large caps have kernels of their own: asked for in the loop, they make prompts without a cap take 1.01 to 1.04 times as long, with one of 30 1.07)
+        if constexpr (sizeof(T) == 2)
+            if (has_far_cap<T>(a) && a.tile_rows >= 128) {
+                if constexpr (D * sizeof(T) < 512)
+                    if (a.tile_rows == 256) return launch_rows<T, D, 2, false, true>(a, st);
+                return launch_rows<T, D, 1, false, true>(a, st);
+            }
         if (a.tile_rows == 128) return whole ? launch_rows<T, D, 1, true>(a, st) : launch_rows<T, D, 1, false>(a, st);
         if constexpr (D * sizeof(T) < 512)
             if (a.tile_rows == 256) return whole ? launch_rows<T, D, 2, true>(a, st) : launch_rows<T, D, 2, false>(a, st);

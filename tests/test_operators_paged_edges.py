@@ -106,3 +106,34 @@ def test_one_position_that_outweighs_a_long_tail(name, new):
         off = (most + (4 * 25 * 0.7 + 2 * 15360) * 2.0 ** -24) * want + tiny + UNIT[name] * want + TINY[name]
         worst = ((out[i].double() - want).abs() / off).max().item()
         assert worst <= 1, f"row {i}: {worst:.3g} times what is allowed"
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("name", TYPES)
+def test_caps_far_above_the_scores(name):
+    """Caps of 10 to 10^30, and scores of a hundredth of the cap to three times it: what is lost in a capped score is relative to the score, not to the cap."""
+    for sizes, page in (([(2, 500), (1, 90)], 16), ([(2, 90)], 5), ([(50, 500)], 16)):
+        for cap, spread in ((10.0, 4.0), (127.0, 4.0), (129.0, 4.0), (129.0, 30.0), (129.0, 100.0), (1e3, 5.0), (1e3, 600.0), (1e4, 5.0), (1e5, 5.0), (1e6, 5.0), (1e7, 5.0), (1e15, 5.0), (1e30, 5.0)):
+            b = Batch(sizes, name, 1, 2, 128, page, seed=int(cap) % 1000)
+            b.q[:] = b.q * spread
+            b.values[:] = b.values.abs()
+            print(f"[caps] {name} {sizes} cap {cap} scores of {spread}", flush=True)
+            got = b.attend(softcap=cap).double().cpu().numpy()
+            q, keys, values = (t.double().cpu().numpy() for t in (b.q, b.keys, b.values))
+            for s, (n, length) in enumerate(sizes):
+                at, place = b.slots(s, np.arange(length))
+                key, value = keys[at, 0, place], values[at, 0, place]
+                for i in range(n):
+                    row, seen = q[b.starts[s] + i], length - n + i + 1
+                    raw = row @ key[:seen].T * 128 ** -0.5
+                    terms = np.abs(row) @ np.abs(key[:seen]).T * 128 ** -0.5
+                    z = cap * np.tanh(raw / cap)
+                    w = np.exp(z - z.max(1, keepdims=True))
+                    w /= w.sum(1, keepdims=True)
+                    # A score is off by 16 roundings of its terms (fp32: 64), which the cap does not make more of; tanh by 9 of its own size (worked through in fp32) and what it is of by 4, or, up to caps of 128, 4 of the cap; the exponent by 4
+                    # of its size.  A weight is off by what its score and the largest one are; 16-bit types' by half a step and fp16's by 2^-25.
+                    z_off = 2.0 ** -24 * ((16 if name != "f32" else 64) * terms + 20 * np.abs(z) + (4 * cap if cap <= 128 and name != "f32" else 0.0) + 4)
+                    w_off = 2 * z_off.max(1, keepdims=True) + 32 * 2.0 ** -24 + (UNIT[name] if name != "f32" else 0.0)
+                    want = w @ value[:seen]
+                    off = w_off * want + (2.0 ** -25 * value[:seen].sum(0) if name == "f16" else 0.0) + UNIT[name] * np.abs(want) + TINY[name]
+                    worst = np.max(np.abs(got[b.starts[s] + i] - want) / off)
+                    assert worst <= 1, f"{sizes} cap {cap} scores of {spread}: {worst:.3g} times what is allowed"
