@@ -435,7 +435,7 @@ int hbp_paged_append(const hbp_paged_t *cache /* HOST */, int64_t tokens, const 
 
 /* Attention of new tokens over the cache that already holds their own keys and values: for the query of row r and head h, at position p,
  *   out[r][h] = sum over j of w_j value_j, w = softmax over j of cap(scale q . key_j), j <= p and, with a window > 0, j > p - window,
- * over the positions that the cache holds, keys and values of head h / (heads / kv_heads); cap(s) = softcap tanh(s / softcap), or s where softcap is 0.  A query that
+ * over the positions that the cache holds, keys and values of head h / (heads / kv_heads); cap(s) = softcap tanh(s / softcap), or s where softcap is 0; softcap at most 1e30, scale below 2e38.  A query that
  * sees no position, or none with a score above -inf, gives 0.  What lies in slots that a query does not see has no part in its result, whatever it is.
  *   q, out [tokens][heads][head_dim], row strides ldq, ldo, `type` of the cache; out may be q.  heads a multiple of kv_heads.
  *   most_new  no sequence has more new tokens than this (rows of one behind it are not computed); 1 for decoding

@@ -68,7 +68,9 @@ int hbp_paged_attention(const hbp_paged_t *cache, int64_t tokens, const void *q,
     size_t need = 0;
     int rc = plan(cache, tokens, heads, window, most_new, &a, &need);
     if (rc != HBP_OK) return rc;
-    if (!std::isfinite(scale) || !std::isfinite(softcap) || softcap < 0 || (softcap > 0 && !std::isfinite(scale / softcap * 3.0f))) return HBP_ERR_INVALID_ARGUMENT;
+    constexpr float kPerLog2 = 1.4426950408889634f;
+    // (both are multiplied by 1 / log 2 below, and a larger cap's reciprocal would be no normal number)
+    if (!std::isfinite(scale * kPerLog2) || !(softcap >= 0 && softcap <= 1e30f) || (softcap > 0 && !std::isfinite(scale / softcap * 3.0f))) return HBP_ERR_INVALID_ARGUMENT;
     if (a.tokens == 0) return HBP_OK;
     const int64_t bytes = type_bytes(cache->type), row = (int64_t)heads * cache->head_dim;
     if (!q || !out || !aligned(q, bytes) || !aligned(out, bytes) || (tokens > 1 && (ldq < row || ldo < row))) return HBP_ERR_INVALID_ARGUMENT;
@@ -76,7 +78,6 @@ int hbp_paged_attention(const hbp_paged_t *cache, int64_t tokens, const void *q,
     rc = earlier_error();
     if (rc != HBP_OK) return rc;
     a.q = q; a.ldq = ldq; a.out = out; a.ldo = ldo;
-    constexpr float kPerLog2 = 1.4426950408889634f;
     a.keep = scale == 0 ? 0u : 0xffffffffu;
     a.flip = scale < 0 ? (cache->type == HBP_F32 ? 0x80000000u : 0x80008000u) : 0u;
     a.per = scale == 0 ? 1.0f : std::fabs(scale) * kPerLog2;

@@ -137,3 +137,12 @@ def test_caps_far_above_the_scores(name):
                     off = w_off * want + (2.0 ** -25 * value[:seen].sum(0) if name == "f16" else 0.0) + UNIT[name] * np.abs(want) + TINY[name]
                     worst = np.max(np.abs(got[b.starts[s] + i] - want) / off)
                     assert worst <= 1, f"{sizes} cap {cap} scores of {spread}: {worst:.3g} times what is allowed"
+
+def test_scales_and_caps_that_32_bits_do_not_hold():
+    """Refused before anything else is looked at, so also without rows."""
+    def attend(scale, cap):
+        return H.lib().hbp_paged_attention(cache_of(), 0, None, 0, 8, None, 0, scale, cap, 0, 1, None, 0, None)
+    for scale, cap in ((3e38, 0.0), (-3e38, 0.0), (1.0, 3e38), (1.0, 2e30), (0.0, 3e38)):
+        assert attend(scale, cap) == -1, (scale, cap)
+    for scale, cap in ((1e38, 0.0), (1.0, 1e30), (0.0, 1e30), (1e-20, 1e10), (-0.1, 50.0)):
+        assert attend(scale, cap) == 0, (scale, cap)
