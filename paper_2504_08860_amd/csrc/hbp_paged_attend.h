@@ -91,23 +91,23 @@ template <bool BY_TILE, int THREADS> __device__ __forceinline__ bool find_unit(c
         work += (int64_t)q.tiles * q.span;
     }
     // the sum in three pieces of 24 bits, so that it is the same in every kernel in whatever order it is added
-    int32_t piece[3] = {(int32_t)(work & 0xffffff), (int32_t)(work >> 24 & 0xffffff), (int32_t)(work >> 48)};
+    int32_t piece[3] = {(int32_t)(work & 0xffffff), (int32_t)(work >> 24 & 0xffffff), (int32_t)(work >> 48)};   // (64 lanes' sums are below 2^30; those of wavefronts are added in 64 bits)
 #pragma unroll
     for (int i = 0; i < 3; i++) piece[i] = wave_reduce(piece[i], [](int32_t p, int32_t q) { return p + q; });
-    if (!few) {
+    auto whole_of = [](const int32_t (&p)[3]) { return p[0] + ((int64_t)p[1] << 24) + ((int64_t)p[2] << 48); };
+    int64_t all_work = 0;
+    if (few) {
+        all_work = whole_of(piece);
+    } else {
         if (lane == 0)
 #pragma unroll
             for (int i = 0; i < 3; i++) work_of[wave][i] = piece[i];
         if (threadIdx.x == 0) found[0] = -1;
         __syncthreads();
 #pragma unroll
-        for (int i = 0; i < 3; i++) {
-            piece[i] = 0;
-#pragma unroll
-            for (int w = 0; w < kWaves; w++) piece[i] += work_of[w][i];
-        }
+        for (int w = 0; w < kWaves; w++) all_work += whole_of(work_of[w]);
     }
-    const double total = piece[0] + 16777216.0 * piece[1] + 281474976710656.0 * piece[2];
+    const double total = (double)all_work;
     const double share = fmax(fmax(ceil(total / a.aim), fmin(ceil(total / a.places), (double)a.enough)), (double)a.least);
     int32_t length = ((int32_t)fmin(share, 1073741824.0) + kStep - 1) / kStep * kStep;
     // (what the last part of each tile is shorter by makes them more than the places: a second turn of the chip for a few)

@@ -146,3 +146,21 @@ def test_scales_and_caps_that_32_bits_do_not_hold():
         assert attend(scale, cap) == -1, (scale, cap)
     for scale, cap in ((1e38, 0.0), (1.0, 1e30), (0.0, 1e30), (1e-20, 1e10), (-0.1, 50.0)):
         assert attend(scale, cap) == 0, (scale, cap)
+
+@pytest.mark.gpu
+def test_many_long_texts():
+    """256 texts of 129 times the same page of 65536 positions, 2^31 in all: as over the page once."""
+    import torch
+    n, size, dim, times = 256, 65536, 8, 129
+    g = torch.Generator(device="cuda").manual_seed(0)
+    r = lambda *shape: torch.randn(*shape, generator=g, device="cuda")  # noqa: E731
+    keys, values, q = r(1, 1, size, dim).bfloat16(), (1 + 0.2 * r(1, 1, size, dim)).bfloat16(), r(n, 1, dim).bfloat16()
+    table = torch.zeros(n, times, dtype=torch.int32, device="cuda")
+    starts, lengths = torch.arange(n + 1, dtype=torch.int32, device="cuda"), torch.full((n,), size * times, dtype=torch.int32, device="cuda")
+    out = torch.full_like(q, float("nan"))
+    H.hbp_paged_attention(q, keys, values, table, starts, lengths, out, most_new=1)
+    z = q[:, 0].double() @ keys[0, 0].double().t().contiguous() * dim ** -0.5
+    want = torch.softmax(z, 1) @ values[0, 0].double()
+    assert not torch.isnan(out).any(), f"{int(torch.isnan(out).sum())} values were not written"
+    # weights and the result are rounded to bf16, 2^-8 each at most; sums of 8 million terms over some thousand lanes, steps and parts are off by less than a thousandth of that
+    assert ((out[:, 0].double() - want).abs() <= (2 * 2.0 ** -8 + 2.0 ** -10) * want.abs()).all()
