@@ -2,6 +2,7 @@
 #pragma once
 
 #include "hbp_paged.h"
+#include "hbp_paged_split.h"
 
 namespace hbp {
 
@@ -22,8 +23,6 @@ struct Attend {
     float2 *partial_stats;     // [slots][kv_heads][tile_rows]: the largest exponent, the sum of weights
     int64_t tiles, units;      // at most, of one head of keys
 };
-
-constexpr int kStep = 32;   // positions that a matrix instruction takes at once; parts begin at multiples of it
 
 int launch_attend_f32(const Attend &a, hipStream_t st);
 int launch_attend_f16(const Attend &a, hipStream_t st);
@@ -107,18 +106,16 @@ template <bool BY_TILE, int THREADS> __device__ __forceinline__ bool find_unit(c
 #pragma unroll
         for (int w = 0; w < kWaves; w++) all_work += whole_of(work_of[w]);
     }
-    const double total = (double)all_work;
-    const double share = fmax(fmax(ceil(total / a.aim), fmin(ceil(total / a.places), (double)a.enough)), (double)a.least);
-    int32_t length = ((int32_t)fmin(share, 1073741824.0) + kStep - 1) / kStep * kStep;
+    int32_t length = part_length((double)all_work, a.places, a.aim, a.enough, a.least);
     // (what the last part of each tile is shorter by makes them more than the places: a second turn of the chip for a few)
     if (few && length < a.enough)
         for (int i = 0; i < 4; i++) {
-            const int32_t all = wave_reduce(own.tiles * (own.span <= a.whole ? 1 : max(1, (own.span + length - 1) / length)), [](int32_t p, int32_t q) { return p + q; });
+            const int32_t all = wave_reduce(own.tiles * part_count(own.span, length, a.whole), [](int32_t p, int32_t q) { return p + q; });
             const int64_t longer = ((int64_t)length * all / a.places + kStep) / kStep * kStep;
             if (all <= a.places || longer > a.enough) break;
             length = (int32_t)longer;
         }
-    auto parts_of = [&](const Sequence &q) { return q.span <= a.whole ? 1 : max(1, (int32_t)((q.span + length - 1) / length)); };
+    auto parts_of = [&](const Sequence &q) { return part_count(q.span, length, a.whole); };
     auto add = [&](const Sequence &q, int32_t &units, int32_t &slots) {
         const int32_t parts = parts_of(q);
         units += BY_TILE ? q.tiles : q.tiles * parts;

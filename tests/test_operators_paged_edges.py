@@ -164,3 +164,46 @@ def test_many_long_texts():
     assert not torch.isnan(out).any(), f"{int(torch.isnan(out).sum())} values were not written"
     # weights and the result are rounded to bf16, 2^-8 each at most; sums of 8 million terms over some thousand lanes, steps and parts are off by less than a thousandth of that
     assert ((out[:, 0].double() - want).abs() <= (2 * 2.0 ** -8 + 2.0 ** -10) * want.abs()).all()
+
+def test_parts_and_places_for_them(tmp_path):
+    """The rule by which texts are split, as the kernels have it, compiled for the CPU: never more parts than the host has counted on, for up to the most and the longest texts, and few heads of keys or many."""
+    import os
+    import subprocess
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    (tmp_path / "split.cc").write_text(r"""
+#include <stdio.h>
+#include <stdlib.h>
+#include "hbp_paged_split.h"
+int main()
+{
+    unsigned long long state = 1;
+    auto below = [&](double most) { state = state * 6364136223846793005ull + 1442695040888963407ull; return (long long)((state >> 11) / 9007199254740992.0 * most); };
+    for (int i = 0; i < 200000; i++) {
+        const int heads = 1 << below(17), wide = below(2);
+        const int places = (wide ? 256 : 512) / heads > 1 ? (wide ? 256 : 512) / heads : 1, aim = (wide ? 512 : 1024) / heads > 1 ? (wide ? 512 : 1024) / heads : 1;
+        const int enough = wide ? 2048 : 512, least = wide ? 256 : 128, whole = below(2) ? 512 : 1024, sequences = 1 + (int)below(40);
+        const double longest = below(2) ? 2147418111.0 : 1 << below(31);     // 2^31 - 65537, the most
+        long long total = 0, tiles_in_all = 0, units = 0, slots = 0;
+        int spans[40], tiles[40];
+        for (int s = 0; s < sequences; s++) {
+            spans[s] = (int)(below(3) ? longest : below(longest + 1));
+            tiles[s] = (int)below(below(2) ? 4 : 100000);
+            total += (long long)spans[s] * tiles[s];
+            tiles_in_all += tiles[s];
+        }
+        const int length = hbp::part_length((double)total, places, aim, enough, least);
+        if (length < least || length % hbp::kStep) return printf("a length of %d\n", length), 1;
+        for (int s = 0; s < sequences; s++) {
+            const int parts = hbp::part_count(spans[s], length, whole);
+            if (parts < 1) return printf("%d parts of %d positions\n", parts, spans[s]), 1;
+            units += (long long)tiles[s] * parts;
+            slots += parts > 1 ? (long long)tiles[s] * parts : 0;
+        }
+        if (units > tiles_in_all + aim + 1 || slots > 2 * aim + 2)
+            return printf("%lld units of %lld tiles, %lld places for parts, aim %d, parts of %d positions\n", units, tiles_in_all, slots, aim, length), 1;
+    }
+    return 0;
+}
+""")
+    subprocess.check_call(["g++", "-std=c++17", "-O1", "-I" + os.path.join(root, "paper_2504_08860_amd", "csrc"), str(tmp_path / "split.cc"), "-o", str(tmp_path / "split")])
+    subprocess.check_call([str(tmp_path / "split")])
