@@ -139,7 +139,7 @@ __device__ __forceinline__ Slot slot_of(const Paged &c, const int32_t *table, in
 }
 template <typename T> __device__ __forceinline__ const T *row_of(const void *pages, int64_t ld, const Paged &c, int32_t kv_head, Slot s)
 {
-    return static_cast<const T *>(pages) + (int64_t)max(s.page, 0) * ld + (int64_t)(kv_head * c.page_size + s.within) * c.head_dim;
+    return static_cast<const T *>(pages) + (int64_t)max(s.page, 0) * ld + (int64_t)kv_head * c.page_size * c.head_dim + s.within * c.head_dim;   // (the last one is below 2^24)
 }
 
 // N values (2 to 16, 4 or more bytes) of a row in the cache: rows are 16-byte aligned

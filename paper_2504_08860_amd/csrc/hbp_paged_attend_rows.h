@@ -115,7 +115,7 @@ template <typename T, int D, int NQ, bool WHOLE, bool FAR_CAP> __global__ __laun
     };
     auto tell = [&](int which, int i) {
         const bool held = entry >= 0 && entry < a.c.pages;
-        const int64_t page = held ? entry : 0, row = (int64_t)(kv_head * a.c.page_size + entry_position - a.c.by_page.divide(entry_position) * a.c.page_size) * dim;
+        const int64_t page = held ? entry : 0, row = (int64_t)kv_head * a.c.page_size * dim + (entry_position - a.c.by_page.divide(entry_position) * a.c.page_size) * dim;
         keys_at[which][i] = (page * a.c.ldk + row) | !held;   // (rows are of whole eights of values)
         values_at[which][i] = (page * a.c.ldv + row) | !held;
         return held;

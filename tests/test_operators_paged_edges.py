@@ -207,3 +207,33 @@ int main()
 """)
     subprocess.check_call(["g++", "-std=c++17", "-O1", "-I" + os.path.join(root, "paper_2504_08860_amd", "csrc"), str(tmp_path / "split.cc"), "-o", str(tmp_path / "split")])
     subprocess.check_call([str(tmp_path / "split")])
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("size", [65536, 65533])
+def test_pages_of_more_than_2_31_positions_of_heads(size):
+    """32800 heads of a page of 65536 positions: a page of 34 GB (keys and values are the same numbers in the same place), few rows and many."""
+    import torch
+    heads, dim = 32800, 8
+    assert heads * size > 2 ** 31
+    cache = torch.empty(1, heads, size, dim, dtype=torch.float16, device="cuda")
+    table, starts, lengths = (torch.tensor(v, dtype=torch.int32, device="cuda") for v in ([[0]], [0, 50], [50]))
+    g = torch.Generator(device="cuda").manual_seed(1)
+    q, k = (torch.randn(50, heads, dim, generator=g, device="cuda").half() for _ in range(2))
+    print(f"[large pages] {size}: append", flush=True)
+    H.hbp_paged_append(k, k, cache, cache, table, starts, lengths)
+    looked_at = [0, 1, 16400, 32767, 32768, 32799]
+    for h in looked_at:
+        assert torch.equal(cache[0, h, :50], k[:, h])
+    out = torch.full_like(q, float("nan"))
+    for new in (50, 1):
+        print(f"[large pages] {size}: {new} rows", flush=True)
+        starts[1] = new
+        H.hbp_paged_attention(q[-new:], cache, cache, table, starts, lengths, out[-new:], most_new=new)
+        assert torch.isfinite(out[-new:]).all()
+        for h in looked_at:
+            z = q[-new:, h].double() @ k[:, h].double().t().contiguous() * dim ** -0.5
+            z = z.masked_fill(torch.arange(50, device="cuda") > torch.arange(50 - new, 50, device="cuda")[:, None], -INF)
+            w = torch.softmax(z, 1)
+            want, size_of = w @ k[:, h].double(), w @ k[:, h].double().abs()
+            # weights are rounded to fp16 (half a step, or 2^-32 of the largest one) and the result; scores of 8 terms of up to 16, and sums of 50, are off by 2^-16 of a weight at the most
+            assert ((out[-new:, h].double() - want).abs() <= (2.0 ** -11 + 2.0 ** -15) * size_of + 2.0 ** -11 * want.abs() + 2.0 ** -24).all(), (new, h)
