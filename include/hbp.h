@@ -411,7 +411,7 @@ int hbp_token_logprobs_backward(int type, const void *logits, int64_t ldz, int64
  *          table[s][i].  A number that is no page (below 0 or from `pages` on) is a page that is not held: nothing is written there, and no query sees
  *          those positions.  A page may be in several sequences' rows (a shared prefix), for reading; where two rows write to one slot, either one's value is there.
  *   starts DEVICE int32 [sequences + 1], ascending: the new tokens of sequence s are rows starts[s] .. starts[s + 1] - 1 of every array of
- *          [tokens] rows; none, or many.  Rows of no sequence are not touched.
+ *          [tokens] rows; none, or many.  Rows of no sequence are not touched.  A sequence whose rows do not lie among them has none.
  *   lengths DEVICE int32 [sequences]: positions of sequence s with its new tokens, which are the last ones: row starts[s + 1] - 1 has position
  *          lengths[s] - 1.  Positions below 0 or from table_width * page_size on are not in the cache.
  * Read when the kernels run, so a captured graph takes the values that these arrays hold at each replay.

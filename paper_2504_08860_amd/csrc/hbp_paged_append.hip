@@ -87,8 +87,10 @@ template <typename T, int U> __global__ __launch_bounds__(kThreads) void k_paged
         };
         load(0);
         const int32_t s = sequence_of(a.c.starts, a.c.sequences, t);
-        if (s >= a.c.sequences || a.c.starts[s] > t) continue;   // (the same in all threads)
-        const int64_t position = (int64_t)a.c.lengths[s] - (a.c.starts[s + 1] - t);
+        if (s >= a.c.sequences) continue;   // (the same in all threads)
+        const int32_t begin = a.c.starts[s], end = a.c.starts[s + 1];
+        if (begin < 0 || begin > t || end > a.tokens) continue;   // (of no sequence, or of one whose rows are not all there, as in the attention)
+        const int64_t position = (int64_t)a.c.lengths[s] - (end - t);
         int64_t page = -1, within = 0;
         if (position >= 0 && position < a.c.capacity) {
             const int32_t which = a.c.by_page.divide((int32_t)position);

@@ -237,3 +237,26 @@ def test_pages_of_more_than_2_31_positions_of_heads(size):
             want, size_of = w @ k[:, h].double(), w @ k[:, h].double().abs()
             # weights are rounded to fp16 (half a step, or 2^-32 of the largest one) and the result; scores of 8 terms of up to 16, and sums of 50, are off by 2^-16 of a weight at the most
             assert ((out[-new:, h].double() - want).abs() <= (2.0 ** -11 + 2.0 ** -15) * size_of + 2.0 ** -11 * want.abs() + 2.0 ** -24).all(), (new, h)
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("name", TYPES)
+def test_rows_and_slots_beside_starts_that_are_none(name):
+    """Starts that fall, lie below 0 or beyond the rows: rows of the other sequences are what they were, those of no sequence are left, in results and in the cache."""
+    import torch
+    # (starts, {rows that the attention computes: as with good starts}, {rows that are appended})
+    for starts, good in (((0, 2, 99, 6), [0, 1]), ((-5, 2, 3, 6), [2, 3, 4, 5]), ((0, 2, 3, 7), [0, 1, 2]), ((0, 2, 3, 2 ** 31 - 1), [0, 1, 2]), ((-2 ** 31, 2, 3, 6), [2, 3, 4, 5])):
+        b = Batch([(2, 40), (1, 9), (3, 50)], name, 1, 2, 64, 16)
+        want, others = b.attend(), [i for i in range(6) if i not in good]
+        places = [b.slots(s, np.arange(length - n, length)) for s, (n, length) in enumerate(b.sizes)]
+        at, place = (np.concatenate(p) for p in zip(*places))
+        b.args[1] = b.on(np.array(starts, np.int32))
+        print(f"[starts that are none] {name} {starts}", flush=True)
+        out = b.attend(out=torch.full_like(want, 7.0))
+        assert bool(torch.equal(out[good], want[good])) and bool((out[others] == 7).all()), starts
+        keys, values = b.keys.clone(), b.values.clone()
+        keys[at[good], :, place[good]], values[at[good], :, place[good]] = b.k[good], b.v[good]
+        H.hbp_paged_append(b.k, b.v, b.keys, b.values, *b.args)
+        assert torch.equal(b.keys, keys) and torch.equal(b.values, values), starts
+        q_out = torch.full_like(b.q, 7.0)
+        H.hbp_paged_append(b.k, b.v, b.keys, b.values, *b.args, q=b.q, q_out=q_out)
+        assert bool(torch.equal(q_out[good], b.q[good])) and bool((q_out[others] == 7).all()), starts
