@@ -94,7 +94,9 @@ def decode(model, prompts, steps, drafts=4, temperature=0.0, seed=0):
     """`steps` new tokens (at least) behind each of `prompts` (lists of tokens): (the texts with them, drafts that stood, drafts that were made)."""
     gen = torch.Generator(device="cuda").manual_seed(seed)
     texts, count = [list(p) for p in prompts], len(prompts)
-    cache = model.cache(count, max(len(p) for p in prompts) + steps + 2 * drafts + 2)
+    # (while the slowest text gets one token a round, another one may get all its drafts and one more, and a last round's lie behind that)
+    most = max(len(p) for p in prompts) + (max(steps, 0) + 1) * (drafts + 1)
+    cache = model.cache(count, most)
     heat = torch.full((count,), temperature, device="cuda")
 
     # all of a prompt but its last token goes into the cache, the prompts of a batch at once
@@ -113,6 +115,7 @@ def decode(model, prompts, steps, drafts=4, temperature=0.0, seed=0):
     while min(len(t) - len(p) for t, p in zip(texts, prompts)) < steps:
         chunk = torch.empty(count, rows, dtype=torch.int32, device="cuda")
         chunk[:, 0] = _int32([t[-1] for t in texts])
+        assert max(len(t) for t in texts) + drafts <= most      # (what the table has no page for would not be cached, and nobody told)
         cached = _int32([len(t) for t in texts])     # (with the last token, which the first draft appends)
         for i in range(drafts):
             logits = model(chunk[:, i].long(), draft_starts, cached + i, cache, blocks=1, most_new=1).float()

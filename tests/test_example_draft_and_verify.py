@@ -85,3 +85,25 @@ def test_16_bit_models_run(example):
         m = example.Model(256, 2, 300, dtype=dtype, seed=7)
         texts, stood, made = example.decode(m, [[1, 2, 3], list(range(30))], 10, drafts=4, temperature=0.8)
         assert all(0 <= t < 300 for text in texts for t in text) and 0 <= stood <= made
+
+
+def test_one_text_whose_drafts_all_stand_beside_one_whose_never_do(example):
+    """The first text gets drafts + 1 tokens a round and the second one 1: the table has pages for all of them."""
+    import torch
+
+    class Steered(example.Model):
+        def cache(self, texts, most, **how):
+            made = super().cache(texts, most, **how)
+            self.room = made[1].shape[1] * made[0][0][0].shape[2]
+            return made
+
+        def __call__(self, tokens, starts, lengths, cache, blocks=None, most_new=None):
+            logits = super().__call__(tokens, starts, lengths, cache, blocks, most_new)
+            assert int(lengths.max()) <= self.room, f"{lengths.tolist()} positions in a table for {self.room}"
+            wanted = torch.zeros(len(tokens), dtype=torch.long, device="cuda") + 7
+            wanted[int(starts[1]):] = 8 if blocks else 9      # (drafts of the second text are 8, and the whole model wants 9)
+            return torch.full_like(logits, -20.0).scatter_(1, wanted[:, None], 20.0)
+    m = Steered(192, 2, 50, heads=6, kv_heads=2, seed=1)
+    for steps, drafts in ((12, 3), (5, 7), (1, 1)):
+        texts, stood, made = example.decode(m, [[1, 2, 3], [4] * 9], steps, drafts=drafts)
+        assert texts[0][3:] == [7] * (steps * (drafts + 1)) and texts[1][9:] == [9] * steps and 2 * stood == made == 2 * steps * drafts
