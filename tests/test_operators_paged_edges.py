@@ -43,9 +43,11 @@ def test_scores_whose_differences_are_large(name):
     """Whole multiples of 2^10 to 2^100 as scores, exact in fp32, of which any two are equal or far apart: the result is the value at the largest one, or the mean of two values where there are two."""
     import torch
     rng = np.random.default_rng(7)
-    for sizes, page in (([(3, 300), (1, 40)], 16), ([(2, 300)], 5), ([(50, 300)], 16), ([(1, 9000)], 16), ([(50, 9000)], 16)):
+    # few rows, any page, 128 rows a workgroup, parts of both; 256 rows (a table with room for many positions) and wide heads
+    for sizes, page, dim, kv_heads, wide in (([(3, 300), (1, 40)], 16, 64, 1, 0), ([(2, 300)], 5, 64, 1, 0), ([(50, 300)], 16, 64, 1, 0), ([(1, 9000)], 16, 64, 1, 0), ([(50, 9000)], 16, 64, 1, 0),
+                                             ([(150, 300), (7, 100)], 16, 64, 4, 2048), ([(150, 300)], 16, 128, 4, 2048), ([(50, 300), (70, 9000)], 16, 256, 1, 0), ([(5, 300)], 16, 256, 1, 0)):
         for power in (10, 15, 16, 17, 18, 19, 20, 22, 26) if name == "f16" else (10, 18, 20, 26, 34, 60, 100):
-            b = Batch(sizes, name, 1, 2, 64, page, seed=power)
+            b = Batch(sizes, name, kv_heads, 2, dim, page, seed=power, wide=wide)
             # scores are n 2^power with whole numbers n up to 251, of 16 columns of queries times 16 of keys
             of_q = 2.0 ** min(power // 2 + 1, 14)
             of_k = 2.0 ** (power - 4) / of_q
@@ -59,26 +61,26 @@ def test_scores_whose_differences_are_large(name):
                         tops.append(rng.choice(length - n + 1, 2 if ties else 1, replace=False))
                         numbers[tops[-1]] = 251
                         at, place = b.slots(s, np.arange(length))
-                        b.keys[at, 0, place, :16] = b.on(np.sign(scale) * numbers[:, None] * of_k).to(b.keys.dtype).expand(-1, 16)
+                        b.keys[at, :, place, :16] = b.on(np.sign(scale) * numbers[:, None, None] * of_k).to(b.keys.dtype).expand(-1, kv_heads, 16)
                     assert torch.isfinite(b.keys).all()
-                    print(f"[large scores] {name} {sizes} page {page} 2^{power} scale {scale} ties {ties}", flush=True)
+                    print(f"[large scores] {name} {sizes} page {page} dim {dim} 2^{power} scale {scale} ties {ties}", flush=True)
                     got = b.attend(scale=scale).double().cpu().numpy()
                     for s, (n, length) in enumerate(sizes):
                         at, place = b.slots(s, tops[s])
-                        v = b.values[at, 0, place].double().cpu().numpy()
+                        v = b.values[at, :, place].double().cpu().numpy().repeat(2, 1)     # (of each query's head of keys)
                         # One weight times a value, or two equal ones: a 16-bit type's weights are rounded for the product and not for the sum, half a step; products, sums and their quotient are off
                         # by 8 roundings of fp32 at most, and the result is rounded once.
                         off = (8 * 2.0 ** -24 + (2 if name != "f32" else 1) * UNIT[name]) * np.abs(v).mean(0) + TINY[name]
                         rows = got[b.starts[s]:b.starts[s] + n]
-                        assert (np.abs(rows - v.mean(0)) <= off).all(), f"{sizes} page {page} 2^{power} scale {scale} ties {ties}: {np.abs(rows - v.mean(0)).max()}"
+                        assert (np.abs(rows - v.mean(0)) <= off).all(), f"{sizes} page {page} dim {dim} 2^{power} scale {scale} ties {ties}: {np.abs(rows - v.mean(0)).max()}"
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("name", TYPES)
-@pytest.mark.parametrize("new", [1, 40])
-def test_one_position_that_outweighs_a_long_tail(name, new):
+@pytest.mark.parametrize("new,dim", [(1, 8), (40, 8), (300, 8), (40, 136)])
+def test_one_position_that_outweighs_a_long_tail(name, new, dim):
     """One position with a score of 0 and 122879 of about -17.4: weights of 2^-25.1 of the largest one, which are 0.3 % of the sum together.  As many heads of keys as keep texts whole."""
     import torch
-    size, times, heads, dim = 4096, 30, 512, 8
+    size, times, heads = 4096, 30, 512
     length = size * times
     g = torch.Generator(device="cuda").manual_seed(new)
     keys, values = (torch.zeros(2, heads, size, dim, dtype=dtype(name), device="cuda") for _ in range(2))
@@ -111,32 +113,36 @@ def test_one_position_that_outweighs_a_long_tail(name, new):
 @pytest.mark.parametrize("name", TYPES)
 def test_caps_far_above_the_scores(name):
     """Caps of 10 to 10^30, and scores of a hundredth of the cap to three times it: what is lost in a capped score is relative to the score, not to the cap."""
-    for sizes, page in (([(2, 500), (1, 90)], 16), ([(2, 90)], 5), ([(50, 500)], 16)):
-        for cap, spread in ((10.0, 4.0), (127.0, 4.0), (129.0, 4.0), (129.0, 30.0), (129.0, 100.0), (1e3, 5.0), (1e3, 600.0), (1e4, 5.0), (1e5, 5.0), (1e6, 5.0), (1e7, 5.0), (1e15, 5.0), (1e30, 5.0)):
-            b = Batch(sizes, name, 1, 2, 128, page, seed=int(cap) % 1000)
+    caps = (10.0, 4.0), (127.0, 4.0), (129.0, 4.0), (129.0, 30.0), (129.0, 100.0), (1e3, 5.0), (1e3, 600.0), (1e4, 5.0), (1e5, 5.0), (1e6, 5.0), (1e7, 5.0), (1e15, 5.0), (1e30, 5.0)
+    few = (129.0, 100.0), (1e3, 600.0), (1e5, 5.0), (1e7, 5.0)
+    for sizes, page, dim, kv_heads, wide, some in (([(2, 500), (1, 90)], 16, 128, 1, 0, caps), ([(2, 90)], 5, 128, 1, 0, caps), ([(50, 500)], 16, 128, 1, 0, caps), ([(60, 200)], 16, 40, 1, 0, few),
+                                                   ([(100, 200)], 16, 64, 4, 2048, few), ([(100, 200)], 16, 96, 4, 2048, few), ([(40, 200)], 16, 256, 1, 0, few), ([(2, 200)], 16, 256, 1, 0, few)):
+        for cap, spread in some:
+            b = Batch(sizes, name, kv_heads, 2, dim, page, seed=int(cap) % 1000, wide=wide)
             b.q[:] = b.q * spread
             b.values[:] = b.values.abs()
-            print(f"[caps] {name} {sizes} cap {cap} scores of {spread}", flush=True)
+            print(f"[caps] {name} {sizes} dim {dim} cap {cap} scores of {spread}", flush=True)
             got = b.attend(softcap=cap).double().cpu().numpy()
             q, keys, values = (t.double().cpu().numpy() for t in (b.q, b.keys, b.values))
             for s, (n, length) in enumerate(sizes):
                 at, place = b.slots(s, np.arange(length))
-                key, value = keys[at, 0, place], values[at, 0, place]
-                for i in range(n):
-                    row, seen = q[b.starts[s] + i], length - n + i + 1
-                    raw = row @ key[:seen].T * 128 ** -0.5
-                    terms = np.abs(row) @ np.abs(key[:seen]).T * 128 ** -0.5
-                    z = cap * np.tanh(raw / cap)
-                    w = np.exp(z - z.max(1, keepdims=True))
-                    w /= w.sum(1, keepdims=True)
-                    # A score is off by 16 roundings of its terms (fp32: 64), which the cap does not make more of; tanh by 9 of its own size (worked through in fp32) and what it is of by 4, or, up to caps of 128, 4 of the cap; the exponent by 4
-                    # of its size.  A weight is off by what its score and the largest one are; 16-bit types' by half a step and fp16's by 2^-25.
-                    z_off = 2.0 ** -24 * ((16 if name != "f32" else 64) * terms + 20 * np.abs(z) + (4 * cap if cap <= 128 and name != "f32" else 0.0) + 4)
-                    w_off = 2 * z_off.max(1, keepdims=True) + 32 * 2.0 ** -24 + (UNIT[name] if name != "f32" else 0.0)
-                    want = w @ value[:seen]
-                    off = w_off * want + (2.0 ** -25 * value[:seen].sum(0) if name == "f16" else 0.0) + UNIT[name] * np.abs(want) + TINY[name]
-                    worst = np.max(np.abs(got[b.starts[s] + i] - want) / off)
-                    assert worst <= 1, f"{sizes} cap {cap} scores of {spread}: {worst:.3g} times what is allowed"
+                for h in range(kv_heads):
+                    key, value = keys[at, h, place], values[at, h, place]
+                    for i in range(n):
+                        row, seen = q[b.starts[s] + i, 2 * h:2 * h + 2], length - n + i + 1
+                        raw = row @ key[:seen].T * dim ** -0.5
+                        terms = np.abs(row) @ np.abs(key[:seen]).T * dim ** -0.5
+                        z = cap * np.tanh(raw / cap)
+                        w = np.exp(z - z.max(1, keepdims=True))
+                        w /= w.sum(1, keepdims=True)
+                        # A score is off by 16 roundings of its terms (fp32: 64), which the cap does not make more of; tanh by 9 of its own size (worked through in fp32) and what it is of by 4, or, up to
+                        # caps of 128, 4 of the cap; the exponent by 4 of its size.  A weight is off by what its score and the largest one are; 16-bit types' by half a step and fp16's by 2^-32.
+                        z_off = 2.0 ** -24 * ((16 if name != "f32" else 64) * terms + 20 * np.abs(z) + (4 * cap if cap <= 128 and name != "f32" else 0.0) + 4)
+                        w_off = 2 * z_off.max(1, keepdims=True) + 32 * 2.0 ** -24 + (UNIT[name] if name != "f32" else 0.0)
+                        want = w @ value[:seen]
+                        off = w_off * want + (2.0 ** -32 * value[:seen].sum(0) if name == "f16" else 0.0) + UNIT[name] * np.abs(want) + TINY[name]
+                        worst = np.max(np.abs(got[b.starts[s] + i, 2 * h:2 * h + 2] - want) / off)
+                        assert worst <= 1, f"{sizes} dim {dim} cap {cap} scores of {spread}: {worst:.3g} times what is allowed"
 
 def test_scales_and_caps_that_32_bits_do_not_hold():
     """Refused before anything else is looked at, so also without rows."""
