@@ -28,6 +28,7 @@ template <typename T, int D, int NQ, bool WHOLE, bool FAR_CAP> __global__ __laun
     constexpr int kColumns = D * kEights / kRowThreads, kQuads = D / kColumns;                       // values: one or two columns of eight positions
     constexpr int kApart = 16 / (kTiles / kColumns), kSums = sizeof(T) == 4 && D < 256 ? 2 : 1;   // kSums: sums taken in turn
     constexpr bool kOrdered = sizeof(T) == 2 && (NQ == 2 || D == 256);   // weights first, then both products in an order that is given, see below (16 rows of 128: 4 x 60 tokens over 400 22.1 us, and 20.0 without)
+    constexpr bool kLate = kOrdered && NQ == 2;                // where rows with far exponents are seen to, see below
     constexpr int kHead = kOrdered ? 2 : 0, kAtOnce = 8;       // key steps whose operands are read before weights are made; operands on their way
     static_assert(kKeyLoads >= 1 && 8 % kKeyLoads == 0 && kColumns >= 1 && kQuads * kEights == kRowThreads, "");
     extern __shared__ uint4 lds[];
@@ -357,9 +358,8 @@ template <typename T, int D, int NQ, bool WHOLE, bool FAR_CAP> __global__ __laun
                                 for (int i = 0; i < 4; i++) o[n][j][i] *= f;
                         }
                     }
-                    // (far rows' scores are changed here, or their weights below where the order is given: 16-bit prompts of heads of 128 735 us, and 812 with scores changed; fp32 prompts the other way
-                    // round, 224 and 232)
-                    if constexpr (!kOrdered) {
+                    // (far rows' scores are changed here, or their weights below: with 2 x 16 rows of 16 bits 812 us and 735, 4 x 2048 tokens; with heads of 256 873 and 889, fp32 prompts 224 and 232)
+                    if constexpr (!kLate) {
 #pragma unroll
                         for (int n = 0; n < NQ; n++) less[n] = m[n];
                         if (one(far))
@@ -386,8 +386,8 @@ template <typename T, int D, int NQ, bool WHOLE, bool FAR_CAP> __global__ __laun
 #pragma unroll
                     for (int n = 0; n < NQ; n++)
 #pragma unroll
-                        for (int i = 0; i < 8; i++) p[n][i] = __builtin_amdgcn_exp2f(fmaf(s[n][i / 4][i % 4], per, -(kOrdered ? m[n] : less[n])));
-                    if constexpr (kOrdered)
+                        for (int i = 0; i < 8; i++) p[n][i] = __builtin_amdgcn_exp2f(fmaf(s[n][i / 4][i % 4], per, -(kLate ? m[n] : less[n])));
+                    if constexpr (kLate)
                         if (one(far))
 #pragma unroll
                             for (int n = 0; n < NQ; n++) {
