@@ -425,7 +425,8 @@ typedef struct {
 
 /* Puts the keys k and the values v [tokens][kv_heads][head_dim] of new tokens into the cache, and rotates keys and queries by their positions on the
  * way: with the angle a = position * frequencies[i], of the first 2 * pairs values of each head the pair (x, y) of values i and i + pairs
- * (interleaved: 2 i and 2 i + 1) becomes (x cos a - y sin a, y cos a + x sin a); the others stay.  Angles are held in 64 bits.
+ * (interleaved: 2 i and 2 i + 1) becomes (x cos a - y sin a, y cos a + x sin a); the others stay.  Angles are taken in 64 bits, and their place in a turn
+ * is rounded to fp32 before its sine and cosine (2^-25 of half a turn).
  *   k, v   row strides ldk, ldv (of tokens; the heads of a token lie together), `type` of the cache
  *   q, q_out  [tokens][heads][head_dim], row strides ldq, ldqo: queries, and where the rotated ones go (may be q); both NULL with heads = 0: none
  *   frequencies  DEVICE float [pairs], 0 <= pairs <= head_dim / 2; pairs = 0: no rotation
@@ -438,7 +439,8 @@ int hbp_paged_append(const hbp_paged_t *cache /* HOST */, int64_t tokens, const 
  * over the positions that the cache holds, keys and values of head h / (heads / kv_heads); cap(s) = softcap tanh(s / softcap), or s where softcap is 0; softcap at most 1e30, scale below 2e38.  A query that
  * sees no position, or none with a score above -inf, gives 0.  What lies in slots that a query does not see has no part in its result, whatever it is.
  *   q, out [tokens][heads][head_dim], row strides ldq, ldo, `type` of the cache; out may be q.  heads a multiple of kv_heads.
- *   most_new  no sequence has more new tokens than this (rows of one behind it are not computed); 1 for decoding
+ *   most_new  no sequence has more new tokens than this (rows of one behind it are not computed); 1 for decoding.  Tiles, grids and the workspace go by it: with all of a batch's tokens here,
+ *          64 sequences of one token each take tiles of 128 rows with one token's heads in each (over up to 16000 positions 704 us, with 1 here 425).
  * Scores, the softmax and sums are fp32; the weights of a row are rounded to 16-bit `type`s for their product with the values (in fp16 to multiples of 2^-31 of its largest one where they
  * are below 2^-21 of it; an infinite value whose weight comes out as 0 gives NaN).  A capped score is off by 2^-20 of itself, or with 16-bit `type`s and caps up to 128 by 2^-22 of the cap.  fp32 products are sums of products of bf16 parts, 2^-22 relative.  tokens * (heads / kv_heads) below 2^31; tokens = 0 does nothing. */
 int hbp_paged_attention(const hbp_paged_t *cache /* HOST */, int64_t tokens, const void *q, int64_t ldq, int heads, void *out, int64_t ldo,

@@ -294,8 +294,8 @@ __device__ __forceinline__ void add_odd(const Attend &a, const int32_t *table, i
 
 // Few rows: a workgroup of four wavefronts takes 16 NQ rows, and each wavefront every fourth step of their positions, straight from the cache into registers; the four
 // results are joined in LDS.  The next step's keys are on their way from the scores on, this one's values until the weights are there.  Bound: HBM where there are many positions (64 sequences over up
-// to 16000, fp16, heads of 128: 397 us, 5.8 TB/s), its latency with heads of 256, whose 32 KB of a step leave two wavefronts a SIMD (24 x 5 tokens, a window of 4096: 152 us, 5.3 TB/s), and a chain of
-// loads (starts, the table, keys) with few: 6.4 us for one token over 4096.  Nothing is shared in LDS: with at most 32 rows no wavefront would read what another one has loaded.
+// to 16000, fp16, heads of 128: 396 us, 5.8 TB/s), its latency with heads of 256, whose 32 KB of a step leave two wavefronts a SIMD (24 x 5 tokens, a window of 4096: 152 us, 5.3 TB/s), and a chain of
+// loads (starts, the table, keys) with few: 6.7 us for one token over 4096.  Nothing is shared in LDS: with at most 32 rows no wavefront would read what another one has loaded.
 template <typename T, int D, int NQ, bool ANY_PAGE> __global__ __launch_bounds__(256, sizeof(T) == 4 && D > 64 ? 1 : 2) void k_attend(Attend a, int64_t first_unit)
 {
     constexpr int kSteps = D / 32, kTiles = D / 16;   // of 32 columns in Q K^T; of 16 in the result, which a lane holds D / 16 neighbouring columns of
@@ -597,7 +597,8 @@ template <typename T, int D, int NQ, bool ANY_PAGE> __global__ __launch_bounds__
 }
 
 // Joins the parts of tiles that were split: a workgroup sixteen rows of a tile, LANES lanes a part of a row with eight columns each.  A wavefront has ROWS rows at once, or one with as many parts
-// on their way: what it waits for is the latency of loads: 4.3 us for one token over 4096 positions, 29 for the 1024 tiles of 4 x 2048 tokens over up to 8000, 136 MB of parts.
+// on their way: what it waits for is the latency of loads: 4.9 us for one token over 4096 positions, 15 for 512 of 32 heads over
+// 30000.  The grid is as large as the lengths could make it: 28 us for the 13696 workgroups behind 4 x 2048 tokens over up to 8000, whose 832 tiles are all whole, so that none of them has anything to join.
 template <typename T, int LANES, int ROWS> __global__ __launch_bounds__(256) void k_attend_join(Attend a, int64_t first)
 {
     constexpr int kAtOnce = kWave / LANES, kAhead = 4 / ROWS;   // parts side by side, and one behind the other on their way

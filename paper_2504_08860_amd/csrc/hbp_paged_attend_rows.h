@@ -10,7 +10,8 @@ namespace {
 // from the cache into registers two turns ahead, values are turned there (eight positions of one column become a lane's share of an operand), and both lie in LDS as operands of the matrix
 // instruction, lane after lane, so that every read is one of 16 bytes a lane without conflicts.  Three buffers and one barrier a turn.  The scores of the next block of 32 positions are
 // multiplied when this one's have become weights, or while they do.  Bound: the matrix cores (515 cycles a block of a wavefront with 2 x 16 rows of heads of 128) and the vector unit (some 80 instructions and 16 exponentials)
-// in turn; 4 x 2048 bf16 tokens over up to 6000 positions, 32 heads of 128, 8 of keys: 730 us, 840 TFLOP/s; one prompt of 16384: 2.25 ms, 980 TFLOP/s.  With 32 rows a wavefront an operand that
+// in turn; 4 x 2048 bf16 tokens over up to 6000 positions, 32 heads of 128, 8 of keys: 735 us, 835 TFLOP/s, of which 28 are workgroups that find nothing to join, and the last turn of the chip, whose 256 places take 832 tiles of unequal length, leaves some 9 % of them idle;
+// one prompt of 16384, whose tiles come out even: 2.26 ms, 975 TFLOP/s.  With 32 rows a wavefront an operand that
 // has been read is multiplied twice; 64 would need accumulation registers, and copies from them (1356 us where this was 818); workgroups of four wavefronts, two on a compute unit, take 1.05 to 1.25 times as
 // long; the two wavefronts of a SIMD in opposite phases, held there by barriers, 1.15 times.
 constexpr int kRowThreads = 512;

@@ -421,7 +421,7 @@ def hbp_paged_attention(q, keys, values, table, starts, lengths, out, scale: flo
                         most_new: int | None = None, workspace=None, stream=None) -> None:
     """Attention of new tokens' queries ``q`` [tokens, heads, head_dim] over the cache that holds their own keys and values already (as hbp_paged_append has
     them), into ``out``: causal, at most the last ``window`` positions if given, scores times ``scale`` (1 / sqrt(head_dim)) and capped at ``softcap`` if given.
-    ``most_new``: no sequence has more new tokens than this (1 for decoding; without it, tokens)."""
+    ``most_new``: no sequence has more new tokens than this (1 for decoding; without it, tokens, for which a batch that decodes takes up to twice as long: tiles go by it)."""
     L, device = _start()
     packed, dtype, kv_heads, dim, sizes = _cache(keys, values, table, starts, lengths, device)
     shape = q.shape
