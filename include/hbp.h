@@ -441,8 +441,10 @@ int hbp_paged_append(const hbp_paged_t *cache /* HOST */, int64_t tokens, const 
  *   q, out [tokens][heads][head_dim], row strides ldq, ldo, `type` of the cache; out may be q.  heads a multiple of kv_heads.
  *   most_new  no sequence has more new tokens than this (rows of one behind it are not computed); 1 for decoding.  Tiles, grids and the workspace go by it: with all of a batch's tokens here,
  *          64 sequences of one token each take tiles of 128 rows with one token's heads in each (over up to 16000 positions 704 us, with 1 here 425).
- * Scores, the softmax and sums are fp32; the weights of a row are rounded to 16-bit `type`s for their product with the values (in fp16 to multiples of 2^-31 of its largest one where they
- * are below 2^-21 of it; an infinite value whose weight comes out as 0 gives NaN).  A capped score is off by 2^-20 of itself, or with 16-bit `type`s and caps up to 128 by 2^-22 of the cap.  fp32 products are sums of products of bf16 parts, 2^-22 relative.  tokens * (heads / kv_heads) below 2^31; tokens = 0 does nothing. */
+ * Scores, the softmax and sums are fp32.  The weights of a row, whose largest one may be held as 2^8, are rounded to 16-bit `type`s for their product with the values (in fp16 to
+ * multiples of 2^-31 of the largest one where they are below 2^-21 of it); an infinite value whose weight comes out as 0 gives NaN, and bf16 and fp32 values of more than 2^120 / positions
+ * may overflow.  A capped score is off by 2^-20 of itself, or with 16-bit `type`s and caps up to 128 by 2^-22 of the cap.  fp32 products are sums of products of bf16 parts, 2^-22
+ * relative.  tokens * (heads / kv_heads) below 2^31; tokens = 0 does nothing. */
 int hbp_paged_attention(const hbp_paged_t *cache /* HOST */, int64_t tokens, const void *q, int64_t ldq, int heads, void *out, int64_t ldo,
                         float scale, float softcap, int window, int64_t most_new, void *workspace, size_t workspace_bytes, void *stream);
 int hbp_paged_attention_workspace(const hbp_paged_t *cache, int64_t tokens, int heads, int window, int64_t most_new, size_t *bytes /* HOST */);
